@@ -63,7 +63,8 @@ typedef enum {
     WHT_ERR_CUDA = -7,        /* a CUDA runtime call failed; see wht_affine_last_cuda_error */
     WHT_ERR_BAD_VARIANT = -8, /* unknown kernel variant id                           */
     WHT_ERR_DEVICE_WAIT = -9, /* a kernel's bounded wait (copy, product, hand-over) expired */
-    WHT_ERR_GUARD = -10       /* debug build only: a kernel wrote outside an output or scratch buffer */
+    WHT_ERR_GUARD = -10,      /* debug build only: a kernel wrote outside an output or scratch buffer */
+    WHT_ERR_DEVICE_INDEX = -11 /* serving attention: a page, slot, position or length read on the device is out of range */
 } wht_status;
 
 /*

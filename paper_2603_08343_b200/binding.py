@@ -29,6 +29,12 @@ EXPORTS = (
     "wht_affine_shutdown",
 )
 
+# the serving attention of include/wht_attention.h (wrapped by attention.py)
+ATTENTION_EXPORTS = (
+    "wht_kv_append", "wht_attn_prefix", "wht_attn_prefix_workspace_bytes",
+    "wht_attn_select", "wht_attn_select_workspace_bytes", "wht_attn_device_status",
+)
+
 
 class WhtError(RuntimeError):
     def __init__(self, status: int, where: str):
@@ -79,7 +85,19 @@ def _load(path: str | None = None) -> ctypes.CDLL:
     lib.wht_affine_debug_build.argtypes = []
     lib.wht_affine_debug_selftest_guard.argtypes = [ci]
     lib.wht_affine_test_fail_allocations.argtypes = [ci]
-    for name in EXPORTS:
+    f32 = ctypes.c_float
+    lib.wht_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                  i64, i32, i32, i32, i32, i32, i64, i64, i32, ci, vp]
+    lib.wht_attn_prefix.argtypes = [vp, i64, i64, vp, vp, vp, i64, vp, i32, vp, vp, vp,
+                                    i64, i32, i32, i32, i32, i32, i64, i32, f32, ci, vp, sz, vp]
+    lib.wht_attn_prefix_workspace_bytes.argtypes = [i64, i32, i64, i32, i32, i32, i32, i32, i32, ci]
+    lib.wht_attn_prefix_workspace_bytes.restype = sz
+    lib.wht_attn_select.argtypes = [vp, i64, i64, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp,
+                                    i64, i32, i32, i32, i32, i32, i64, i32, f32, ci, vp, sz, vp]
+    lib.wht_attn_select_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32, i32, i32, i32, ci]
+    lib.wht_attn_select_workspace_bytes.restype = sz
+    lib.wht_attn_device_status.argtypes = []
+    for name in EXPORTS + ATTENTION_EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int or fn.restype is None:
             fn.restype = ctypes.c_int

@@ -1,0 +1,41 @@
+// Host-side pieces shared by the serving-attention translation units: launch functions and the split of work.
+#pragma once
+#include "../../include/wht_attention.h"
+#include "host_common.h"
+
+namespace wht {
+struct AppendParams;
+struct AttnParams;
+struct SelectParams;
+}  // namespace wht
+
+namespace wht_host {
+
+// attn_append.cu
+int launch_append(wht::AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s);
+// attn_paged.cuh, instantiated per storage type in attn_paged_bf16.cu and attn_paged_f32.cu
+template <typename T> int launch_attn_prefix(const wht::AttnParams& p, int d, int dev, cudaStream_t s);
+template <typename T> int launch_attn_chosen(const wht::AttnParams& p, int d, int dev, cudaStream_t s);
+template <typename T> int launch_attn_join(const wht::AttnParams& p, int d, cudaStream_t s);
+// attn_select.cu
+int launch_select(wht::SelectParams& p, int dtype, int d, cudaStream_t s);
+
+int take_attn_error_append(unsigned* flag);
+int take_attn_error_paged_bf16(unsigned* flag);
+int take_attn_error_paged_f32(unsigned* flag);
+int take_attn_error_select(unsigned* flag);
+
+// Defines one of the four readers above in the translation unit that includes the kernels.
+#define WHT_DEFINE_ATTN_ERROR_READER(name)                                                            \
+    int name(unsigned* flag) {                                                                        \
+        unsigned v = 0;                                                                               \
+        WHT_CUDA_TRY(cudaMemcpyFromSymbol(&v, ::wht::g_attn_device_error, sizeof(v)));                \
+        if (v != 0) {                                                                                 \
+            const unsigned zero = 0;                                                                  \
+            WHT_CUDA_TRY(cudaMemcpyToSymbol(::wht::g_attn_device_error, &zero, sizeof(zero)));        \
+        }                                                                                             \
+        *flag = v;                                                                                    \
+        return WHT_OK;                                                                                \
+    }
+
+}  // namespace wht_host

@@ -23,6 +23,8 @@ int cuda_fail(cudaError_t e);
 // A kernel of which not even one CTA fits on an SM: reports the runtime's error if it raised one,
 // else "launch out of resources", so that WHT_ERR_CUDA never comes with a last-error of 0.
 int occupancy_fail();
+// The current device and its SM count (state lives in wht_affine.cu).
+int device_info(int* dev, int* sms);
 
 #define WHT_CUDA_TRY(expr)                                        \
     do {                                                          \

@@ -1,0 +1,246 @@
+// Selection of pages by a whole-number score.
+//
+//     q8 = rint(q * (127 * (1 / max|q|)))      score(page) = sum_channels up . most(page) + down . least(page)
+//     up = sum over the heads of the positive q8, down = of the negative: the heads of a key head add up first,
+// so a page costs two products of length D whatever the group.  Sums of whole numbers have no order: the scores, and
+// so the selection, are the same for every batch shape and split.
+//
+// attn_score_kernel: one thread per page, its summary (2 D bytes) in registers, the queries' sums in shared memory as
+// base-64 digits (two signed bytes each), four dp4a chains per query.  A block takes up to TQ tokens of a
+// sequence, so that prompts read each summary once per TQ queries; single tokens stream summaries at the rate of memory.
+// attn_pick_kernel: one block per query and key head.  The threshold is built bit by bit from the top (the scores less
+// their minimum, so only as many steps as their range has bits), each step a count over the block; then one ordered pass
+// writes the pages above it and, lowest first, as many that equal it as are still wanted.
+#pragma once
+#include "attn_kernels.cuh"
+
+namespace wht {
+
+struct SelectParams {
+    AttnParams a;           // queries, tables, lengths
+    const int8_t* summary;  // [num_pages x Hkv x 2 x D]
+    int32_t* scores;        // [T x Hkv x stride]
+    int32_t* pages;         // [T x Hkv x select]
+    int stride;             // candidates a row has room for (the table's width)
+    int token_tiles;        // token tiles per sequence
+    int chunks;             // blocks of pages
+};
+
+constexpr int kScoreThreads = 128;
+
+template <typename T>
+__device__ __forceinline__ float load_f32(const T* p) {
+    if constexpr (std::is_same<T, float>::value) return __ldg(p);
+    else return __bfloat162float(*p);
+}
+
+template <typename T, int D, int TQ>
+__global__ void __launch_bounds__(kScoreThreads)
+attn_score_kernel(const SelectParams sp) {
+    __shared__ __align__(16) int8_t digits[TQ][4][D];
+    const AttnParams& p = sp.a;
+    grid_launch_dependents();
+    int64_t b = blockIdx.x;
+    const int chunk = static_cast<int>(b % sp.chunks);
+    b /= sp.chunks;
+    const int head = static_cast<int>(b % p.hkv);
+    b /= p.hkv;
+    const int tile = static_cast<int>(b % sp.token_tiles), seq = static_cast<int>(b / sp.token_tiles);
+    int64_t first;
+    int count;
+    attn_tokens(p, seq, first, count);
+    const int n = min(TQ, count - tile * TQ);
+    if (n <= 0) return;
+    const int64_t t0 = first + tile * TQ;
+    // own page of each token: the pages before it are candidates
+    const int64_t place0 = static_cast<int64_t>(attn_length(p, seq)) - count + tile * TQ;
+    const int64_t last = place0 + n - 1;
+    const int most = last < 0 ? 0 : static_cast<int>(last >> p.page_shift);
+    if (most <= p.select - 1 || chunk * kScoreThreads >= most) return;  // all are taken / no page of this chunk is before a token
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int C = D / 32;
+    for (int i = warp; i < n; i += kScoreThreads / 32) {
+        const T* q = static_cast<const T*>(p.q) + (t0 + i) * p.q_st + static_cast<int64_t>(head) * p.group * p.q_sh;
+        float top = 0.0f;
+        for (int g = 0; g < p.group; ++g)
+#pragma unroll
+            for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(load_f32(q + g * p.q_sh + lane + 32 * c)));
+#pragma unroll
+        for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, k));
+        const float r = top > 1e-30f ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
+        int up[C], down[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) up[c] = down[c] = 0;
+        for (int g = 0; g < p.group; ++g)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                // (an infinite or NaN query gives no number: 0)
+                const int v = max(-127, min(127, __float2int_rn(__fmul_rn(load_f32(q + g * p.q_sh + lane + 32 * c), r))));
+                up[c] += max(v, 0);
+                down[c] += min(v, 0);
+            }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int uh = (up[c] + 32) >> 6, dh = (down[c] + 32) >> 6;
+            digits[i][0][lane + 32 * c] = static_cast<int8_t>(uh);
+            digits[i][1][lane + 32 * c] = static_cast<int8_t>(up[c] - uh * 64);
+            digits[i][2][lane + 32 * c] = static_cast<int8_t>(dh);
+            digits[i][3][lane + 32 * c] = static_cast<int8_t>(down[c] - dh * 64);
+        }
+    }
+    __syncthreads();
+    const int page = chunk * kScoreThreads + threadIdx.x;
+    if (page >= most) return;
+    int phys = __ldg(p.page_table + static_cast<int64_t>(seq) * p.table_width + page);
+    if (phys < 0 || phys >= p.num_pages) {
+        attn_report(kAttnErrIndex);
+        phys = 0;
+    }
+    constexpr int V = D / 16;
+    uint4 least[V], largest[V];
+    const uint4* row = reinterpret_cast<const uint4*>(sp.summary + (static_cast<int64_t>(phys) * p.hkv + head) * 2 * D);
+#pragma unroll
+    for (int v = 0; v < V; ++v) least[v] = __ldg(row + v);
+#pragma unroll
+    for (int v = 0; v < V; ++v) largest[v] = __ldg(row + V + v);
+    for (int i = 0; i < n; ++i) {
+        const int64_t mine = (place0 + i) >> p.page_shift;
+        if (place0 + i < 0 || page >= mine) continue;
+        int hi = 0, lo = 0;
+        auto dot = [](const uint4& x, const uint4& y, int acc) {
+            acc = __dp4a(static_cast<int>(x.x), static_cast<int>(y.x), acc);
+            acc = __dp4a(static_cast<int>(x.y), static_cast<int>(y.y), acc);
+            acc = __dp4a(static_cast<int>(x.z), static_cast<int>(y.z), acc);
+            return __dp4a(static_cast<int>(x.w), static_cast<int>(y.w), acc);
+        };
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            hi = dot(*reinterpret_cast<const uint4*>(&digits[i][0][v * 16]), largest[v], hi);
+            lo = dot(*reinterpret_cast<const uint4*>(&digits[i][1][v * 16]), largest[v], lo);
+            hi = dot(*reinterpret_cast<const uint4*>(&digits[i][2][v * 16]), least[v], hi);
+            lo = dot(*reinterpret_cast<const uint4*>(&digits[i][3][v * 16]), least[v], lo);
+        }
+        sp.scores[((t0 + i) * p.hkv + head) * sp.stride + page] = hi * 64 + lo;
+    }
+}
+
+// Sum of `v` over the block, the same for every thread.  `slot` alternates between calls.
+template <int THREADS>
+__device__ __forceinline__ int block_sum(int v, int* buf) {
+    const int w = __reduce_add_sync(kFullMask, v);
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = w;
+    __syncthreads();
+    int s = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) s += buf[i];
+    return s;
+}
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+attn_pick_kernel(const SelectParams sp) {
+    extern __shared__ uint32_t keys[];
+    __shared__ int buf[3][2 * (THREADS / 32)];
+    const AttnParams& p = sp.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x;  // token * Hkv + head
+    const int64_t t = row / p.hkv;
+    int32_t* out = sp.pages + row * p.select;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int seq = attn_sequence_of(p, t);
+    int64_t first;
+    int count;
+    attn_tokens(p, seq, first, count);
+    const int64_t place = attn_place(p, seq, t, first, count);
+    const int n = place < 0 ? -1 : static_cast<int>(place >> p.page_shift);  // candidates, and the token's own page
+    const int k = p.select - 1;
+    if (n <= k) {
+        for (int i = tid; i < p.select; i += THREADS) out[i] = i <= n ? i : -1;
+        return;
+    }
+    if (k == 0) {
+        if (tid == 0) out[0] = n;
+        return;
+    }
+    const int32_t* src = sp.scores + row * sp.stride;
+    uint32_t least = 0xffffffffu, most = 0;
+    for (int i = tid; i < n; i += THREADS) {
+        const uint32_t v = static_cast<uint32_t>(src[i]) ^ 0x80000000u;
+        keys[i] = v;
+        least = min(least, v);
+        most = max(most, v);
+    }
+    least = __reduce_min_sync(kFullMask, least);
+    most = __reduce_max_sync(kFullMask, most);
+    if (lane == 0) {
+        buf[0][warp] = static_cast<int>(least);
+        buf[0][THREADS / 32 + warp] = static_cast<int>(most);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+        least = min(least, static_cast<uint32_t>(buf[0][i]));
+        most = max(most, static_cast<uint32_t>(buf[0][THREADS / 32 + i]));
+    }
+    // the largest threshold that at least k keys reach
+    uint32_t cut = 0;
+    bool exact = false;  // exactly k keys reach it
+    for (int bit = 31 - __clz(static_cast<int>((most - least) | 1u)), turn = 1; bit >= 0 && !exact; --bit) {
+        const uint32_t want = cut | (1u << bit);
+        int c = 0;
+        for (int i = tid; i < n; i += THREADS) c += keys[i] - least >= want;
+        c = block_sum<THREADS>(c, buf[turn]);
+        turn = turn == 2 ? 0 : turn + 1;
+        if (c >= k) {
+            cut |= 1u << bit;
+            exact = c == k;
+        }
+    }
+    // ordered pass: thread i has the i-th run of consecutive pages
+    const int per = (n + THREADS - 1) / THREADS;
+    const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+    int above = 0, equal = 0;
+    for (int i = i0; i < i1; ++i) {
+        const uint32_t v = keys[i] - least;
+        above += exact ? v >= cut : v > cut;
+        equal += !exact && v == cut;
+    }
+    int sa = above, se = equal;  // inclusive scans
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const int xa = __shfl_up_sync(kFullMask, sa, s), xe = __shfl_up_sync(kFullMask, se, s);
+        if (lane >= s) {
+            sa += xa;
+            se += xe;
+        }
+    }
+    __syncthreads();
+    if (lane == 31) {
+        buf[0][warp] = sa;
+        buf[0][THREADS / 32 + warp] = se;
+    }
+    __syncthreads();
+    int total = 0, before_a = 0, before_e = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+        if (i < warp) {
+            before_a += buf[0][i];
+            before_e += buf[0][THREADS / 32 + i];
+        }
+        total += buf[0][i];
+    }
+    const int wanted = k - total;  // of those that equal the threshold
+    int a = before_a + sa - above, e = before_e + se - equal;
+    for (int i = i0; i < i1; ++i) {
+        const uint32_t v = keys[i] - least;
+        const bool is_above = exact ? v >= cut : v > cut, is_equal = !exact && v == cut;
+        if (is_above || (is_equal && e < wanted)) out[a + min(e, wanted)] = i;
+        a += is_above;
+        e += is_equal;
+    }
+    if (tid == 0) out[k] = n;
+}
+
+}  // namespace wht

@@ -383,6 +383,10 @@ int query_bwd_bytes(int64_t T, int32_t d, int dtype, size_t* need) {
 
 }  // namespace
 
+namespace wht_host {
+int device_info(int* dev, int* sms) { return current_device(dev, sms); }
+}  // namespace wht_host
+
 extern "C" {
 
 int wht_affine_fwd(const void* x, const void* a, const void* b, void* y, int64_t T, int32_t d,
@@ -708,6 +712,8 @@ const char* wht_affine_status_string(int status) {
             return "WHT_ERR_DEVICE_WAIT: a kernel gave up waiting for an async copy; that launch's results are invalid";
         case WHT_ERR_GUARD:
             return "WHT_ERR_GUARD: debug build: a kernel wrote outside an output or scratch buffer";
+        case WHT_ERR_DEVICE_INDEX:
+            return "WHT_ERR_DEVICE_INDEX: a kernel met a page number, slot, position or length out of range; its results are invalid";
         default: return "unknown wht_status";
     }
 }

@@ -1,0 +1,253 @@
+// C ABI of the serving attention (see include/wht_attention.h): argument checks and the split of work.
+#include <algorithm>
+
+#include "attn_host.h"
+#include "kv_append_kernels.cuh"
+#include "select_kernels.cuh"
+
+namespace {
+
+using namespace wht_host;
+using wht::AppendParams;
+using wht::AttnParams;
+using wht::SelectParams;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+size_t elem(int dtype) { return dtype == WHT_F32 ? 4 : 2; }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+int page_shift_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : -1; }
+
+// Rows of a strided [T x H x D] tensor start on 16-byte boundaries.
+bool strides_ok(const void* p, int64_t st, int64_t sh, int dtype) {
+    const int64_t unit = 16 / static_cast<int64_t>(elem(dtype));
+    return aligned16(p) && st % unit == 0 && sh % unit == 0;
+}
+
+int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages, int32_t page, int dtype) {
+    if (dtype != WHT_F32 && dtype != WHT_BF16) return WHT_ERR_BAD_DTYPE;
+    if (D != 64 && D != 96 && D != 128) return WHT_ERR_BAD_DIM;
+    if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 64 || Hq > 65536) return WHT_ERR_BAD_DIM;
+    if (page_shift_of(page) < 0 || num_pages < 0 || num_pages > 0x7fffffff) return WHT_ERR_BAD_DIM;
+    if (T < 0 || T * Hq > 0x7fffffff) return WHT_ERR_BAD_T;
+    return WHT_OK;
+}
+
+int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, int32_t page, bool ragged) {
+    if (B < 0 || max_q_len < 1 || table_width < 0 || static_cast<int64_t>(table_width) * page > 0x7fffffff) return WHT_ERR_BAD_DIM;
+    if (max_q_len > (1 << 20) || (!ragged && (T != B || max_q_len != 1))) return WHT_ERR_BAD_T;
+    return WHT_OK;
+}
+
+int row_tiles_per_block(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+int keys_per_tile(int dtype) { return dtype == WHT_F32 ? 32 : 64; }
+
+// How many blocks the keys of `units` row sets are divided over: enough to occupy two blocks on every SM, but no
+// block with fewer than four tiles (its own set-up and the join of its part would cost more than they save).
+int splits_for(int64_t units, int64_t keys, int dtype, int sms) {
+    const int64_t tiles = ceil_div(keys, keys_per_tile(dtype));
+    const int64_t want = units > 0 ? (2 * sms) / units : 1;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, tiles / 4)));
+}
+
+struct PrefixPlan {
+    int prefix_rw, prefix_row_tiles, prefix_splits, own_rw, own_row_tiles, own_splits, parts;
+    size_t bytes;
+};
+
+PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv,
+                       int32_t D, int32_t page, int dtype, int sms) {
+    PrefixPlan f{};
+    const int group = Hq / Hkv;
+    const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
+    f.own_rw = row_tiles_per_block(own_rows);
+    f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 16 * f.own_rw));
+    f.own_splits = splits_for(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, dtype, sms);
+    f.prefix_rw = 1;
+    if (prefix_len > 0) {
+        f.prefix_rw = row_tiles_per_block(T * group);
+        f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 16 * f.prefix_rw));
+        f.prefix_splits = splits_for(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, dtype, sms);
+    }
+    f.parts = f.prefix_splits + f.own_splits;
+    const size_t rows = static_cast<size_t>(T) * Hq;
+    f.bytes = f.parts > 1 ? up256(rows * f.parts * sizeof(float2)) + rows * f.parts * D * sizeof(float) : 0;
+    return f;
+}
+
+struct SelectPlan {
+    int rw, row_tiles, splits;
+    size_t scores_bytes, bytes;
+};
+
+SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int dtype, int sms) {
+    SelectPlan f{};
+    const int group = Hq / Hkv;
+    f.rw = row_tiles_per_block(group);
+    f.row_tiles = static_cast<int>(ceil_div(group, 16 * f.rw));
+    f.splits = splits_for(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, dtype, sms);
+    f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
+    const size_t rows = static_cast<size_t>(T) * Hq;
+    f.bytes = f.scores_bytes + (f.splits > 1 ? up256(rows * f.splits * sizeof(float2)) + rows * f.splits * D * sizeof(float) : 0);
+    return f;
+}
+
+void set_parts(AttnParams& p, unsigned char* at, int64_t rows) {
+    if (p.parts <= 1) return;
+    p.part_ml = reinterpret_cast<float2*>(at);
+    p.part_o = reinterpret_cast<float*>(at + up256(static_cast<size_t>(rows) * p.parts * sizeof(float2)));
+}
+
+int join(const AttnParams& p, int dtype, int32_t D, cudaStream_t s) {
+    if (p.parts <= 1) return WHT_OK;
+    return dtype == WHT_F32 ? launch_attn_join<float>(p, D, s) : launch_attn_join<__nv_bfloat16>(p, D, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int wht_kv_append(const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v, int64_t v_stride_t, int64_t v_stride_h,
+                  const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out, const int64_t* slots,
+                  const int32_t* positions, const float* cos_table, const float* sin_table, void* k_cache, void* v_cache,
+                  int8_t* summary, const float* summary_scale, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t rot,
+                  int32_t interleaved, int64_t max_pos, int64_t num_pages, int32_t page, int dtype, void* stream) {
+    int rc = check_shape(T, q ? Hq : Hkv, Hkv, D, num_pages, page, dtype);
+    if (rc != WHT_OK) return rc;
+    if (rot < 0 || rot > D || rot % 16 != 0 || (rot > 0 && max_pos < 1)) return WHT_ERR_BAD_DIM;
+    if ((q == nullptr) != (q_out == nullptr)) return WHT_ERR_NULL;
+    if (T == 0) return WHT_OK;
+    if (!k || !v || !slots || !k_cache || !v_cache) return WHT_ERR_NULL;
+    if (rot > 0 && (!positions || !cos_table || !sin_table)) return WHT_ERR_NULL;
+    if (summary && !summary_scale) return WHT_ERR_NULL;
+    if (!strides_ok(k, k_stride_t, k_stride_h, dtype) || !strides_ok(v, v_stride_t, v_stride_h, dtype) ||
+        (q && !strides_ok(q, q_stride_t, q_stride_h, dtype)) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache) ||
+        !aligned16(summary) || !aligned16(cos_table) || !aligned16(sin_table))
+        return WHT_ERR_MISALIGNED;
+    int dev = 0, sms = 0;
+    rc = device_info(&dev, &sms);
+    if (rc != WHT_OK) return rc;
+    AppendParams p{};
+    p.k = k; p.v = v; p.q = q;
+    p.k_st = k_stride_t; p.k_sh = k_stride_h;
+    p.v_st = v_stride_t; p.v_sh = v_stride_h;
+    p.q_st = q_stride_t; p.q_sh = q_stride_h;
+    p.q_out = q_out; p.k_cache = k_cache; p.v_cache = v_cache;
+    p.slots = slots; p.positions = positions; p.cos_t = cos_table; p.sin_t = sin_table;
+    p.summary = summary; p.summary_scale = summary_scale;
+    p.T = T; p.max_pos = max_pos; p.num_slots = num_pages * page;
+    p.hq = q ? Hq : 0; p.hkv = Hkv; p.d = D; p.rot = rot; p.page_shift = page_shift_of(page);
+    return launch_append(p, dtype, interleaved != 0, sms, static_cast<cudaStream_t>(stream));
+}
+
+size_t wht_attn_prefix_workspace_bytes(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq,
+                                       int32_t Hkv, int32_t D, int32_t page, int dtype) {
+    int dev = 0, sms = 0;
+    if (check_shape(T, Hq, Hkv, D, 0, page, dtype) != WHT_OK || check_batch(T, B, max_q_len, table_width, page, true) != WHT_OK ||
+        prefix_len < 0 || device_info(&dev, &sms) != WHT_OK)
+        return 0;
+    return plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms).bytes;
+}
+
+int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k_cache, const void* v_cache,
+                    const int32_t* prefix_pages, int64_t prefix_len, const int32_t* page_table, int32_t table_width,
+                    const int32_t* kv_lens, const int32_t* q_start, void* out, int64_t T, int32_t B, int32_t max_q_len,
+                    int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages, int32_t page, float scale, int dtype,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_shape(T, Hq, Hkv, D, num_pages, page, dtype);
+    if (rc == WHT_OK) rc = check_batch(T, B, max_q_len, table_width, page, q_start != nullptr);
+    if (rc != WHT_OK) return rc;
+    if (prefix_len < 0 || prefix_len > 0x7fffff00) return WHT_ERR_BAD_T;
+    if (T == 0) return WHT_OK;
+    if (!q || !k_cache || !v_cache || !out || !kv_lens || (table_width > 0 && !page_table) || (prefix_len > 0 && !prefix_pages))
+        return WHT_ERR_NULL;
+    if (!strides_ok(q, q_stride_t, q_stride_h, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
+        return WHT_ERR_MISALIGNED;
+    int dev = 0, sms = 0;
+    rc = device_info(&dev, &sms);
+    if (rc != WHT_OK) return rc;
+    const PrefixPlan f = plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms);
+    if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return WHT_ERR_WORKSPACE;
+    AttnParams p{};
+    p.q = q; p.k_cache = k_cache; p.v_cache = v_cache;
+    p.q_st = q_stride_t; p.q_sh = q_stride_h;
+    p.out = out;
+    p.parts = f.parts;
+    set_parts(p, static_cast<unsigned char*>(workspace), T * Hq);
+    p.prefix_pages = prefix_pages; p.prefix_len = prefix_len;
+    p.prefix_splits = f.prefix_splits; p.prefix_row_tiles = f.prefix_row_tiles; p.prefix_rw = f.prefix_rw;
+    p.page_table = page_table; p.kv_lens = kv_lens; p.q_start = q_start;
+    p.table_width = table_width; p.B = B; p.max_q_len = max_q_len;
+    p.own_splits = f.own_splits; p.own_row_tiles = f.own_row_tiles; p.own_rw = f.own_rw;
+    p.T = T; p.num_pages = num_pages;
+    p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
+    p.scale_log2 = scale * wht::kLog2e;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    rc = dtype == WHT_F32 ? launch_attn_prefix<float>(p, D, dev, s) : launch_attn_prefix<__nv_bfloat16>(p, D, dev, s);
+    return rc != WHT_OK ? rc : join(p, dtype, D, s);
+}
+
+size_t wht_attn_select_workspace_bytes(int32_t table_width, int32_t select, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq,
+                                       int32_t Hkv, int32_t D, int32_t page, int dtype) {
+    int dev = 0, sms = 0;
+    if (check_shape(T, Hq, Hkv, D, 0, page, dtype) != WHT_OK || check_batch(T, B, max_q_len, table_width, page, true) != WHT_OK ||
+        select < 1 || select > 1024 || device_info(&dev, &sms) != WHT_OK)
+        return 0;
+    return plan_select(table_width, select, T, Hq, Hkv, D, page, dtype, sms).bytes;
+}
+
+int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k_cache, const void* v_cache,
+                    const int8_t* summary, const int32_t* page_table, int32_t table_width, const int32_t* kv_lens,
+                    const int32_t* q_start, int32_t select, void* out, int32_t* pages_out, int64_t T, int32_t B,
+                    int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages, int32_t page, float scale,
+                    int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_shape(T, Hq, Hkv, D, num_pages, page, dtype);
+    if (rc == WHT_OK) rc = check_batch(T, B, max_q_len, table_width, page, q_start != nullptr);
+    if (rc != WHT_OK) return rc;
+    if (select < 1 || select > 1024 || table_width > 49152) return WHT_ERR_BAD_DIM;
+    if (T == 0) return WHT_OK;
+    if (!q || !k_cache || !v_cache || !summary || !out || !pages_out || !kv_lens || (table_width > 0 && !page_table)) return WHT_ERR_NULL;
+    if (!strides_ok(q, q_stride_t, q_stride_h, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(summary) ||
+        !aligned16(out) || !aligned16(workspace))
+        return WHT_ERR_MISALIGNED;
+    int dev = 0, sms = 0;
+    rc = device_info(&dev, &sms);
+    if (rc != WHT_OK) return rc;
+    const SelectPlan f = plan_select(table_width, select, T, Hq, Hkv, D, page, dtype, sms);
+    if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return WHT_ERR_WORKSPACE;
+    SelectParams sp{};
+    AttnParams& p = sp.a;
+    p.q = q; p.k_cache = k_cache; p.v_cache = v_cache;
+    p.q_st = q_stride_t; p.q_sh = q_stride_h;
+    p.out = out;
+    p.parts = f.splits;
+    set_parts(p, static_cast<unsigned char*>(workspace) + f.scores_bytes, T * Hq);
+    p.page_table = page_table; p.kv_lens = kv_lens; p.q_start = q_start;
+    p.table_width = table_width; p.B = B; p.max_q_len = max_q_len;
+    p.own_splits = f.splits; p.own_row_tiles = f.row_tiles; p.own_rw = f.rw;
+    p.chosen = pages_out; p.select = select;
+    p.T = T; p.num_pages = num_pages;
+    p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
+    p.scale_log2 = scale * wht::kLog2e;
+    sp.summary = summary;
+    sp.scores = static_cast<int32_t*>(workspace);
+    sp.pages = pages_out;
+    sp.stride = table_width;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    rc = launch_select(sp, dtype, D, s);
+    if (rc == WHT_OK) rc = dtype == WHT_F32 ? launch_attn_chosen<float>(p, D, dev, s) : launch_attn_chosen<__nv_bfloat16>(p, D, dev, s);
+    return rc != WHT_OK ? rc : join(p, dtype, D, s);
+}
+
+int wht_attn_device_status(void) {
+    unsigned any = 0;
+    for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select}) {
+        unsigned flag = 0;
+        const int rc = take(&flag);
+        if (rc != WHT_OK) return rc;
+        any |= flag;
+    }
+    return any & wht::kAttnErrIndex ? WHT_ERR_DEVICE_INDEX : any ? WHT_ERR_DEVICE_WAIT : WHT_OK;
+}
+
+}  // extern "C"
