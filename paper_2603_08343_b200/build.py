@@ -19,6 +19,8 @@ LIB_PATH = os.path.join(HERE, "libwht_affine.so")
 SOURCES = ["wht_affine.cu", "family_misc.cu", "family_bfly_fwd.cu", "family_bfly_bwd.cu", "family_tp.cu",
            "family_mma.cu", "family_umma_fwd.cu", "family_umma_bwd.cu", "family_umma_tp.cu",
            "wht_attention.cu", "attn_append.cu", "attn_paged_bf16.cu", "attn_paged_f32.cu", "attn_select.cu"]
+PYTHON_SOURCE = "attn_python.cpp"  # the Python entry of the serving attention: a CPython module beside the library
+PYTHON_PATH = os.path.join(HERE, "_attention.so")
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 
@@ -60,7 +62,7 @@ def source_digest(names) -> str:
 def _run(cmd):
     proc = subprocess.run(cmd, capture_output=True, text=True)
     if proc.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + proc.stdout + proc.stderr)
+        raise RuntimeError("the compiler failed:\n" + " ".join(cmd) + "\n" + proc.stdout + proc.stderr)
     return proc.stderr
 
 
@@ -70,13 +72,20 @@ LIB_DEBUG_PATH = os.path.join(HERE, "libwht_affine_debug.so")
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compile what is missing or older than its sources; return the library's path.
+    """Compile what is missing or older than its sources (the library, and the CPython module of the serving
+    attention beside it); return the library's path.
 
     `verbose` adds -Xptxas -v (registers, spills and shared memory of every kernel, on stderr) and
     rebuilds everything.  `debug` builds libwht_affine_debug.so instead: the same kernels with the C ABI
     compiled with -DWHT_DEBUG (guard regions around every output and scratch buffer, see the header).
     """
-    force = force or verbose
+    lib = _build_library(force or verbose, verbose, debug)
+    if not debug:
+        build_python(force)
+    return lib
+
+
+def _build_library(force: bool, verbose: bool, debug: bool) -> str:
     lib = LIB_DEBUG_PATH if debug else LIB_PATH
     sources = [os.path.join(CSRC, s) for s in SOURCES]
     if not force and os.path.exists(lib) and \
@@ -106,6 +115,23 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
         sys.stderr.write("".join(logs))
     _run([nvcc, *ARCH, "-Xcompiler", "-fPIC", "-shared", "-o", lib, *objs])
     return lib
+
+
+def build_python(force: bool = False) -> str:
+    """Compile the CPython module of attention.py (host code only; links against libwht_affine.so beside it)."""
+    src = os.path.join(CSRC, PYTHON_SOURCE)
+    if not force and os.path.exists(PYTHON_PATH) and os.path.getmtime(PYTHON_PATH) >= _newest_dependency_mtime(src):
+        return PYTHON_PATH
+    import sysconfig
+    import torch
+    home = os.path.dirname(torch.__file__)
+    inc = [f"-isystem{d}" for d in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                                    sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"))]
+    libs = os.path.join(home, "lib")
+    _run(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, src,
+          "-o", PYTHON_PATH, f"-L{HERE}", "-l:libwht_affine.so", f"-L{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda",
+          "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
+    return PYTHON_PATH
 
 
 def ptxas_summary() -> str:

@@ -20,17 +20,21 @@ void launch(const AppendParams& p, int blocks, cudaStream_t s) {
 
 int launch_append(AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s) {
     (void)sms;
-    p.rows = p.hq + (p.summary ? 1 : 2) * p.hkv;
-    const int per_token = p.rows * (p.d / 16);
-    // tokens per tile: about two items per thread and block row, so that a tile's index arithmetic stays small
-    p.tile = per_token >= 2 * kAppendThreads ? 1 : 2 * kAppendThreads / per_token;
+    const int hb = dtype == WHT_F32 ? kHeadBlock<float> : kHeadBlock<__nv_bfloat16>;
+    p.q_blocks = static_cast<int>(ceil_div(p.hq, hb));
+    p.kv_blocks = static_cast<int>(ceil_div(p.hkv, hb));
+    const int per_token = (p.q_blocks + (p.summary ? 1 : 2) * p.kv_blocks) * (p.d / 16);
+    p.tile = per_token >= kAppendThreads ? 1 : kAppendThreads / per_token;
     p.flat_x = static_cast<int>(ceil_div(p.T, p.tile));
-    p.flat_y = static_cast<int>(ceil_div(static_cast<long long>(p.tile) * per_token, 2 * kAppendThreads));
+    p.flat_y = static_cast<int>(ceil_div(static_cast<long long>(p.tile) * per_token, kAppendThreads));
     long long blocks = static_cast<long long>(p.flat_x) * p.flat_y;
     if (p.summary) {
-        // few tokens: every run gets a warp at once; many: fewer blocks, most of which find no run to own
-        p.run_tile = p.T * p.hkv <= 8192 ? 8 : 32;
-        blocks += ceil_div(p.T, p.run_tile) * p.hkv;
+        // A block's eight warps take (run, head) pairs of a tile of tokens.  Few tokens (a decode step, where every token
+        // is a run): a block per token and eight heads.  Many (prompts, a run per page): wider tiles, or most blocks
+        // would find no run to own.
+        p.run_heads = p.hkv < 8 ? p.hkv : 8;
+        p.run_tile = p.T < 1024 ? 1 : p.T < 32 * 512 ? static_cast<int>(p.T / 512) : 32;
+        blocks += ceil_div(p.T, p.run_tile) * ceil_div(p.hkv, p.run_heads);
     }
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     if (dtype == WHT_F32)

@@ -26,16 +26,12 @@ struct AppendParams {
     const float* summary_scale;
     int64_t T, max_pos, num_slots;
     int hq, hkv, d, rot, page_shift;
-    int rows;            // rows per token that the flat part handles: hq (q) [+ hkv (k)] + hkv (v)
-    int tile;            // tokens per block of the flat part
-    int flat_x, flat_y;  // its blocks: token tiles, and blocks per tile
-    int run_tile;        // tokens per block of the page part
+    int q_blocks, kv_blocks;  // blocks of heads
+    int tile;                 // tokens per tile of the flat part
+    int flat_x, flat_y;       // its thread blocks: token tiles, and blocks per tile
+    int run_tile;             // tokens per block of the page part
+    int run_heads;            // heads per block of the page part
 };
-
-__device__ __forceinline__ void load16(const float* p, float (&v)[16]) {
-    load8(p, reinterpret_cast<float(&)[8]>(v[0]));
-    load8(p + 8, reinterpret_cast<float(&)[8]>(v[8]));
-}
 
 template <typename T>
 __device__ __forceinline__ T* row_of(void* base, int64_t off) { return static_cast<T*>(base) + off; }
@@ -63,11 +59,7 @@ struct RowItem {
             hi = lo + 8;
         }
     }
-    __device__ __forceinline__ void turn(float (&a)[8], float (&b)[8], const float* cos_row, const float* sin_row) const {
-        if (angle < 0) return;
-        float c[8], s[8];
-        load8(cos_row + angle, c);
-        load8(sin_row + angle, s);
+    __device__ __forceinline__ void turn(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) const {
         if constexpr (INTERLEAVED) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -110,48 +102,113 @@ __device__ __forceinline__ int64_t cache_offset(const AppendParams& p, int64_t s
     return (((page * p.hkv + head) << p.page_shift) + place) * p.d;
 }
 
+// Eight stored elements as they lie in memory, so that several loads can be in flight in few registers.
+template <typename T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                v[4 * i] = __uint_as_float(w[i].x); v[4 * i + 1] = __uint_as_float(w[i].y);
+                v[4 * i + 2] = __uint_as_float(w[i].z); v[4 * i + 3] = __uint_as_float(w[i].w);
+            }
+        } else {
+            v[0] = bf16lo_to_f32(w[0].x); v[1] = bf16hi_to_f32(w[0].x);
+            v[2] = bf16lo_to_f32(w[0].y); v[3] = bf16hi_to_f32(w[0].y);
+            v[4] = bf16lo_to_f32(w[0].z); v[5] = bf16hi_to_f32(w[0].z);
+            v[6] = bf16lo_to_f32(w[0].w); v[7] = bf16hi_to_f32(w[0].w);
+        }
+    }
+};
+
+// Heads that a thread takes one after the other, all loads in flight at once; they share the angles.
+template <typename T>
+constexpr int kHeadBlock = sizeof(T) == 4 ? 2 : 4;
+
 // Flat part: queries, values and (without summaries) keys, item by item.
 template <typename T, bool INTERLEAVED, bool SUMMARY>
 __device__ __forceinline__ void append_flat(const AppendParams& p, int block) {
-    const int per_row = p.d / 16, per_token = p.rows * per_row;
+    constexpr int HB = kHeadBlock<T>;
+    const int per_row = p.d / 16;
+    const int per_token = (p.q_blocks + (SUMMARY ? 1 : 2) * p.kv_blocks) * per_row;
     const int bx = block / p.flat_y, by = block - bx * p.flat_y;
     const int64_t t0 = static_cast<int64_t>(bx) * p.tile;
     const int count = static_cast<int>(p.T - t0 < p.tile ? p.T - t0 : p.tile) * per_token;
-    for (int j = by * blockDim.x + threadIdx.x; j < count; j += p.flat_y * blockDim.x) {
-        const int dt = j / per_token;
-        int r = j - dt * per_token;
-        int row = r / per_row;
-        const RowItem<T, INTERLEAVED> it(r - row * per_row, p.rot);
-        const int64_t t = t0 + dt;
-        const T* src;
-        T* dst;
-        bool turns = true;
-        if (row < p.hq) {
-            src = row_of<T>(p.q, t * p.q_st + row * p.q_sh);
-            dst = row_of<T>(p.q_out, (t * p.hq + row) * p.d);
-        } else {
-            row -= p.hq;
-            const int64_t slot = append_slot(p, t);
-            if (slot < 0) continue;
-            if (!SUMMARY && row < p.hkv) {
-                src = row_of<T>(p.k, t * p.k_st + row * p.k_sh);
-                dst = row_of<T>(p.k_cache, cache_offset(p, slot, row));
-            } else {
-                if (!SUMMARY) row -= p.hkv;
-                src = row_of<T>(p.v, t * p.v_st + row * p.v_sh);
-                dst = row_of<T>(p.v_cache, cache_offset(p, slot, row));
-                turns = false;
+    const int j = by * blockDim.x + threadIdx.x;
+    if (j >= count) return;
+    const int dt = j / per_token;
+    const int r = j - dt * per_token;
+    int rb = r / per_row;
+    const RowItem<T, INTERLEAVED> it(r - rb * per_row, p.rot);
+    const int64_t t = t0 + dt;
+    const T* src;
+    T* dst;
+    int64_t step, out_step;  // from head to head
+    int heads;
+    bool turns = it.angle >= 0;
+    int64_t pos = 0;
+    if (turns) pos = append_position(p, t);
+    if (rb < p.q_blocks) {
+        const int h = rb * HB;
+        heads = p.hq - h;
+        src = row_of<T>(p.q, t * p.q_st + h * p.q_sh);
+        dst = row_of<T>(p.q_out, (t * p.hq + h) * p.d);
+        step = p.q_sh;
+        out_step = p.d;
+    } else {
+        rb -= p.q_blocks;
+        const int64_t slot = append_slot(p, t);
+        if (slot < 0) return;
+        const bool is_k = !SUMMARY && rb < p.kv_blocks;
+        if (!SUMMARY && !is_k) rb -= p.kv_blocks;
+        const int h = rb * HB;
+        heads = p.hkv - h;
+        src = is_k ? row_of<T>(p.k, t * p.k_st + h * p.k_sh) : row_of<T>(p.v, t * p.v_st + h * p.v_sh);
+        dst = row_of<T>(is_k ? p.k_cache : p.v_cache, cache_offset(p, slot, h));
+        step = is_k ? p.k_sh : p.v_sh;
+        out_step = static_cast<int64_t>(p.d) << p.page_shift;
+        turns = turns && is_k;
+    }
+    Raw8<T> lo[HB], hi[HB];
+#pragma unroll
+    for (int i = 0; i < HB; ++i) {
+        if (i < heads) {
+            lo[i].load(src + i * step + it.lo);
+            hi[i].load(src + i * step + it.hi);
+        }
+    }
+    if (!turns) {
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+            if (i < heads) {
+                lo[i].store(dst + i * out_step + it.lo);
+                hi[i].store(dst + i * out_step + it.hi);
             }
         }
-        float a[8], b[8];
-        load8(src + it.lo, a);
-        load8(src + it.hi, b);
-        if (turns && it.angle >= 0) {
-            const int64_t pos = append_position(p, t);
-            it.turn(a, b, p.cos_t + pos * (p.rot / 2), p.sin_t + pos * (p.rot / 2));
+        return;
+    }
+    float c[8], s[8];
+    load8(p.cos_t + pos * (p.rot / 2) + it.angle, c);
+    load8(p.sin_t + pos * (p.rot / 2) + it.angle, s);
+#pragma unroll
+    for (int i = 0; i < HB; ++i) {
+        if (i < heads) {
+            float a[8], b[8];
+            lo[i].widen(a);
+            hi[i].widen(b);
+            it.turn(a, b, c, s);
+            store8(dst + i * out_step + it.lo, a);
+            store8(dst + i * out_step + it.hi, b);
         }
-        store8(dst + it.lo, a);
-        store8(dst + it.hi, b);
     }
 }
 
@@ -159,9 +216,9 @@ __device__ __forceinline__ unsigned pack_s16(int lo, int hi) {
     return (static_cast<unsigned>(lo) & 0xffffu) | (static_cast<unsigned>(hi) << 16);
 }
 
-// Page part: this warp's runs of one head.
+// Page part: the warps of a block share the tile's runs and the block's heads.
 template <typename T, bool INTERLEAVED>
-__device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile0, int head) {
+__device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile0, int head0) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int per_row = p.d / 16;
     int rows = 1;  // rows of a warp's step: a power of two, so that they fold by shuffles
@@ -169,6 +226,7 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
     const int sub = lane / per_row;
     const RowItem<T, INTERLEAVED> it(lane - sub * per_row, p.rot);
     const bool active = sub < rows;
+    const int heads = min(p.run_heads, p.hkv - head0);
     // which of the tile's tokens begin a run
     int64_t page = -1, before = -1;
     if (lane < p.run_tile && tile0 + lane < p.T) {
@@ -179,64 +237,72 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
             if (s1 >= 0) before = s1 >> p.page_shift;
         }
     }
-    unsigned leaders = __ballot_sync(kFullMask, page >= 0 && page != before);
-    const float scale = __ldg(p.summary_scale + head);
-    for (int n = 0; leaders; ++n) {
-        const int l = __ffs(leaders) - 1;
-        leaders &= leaders - 1;
-        if (n % warps != warp) continue;
+    const unsigned leaders = __ballot_sync(kFullMask, page >= 0 && page != before);
+    const int pairs = __popc(leaders) * heads;
+    for (int pair = warp; pair < pairs; pair += warps) {
+        const int head = head0 + pair % heads;
+        const int l = __fns(leaders, 0, pair / heads + 1);
+        const float scale = __ldg(p.summary_scale + head);
         const int64_t first = tile0 + l;
         const int64_t run_page = __shfl_sync(kFullMask, page, l);
-        // the run's length: the tokens that follow on the same page
-        int len = 1;
-        for (;;) {
-            const int64_t t = first + len + lane;
-            bool same = false;
-            if (t < p.T) {
-                const int64_t s = append_slot(p, t);
-                same = s >= 0 && (s >> p.page_shift) == run_page;
-            }
-            const unsigned other = ~__ballot_sync(kFullMask, same);
-            if (other) {
-                len += __ffs(other) - 1;
-                break;
-            }
-            len += 32;
-        }
         unsigned least[8], most[8];  // 16 channels as 16-bit pairs
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             least[i] = pack_s16(127, 127);
             most[i] = pack_s16(-127, -127);
         }
+        int first_place = 0;
+        const T* src = row_of<T>(p.k, head * p.k_sh);
+        T* dst = row_of<T>(p.k_cache, cache_offset(p, run_page << p.page_shift, head));
+        // 32 tokens at a time: the lanes read their slots and positions at once, and find where the run ends
+        for (int64_t c0 = first;; c0 += 32) {
+            int place = -1;
+            int pos = 0;
+            if (c0 + lane < p.T) {
+                const int64_t s = append_slot(p, c0 + lane);
+                if (s >= 0 && (s >> p.page_shift) == run_page) place = static_cast<int>(s & ((1 << p.page_shift) - 1));
+                pos = static_cast<int>(append_position(p, c0 + lane));
+            }
+            const unsigned other = ~__ballot_sync(kFullMask, place >= 0);
+            const int n = other ? __ffs(other) - 1 : 32;
+            if (c0 == first) first_place = __shfl_sync(kFullMask, place, 0);
 #pragma unroll 2
-        for (int r = sub; r < len; r += rows) {
-            if (!active) break;
-            const int64_t t = first + r;
-            const int64_t slot = append_slot(p, t);
-            const T* src = row_of<T>(p.k, t * p.k_st + head * p.k_sh);
-            T* dst = row_of<T>(p.k_cache, cache_offset(p, slot, head));
-            float a[8], b[8];
-            load8(src + it.lo, a);
-            load8(src + it.hi, b);
-            if (it.angle >= 0) {
-                const int64_t pos = append_position(p, t);
-                it.turn(a, b, p.cos_t + pos * (p.rot / 2), p.sin_t + pos * (p.rot / 2));
-            }
-            store8(dst + it.lo, a);
-            store8(dst + it.hi, b);
-            int w[16];
+            for (int r0 = 0; r0 < n; r0 += rows) {
+                const int r = r0 + sub;
+                const int at = __shfl_sync(kFullMask, place, r & 31), ps = __shfl_sync(kFullMask, pos, r & 31);
+                if (!active || r >= n) continue;
+                const T* row = src + (c0 + r) * p.k_st;
+                Raw8<T> lo, hi;
+                lo.load(row + it.lo);
+                hi.load(row + it.hi);
+                float a[8], b[8];
+                if (it.angle >= 0) {
+                    float c[8], s[8];
+                    load8(p.cos_t + static_cast<int64_t>(ps) * (p.rot / 2) + it.angle, c);
+                    load8(p.sin_t + static_cast<int64_t>(ps) * (p.rot / 2) + it.angle, s);
+                    lo.widen(a);
+                    hi.widen(b);
+                    it.turn(a, b, c, s);
+                } else {
+                    lo.widen(a);
+                    hi.widen(b);
+                }
+                store8(dst + at * p.d + it.lo, a);
+                store8(dst + at * p.d + it.hi, b);
+                int w[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(a[i], src), scale))));
-                w[8 + i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(b[i], src), scale))));
-            }
+                for (int i = 0; i < 8; ++i) {
+                    w[i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(a[i], src), scale))));
+                    w[8 + i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(b[i], src), scale))));
+                }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const unsigned x = pack_s16(w[2 * i], w[2 * i + 1]);
-                least[i] = __vmins2(least[i], x);
-                most[i] = __vmaxs2(most[i], x);
+                for (int i = 0; i < 8; ++i) {
+                    const unsigned x = pack_s16(w[2 * i], w[2 * i + 1]);
+                    least[i] = __vmins2(least[i], x);
+                    most[i] = __vmaxs2(most[i], x);
+                }
             }
+            if (n < 32) break;
         }
         for (int step = rows / 2; step >= 1; step >>= 1) {
 #pragma unroll
@@ -246,7 +312,7 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
             }
         }
         if (lane < per_row) {
-            const bool anew = (append_slot(p, first) & ((1 << p.page_shift) - 1)) == 0;
+            const bool anew = first_place == 0;
             int8_t* at = p.summary + ((run_page * p.hkv + head) * 2) * p.d;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -284,12 +350,15 @@ template <typename T, bool INTERLEAVED, bool SUMMARY>
 __global__ void __launch_bounds__(kAppendThreads)
 kv_append_kernel(const AppendParams p) {
     const int flat = p.flat_x * p.flat_y;
-    if (SUMMARY && static_cast<int>(blockIdx.x) >= flat) {
-        const int b = static_cast<int>(blockIdx.x) - flat;
-        append_pages<T, INTERLEAVED>(p, static_cast<int64_t>(b / p.hkv) * p.run_tile, b % p.hkv);
+    // (the page blocks come first: theirs is the longer work)
+    const int page_blocks = static_cast<int>(gridDim.x) - flat;
+    if (SUMMARY && static_cast<int>(blockIdx.x) < page_blocks) {
+        const int hb = (p.hkv + p.run_heads - 1) / p.run_heads;
+        const int tile = static_cast<int>(blockIdx.x) / hb;
+        append_pages<T, INTERLEAVED>(p, static_cast<int64_t>(tile) * p.run_tile, (static_cast<int>(blockIdx.x) - tile * hb) * p.run_heads);
         return;
     }
-    append_flat<T, INTERLEAVED, SUMMARY>(p, blockIdx.x);
+    append_flat<T, INTERLEAVED, SUMMARY>(p, static_cast<int>(blockIdx.x) - page_blocks);
 }
 
 }  // namespace wht
