@@ -7,6 +7,7 @@ namespace wht {
 struct AppendParams;
 struct AttnParams;
 struct SelectParams;
+struct UmmaAttnParams;
 }  // namespace wht
 
 namespace wht_host {
@@ -14,9 +15,12 @@ namespace wht_host {
 // attn_append.cu
 int launch_append(wht::AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s);
 // attn_paged.cuh, instantiated per storage type in attn_paged_bf16.cu and attn_paged_f32.cu
-template <typename T> int launch_attn_prefix(const wht::AttnParams& p, int d, int dev, cudaStream_t s);
+// overlapped: launched right after the tensor-core kernel of the prefix, to run next to it
+template <typename T> int launch_attn_prefix(const wht::AttnParams& p, int d, int dev, bool overlapped, cudaStream_t s);
 template <typename T> int launch_attn_chosen(const wht::AttnParams& p, int d, int dev, cudaStream_t s);
 template <typename T> int launch_attn_join(const wht::AttnParams& p, int d, cudaStream_t s);
+// attn_umma.cu
+int launch_attn_umma_prefix(const wht::UmmaAttnParams& p, int d, int dev, cudaStream_t s);
 // attn_select.cu
 int launch_select(wht::SelectParams& p, int dtype, int d, cudaStream_t s);
 
@@ -24,8 +28,10 @@ int take_attn_error_append(unsigned* flag);
 int take_attn_error_paged_bf16(unsigned* flag);
 int take_attn_error_paged_f32(unsigned* flag);
 int take_attn_error_select(unsigned* flag);
+int take_attn_error_umma(unsigned* flag);
+int take_device_error_attn_umma(unsigned* flag);  // expired waits
 
-// Defines one of the four readers above in the translation unit that includes the kernels.
+// Defines one of the readers above in the translation unit that includes the kernels.
 #define WHT_DEFINE_ATTN_ERROR_READER(name)                                                            \
     int name(unsigned* flag) {                                                                        \
         unsigned v = 0;                                                                               \

@@ -54,6 +54,14 @@ struct AttnParams {
     float scale_log2;      // scale * log2(e)
 };
 
+// The tensor-core form of the prefix (attn_umma_kernels.cuh).
+struct UmmaAttnParams {
+    AttnParams a;    // queries, prefix, partial results
+    int splits;      // key ranges
+    int row_blocks;  // blocks of 256 rows
+    int same_rows;   // 128 rows or fewer: both of a block's tiles hold them, each with every second key tile
+};
+
 template <typename T, int D>
 struct AttnGeo {
     static constexpr bool F32 = std::is_same<T, float>::value;
@@ -526,7 +534,10 @@ attn_prefix_kernel(const AttnParams p) {
     int count;
     attn_tokens(p, seq, u.token0, count);
     u.rows = count * p.group;
-    if (u.row0 >= u.rows) return;
+    if (u.row0 >= u.rows) {
+        if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
+        return;
+    }
     const int keys = attn_length(p, seq);
     u.ids = p.page_table + static_cast<int64_t>(seq) * p.table_width;
     u.table = nullptr;
@@ -538,6 +549,9 @@ attn_prefix_kernel(const AttnParams p) {
     attn_part(keys, KEYS, p.own_splits, split, u.key0, u.key1);
     u.key1 = max(u.key0, min(u.key1, u.limit0 + last_tok));
     attn_block_rw<T, D>(p.own_rw, p, u, smem_attn);
+    // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
+    // for this grid alone, so this grid does not end before that one has.
+    if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
 }
 
 // The sequence that token t belongs to (q_start ascending): 32 lanes probe at once.

@@ -17,7 +17,7 @@ int attn_prepare(Kernel kernel, int smem, int dev, int* cache) {
 }
 
 template <typename T, int D>
-int attn_prefix_d(const AttnParams& p, int dev, cudaStream_t s) {
+int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
     using Geo = AttnGeo<T, D>;
     const int rc = attn_prepare(attn_prefix_kernel<T, D>, Geo::SMEM, dev, ready);
@@ -25,7 +25,8 @@ int attn_prefix_d(const AttnParams& p, int dev, cudaStream_t s) {
     const long long blocks = static_cast<long long>(p.prefix_splits) * p.prefix_row_tiles * p.hkv +
                              static_cast<long long>(p.B) * p.hkv * p.own_row_tiles * p.own_splits;
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
-    attn_prefix_kernel<T, D><<<static_cast<unsigned>(blocks), kAttnThreads, Geo::SMEM, s>>>(p);
+    if (overlapped) launch_overlapped(attn_prefix_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::SMEM, s, p);
+    else attn_prefix_kernel<T, D><<<static_cast<unsigned>(blocks), kAttnThreads, Geo::SMEM, s>>>(p);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }
@@ -53,8 +54,8 @@ int attn_join_d(const AttnParams& p, cudaStream_t s) {
 }
 
 template <typename T>
-int launch_attn_prefix(const AttnParams& p, int d, int dev, cudaStream_t s) {
-    return d == 64 ? attn_prefix_d<T, 64>(p, dev, s) : d == 96 ? attn_prefix_d<T, 96>(p, dev, s) : attn_prefix_d<T, 128>(p, dev, s);
+int launch_attn_prefix(const AttnParams& p, int d, int dev, bool o, cudaStream_t s) {
+    return d == 64 ? attn_prefix_d<T, 64>(p, dev, o, s) : d == 96 ? attn_prefix_d<T, 96>(p, dev, o, s) : attn_prefix_d<T, 128>(p, dev, o, s);
 }
 template <typename T>
 int launch_attn_chosen(const AttnParams& p, int d, int dev, cudaStream_t s) {

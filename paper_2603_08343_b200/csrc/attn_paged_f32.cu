@@ -5,7 +5,7 @@ namespace wht_host {
 
 WHT_DEFINE_ATTN_ERROR_READER(take_attn_error_paged_f32)
 
-template int launch_attn_prefix<float>(const AttnParams&, int, int, cudaStream_t);
+template int launch_attn_prefix<float>(const AttnParams&, int, int, bool, cudaStream_t);
 template int launch_attn_chosen<float>(const AttnParams&, int, int, cudaStream_t);
 template int launch_attn_join<float>(const AttnParams&, int, cudaStream_t);
 

@@ -11,6 +11,7 @@ using namespace wht_host;
 using wht::AppendParams;
 using wht::AttnParams;
 using wht::SelectParams;
+using wht::UmmaAttnParams;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 size_t elem(int dtype) { return dtype == WHT_F32 ? 4 : 2; }
@@ -52,11 +53,31 @@ int splits_for(int64_t units, int64_t keys, int dtype, int sms) {
 
 struct PrefixPlan {
     int prefix_rw, prefix_row_tiles, prefix_splits, own_rw, own_row_tiles, own_splits, parts;
+    bool umma;                                  // the prefix on the tcgen05 kernel
+    int umma_splits, umma_row_blocks, same_rows;
     size_t bytes;
 };
 
+constexpr int kUmmaMinRows = 65;   // rows per key head from which the tcgen05 kernel takes the prefix
+constexpr int kUmmaMinKeys = 256;
+
+// Key ranges of the tcgen05 kernel: the number that makes the longest SM's time least, in units of 128-key tiles, a block's set-up
+// and the join of its part counted as kSetUp tiles.
+int umma_splits_for(int64_t units, int64_t tiles, int sms) {
+    constexpr int64_t kSetUp = 4;
+    int64_t best = 1, best_cost = INT64_MAX;
+    for (int64_t n = 1; n <= tiles && n <= 64; ++n) {
+        const int64_t cost = ceil_div(units * n, sms) * (ceil_div(tiles, n) + kSetUp);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = n;
+        }
+    }
+    return static_cast<int>(best);
+}
+
 PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv,
-                       int32_t D, int32_t page, int dtype, int sms) {
+                       int32_t D, int32_t page, int dtype, bool umma_allowed, int sms) {
     PrefixPlan f{};
     const int group = Hq / Hkv;
     const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
@@ -64,12 +85,18 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 16 * f.own_rw));
     f.own_splits = splits_for(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, dtype, sms);
     f.prefix_rw = 1;
-    if (prefix_len > 0) {
+    f.umma = umma_allowed && dtype == WHT_BF16 && T * group >= kUmmaMinRows && prefix_len >= kUmmaMinKeys;
+    if (f.umma) {
+        f.same_rows = T * group <= 128;
+        f.umma_row_blocks = static_cast<int>(ceil_div(T * group, 256));
+        // with the same rows in both tiles a block takes two key tiles at a time
+        f.umma_splits = umma_splits_for(static_cast<int64_t>(Hkv) * f.umma_row_blocks, ceil_div(prefix_len, f.same_rows ? 256 : 128), sms);
+    } else if (prefix_len > 0) {
         f.prefix_rw = row_tiles_per_block(T * group);
         f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 16 * f.prefix_rw));
         f.prefix_splits = splits_for(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, dtype, sms);
     }
-    f.parts = f.prefix_splits + f.own_splits;
+    f.parts = f.prefix_splits + f.own_splits + (f.same_rows ? 2 : 1) * f.umma_splits;
     const size_t rows = static_cast<size_t>(T) * Hq;
     f.bytes = f.parts > 1 ? up256(rows * f.parts * sizeof(float2)) + rows * f.parts * D * sizeof(float) : 0;
     return f;
@@ -146,7 +173,9 @@ size_t wht_attn_prefix_workspace_bytes(int64_t prefix_len, int32_t table_width, 
     if (check_shape(T, Hq, Hkv, D, 0, page, dtype) != WHT_OK || check_batch(T, B, max_q_len, table_width, page, true) != WHT_OK ||
         prefix_len < 0 || device_info(&dev, &sms) != WHT_OK)
         return 0;
-    return plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms).bytes;
+    // either form of the prefix may be taken (the tcgen05 one has conditions that are not known here)
+    return std::max(plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, true, sms).bytes,
+                    plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, false, sms).bytes);
 }
 
 int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k_cache, const void* v_cache,
@@ -166,7 +195,10 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     int dev = 0, sms = 0;
     rc = device_info(&dev, &sms);
     if (rc != WHT_OK) return rc;
-    const PrefixPlan f = plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms);
+    // The tcgen05 kernel finds a row's maximum before it scales (so the scale is positive), and its copies count the
+    // cache's rows in 31 bits.
+    const bool umma_allowed = scale > 0.0f && num_pages * Hkv * page <= 0x7fffffff && num_pages > 0;
+    const PrefixPlan f = plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, umma_allowed, sms);
     if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return WHT_ERR_WORKSPACE;
     AttnParams p{};
     p.q = q; p.k_cache = k_cache; p.v_cache = v_cache;
@@ -183,7 +215,12 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
     p.scale_log2 = scale * wht::kLog2e;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    rc = dtype == WHT_F32 ? launch_attn_prefix<float>(p, D, dev, s) : launch_attn_prefix<__nv_bfloat16>(p, D, dev, s);
+    if (f.umma) {
+        const UmmaAttnParams up{p, f.umma_splits, f.umma_row_blocks, f.same_rows};
+        rc = launch_attn_umma_prefix(up, D, dev, s);
+        if (rc != WHT_OK) return rc;
+    }
+    rc = dtype == WHT_F32 ? launch_attn_prefix<float>(p, D, dev, f.umma, s) : launch_attn_prefix<__nv_bfloat16>(p, D, dev, f.umma, s);
     return rc != WHT_OK ? rc : join(p, dtype, D, s);
 }
 
@@ -241,12 +278,17 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
 
 int wht_attn_device_status(void) {
     unsigned any = 0;
-    for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select}) {
+    for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select,
+                      take_attn_error_umma}) {
         unsigned flag = 0;
         const int rc = take(&flag);
         if (rc != WHT_OK) return rc;
         any |= flag;
     }
+    unsigned waits = 0;
+    const int rc = take_device_error_attn_umma(&waits);
+    if (rc != WHT_OK) return rc;
+    if (waits) any |= wht::kAttnErrWait;
     return any & wht::kAttnErrIndex ? WHT_ERR_DEVICE_INDEX : any ? WHT_ERR_DEVICE_WAIT : WHT_OK;
 }
 

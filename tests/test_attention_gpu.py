@@ -199,6 +199,16 @@ PREFIX = [
     (70, 2, 2, 64, 64, 190, [1] * 70, [(5 * i) % 40 + 1 for i in range(70)]),
     (33, 4, 1, 128, 128, 640, [1] * 33, [(11 * i) % 60 + 1 for i in range(33)]),
     (6, 8, 4, 128, 32, 385, [30, 1, 25, 7, 64, 2], [30, 1, 60, 20, 64, 5]),
+    # rows enough for the tcgen05 kernel: one tile of rows twice, two tiles, more than one block of rows; whole and ragged key tiles
+    (66, 2, 2, 64, 16, 256, [1] * 66, [(3 * i) % 20 for i in range(66)]),
+    (70, 1, 1, 64, 64, 1111, [1] * 70, [1] * 70),
+    (65, 2, 1, 64, 128, 1280, [1] * 65, [2] * 65),
+    (100, 3, 1, 96, 32, 700, [1] * 100, [5] * 100),
+    (65, 1, 1, 96, 128, 300, [1] * 65, [9] * 65),
+    (300, 2, 2, 128, 16, 401, [1] * 300, [3] * 300),
+    (128, 1, 1, 128, 64, 5000, [1] * 128, [3] * 128),
+    (129, 2, 2, 128, 128, 4096, [1] * 129, [2] * 129),
+    (2, 16, 1, 64, 32, 600, [40, 3], [41, 3]),
 ]
 
 
@@ -213,9 +223,13 @@ def test_shared_prefix(A, B, hq, hkv, d, page, prefix, q_lens, kv_lens, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
-def test_shared_prefix_large_scores(A, dtype):
+@pytest.mark.parametrize("B", [9, 70])
+def test_shared_prefix_large_scores(A, dtype, B):
     # scores of both signs in the hundreds: one key takes all the weight, or all weights would underflow without the maximum
-    c = _paged(7, 9, 4, 2, 128, 16, dtype, 300, [1] * 9, [20] * 9, q_scale=40.0)
+    c = _paged(7, B, 4, 2, 128, 16, dtype, 300, [1] * B, [20] * B, q_scale=40.0)
+    # keys that grow along the prefix: the running maximum moves again and again
+    for i, pg in enumerate(c["pre"].tolist()):
+        c["kc"][pg] *= 0.2 + 0.05 * i
     want = R.prefix_attention(c["q"], c["kc"], c["vc"], c["pre"], 300, c["table"], c["lens"], None, 0.5)
     got = _run_prefix(A, c, 300, 0.5).double().cpu()
     assert torch.isfinite(got).all()
