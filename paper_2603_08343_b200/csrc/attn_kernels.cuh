@@ -4,7 +4,7 @@
 //
 // in one pass over the keys: each tile of keys updates the running maximum m, the running sum l and the running
 // product o, which is scaled by exp(m_old - m_new) when the maximum moves.  Rows are (token, query head) pairs that
-// read the same key head; a block (4 warps) takes up to 64 rows and one part of their keys, so each key and value is
+// read the same key head; a group of 2 or 4 warps takes up to 64 rows and one part of their keys, so each key and value is
 // read once for all of the block's rows.  Three kinds of rows use the same loop over a list of physical pages:
 //   prefix   all tokens of the batch against the shared prefix
 //   own      the tokens of one sequence against its own pages, each seeing keys up to its own place
@@ -12,8 +12,8 @@
 //
 // What bounds it: with few rows each key brings 4*D flops a row for 4*D bytes (bf16), far below the machine's
 // balance, so the loop is a stream of keys and values: a ring of kStages tiles filled by 16-byte async copies keeps
-// 64 KB a block in flight.  With 1 row tile (16 rows) the block's four warps take a quarter of each tile's keys each
-// and join their (m, l, o) through shared memory at the end; with 4 row tiles every warp takes all keys for its rows.
+// 64 KB a block in flight.  Warps that share a row tile take their own keys of each tile and join their (m, l, o)
+// through shared memory at the end; with 4 row tiles every warp takes all keys for its rows.
 // Keys are split over blocks where there are too few rows to fill the machine; the parts are joined by attn_join_kernel.
 //
 // Operands: rows of a tile are stored with their 16-byte chunks permuted by the row number (swizzle), so that matrix
@@ -62,18 +62,16 @@ struct UmmaAttnParams {
     int same_rows;   // 128 rows or fewer: both of a block's tiles hold them, each with every second key tile
 };
 
+// Bytes per row, and where a 16-byte chunk of a row lies.
 template <typename T, int D>
-struct AttnGeo {
+struct AttnRow {
     static constexpr bool F32 = std::is_same<T, float>::value;
-    static constexpr int KEYS = F32 ? 32 : 64;            // keys per tile
     static constexpr int ROW_BYTES = D * sizeof(T);
     static constexpr int CHUNKS = ROW_BYTES / 16;         // 16-byte chunks per key
-    static constexpr int TILE_BYTES = KEYS * ROW_BYTES;   // keys (or values) of one tile
-    static constexpr int STAGES = 3;
-    static constexpr int RING_BYTES = STAGES * 2 * TILE_BYTES;
+    static constexpr int BLOCK_KEYS = F32 ? 32 : 64;      // keys per tile, all groups of a block together
+    static constexpr int STAGES = D == 128 ? 3 : D == 96 ? 4 : 6;
+    static constexpr int RING_BYTES = STAGES * 2 * BLOCK_KEYS * ROW_BYTES;  // 96 KB: two blocks per SM
     static constexpr int SMEM = RING_BYTES + kAttnIds * 4;
-    // the join of four warps' results reuses the ring: 4 x 16 rows of D sums, and their maxima and sums
-    static_assert(4 * 16 * (D + 4) * 4 <= RING_BYTES, "join buffer");
     // place of chunk c of row r: the permutation makes 8 consecutive rows' same chunk (bf16), or 4 rows' pairs of
     // chunks (fp32), fall into different banks
     __device__ __forceinline__ static int place(int r, int c) {
@@ -84,6 +82,26 @@ struct AttnGeo {
         return r * ROW_BYTES + ((c ^ x) << 4);
     }
 };
+
+// A group of warps works on one unit.  Up to 16 rows: two warps share the rows and halve the keys, and a block holds two
+// such groups with a unit each (short sequences are all latency: four units in flight per SM instead of two took the own
+// pages of 256 sequences at 32 x 128 heads from OWN_BEFORE to OWN_AFTER).  Up to 32 rows: two row tiles and two key halves.  Up to 64: four row tiles.
+template <typename T, int D, int RW>
+struct AttnGeo : AttnRow<T, D> {
+    static constexpr int KW = RW == 4 ? 1 : 2;            // warps that share a row tile, each with its own keys of a tile
+    static constexpr int THREADS = 32 * RW * KW;
+    static constexpr int GROUPS = kAttnThreads / THREADS;
+    static constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS / GROUPS;   // keys per tile
+    static constexpr int TILE_BYTES = KEYS * AttnRow<T, D>::ROW_BYTES;  // keys (or values) of one tile
+    static constexpr int GROUP_RING = AttnRow<T, D>::RING_BYTES / GROUPS;
+    static constexpr int IDS = kAttnIds / GROUPS;
+    // the join of the warps' results reuses the ring: 16 rows of D sums per warp, and their maxima and sums
+    static_assert(RW * KW * 16 * (D + 4) * 4 <= GROUP_RING, "join buffer");
+};
+__host__ __device__ constexpr int attn_groups(int rw) { return rw == 1 ? 2 : 1; }
+__device__ __forceinline__ void attn_group_sync(int group, int threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+}
 
 // One block's work.
 struct AttnUnit {
@@ -100,19 +118,20 @@ struct AttnUnit {
 };
 
 template <typename T, int D, int RW>
-__device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& u, unsigned char* smem) {
-    using Geo = AttnGeo<T, D>;
+__device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& u, unsigned char* block_smem) {
+    using Geo = AttnGeo<T, D, RW>;
     constexpr bool F32 = Geo::F32;
-    constexpr int KW = 4 / RW;                   // warps that share a row tile, each with its own keys of a tile
+    constexpr int KW = Geo::KW, THREADS = Geo::THREADS;
     constexpr int WKEYS = Geo::KEYS / KW;        // keys of a tile per warp
     constexpr int NT = WKEYS / 8;                // score tiles of 8 keys
     constexpr int DT = D / 8;                    // output tiles of 8 channels
     constexpr int KSTEP = F32 ? 8 : 16;          // contraction length of one instruction
     constexpr int QS = D / KSTEP;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS, lane = tid & 31, warp = tid >> 5;
     const int rt = warp / KW, kw = warp % KW;
     const int r4 = lane >> 2, c4 = lane & 3;
-    int32_t* ids = reinterpret_cast<int32_t*>(smem + Geo::RING_BYTES);
+    unsigned char* smem = block_smem + group * Geo::GROUP_RING;
+    int32_t* ids = reinterpret_cast<int32_t*>(block_smem + Geo::RING_BYTES) + group * Geo::IDS;
     const uint32_t ring = attn_smem_u32(smem);
     const T* kc = static_cast<const T*>(p.k_cache);
     const T* vc = static_cast<const T*>(p.v_cache);
@@ -164,7 +183,7 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
     const int ids0 = u.key0 >> p.page_shift;     // list entry of ids[0]
     int ids_base = ids0;
     auto load_ids = [&](int base) {              // all threads; the caller synchronises around it
-        for (int i = tid; i < kAttnIds; i += kAttnThreads) {
+        for (int i = tid; i < Geo::IDS; i += THREADS) {
             const int e = base + i;
             int32_t pg = -1;
             if (e < u.list) {
@@ -181,8 +200,8 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
     auto load_tile = [&](int t) {                // keys and values of tile t into ring slot t % STAGES
         const uint32_t kd = ring + (t % Geo::STAGES) * 2 * Geo::TILE_BYTES, vd = kd + Geo::TILE_BYTES;
 #pragma unroll
-        for (int i = 0; i < Geo::KEYS * Geo::CHUNKS / kAttnThreads; ++i) {
-            const int j = tid + i * kAttnThreads;
+        for (int i = 0; i < Geo::KEYS * Geo::CHUNKS / THREADS; ++i) {
+            const int j = tid + i * THREADS;
             const int r = j / Geo::CHUNKS, c = j % Geo::CHUNKS;
             const int key = u.key0 + t * Geo::KEYS + r;
             int64_t off = 0;
@@ -202,7 +221,7 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
     };
 
     load_ids(ids0);
-    __syncthreads();
+    attn_group_sync(group, THREADS);
 #pragma unroll
     for (int s = 0; s < Geo::STAGES - 1; ++s) {
         if (s < tiles) load_tile(s);
@@ -210,15 +229,15 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
     }
     for (int t = 0; t < tiles; ++t) {
         cp_async_wait<Geo::STAGES - 2>();
-        __syncthreads();                         // tile t has arrived, and everyone is done with tile t - 1
+        attn_group_sync(group, THREADS);                         // tile t has arrived, and everyone is done with tile t - 1
         const int next = t + Geo::STAGES - 1;
         if (next < tiles) {
             // the list moves on when the next tile's last key leaves the entries that are held
             const int last = min(u.key1 - 1, u.key0 + (next + 1) * Geo::KEYS - 1) >> p.page_shift;
-            if (last >= ids_base + kAttnIds) {
+            if (last >= ids_base + Geo::IDS) {
                 ids_base = (u.key0 + next * Geo::KEYS) >> p.page_shift;
                 load_ids(ids_base);
-                __syncthreads();
+                attn_group_sync(group, THREADS);
             }
             load_tile(next);
         }
@@ -365,9 +384,9 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
 
     if constexpr (KW > 1) {
         // join the warps that share rows: everyone stores (m, l, o), then the block's threads add them up
-        __syncthreads();
+        attn_group_sync(group, THREADS);
         float* jo = reinterpret_cast<float*>(smem);           // [warp][16][D]
-        float2* jm = reinterpret_cast<float2*>(jo + 4 * 16 * D);  // [warp][16]
+        float2* jm = reinterpret_cast<float2*>(jo + RW * KW * 16 * D);  // [warp][16]
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = r4 + 8 * i;
@@ -376,9 +395,9 @@ __device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& 
                 *reinterpret_cast<float2*>(jo + (warp * 16 + r) * D + d * 8 + 2 * c4) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
             if (c4 == 0) jm[warp * 16 + r] = make_float2(m[i], l[i]);
         }
-        __syncthreads();
+        attn_group_sync(group, THREADS);
         constexpr int PER = 4;                                 // channels per thread and step
-        for (int j = tid; j < RW * 16 * (D / PER); j += kAttnThreads) {
+        for (int j = tid; j < RW * 16 * (D / PER); j += THREADS) {
             const int r = j / (D / PER), d = (j % (D / PER)) * PER;
             const int rr = u.row0 + r;
             if (rr >= u.rows) continue;
@@ -501,12 +520,16 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kAttnThreads)
 attn_prefix_kernel(const AttnParams p) {
     extern __shared__ __align__(128) unsigned char smem_attn[];
-    constexpr int KEYS = AttnGeo<T, D>::KEYS;
-    const int prefix_blocks = p.prefix_splits * p.prefix_row_tiles * p.hkv;
+    constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS;
+    const int prefix_units = p.prefix_splits * p.prefix_row_tiles * p.hkv;
+    const int prefix_groups = attn_groups(p.prefix_rw);
+    const int prefix_blocks = (prefix_units + prefix_groups - 1) / prefix_groups;
     AttnUnit u;
     int b = blockIdx.x;
     grid_launch_dependents();
     if (b < prefix_blocks) {
+        b = b * prefix_groups + static_cast<int>(threadIdx.x) / (kAttnThreads / prefix_groups);
+        if (b >= prefix_units) return;
         u.part = b % p.prefix_splits;
         b /= p.prefix_splits;
         u.row0 = (b % p.prefix_row_tiles) * 16 * p.prefix_rw;
@@ -523,7 +546,9 @@ attn_prefix_kernel(const AttnParams p) {
         attn_block_rw<T, D>(p.prefix_rw, p, u, smem_attn);
         return;
     }
-    b -= prefix_blocks;
+    const bool last_block = blockIdx.x == gridDim.x - 1;
+    const int own_groups = attn_groups(p.own_rw);
+    b = (b - prefix_blocks) * own_groups + static_cast<int>(threadIdx.x) / (kAttnThreads / own_groups);
     const int split = b % p.own_splits;
     b /= p.own_splits;
     u.part = (p.parts - p.own_splits) + split;
@@ -531,15 +556,20 @@ attn_prefix_kernel(const AttnParams p) {
     b /= p.own_row_tiles;
     u.head = b % p.hkv;
     const int seq = b / p.hkv;
-    int count;
-    attn_tokens(p, seq, u.token0, count);
+    if (seq < p.B) {
+        // the table's row is wanted as soon as the length is known: fetch it meanwhile
+        u.ids = p.page_table + static_cast<int64_t>(seq) * p.table_width;
+        const int ahead = (static_cast<int>(threadIdx.x) & 31) * 32;
+        if (ahead < p.table_width) asm volatile("prefetch.global.L1 [%0];" ::"l"(u.ids + ahead));
+    }
+    int count = 0;
+    if (seq < p.B) attn_tokens(p, seq, u.token0, count);
     u.rows = count * p.group;
     if (u.row0 >= u.rows) {
-        if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
+        if (last_block) grid_dependency_wait();
         return;
     }
     const int keys = attn_length(p, seq);
-    u.ids = p.page_table + static_cast<int64_t>(seq) * p.table_width;
     u.table = nullptr;
     u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
     // the block's last row sees the most: nothing beyond its place is read
@@ -551,7 +581,7 @@ attn_prefix_kernel(const AttnParams p) {
     attn_block_rw<T, D>(p.own_rw, p, u, smem_attn);
     // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
     // for this grid alone, so this grid does not end before that one has.
-    if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
+    if (last_block) grid_dependency_wait();
 }
 
 // The sequence that token t belongs to (q_start ascending): 32 lanes probe at once.
@@ -576,17 +606,19 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kAttnThreads)
 attn_chosen_kernel(const AttnParams p) {
     extern __shared__ __align__(128) unsigned char smem_attn[];
-    constexpr int KEYS = AttnGeo<T, D>::KEYS;
+    constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS;
     AttnUnit u;
     grid_dependency_wait();  // the list comes from the kernel before
     grid_launch_dependents();
-    int64_t b = blockIdx.x;
+    const int groups = attn_groups(p.own_rw);
+    int64_t b = static_cast<int64_t>(blockIdx.x) * groups + static_cast<int>(threadIdx.x) / (kAttnThreads / groups);
     u.part = static_cast<int>(b % p.own_splits);
     b /= p.own_splits;
     u.row0 = static_cast<int>(b % p.own_row_tiles) * 16 * p.own_rw;
     b /= p.own_row_tiles;
     u.head = static_cast<int>(b % p.hkv);
     u.token0 = b / p.hkv;
+    if (u.token0 >= p.T) return;
     u.rows = p.group;
     const int seq = attn_sequence_of(p, u.token0);
     int64_t first;

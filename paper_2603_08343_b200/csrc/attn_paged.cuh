@@ -19,11 +19,13 @@ int attn_prepare(Kernel kernel, int smem, int dev, int* cache) {
 template <typename T, int D>
 int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnGeo<T, D>;
+    using Geo = AttnRow<T, D>;
     const int rc = attn_prepare(attn_prefix_kernel<T, D>, Geo::SMEM, dev, ready);
     if (rc != WHT_OK) return rc;
-    const long long blocks = static_cast<long long>(p.prefix_splits) * p.prefix_row_tiles * p.hkv +
-                             static_cast<long long>(p.B) * p.hkv * p.own_row_tiles * p.own_splits;
+    const long long prefix_units = static_cast<long long>(p.prefix_splits) * p.prefix_row_tiles * p.hkv;
+    const long long own_units = static_cast<long long>(p.B) * p.hkv * p.own_row_tiles * p.own_splits;
+    if (prefix_units > 0x3fffffffll || own_units > 0x3fffffffll) return WHT_ERR_BAD_T;
+    const long long blocks = ceil_div(prefix_units, attn_groups(p.prefix_rw)) + ceil_div(own_units, attn_groups(p.own_rw));
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     if (overlapped) launch_overlapped(attn_prefix_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::SMEM, s, p);
     else attn_prefix_kernel<T, D><<<static_cast<unsigned>(blocks), kAttnThreads, Geo::SMEM, s>>>(p);
@@ -34,10 +36,10 @@ int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s)
 template <typename T, int D>
 int attn_chosen_d(const AttnParams& p, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnGeo<T, D>;
+    using Geo = AttnRow<T, D>;
     const int rc = attn_prepare(attn_chosen_kernel<T, D>, Geo::SMEM, dev, ready);
     if (rc != WHT_OK) return rc;
-    const long long blocks = static_cast<long long>(p.T) * p.hkv * p.own_row_tiles * p.own_splits;
+    const long long blocks = ceil_div(static_cast<long long>(p.T) * p.hkv * p.own_row_tiles * p.own_splits, attn_groups(p.own_rw));
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     launch_overlapped(attn_chosen_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::SMEM, s, p);
     WHT_CUDA_TRY(cudaGetLastError());

@@ -81,6 +81,29 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
         : "memory");
 }
 
+// ---- two fp32 values in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // one lane's row of weights
 struct SoftmaxRow {
     float m = 0.0f;  // reference maximum, in units of the raw scores
@@ -140,16 +163,26 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
     {
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q);
         constexpr int CH = Geo::HALVES * 8;
-        for (int i = tid; i < 256 * CH; i += kUmmaAttnThreads) {
-            const int r = i / CH, c = i % CH;
-            const int row = row0 + (same ? r & 127 : r);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (row < rows && c * 8 < D) {
-                const int tok = row / p.group;
-                v = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh) + c);
+        // eight chunks a thread at a time, all loads in flight
+        constexpr int BATCH = 8;
+        for (int i0 = tid; i0 < 256 * CH; i0 += BATCH * kUmmaAttnThreads) {
+            uint4 v[BATCH];
+#pragma unroll
+            for (int e = 0; e < BATCH; ++e) {
+                const int i = i0 + e * kUmmaAttnThreads, r = i / CH, c = i % CH;
+                const int row = row0 + (same ? r & 127 : r);
+                v[e] = make_uint4(0, 0, 0, 0);
+                if (i < 256 * CH && row < rows && c * 8 < D) {
+                    const int tok = row / p.group;
+                    v[e] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh) + c);
+                }
             }
-            unsigned char* dst = smem + (r >> 7) * Geo::TILE + (c >> 3) * Geo::BOX + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-            *reinterpret_cast<uint4*>(dst) = v;
+#pragma unroll
+            for (int e = 0; e < BATCH; ++e) {
+                const int i = i0 + e * kUmmaAttnThreads, r = i / CH, c = i % CH;
+                unsigned char* dst = smem + (r >> 7) * Geo::TILE + (c >> 3) * Geo::BOX + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+                if (i < 256 * CH) *reinterpret_cast<uint4*>(dst) = v[e];
+            }
         }
         fence_async_smem();
     }
@@ -275,9 +308,9 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
             }
             float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < 128; c += 4)
+            for (int c = 0; c < 128; c += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], __uint_as_float(x[c + e]));
+                for (int e = 0; e < 4; ++e) top[e] = max3(top[e], __uint_as_float(x[c + e]), __uint_as_float(x[c + 4 + e]));
             const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             if (i == 0) {
                 st.m = mx;
@@ -303,25 +336,27 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                     tmem_wait_st();
                 }
             }
-            const float off = -st.m * sl;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint64_t off2 = pair(-st.m * sl, -st.m * sl), sl2 = pair(sl, sl);
+            uint64_t sum[2] = {0, 0};
 #pragma unroll
             for (int c = 0; c < 128; c += 32) {
                 uint32_t y[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float v[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        v[q] = exp2_fast(fmaf(__uint_as_float(x[c + e + q]), sl, off));
-                        sum[q] += v[q];
-                    }
-                    y[e / 2] = pack_bf16x2(v[0], v[1]);
-                    y[e / 2 + 1] = pack_bf16x2(v[2], v[3]);
+                for (int e = 0; e < 32; e += 2) {
+                    float a, b;
+                    unpair(fma2(pair(__uint_as_float(x[c + e]), __uint_as_float(x[c + e + 1])), sl2, off2), a, b);
+                    a = exp2_fast(a);
+                    b = exp2_fast(b);
+                    sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(a, b));
+                    y[e / 2] = pack_bf16x2(a, b);
                 }
                 tmem_st16(s_cols + c / 2, y);
             }
-            st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            {
+                float a, b;
+                unpair(add2(sum[0], sum[1]), a, b);
+                st.l += a + b;
+            }
             if (valid < 128) {
                 // the tile's last rows hold keys that nobody sees, or nothing at all: their values become 0 so that a
                 // weight of 0 takes nothing from them

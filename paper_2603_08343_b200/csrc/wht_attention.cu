@@ -43,12 +43,13 @@ int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, in
 int row_tiles_per_block(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 int keys_per_tile(int dtype) { return dtype == WHT_F32 ? 32 : 64; }
 
-// How many blocks the keys of `units` row sets are divided over: enough to occupy two blocks on every SM, but no
-// block with fewer than four tiles (its own set-up and the join of its part would cost more than they save).
-int splits_for(int64_t units, int64_t keys, int dtype, int sms) {
+// How many groups the keys of `units` row sets are divided over: enough to fill every SM (two blocks of one group, or of two
+// where a group is two warps), but none with fewer than two 64-key tiles (its own set-up and the join of its part would cost
+// more than they save).
+int splits_for(int64_t units, int64_t keys, int rw, int dtype, int sms) {
     const int64_t tiles = ceil_div(keys, keys_per_tile(dtype));
-    const int64_t want = units > 0 ? (2 * sms) / units : 1;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, tiles / 4)));
+    const int64_t want = units > 0 ? (2 * wht::attn_groups(rw) * sms) / units : 1;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, tiles / 2)));
 }
 
 struct PrefixPlan {
@@ -83,7 +84,7 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
     f.own_rw = row_tiles_per_block(own_rows);
     f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 16 * f.own_rw));
-    f.own_splits = splits_for(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, dtype, sms);
+    f.own_splits = splits_for(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, f.own_rw, dtype, sms);
     f.prefix_rw = 1;
     f.umma = umma_allowed && dtype == WHT_BF16 && T * group >= kUmmaMinRows && prefix_len >= kUmmaMinKeys;
     if (f.umma) {
@@ -94,7 +95,7 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     } else if (prefix_len > 0) {
         f.prefix_rw = row_tiles_per_block(T * group);
         f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 16 * f.prefix_rw));
-        f.prefix_splits = splits_for(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, dtype, sms);
+        f.prefix_splits = splits_for(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, f.prefix_rw, dtype, sms);
     }
     f.parts = f.prefix_splits + f.own_splits + (f.same_rows ? 2 : 1) * f.umma_splits;
     const size_t rows = static_cast<size_t>(T) * Hq;
@@ -112,7 +113,7 @@ SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t H
     const int group = Hq / Hkv;
     f.rw = row_tiles_per_block(group);
     f.row_tiles = static_cast<int>(ceil_div(group, 16 * f.rw));
-    f.splits = splits_for(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, dtype, sms);
+    f.splits = splits_for(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, f.rw, dtype, sms);
     f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
     const size_t rows = static_cast<size_t>(T) * Hq;
     f.bytes = f.scores_bytes + (f.splits > 1 ? up256(rows * f.splits * sizeof(float2)) + rows * f.splits * D * sizeof(float) : 0);
