@@ -1,7 +1,9 @@
-// Device helpers shared by the serving-attention kernels: the error word, 16-byte async copies into swizzled
-// shared memory, matrix fragments, element conversion.
+// Device helpers shared by the serving-attention kernels: the error word, tiled copies into swizzled shared memory,
+// matrix fragments.
 #pragma once
-#include "wht_common.cuh"
+#include <cuda.h>
+
+#include "mma_pipe_kernels.cuh"
 
 namespace wht {
 
@@ -12,18 +14,12 @@ constexpr unsigned int kAttnErrIndex = 1, kAttnErrWait = 2;
 
 __device__ __forceinline__ void attn_report(unsigned int what) { atomicOr(&g_attn_device_error, what); }
 
-// ---- asynchronous 16-byte copies; src_bytes = 0 fills the destination with zeros and reads nothing ----
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ uint32_t attn_smem_u32(const void* p) {
-    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+// Copy of one box of a 2-D tensor map, counted on `bar`.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+        : "memory");
 }
 
 // ---- matrix fragments ----
@@ -48,6 +44,12 @@ __device__ __forceinline__ void mma_tf32_1688(float (&d)[4], const uint32_t (&a)
         "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 8x8 block of 16-bit values, a row per quad of lanes: transposed
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 // x = hi + lo, both of 11 significant bits; what is lost is below 2^-22 |x|.
 __device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {

@@ -1,5 +1,7 @@
 // Host-side pieces shared by the serving-attention translation units: launch functions and the split of work.
 #pragma once
+#include <cuda.h>
+
 #include "../../include/wht_attention.h"
 #include "host_common.h"
 
@@ -12,6 +14,8 @@ struct UmmaAttnParams;
 
 namespace wht_host {
 
+// attn_tma.cu: the caches as [num_pages * Hkv * page] rows of d channels, copied in boxes of box_rows rows by 128 bytes
+int cache_maps(CUtensorMap* k_map, CUtensorMap* v_map, const wht::AttnParams& p, int d, int dtype, int box_rows);
 // attn_append.cu
 int launch_append(wht::AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s);
 // attn_paged.cuh, instantiated per storage type in attn_paged_bf16.cu and attn_paged_f32.cu
@@ -29,7 +33,10 @@ int take_attn_error_paged_bf16(unsigned* flag);
 int take_attn_error_paged_f32(unsigned* flag);
 int take_attn_error_select(unsigned* flag);
 int take_attn_error_umma(unsigned* flag);
-int take_device_error_attn_umma(unsigned* flag);  // expired waits
+// expired waits
+int take_device_error_attn_umma(unsigned* flag);
+int take_device_error_attn_paged_bf16(unsigned* flag);
+int take_device_error_attn_paged_f32(unsigned* flag);
 
 // Defines one of the readers above in the translation unit that includes the kernels.
 #define WHT_DEFINE_ATTN_ERROR_READER(name)                                                            \

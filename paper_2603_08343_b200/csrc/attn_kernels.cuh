@@ -1,26 +1,32 @@
 // Attention of a few rows over a list of pages, by warp-level matrix products.
 //
-//     o = sum_j p_j v_j / sum_j p_j,    p_j = exp(scale q.k_j - m),   m = max_j scale q.k_j
+//     o = sum_j p_j v_j / sum_j p_j,    p_j = exp(scale q.k_j - m)
 //
-// in one pass over the keys: each tile of keys updates the running maximum m, the running sum l and the running
-// product o, which is scaled by exp(m_old - m_new) when the maximum moves.  Rows are (token, query head) pairs that
-// read the same key head; a group of 2 or 4 warps takes up to 64 rows and one part of their keys, so each key and value is
-// read once for all of the block's rows.  Three kinds of rows use the same loop over a list of physical pages:
+// in one pass over the keys: each chunk of 16 keys updates the running reference maximum m, the running sum l and the
+// running product o.  Rows are (token, query head) pairs that read the same key head.  Three kinds of rows use the same
+// loop over a list of physical pages:
 //   prefix   all tokens of the batch against the shared prefix
 //   own      the tokens of one sequence against its own pages, each seeing keys up to its own place
 //   chosen   one token against the pages selected for it
 //
-// What bounds it: with few rows each key brings 4*D flops a row for 4*D bytes (bf16), far below the machine's
-// balance, so the loop is a stream of keys and values: a ring of kStages tiles filled by 16-byte async copies keeps
-// 64 KB a block in flight.  Warps that share a row tile take their own keys of each tile and join their (m, l, o)
-// through shared memory at the end; with 4 row tiles every warp takes all keys for its rows.
-// Keys are split over blocks where there are too few rows to fill the machine; the parts are joined by attn_join_kernel.
+// What bounds it: with few rows each key brings 4*D flops a row for 4*D bytes (bf16), far below the machine's balance,
+// so the loop has to be a stream of keys and values with as few instructions per byte as possible.  (A first version
+// with rows as the left operand and 16-byte copies by all threads issued 1640 warp instructions per 16 KB and was bound by
+// them at 4.1 TB/s: half of a 16-row operand empty, two thirds of the instructions addresses of copies.)  Hence:
+//   - Products are taken transposed, S^T = K Q^T and O^T = V^T P^T: keys and channels fill the 16-row operand and the rows sit
+//     on the 8-column one, so 8 rows waste nothing.  P^T changes from accumulator to operand layout by one 8x8 transposition.
+//   - Each warp streams its own chunks: one lane asks the copy engine (TMA, 128-byte swizzle) for the key and value boxes
+//     of a chunk, and a ring of chunks per warp keeps up to 24 KB in flight; no warp waits for another in the loop.
+//   - m moves only when a score passes it by more than 2^8, found by one vote: weights up to 2^8 are as exact as weights up to 1, and
+//     neither the reduction over lanes nor the scaling of o is in the common path.
+// A unit's keys are divided over 1, 2 or 4 warps of a block, which join their (m, l, o) through shared memory, and over
+// blocks where there are too few units to fill the machine (attn_join_kernel adds those parts up).
 //
-// Operands: rows of a tile are stored with their 16-byte chunks permuted by the row number (swizzle), so that matrix
-// loads touch all banks.  The score accumulators' layout is the layout of the next product's left operand, so the
-// weights never leave registers.  fp32 tensors: both operands of each product are split in two tf32 terms
-// (three products, what is dropped is below 2^-21 relative), contraction indices paired so that a thread's two values are neighbours.
+// fp32 tensors: both operands of each product are split in two tf32 terms (three products; what is dropped is below 2^-21
+// relative), contraction indices paired so that a thread's two values are neighbours.
 #pragma once
+#include <cuda.h>
+
 #include <type_traits>
 
 #include "attn_common.cuh"
@@ -28,7 +34,8 @@
 namespace wht {
 
 constexpr int kAttnThreads = 128;
-constexpr int kAttnIds = 512;  // pages of a block's list that are held at a time
+constexpr int kChunk = 16;       // keys per chunk: they lie in one page
+constexpr float kSlack = 8.0f;   // log2 of how far a score may pass the reference maximum
 
 struct AttnParams {
     const void *q, *k_cache, *v_cache;
@@ -41,11 +48,11 @@ struct AttnParams {
     // shared prefix
     const int32_t* prefix_pages;
     int64_t prefix_len;
-    int prefix_splits, prefix_row_tiles, prefix_rw;  // rw: row tiles of 16 per block
+    int prefix_splits, prefix_row_tiles, prefix_nr, prefix_wpu;  // nr: 8-row tiles per unit; wpu: warps per unit
     // own pages
     const int32_t *page_table, *kv_lens, *q_start;
     int table_width, B, max_q_len;
-    int own_splits, own_row_tiles, own_rw;
+    int own_splits, own_row_tiles, own_nr, own_wpu;
     // chosen pages: [T x Hkv x select] indices into the sequence's table
     const int32_t* chosen;
     int select;
@@ -62,411 +69,369 @@ struct UmmaAttnParams {
     int same_rows;   // 128 rows or fewer: both of a block's tiles hold them, each with every second key tile
 };
 
-// Bytes per row, and where a 16-byte chunk of a row lies.
 template <typename T, int D>
-struct AttnRow {
+struct AttnGeo {
     static constexpr bool F32 = std::is_same<T, float>::value;
-    static constexpr int ROW_BYTES = D * sizeof(T);
-    static constexpr int CHUNKS = ROW_BYTES / 16;         // 16-byte chunks per key
-    static constexpr int BLOCK_KEYS = F32 ? 32 : 64;      // keys per tile, all groups of a block together
-    static constexpr int STAGES = D == 128 ? 3 : D == 96 ? 4 : 6;
-    static constexpr int RING_BYTES = STAGES * 2 * BLOCK_KEYS * ROW_BYTES;  // 96 KB: two blocks per SM
-    static constexpr int SMEM = RING_BYTES + kAttnIds * 4;
-    // place of chunk c of row r: the permutation makes 8 consecutive rows' same chunk (bf16), or 4 rows' pairs of
-    // chunks (fp32), fall into different banks
-    __device__ __forceinline__ static int place(int r, int c) {
-        int x;
-        if constexpr (F32) x = ((r & 3) ^ ((r >> 2) & 1)) << 1;
-        else if constexpr (D == 96) x = (r >> 1) & 3;
-        else x = r & 7;
-        return r * ROW_BYTES + ((c ^ x) << 4);
-    }
+    static constexpr int BOX_CH = 128 / static_cast<int>(sizeof(T));    // channels per 128-byte box
+    static constexpr int BOXES = (D + BOX_CH - 1) / BOX_CH;             // per key row (the last may reach over the row's end: zeros)
+    static constexpr int BOX_BYTES = kChunk * 128;
+    static constexpr int SIDE = BOXES * BOX_BYTES;                      // keys (or values) of a chunk
+    static constexpr int STAGES = 2 * SIDE >= 16384 ? 2 : 24576 / (2 * SIDE);
+    static constexpr int RING = STAGES * 2 * SIDE;                      // per warp
+    static constexpr int OFF_BARS = 4 * RING;
+    static constexpr int BYTES = OFF_BARS + 4 * STAGES * 8 + 1024;      // and what aligning the start to 1024 bytes takes
+    static constexpr int JOIN_LD = D + 4;                               // floats per row of the join buffer: no bank conflicts
+    static_assert(32 * (JOIN_LD + 2) * 4 <= RING, "the join buffer reuses the ring");
+    // byte offset of 16-byte piece c of row r (the copy engine's 128-byte swizzle)
+    __device__ __forceinline__ static int place(int r, int c) { return (c >> 3) * BOX_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 };
 
-// A group of warps works on one unit.  Up to 16 rows: two warps share the rows and halve the keys, and a block holds two
-// such groups with a unit each (short sequences are all latency: four units in flight per SM instead of two took the own
-// pages of 256 sequences at 32 x 128 heads from OWN_BEFORE to OWN_AFTER).  Up to 32 rows: two row tiles and two key halves.  Up to 64: four row tiles.
-template <typename T, int D, int RW>
-struct AttnGeo : AttnRow<T, D> {
-    static constexpr int KW = RW == 4 ? 1 : 2;            // warps that share a row tile, each with its own keys of a tile
-    static constexpr int THREADS = 32 * RW * KW;
-    static constexpr int GROUPS = kAttnThreads / THREADS;
-    static constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS / GROUPS;   // keys per tile
-    static constexpr int TILE_BYTES = KEYS * AttnRow<T, D>::ROW_BYTES;  // keys (or values) of one tile
-    static constexpr int GROUP_RING = AttnRow<T, D>::RING_BYTES / GROUPS;
-    static constexpr int IDS = kAttnIds / GROUPS;
-    // the join of the warps' results reuses the ring: 16 rows of D sums per warp, and their maxima and sums
-    static_assert(RW * KW * 16 * (D + 4) * 4 <= GROUP_RING, "join buffer");
-};
-__host__ __device__ constexpr int attn_groups(int rw) { return rw == 1 ? 2 : 1; }
-__device__ __forceinline__ void attn_group_sync(int group, int threads) {
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
-}
-
-// One block's work.
+// One unit of work.
 struct AttnUnit {
     int head;            // key head
     int64_t token0;      // first token of the row set
     int rows;            // rows of the set: row r = (token0 + r / group, head * group + r % group)
-    int row0;            // first row of this block
+    int row0;            // first row of this unit
     const int32_t* ids;  // page list: physical pages, or (chosen) indices into `table`
     const int32_t* table;
     int list;            // entries of the list
-    int key0, key1;      // this part's keys, counted along the list
+    int key0, key1;      // this part's keys, counted along the list; key0 a multiple of 16
     int limit0, step;    // row r sees keys < min(key1, limit0 + (r / group) * step)
     int part;            // where the partial result goes
+    int nr, wpu;         // 8-row tiles, warps
 };
 
-template <typename T, int D, int RW>
-__device__ __forceinline__ void attn_block(const AttnParams& p, const AttnUnit& u, unsigned char* block_smem) {
-    using Geo = AttnGeo<T, D, RW>;
+template <typename T, int D, int NR>
+__device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map,
+                                          unsigned char* smem) {
+    using Geo = AttnGeo<T, D>;
     constexpr bool F32 = Geo::F32;
-    constexpr int KW = Geo::KW, THREADS = Geo::THREADS;
-    constexpr int WKEYS = Geo::KEYS / KW;        // keys of a tile per warp
-    constexpr int NT = WKEYS / 8;                // score tiles of 8 keys
-    constexpr int DT = D / 8;                    // output tiles of 8 channels
-    constexpr int KSTEP = F32 ? 8 : 16;          // contraction length of one instruction
-    constexpr int QS = D / KSTEP;
-    const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS, lane = tid & 31, warp = tid >> 5;
-    const int rt = warp / KW, kw = warp % KW;
+    constexpr int QS = D / (F32 ? 8 : 16);       // steps of the first product
+    constexpr int DT = D / 16;                   // 16-channel tiles of the output
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int wi = warp % u.wpu;                 // this warp among the unit's
     const int r4 = lane >> 2, c4 = lane & 3;
-    unsigned char* smem = block_smem + group * Geo::GROUP_RING;
-    int32_t* ids = reinterpret_cast<int32_t*>(block_smem + Geo::RING_BYTES) + group * Geo::IDS;
-    const uint32_t ring = attn_smem_u32(smem);
-    const T* kc = static_cast<const T*>(p.k_cache);
-    const T* vc = static_cast<const T*>(p.v_cache);
-    const int tiles = (u.key1 - u.key0 + Geo::KEYS - 1) / Geo::KEYS;
+    unsigned char* ring = smem + warp * Geo::RING;
+    const uint32_t ring_u32 = smem_u32(ring);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + Geo::OFF_BARS) + warp * Geo::STAGES;
+    const int all = (u.key1 - u.key0 + kChunk - 1) / kChunk;
+    const int chunks = all > wi ? (all - wi + u.wpu - 1) / u.wpu : 0;   // this warp's: wi, wi + wpu, ...
 
-    // this thread's two rows (r4 and r4 + 8 of the warp's tile)
-    int row[2], limit[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        row[i] = u.row0 + rt * 16 + r4 + 8 * i;
-        const int tok = row[i] / p.group;
-        limit[i] = row[i] < u.rows ? min(u.key1, u.limit0 + tok * u.step) : 0;
+    if (lane == 0) {
+        for (int s = 0; s < Geo::STAGES; ++s) mbar_init(full + s, 1);
+        fence_mbar_init();
     }
-    // the least limit of the block's rows: tiles that end before it need no mask
-    const int free_keys = min(u.key1, u.limit0 + (u.row0 / p.group) * u.step);
-
-    uint32_t qf[QS][4];
-    {
-        const T* q = static_cast<const T*>(p.q);
-        const T* src[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int tok = row[i] / p.group;
-            src[i] = q + (u.token0 + tok) * p.q_st + (static_cast<int64_t>(u.head) * p.group + (row[i] - tok * p.group)) * p.q_sh;
+    // cache rows of 32 of this warp's chunks, one per lane, and of the next 32
+    auto rows_of = [&](int j) {
+        const int key = u.key0 + (wi + (j + lane) * u.wpu) * kChunk;
+        int y = 0;
+        if (j + lane < chunks) {
+            int pg = __ldg(u.ids + (key >> p.page_shift));
+            if (u.table) pg = pg >= 0 ? __ldg(u.table + pg) : -1;
+            if (pg < 0 || pg >= p.num_pages) {
+                attn_report(kAttnErrIndex);
+                pg = 0;
+            }
+            y = ((pg * p.hkv + u.head) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
         }
+        return y;
+    };
+    int y_now = rows_of(0), y_next = chunks > 32 ? rows_of(32) : 0;
+    __syncwarp();
+    auto load = [&](int j, int y) {              // lane 0: chunk j, whose first cache row is y
+        const int s = j % Geo::STAGES;
+        const uint32_t dst = ring_u32 + s * 2 * Geo::SIDE;
+        mbar_expect_tx(full + s, 2 * Geo::SIDE);
+#pragma unroll
+        for (int b = 0; b < Geo::BOXES; ++b) {
+            tma_load_2d(dst + b * Geo::BOX_BYTES, k_map, b * Geo::BOX_CH, y, full + s);
+            tma_load_2d(dst + Geo::SIDE + b * Geo::BOX_BYTES, v_map, b * Geo::BOX_CH, y, full + s);
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < Geo::STAGES; ++j) {
+        const int y = __shfl_sync(kFullMask, y_now, j);
+        if (lane == 0 && j < chunks) load(j, y);
+    }
+
+    // rows as the second operand: column r4 of 8-row tile n is row row0 + 8 n + r4
+    uint32_t qf[NR][QS][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        const int row = u.row0 + 8 * n + r4, tok = row / p.group;
+        const T* src = static_cast<const T*>(p.q) + (u.token0 + tok) * p.q_st +
+                       (static_cast<int64_t>(u.head) * p.group + (row - tok * p.group)) * p.q_sh;
 #pragma unroll
         for (int s = 0; s < QS; ++s) {
             if constexpr (F32) {
                 // contraction index c stands for channel 2c, c + 4 for 2c + 1
-                const float2 a = row[0] < u.rows ? *reinterpret_cast<const float2*>(src[0] + s * 8 + 2 * c4) : make_float2(0.f, 0.f);
-                const float2 b = row[1] < u.rows ? *reinterpret_cast<const float2*>(src[1] + s * 8 + 2 * c4) : make_float2(0.f, 0.f);
-                qf[s][0] = __float_as_uint(a.x); qf[s][1] = __float_as_uint(b.x);
-                qf[s][2] = __float_as_uint(a.y); qf[s][3] = __float_as_uint(b.y);
+                const float2 a = row < u.rows ? *reinterpret_cast<const float2*>(src + s * 8 + 2 * c4) : make_float2(0.f, 0.f);
+                qf[n][s][0] = __float_as_uint(a.x);
+                qf[n][s][1] = __float_as_uint(a.y);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    qf[s][i] = row[i & 1] < u.rows
-                                   ? *reinterpret_cast<const uint32_t*>(src[i & 1] + s * 16 + 2 * c4 + (i >> 1) * 8)
-                                   : 0u;
+                for (int i = 0; i < 2; ++i)
+                    qf[n][s][i] = row < u.rows ? *reinterpret_cast<const uint32_t*>(src + s * 16 + i * 8 + 2 * c4) : 0u;
             }
         }
     }
-
-    float o[DT][4];
+    // as accumulator columns a thread's rows are 8 n + 2 c4 and the next
+    int limit[NR][2];
+    int least_limit = u.key1;
 #pragma unroll
-    for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-
-    const int ids0 = u.key0 >> p.page_shift;     // list entry of ids[0]
-    int ids_base = ids0;
-    auto load_ids = [&](int base) {              // all threads; the caller synchronises around it
-        for (int i = tid; i < Geo::IDS; i += THREADS) {
-            const int e = base + i;
-            int32_t pg = -1;
-            if (e < u.list) {
-                pg = __ldg(u.ids + e);
-                if (u.table) pg = pg >= 0 ? __ldg(u.table + pg) : -1;
-                if (pg < 0 || pg >= p.num_pages) {
-                    attn_report(kAttnErrIndex);
-                    pg = -1;
-                }
-            }
-            ids[i] = pg;
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = u.row0 + 8 * n + 2 * c4 + e;
+            limit[n][e] = min(u.key1, u.limit0 + (row / p.group) * u.step);
+            if (row >= u.rows) limit[n][e] = u.key1;
         }
-    };
-    auto load_tile = [&](int t) {                // keys and values of tile t into ring slot t % STAGES
-        const uint32_t kd = ring + (t % Geo::STAGES) * 2 * Geo::TILE_BYTES, vd = kd + Geo::TILE_BYTES;
-#pragma unroll
-        for (int i = 0; i < Geo::KEYS * Geo::CHUNKS / THREADS; ++i) {
-            const int j = tid + i * THREADS;
-            const int r = j / Geo::CHUNKS, c = j % Geo::CHUNKS;
-            const int key = u.key0 + t * Geo::KEYS + r;
-            int64_t off = 0;
-            int bytes = 0;
-            if (key < u.key1) {
-                const int pg = ids[(key >> p.page_shift) - ids_base];
-                if (pg >= 0) {
-                    bytes = 16;
-                    off = (((static_cast<int64_t>(pg) * p.hkv + u.head) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D +
-                          c * (16 / static_cast<int>(sizeof(T)));
-                }
-            }
-            const int at = Geo::place(r, c);
-            cp_async16(kd + at, kc + off, bytes);
-            cp_async16(vd + at, vc + off, bytes);
-        }
-    };
+    least_limit = min(u.key1, u.limit0 + (u.row0 / p.group) * u.step);
 
-    load_ids(ids0);
-    attn_group_sync(group, THREADS);
+    float o[NR][DT][4];
+    float m[NR][2], l[NR][2];
 #pragma unroll
-    for (int s = 0; s < Geo::STAGES - 1; ++s) {
-        if (s < tiles) load_tile(s);
-        cp_async_commit();
+    for (int n = 0; n < NR; ++n) {
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
     }
-    for (int t = 0; t < tiles; ++t) {
-        cp_async_wait<Geo::STAGES - 2>();
-        attn_group_sync(group, THREADS);                         // tile t has arrived, and everyone is done with tile t - 1
-        const int next = t + Geo::STAGES - 1;
-        if (next < tiles) {
-            // the list moves on when the next tile's last key leaves the entries that are held
-            const int last = min(u.key1 - 1, u.key0 + (next + 1) * Geo::KEYS - 1) >> p.page_shift;
-            if (last >= ids_base + Geo::IDS) {
-                ids_base = (u.key0 + next * Geo::KEYS) >> p.page_shift;
-                load_ids(ids_base);
-                attn_group_sync(group, THREADS);
-            }
-            load_tile(next);
-        }
-        cp_async_commit();
 
-        const uint32_t kt = ring + (t % Geo::STAGES) * 2 * Geo::TILE_BYTES, vt = kt + Geo::TILE_BYTES;
-        const unsigned char* kp = smem + (t % Geo::STAGES) * 2 * Geo::TILE_BYTES;
-        const unsigned char* vp = kp + Geo::TILE_BYTES;
-        const int k0 = kw * WKEYS;               // this warp's keys within the tile
-        float s[NT][4];
+    // O^T += V^T P^T for one chunk; w: the chunk's weights as accumulators (keys r4, r4 + 8; rows 2 c4, 2 c4 + 1)
+    auto add_values = [&](const float (&w)[NR][4], int s) {
+        const uint32_t vt = ring_u32 + s * 2 * Geo::SIDE + Geo::SIDE;
+        if constexpr (F32) {
+            const unsigned char* vp = ring + s * 2 * Geo::SIDE + Geo::SIDE;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+            for (int h = 0; h < 2; ++h) {        // keys 8 h .. 8 h + 7
+                // operand layout: keys c4 and c4 + 4 of row r4, held by lanes (key, row / 2)
+                uint32_t bh[NR][2], bl[NR][2];
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int from = (c4 + 4 * i) * 4 + (r4 >> 1);
+                        const float even = __shfl_sync(kFullMask, w[n][2 * h], from), odd = __shfl_sync(kFullMask, w[n][2 * h + 1], from);
+                        split_tf32(r4 & 1 ? odd : even, bh[n][i], bl[n][i]);
+                    }
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    uint32_t ah[4], al[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = 8 * h + c4 + 4 * (i >> 1), ch = d * 16 + r4 + 8 * (i & 1);
+                        split_tf32(*reinterpret_cast<const float*>(vp + Geo::place(key, ch >> 2) + (ch & 3) * 4), ah[i], al[i]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        // (the tensor core's accumulation truncates: one chunk at a time, added up with rounding)
+                        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        mma_tf32_1688(sum, al, bh[n][0], bh[n][1]);
+                        mma_tf32_1688(sum, ah, bl[n][0], bl[n][1]);
+                        mma_tf32_1688(sum, ah, bh[n][0], bh[n][1]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[n][d][i] += sum[i];
+                    }
+                }
+            }
+        } else {
+            uint32_t b[NR][2];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                b[n][0] = transpose_8x8(pack_bf16x2(w[n][0], w[n][1]));
+                b[n][1] = transpose_8x8(pack_bf16x2(w[n][2], w[n][3]));
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                uint32_t a[4];
+                ldmatrix_x4_trans(vt + Geo::place((lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)), a);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) mma_bf16_16816(o[n][d], a, b[n][0], b[n][1]);
+            }
+        }
+    };
+
+    for (int j = 0; j < chunks; ++j) {
+        const int s = j % Geo::STAGES;
+        mbar_wait_bounded(full + s, static_cast<uint32_t>(j / Geo::STAGES) & 1u);
+        const int base = u.key0 + (wi + j * u.wpu) * kChunk;
+        const bool mask = base + kChunk > least_limit;
+        if (base + kChunk > u.key1) {
+            // keys that nobody sees: their values become 0, so that a weight of 0 takes nothing from whatever lies there
+            const int valid = u.key1 - base;
+            unsigned char* v = ring + s * 2 * Geo::SIDE + Geo::SIDE;
+            for (int i = lane; i < (kChunk - valid) * 8 * Geo::BOXES; i += 32) {
+                const int r = valid + i / (8 * Geo::BOXES), c = i % (8 * Geo::BOXES);
+                *reinterpret_cast<uint4*>(v + Geo::place(r, c)) = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+        }
+
+        // S^T = K Q^T: keys r4 (elements 0, 1) and r4 + 8 (2, 3); rows 2 c4, 2 c4 + 1
+        float x[NR][4];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.0f;
         if constexpr (F32) {
             // The tensor core's accumulation truncates, so a long chain of products drifts: the leading products are taken
             // one instruction at a time and added up with rounding, the small ones keep a chain of their own.
-            float small[NT][4];
+            const unsigned char* kp = ring + s * 2 * Geo::SIDE;
+            float small[NR][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) small[n][0] = small[n][1] = small[n][2] = small[n][3] = 0.0f;
+            for (int n = 0; n < NR; ++n) small[n][0] = small[n][1] = small[n][2] = small[n][3] = 0.0f;
 #pragma unroll
             for (int ks = 0; ks < QS; ++ks) {
                 uint32_t ah[4], al[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) split_tf32(__uint_as_float(qf[ks][i]), ah[i], al[i]);
+                for (int i = 0; i < 2; ++i) {
+                    const float2 k = *reinterpret_cast<const float2*>(kp + Geo::place(r4 + 8 * i, ks * 2 + (c4 >> 1)) + (c4 & 1) * 8);
+                    split_tf32(k.x, ah[i], al[i]);
+                    split_tf32(k.y, ah[2 + i], al[2 + i]);
+                }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int r = k0 + n * 8 + r4;
-                    const float2 b = *reinterpret_cast<const float2*>(kp + Geo::place(r, ks * 2 + (c4 >> 1)) + (c4 & 1) * 8);
+                for (int n = 0; n < NR; ++n) {
                     uint32_t h0, h1, l0, l1;
-                    split_tf32(b.x, h0, l0);
-                    split_tf32(b.y, h1, l1);
+                    split_tf32(__uint_as_float(qf[n][ks][0]), h0, l0);
+                    split_tf32(__uint_as_float(qf[n][ks][1]), h1, l1);
                     float lead[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                     mma_tf32_1688(small[n], al, h0, h1);
                     mma_tf32_1688(small[n], ah, l0, l1);
                     mma_tf32_1688(lead, ah, h0, h1);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][i] += lead[i];
+                    for (int i = 0; i < 4; ++i) x[n][i] += lead[i];
                 }
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][i] += small[n][i];
+                for (int i = 0; i < 4; ++i) x[n][i] += small[n][i];
         } else {
+            const uint32_t kt = ring_u32 + s * 2 * Geo::SIDE;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = k0 + n * 8 + (lane & 7);
+            for (int ks = 0; ks < QS; ++ks) {
+                uint32_t a[4];
+                ldmatrix_x4(kt + Geo::place((lane & 7) + ((lane >> 3) & 1) * 8, 2 * ks + (lane >> 4)), a);
 #pragma unroll
-                for (int kk = 0; kk < D / 32; ++kk) {
-                    uint32_t b[4];
-                    ldmatrix_x4(kt + Geo::place(r, kk * 4 + (lane >> 3)), b);
-                    mma_bf16_16816(s[n], qf[2 * kk], b[0], b[1]);
-                    mma_bf16_16816(s[n], qf[2 * kk + 1], b[2], b[3]);
-                }
+                for (int n = 0; n < NR; ++n) mma_bf16_16816(x[n], a, qf[n][ks][0], qf[n][ks][1]);
             }
         }
-        // scores in units of log2, masked; the running maximum
-        const int base = u.key0 + t * Geo::KEYS + k0;
-        const bool mask = u.key0 + (t + 1) * Geo::KEYS > free_keys;
-        float top[2] = {m[0], m[1]};
+        bool passes = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float x = s[n][i] * p.scale_log2;
-                if (mask && base + n * 8 + 2 * c4 + (i & 1) >= limit[i >> 1]) x = -INFINITY;
-                s[n][i] = x;
-                top[i >> 1] = fmaxf(top[i >> 1], x);
+                x[n][i] *= p.scale_log2;
+                if (mask && base + r4 + 8 * (i >> 1) >= limit[n][i & 1]) x[n][i] = -INFINITY;
+                passes = passes || x[n][i] > m[n][i & 1] + kSlack;
             }
-        }
-        float turn[2], zero[2];
+        if (__any_sync(kFullMask, passes)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            top[i] = fmaxf(top[i], __shfl_xor_sync(kFullMask, top[i], 1));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(kFullMask, top[i], 2));
-            zero[i] = top[i] == -INFINITY ? 0.0f : top[i];  // a row that has seen no key: every weight is 0
-            turn[i] = exp2_fast(m[i] - zero[i]);
-        }
-        if (__any_sync(kFullMask, top[0] != m[0] || top[1] != m[1])) {
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                o[i][0] *= turn[0]; o[i][1] *= turn[0];
-                o[i][2] *= turn[1]; o[i][3] *= turn[1];
-            }
-            l[0] *= turn[0];
-            l[1] *= turn[1];
-            m[0] = top[0];
-            m[1] = top[1];
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(x[n][e], x[n][2 + e]);
+#pragma unroll
+                    for (int i = 4; i < 32; i <<= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, i));
+                    if (top > m[n][e]) {
+                        const float f = exp2_fast(m[n][e] - top);
+                        m[n][e] = top;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            o[n][d][e] *= f;
+                            o[n][d][2 + e] *= f;
+                        }
+                    }
+                }
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[n][i] = exp2_fast(s[n][i] - zero[i >> 1]);
-                l[i >> 1] += s[n][i];
+                // a row that has seen no key has m = -infinity: every weight is 0
+                const float z = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
+                x[n][i] = exp2_fast(x[n][i] - z);
+                l[n][i & 1] += x[n][i];
             }
+        add_values(x, s);
+        __syncwarp();                            // every lane has read the slot
+        const int next = j + Geo::STAGES;
+        if ((next & 31) == 0) {
+            y_now = y_next;
+            y_next = next + 32 < chunks ? rows_of(next + 32) : 0;
         }
-        if constexpr (F32) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                // contraction index c stands for key 2c, c + 4 for 2c + 1
-                uint32_t ah[4], al[4];
-                split_tf32(s[n][0], ah[0], al[0]);
-                split_tf32(s[n][2], ah[1], al[1]);
-                split_tf32(s[n][1], ah[2], al[2]);
-                split_tf32(s[n][3], ah[3], al[3]);
-                const int r = k0 + n * 8 + 2 * c4;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const float b0 = *reinterpret_cast<const float*>(vp + Geo::place(r, d * 2 + (r4 >> 2)) + (r4 & 3) * 4);
-                    const float b1 = *reinterpret_cast<const float*>(vp + Geo::place(r + 1, d * 2 + (r4 >> 2)) + (r4 & 3) * 4);
-                    uint32_t h0, h1, l0, l1;
-                    split_tf32(b0, h0, l0);
-                    split_tf32(b1, h1, l1);
-                    mma_tf32_1688(sum, al, h0, h1);
-                    mma_tf32_1688(sum, ah, l0, l1);
-                    mma_tf32_1688(sum, ah, h0, h1);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[d][i] += sum[i];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                const uint32_t a[4] = {pack_bf16x2(s[n][0], s[n][1]), pack_bf16x2(s[n][2], s[n][3]),
-                                       pack_bf16x2(s[n + 1][0], s[n + 1][1]), pack_bf16x2(s[n + 1][2], s[n + 1][3])};
-                const int r = k0 + n * 8 + (lane & 15);
-#pragma unroll
-                for (int d = 0; d < DT; d += 2) {
-                    uint32_t b[4];
-                    ldmatrix_x4_trans(vt + Geo::place(r, d + (lane >> 4)), b);
-                    mma_bf16_16816(o[d], a, b[0], b[1]);
-                    mma_bf16_16816(o[d + 1], a, b[2], b[3]);
-                }
-            }
-        }
+        const int y = __shfl_sync(kFullMask, y_now, next & 31);
+        if (lane == 0 && next < chunks) load(next, y);
     }
-    cp_async_wait<0>();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        l[i] += __shfl_xor_sync(kFullMask, l[i], 1);
-        l[i] += __shfl_xor_sync(kFullMask, l[i], 2);
-    }
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 4; i < 32; i <<= 1) l[n][e] += __shfl_xor_sync(kFullMask, l[n][e], i);
 
-    if constexpr (KW > 1) {
-        // join the warps that share rows: everyone stores (m, l, o), then the block's threads add them up
-        attn_group_sync(group, THREADS);
-        float* jo = reinterpret_cast<float*>(smem);           // [warp][16][D]
-        float2* jm = reinterpret_cast<float2*>(jo + RW * KW * 16 * D);  // [warp][16]
+    // the unit's warps store (m, l, o) over their rings and add them up together
+    {
+        float* jo = reinterpret_cast<float*>(ring);
+        float2* jm = reinterpret_cast<float2*>(jo + 32 * Geo::JOIN_LD);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = r4 + 8 * i;
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-                *reinterpret_cast<float2*>(jo + (warp * 16 + r) * D + d * 8 + 2 * c4) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
-            if (c4 == 0) jm[warp * 16 + r] = make_float2(m[i], l[i]);
-        }
-        attn_group_sync(group, THREADS);
-        constexpr int PER = 4;                                 // channels per thread and step
-        for (int j = tid; j < RW * 16 * (D / PER); j += THREADS) {
-            const int r = j / (D / PER), d = (j % (D / PER)) * PER;
-            const int rr = u.row0 + r;
-            if (rr >= u.rows) continue;
-            const int w0 = (r >> 4) * KW;
-            float2 ml[KW];
-            float mm = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                ml[w] = jm[(w0 + w) * 16 + (r & 15)];
-                mm = fmaxf(mm, ml[w].x);
-            }
-            const float z = mm == -INFINITY ? 0.0f : mm;
-            float ll = 0.0f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const float f = exp2_fast(ml[w].x - z);
-                ll += f * ml[w].y;
-                const float4 x = *reinterpret_cast<const float4*>(jo + ((w0 + w) * 16 + (r & 15)) * D + d);
-                acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
-            }
-            const int tok = rr / p.group;
-            const int64_t at = (u.token0 + tok) * p.hq + u.head * p.group + (rr - tok * p.group);
-            if (p.parts == 1) {
-                const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-                T* dst = static_cast<T*>(p.out) + at * D + d;
-                if constexpr (F32) {
-                    *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-                } else {
-                    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-                }
-            } else {
-                const int64_t slot = static_cast<int64_t>(u.part) * p.T * p.hq + at;
-                *reinterpret_cast<float4*>(p.part_o + slot * D + d) = acc;
-                if (d == 0) p.part_ml[slot] = make_float2(mm, ll);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (row[i] >= u.rows) continue;
-            const int tok = row[i] / p.group;
-            const int64_t at = (u.token0 + tok) * p.hq + u.head * p.group + (row[i] - tok * p.group);
-            if (p.parts == 1) {
-                const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
-                T* dst = static_cast<T*>(p.out) + at * D + 2 * c4;
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * n + 2 * c4 + e;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    if constexpr (F32)
-                        *reinterpret_cast<float2*>(dst + d * 8) = make_float2(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
-                    else
-                        *reinterpret_cast<uint32_t*>(dst + d * 8) = pack_bf16x2(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
+                    jo[r * Geo::JOIN_LD + d * 16 + r4] = o[n][d][e];
+                    jo[r * Geo::JOIN_LD + d * 16 + 8 + r4] = o[n][d][2 + e];
                 }
-            } else {
-                const int64_t slot = static_cast<int64_t>(u.part) * p.T * p.hq + at;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    *reinterpret_cast<float2*>(p.part_o + slot * D + d * 8 + 2 * c4) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
-                if (c4 == 0) p.part_ml[slot] = make_float2(m[i], l[i]);
+                if (r4 == 0) jm[r] = make_float2(m[n][e], l[n][e]);
             }
+    }
+    if (u.wpu == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(warp / u.wpu + 1), "r"(u.wpu * 32) : "memory");
+    const unsigned char* first = smem + (warp - wi) * Geo::RING;
+    const int rows_here = min(NR * 8, u.rows - u.row0);
+    constexpr int PER = 4;                       // channels per thread and step
+    for (int i = wi * 32 + lane; i < rows_here * (D / PER); i += u.wpu * 32) {
+        const int r = i / (D / PER), d = (i % (D / PER)) * PER;
+        float mm = -INFINITY;
+        for (int w = 0; w < u.wpu; ++w)
+            mm = fmaxf(mm, reinterpret_cast<const float2*>(first + w * Geo::RING + 32 * Geo::JOIN_LD * 4)[r].x);
+        const float z = mm == -INFINITY ? 0.0f : mm;
+        float ll = 0.0f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < u.wpu; ++w) {
+            const float* wo = reinterpret_cast<const float*>(first + w * Geo::RING);
+            const float2 ml = reinterpret_cast<const float2*>(wo + 32 * Geo::JOIN_LD)[r];
+            const float f = exp2_fast(ml.x - z);
+            ll += f * ml.y;
+            const float4 v = *reinterpret_cast<const float4*>(wo + r * Geo::JOIN_LD + d);
+            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+        }
+        const int row = u.row0 + r, tok = row / p.group;
+        const int64_t at = (u.token0 + tok) * p.hq + u.head * p.group + (row - tok * p.group);
+        if (p.parts == 1) {
+            const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+            T* dst = static_cast<T*>(p.out) + at * D + d;
+            if constexpr (F32)
+                *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            else
+                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        } else {
+            const int64_t slot = static_cast<int64_t>(u.part) * p.T * p.hq + at;
+            *reinterpret_cast<float4*>(p.part_o + slot * D + d) = acc;
+            if (d == 0) p.part_ml[slot] = make_float2(mm, ll);
         }
     }
 }
 
 template <typename T, int D>
-__device__ __forceinline__ void attn_block_rw(int rw, const AttnParams& p, const AttnUnit& u, unsigned char* smem) {
-    if (rw == 1) attn_block<T, D, 1>(p, u, smem);
-    else if (rw == 2) attn_block<T, D, 2>(p, u, smem);
-    else attn_block<T, D, 4>(p, u, smem);
+__device__ __forceinline__ void attn_run(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map) {
+    extern __shared__ unsigned char smem_attn[];
+    unsigned char* smem = smem_attn + ((1024u - (smem_u32(smem_attn) & 1023u)) & 1023u);
+    if (u.nr == 1) attn_unit<T, D, 1>(p, u, k_map, v_map, smem);
+    else if (u.nr == 2) attn_unit<T, D, 2>(p, u, k_map, v_map, smem);
+    else attn_unit<T, D, 4>(p, u, k_map, v_map, smem);
 }
 
 // A length read on the device, held to what the tables can hold.
@@ -518,67 +483,63 @@ __device__ __forceinline__ void attn_part(int keys, int tile, int splits, int s,
 // Prefix and own pages in one launch: blocks below prefix_blocks take the prefix.
 template <typename T, int D>
 __global__ void __launch_bounds__(kAttnThreads)
-attn_prefix_kernel(const AttnParams p) {
-    extern __shared__ __align__(128) unsigned char smem_attn[];
-    constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS;
+attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     const int prefix_units = p.prefix_splits * p.prefix_row_tiles * p.hkv;
-    const int prefix_groups = attn_groups(p.prefix_rw);
-    const int prefix_blocks = (prefix_units + prefix_groups - 1) / prefix_groups;
+    const int prefix_blocks = (prefix_units * p.prefix_wpu + 3) / 4;
+    const int warp = threadIdx.x >> 5;
+    const bool last_block = blockIdx.x == gridDim.x - 1;
     AttnUnit u;
-    int b = blockIdx.x;
+    bool work;
     grid_launch_dependents();
-    if (b < prefix_blocks) {
-        b = b * prefix_groups + static_cast<int>(threadIdx.x) / (kAttnThreads / prefix_groups);
-        if (b >= prefix_units) return;
+    if (static_cast<int>(blockIdx.x) < prefix_blocks) {
+        int b = (blockIdx.x * 4 + warp) / p.prefix_wpu;
+        work = b < prefix_units;
         u.part = b % p.prefix_splits;
         b /= p.prefix_splits;
-        u.row0 = (b % p.prefix_row_tiles) * 16 * p.prefix_rw;
+        u.row0 = (b % p.prefix_row_tiles) * 8 * p.prefix_nr;
         u.head = b / p.prefix_row_tiles;
         u.token0 = 0;
         u.rows = static_cast<int>(p.T) * p.group;
         u.ids = p.prefix_pages;
-        u.table = nullptr;
         const int keys = static_cast<int>(p.prefix_len);
         u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
-        attn_part(keys, KEYS, p.prefix_splits, u.part, u.key0, u.key1);
+        attn_part(keys, kChunk * 4, p.prefix_splits, u.part, u.key0, u.key1);
         u.limit0 = keys;
         u.step = 0;
-        attn_block_rw<T, D>(p.prefix_rw, p, u, smem_attn);
-        return;
+        u.nr = p.prefix_nr;
+        u.wpu = p.prefix_wpu;
+    } else {
+        int b = ((blockIdx.x - prefix_blocks) * 4 + warp) / p.own_wpu;
+        const int split = b % p.own_splits;
+        b /= p.own_splits;
+        u.part = (p.parts - p.own_splits) + split;
+        u.row0 = (b % p.own_row_tiles) * 8 * p.own_nr;
+        b /= p.own_row_tiles;
+        u.head = b % p.hkv;
+        const int seq = b / p.hkv;
+        int count = 0, keys = 0;
+        if (seq < p.B) {
+            // the table's row is wanted as soon as the length is known: fetch it meanwhile
+            u.ids = p.page_table + static_cast<int64_t>(seq) * p.table_width;
+            const int ahead = (static_cast<int>(threadIdx.x) & 31) * 32;
+            if (ahead < p.table_width) asm volatile("prefetch.global.L1 [%0];" ::"l"(u.ids + ahead));
+            attn_tokens(p, seq, u.token0, count);
+            keys = attn_length(p, seq);
+        }
+        u.rows = count * p.group;
+        work = u.row0 < u.rows;
+        u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
+        // the unit's last row sees the most: nothing beyond its place is read
+        u.limit0 = keys - count + 1;
+        u.step = 1;
+        const int last_tok = (min(u.rows, u.row0 + 8 * p.own_nr) - 1) / p.group;
+        attn_part(keys, kChunk * 4, p.own_splits, split, u.key0, u.key1);
+        u.key1 = max(u.key0, min(u.key1, u.limit0 + last_tok));
+        u.nr = p.own_nr;
+        u.wpu = p.own_wpu;
     }
-    const bool last_block = blockIdx.x == gridDim.x - 1;
-    const int own_groups = attn_groups(p.own_rw);
-    b = (b - prefix_blocks) * own_groups + static_cast<int>(threadIdx.x) / (kAttnThreads / own_groups);
-    const int split = b % p.own_splits;
-    b /= p.own_splits;
-    u.part = (p.parts - p.own_splits) + split;
-    u.row0 = (b % p.own_row_tiles) * 16 * p.own_rw;
-    b /= p.own_row_tiles;
-    u.head = b % p.hkv;
-    const int seq = b / p.hkv;
-    if (seq < p.B) {
-        // the table's row is wanted as soon as the length is known: fetch it meanwhile
-        u.ids = p.page_table + static_cast<int64_t>(seq) * p.table_width;
-        const int ahead = (static_cast<int>(threadIdx.x) & 31) * 32;
-        if (ahead < p.table_width) asm volatile("prefetch.global.L1 [%0];" ::"l"(u.ids + ahead));
-    }
-    int count = 0;
-    if (seq < p.B) attn_tokens(p, seq, u.token0, count);
-    u.rows = count * p.group;
-    if (u.row0 >= u.rows) {
-        if (last_block) grid_dependency_wait();
-        return;
-    }
-    const int keys = attn_length(p, seq);
     u.table = nullptr;
-    u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
-    // the block's last row sees the most: nothing beyond its place is read
-    u.limit0 = keys - count + 1;
-    u.step = 1;
-    const int last_tok = (min(u.rows, u.row0 + 16 * p.own_rw) - 1) / p.group;
-    attn_part(keys, KEYS, p.own_splits, split, u.key0, u.key1);
-    u.key1 = max(u.key0, min(u.key1, u.limit0 + last_tok));
-    attn_block_rw<T, D>(p.own_rw, p, u, smem_attn);
+    if (work) attn_run<T, D>(p, u, &k_map, &v_map);
     // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
     // for this grid alone, so this grid does not end before that one has.
     if (last_block) grid_dependency_wait();
@@ -601,20 +562,17 @@ __device__ __forceinline__ int attn_sequence_of(const AttnParams& p, int64_t t) 
     return lo;
 }
 
-// Chosen pages: one token and key head (and a part of the list) per block.
+// Chosen pages: one token and key head (and a part of the list) per unit.
 template <typename T, int D>
 __global__ void __launch_bounds__(kAttnThreads)
-attn_chosen_kernel(const AttnParams p) {
-    extern __shared__ __align__(128) unsigned char smem_attn[];
-    constexpr int KEYS = AttnRow<T, D>::BLOCK_KEYS;
+attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     AttnUnit u;
     grid_dependency_wait();  // the list comes from the kernel before
     grid_launch_dependents();
-    const int groups = attn_groups(p.own_rw);
-    int64_t b = static_cast<int64_t>(blockIdx.x) * groups + static_cast<int>(threadIdx.x) / (kAttnThreads / groups);
+    int64_t b = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5)) / p.own_wpu;
     u.part = static_cast<int>(b % p.own_splits);
     b /= p.own_splits;
-    u.row0 = static_cast<int>(b % p.own_row_tiles) * 16 * p.own_rw;
+    u.row0 = static_cast<int>(b % p.own_row_tiles) * 8 * p.own_nr;
     b /= p.own_row_tiles;
     u.head = static_cast<int>(b % p.hkv);
     u.token0 = b / p.hkv;
@@ -630,10 +588,12 @@ attn_chosen_kernel(const AttnParams p) {
     const int page = static_cast<int>(place >> p.page_shift);
     u.list = place < 0 ? 0 : min(p.select, page + 1);
     const int keys = place < 0 ? 0 : ((u.list - 1) << p.page_shift) + static_cast<int>(place & ((1 << p.page_shift) - 1)) + 1;
-    attn_part(keys, KEYS, p.own_splits, u.part, u.key0, u.key1);
+    attn_part(keys, kChunk * 4, p.own_splits, u.part, u.key0, u.key1);
     u.limit0 = keys;
     u.step = 0;
-    attn_block_rw<T, D>(p.own_rw, p, u, smem_attn);
+    u.nr = p.own_nr;
+    u.wpu = p.own_wpu;
+    attn_run<T, D>(p, u, &k_map, &v_map);
 }
 
 // Joins the parts of each row: out = sum_s exp(m_s - m) o_s / sum_s exp(m_s - m) l_s.  One warp per row, lanes

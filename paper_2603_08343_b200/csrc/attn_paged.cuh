@@ -16,19 +16,26 @@ int attn_prepare(Kernel kernel, int smem, int dev, int* cache) {
     return WHT_OK;
 }
 
+template <typename T>
+constexpr int attn_code() { return sizeof(T) == 4 ? WHT_F32 : WHT_BF16; }
+
 template <typename T, int D>
 int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnRow<T, D>;
-    const int rc = attn_prepare(attn_prefix_kernel<T, D>, Geo::SMEM, dev, ready);
+    using Geo = AttnGeo<T, D>;
+    int rc = attn_prepare(attn_prefix_kernel<T, D>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     const long long prefix_units = static_cast<long long>(p.prefix_splits) * p.prefix_row_tiles * p.hkv;
     const long long own_units = static_cast<long long>(p.B) * p.hkv * p.own_row_tiles * p.own_splits;
-    if (prefix_units > 0x3fffffffll || own_units > 0x3fffffffll) return WHT_ERR_BAD_T;
-    const long long blocks = ceil_div(prefix_units, attn_groups(p.prefix_rw)) + ceil_div(own_units, attn_groups(p.own_rw));
-    if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
-    if (overlapped) launch_overlapped(attn_prefix_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::SMEM, s, p);
-    else attn_prefix_kernel<T, D><<<static_cast<unsigned>(blocks), kAttnThreads, Geo::SMEM, s>>>(p);
+    if (prefix_units > 0x1fffffffll || own_units > 0x1fffffffll) return WHT_ERR_BAD_T;
+    const long long blocks = ceil_div(prefix_units * p.prefix_wpu, 4) + ceil_div(own_units * p.own_wpu, 4);
+    CUtensorMap k_map, v_map;
+    rc = cache_maps(&k_map, &v_map, p, D, attn_code<T>(), kChunk);
+    if (rc != WHT_OK) return rc;
+    if (overlapped)
+        launch_overlapped(attn_prefix_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::BYTES, s, p, k_map, v_map);
+    else
+        attn_prefix_kernel<T, D><<<static_cast<unsigned>(blocks), kAttnThreads, Geo::BYTES, s>>>(p, k_map, v_map);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }
@@ -36,12 +43,16 @@ int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s)
 template <typename T, int D>
 int attn_chosen_d(const AttnParams& p, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnRow<T, D>;
-    const int rc = attn_prepare(attn_chosen_kernel<T, D>, Geo::SMEM, dev, ready);
+    using Geo = AttnGeo<T, D>;
+    int rc = attn_prepare(attn_chosen_kernel<T, D>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
-    const long long blocks = ceil_div(static_cast<long long>(p.T) * p.hkv * p.own_row_tiles * p.own_splits, attn_groups(p.own_rw));
-    if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
-    launch_overlapped(attn_chosen_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), kAttnThreads, Geo::SMEM, s, p);
+    const long long units = static_cast<long long>(p.T) * p.hkv * p.own_row_tiles * p.own_splits;
+    if (units > 0x1fffffffll) return WHT_ERR_BAD_T;
+    CUtensorMap k_map, v_map;
+    rc = cache_maps(&k_map, &v_map, p, D, attn_code<T>(), kChunk);
+    if (rc != WHT_OK) return rc;
+    launch_overlapped(attn_chosen_kernel<T, D>, dim3(static_cast<unsigned>(ceil_div(units * p.own_wpu, 4))), kAttnThreads, Geo::BYTES, s, p,
+                      k_map, v_map);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }

@@ -12,37 +12,6 @@ WHT_DEFINE_DEVICE_ERROR_READER(take_device_error_attn_umma)
 
 namespace {
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-int encode_function(EncodeTiled* out) {
-    static EncodeTiled cached = nullptr;
-    if (!cached) {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        WHT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found));
-        if (found != cudaDriverEntryPointSuccess || !f) return cuda_fail(cudaErrorNotSupported);
-        cached = reinterpret_cast<EncodeTiled>(f);
-    }
-    *out = cached;
-    return WHT_OK;
-}
-
-// A cache as [num_pages * Hkv * page] rows of D channels, copied in boxes of one page by 64 channels.
-int cache_map(CUtensorMap* map, const void* cache, const AttnParams& p, int d) {
-    EncodeTiled encode = nullptr;
-    const int rc = encode_function(&encode);
-    if (rc != WHT_OK) return rc;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(p.num_pages * p.hkv) << p.page_shift};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(d) * 2};
-    const cuuint32_t box[2] = {64u, 1u << p.page_shift}, unit[2] = {1u, 1u};
-    if (encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(cache), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return cuda_fail(cudaErrorInvalidValue);
-    return WHT_OK;
-}
-
 template <int D>
 int launch(const UmmaAttnParams& up, int dev, cudaStream_t s) {
     using Geo = UmmaAttnGeo<D>;
@@ -51,8 +20,7 @@ int launch(const UmmaAttnParams& up, int dev, cudaStream_t s) {
     int rc = prepare_umma(attn_umma_prefix_kernel<D>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     CUtensorMap k_map, v_map;
-    rc = cache_map(&k_map, up.a.k_cache, up.a, D);
-    if (rc == WHT_OK) rc = cache_map(&v_map, up.a.v_cache, up.a, D);
+    rc = cache_maps(&k_map, &v_map, up.a, D, WHT_BF16, 1 << up.a.page_shift);
     if (rc != WHT_OK) return rc;
     const long long blocks = static_cast<long long>(up.splits) * up.row_blocks * up.a.hkv;
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;

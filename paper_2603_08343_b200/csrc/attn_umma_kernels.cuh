@@ -31,7 +31,6 @@
 namespace wht {
 
 constexpr int kUmmaAttnThreads = 320;
-constexpr float kSlack = 8.0f;
 
 template <int D>
 struct UmmaAttnGeo {
@@ -46,13 +45,6 @@ struct UmmaAttnGeo {
     static constexpr int BYTES = OFF_MISC + 16 + 1024;        // and what aligning the start to 1024 bytes takes
     static constexpr int O_COLS = D > 64 ? 128 : 64;
 };
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
-        : "memory");
-}
 
 // Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart (both majors); `lead` is the distance of 64-channel
 // blocks for the MN-major operand (unused for the K-major one, whose instructions stay within a block).

@@ -29,7 +29,8 @@ int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages
     if (dtype != WHT_F32 && dtype != WHT_BF16) return WHT_ERR_BAD_DTYPE;
     if (D != 64 && D != 96 && D != 128) return WHT_ERR_BAD_DIM;
     if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 64 || Hq > 65536) return WHT_ERR_BAD_DIM;
-    if (page_shift_of(page) < 0 || num_pages < 0 || num_pages > 0x7fffffff) return WHT_ERR_BAD_DIM;
+    // (tiled copies count a cache's rows in 31 bits; one of more rows would not fit the device's memory)
+    if (page_shift_of(page) < 0 || num_pages < 0 || num_pages > 0x7fffffff / page / Hkv) return WHT_ERR_BAD_DIM;
     if (T < 0 || T * Hq > 0x7fffffff) return WHT_ERR_BAD_T;
     return WHT_OK;
 }
@@ -40,20 +41,25 @@ int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, in
     return WHT_OK;
 }
 
-int row_tiles_per_block(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-int keys_per_tile(int dtype) { return dtype == WHT_F32 ? 32 : 64; }
+// 8-row tiles per unit of the paged kernel
+int row_tiles(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
-// How many groups the keys of `units` row sets are divided over: enough to fill every SM (two blocks of one group, or of two
-// where a group is two warps), but none with fewer than two 64-key tiles (its own set-up and the join of its part would cost
-// more than they save).
-int splits_for(int64_t units, int64_t keys, int rw, int dtype, int sms) {
-    const int64_t tiles = ceil_div(keys, keys_per_tile(dtype));
-    const int64_t want = units > 0 ? (2 * wht::attn_groups(rw) * sms) / units : 1;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, tiles / 2)));
+// How the paged kernel divides a set of units of up to `keys` keys: warps per unit, and key ranges (splits).  Eight warps an SM are
+// resident.  Many units: a warp each, which needs no join and no waiting; fewer: more warps per unit, then more
+// ranges, but no warp with fewer than four 16-key chunks (its own set-up and the join would cost more than they save).
+struct Division {
+    int wpu, splits;
+};
+Division divide(int64_t units, int64_t keys, int sms) {
+    const int64_t slots = 8ll * sms, chunks = ceil_div(keys, 16);
+    Division d{1, 1};
+    while (d.wpu < 4 && units * d.wpu < 3 * slots && chunks >= 4 * 2 * d.wpu) d.wpu *= 2;
+    if (d.wpu == 4) d.splits = static_cast<int>(std::max<int64_t>(1, std::min(slots / (units * 4), chunks / 16)));
+    return d;
 }
 
 struct PrefixPlan {
-    int prefix_rw, prefix_row_tiles, prefix_splits, own_rw, own_row_tiles, own_splits, parts;
+    int prefix_nr, prefix_row_tiles, prefix_wpu, prefix_splits, own_nr, own_row_tiles, own_wpu, own_splits, parts;
     bool umma;                                  // the prefix on the tcgen05 kernel
     int umma_splits, umma_row_blocks, same_rows;
     size_t bytes;
@@ -82,10 +88,12 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     PrefixPlan f{};
     const int group = Hq / Hkv;
     const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
-    f.own_rw = row_tiles_per_block(own_rows);
-    f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 16 * f.own_rw));
-    f.own_splits = splits_for(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, f.own_rw, dtype, sms);
-    f.prefix_rw = 1;
+    f.own_nr = row_tiles(own_rows);
+    f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 8 * f.own_nr));
+    const Division own = divide(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, sms);
+    f.own_wpu = own.wpu;
+    f.own_splits = own.splits;
+    f.prefix_nr = f.prefix_wpu = 1;
     f.umma = umma_allowed && dtype == WHT_BF16 && T * group >= kUmmaMinRows && prefix_len >= kUmmaMinKeys;
     if (f.umma) {
         f.same_rows = T * group <= 128;
@@ -93,9 +101,11 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
         // with the same rows in both tiles a block takes two key tiles at a time
         f.umma_splits = umma_splits_for(static_cast<int64_t>(Hkv) * f.umma_row_blocks, ceil_div(prefix_len, f.same_rows ? 256 : 128), sms);
     } else if (prefix_len > 0) {
-        f.prefix_rw = row_tiles_per_block(T * group);
-        f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 16 * f.prefix_rw));
-        f.prefix_splits = splits_for(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, f.prefix_rw, dtype, sms);
+        f.prefix_nr = row_tiles(T * group);
+        f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 8 * f.prefix_nr));
+        const Division pre = divide(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, sms);
+        f.prefix_wpu = pre.wpu;
+        f.prefix_splits = pre.splits;
     }
     f.parts = f.prefix_splits + f.own_splits + (f.same_rows ? 2 : 1) * f.umma_splits;
     const size_t rows = static_cast<size_t>(T) * Hq;
@@ -104,16 +114,18 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
 }
 
 struct SelectPlan {
-    int rw, row_tiles, splits;
+    int nr, row_tiles, wpu, splits;
     size_t scores_bytes, bytes;
 };
 
 SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int dtype, int sms) {
     SelectPlan f{};
     const int group = Hq / Hkv;
-    f.rw = row_tiles_per_block(group);
-    f.row_tiles = static_cast<int>(ceil_div(group, 16 * f.rw));
-    f.splits = splits_for(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, f.rw, dtype, sms);
+    f.nr = row_tiles(group);
+    f.row_tiles = static_cast<int>(ceil_div(group, 8 * f.nr));
+    const Division d = divide(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, sms);
+    f.wpu = d.wpu;
+    f.splits = d.splits;
     f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
     const size_t rows = static_cast<size_t>(T) * Hq;
     f.bytes = f.scores_bytes + (f.splits > 1 ? up256(rows * f.splits * sizeof(float2)) + rows * f.splits * D * sizeof(float) : 0);
@@ -196,9 +208,8 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     int dev = 0, sms = 0;
     rc = device_info(&dev, &sms);
     if (rc != WHT_OK) return rc;
-    // The tcgen05 kernel finds a row's maximum before it scales (so the scale is positive), and its copies count the
-    // cache's rows in 31 bits.
-    const bool umma_allowed = scale > 0.0f && num_pages * Hkv * page <= 0x7fffffff && num_pages > 0;
+    if (num_pages < 1) return WHT_ERR_BAD_DIM;
+    const bool umma_allowed = scale > 0.0f;  // the tcgen05 kernel finds a row's maximum before it scales
     const PrefixPlan f = plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, umma_allowed, sms);
     if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return WHT_ERR_WORKSPACE;
     AttnParams p{};
@@ -208,10 +219,10 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.parts = f.parts;
     set_parts(p, static_cast<unsigned char*>(workspace), T * Hq);
     p.prefix_pages = prefix_pages; p.prefix_len = prefix_len;
-    p.prefix_splits = f.prefix_splits; p.prefix_row_tiles = f.prefix_row_tiles; p.prefix_rw = f.prefix_rw;
+    p.prefix_splits = f.prefix_splits; p.prefix_row_tiles = f.prefix_row_tiles; p.prefix_nr = f.prefix_nr; p.prefix_wpu = f.prefix_wpu;
     p.page_table = page_table; p.kv_lens = kv_lens; p.q_start = q_start;
     p.table_width = table_width; p.B = B; p.max_q_len = max_q_len;
-    p.own_splits = f.own_splits; p.own_row_tiles = f.own_row_tiles; p.own_rw = f.own_rw;
+    p.own_splits = f.own_splits; p.own_row_tiles = f.own_row_tiles; p.own_nr = f.own_nr; p.own_wpu = f.own_wpu;
     p.T = T; p.num_pages = num_pages;
     p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
     p.scale_log2 = scale * wht::kLog2e;
@@ -244,6 +255,7 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     if (rc != WHT_OK) return rc;
     if (select < 1 || select > 1024 || table_width > 49152) return WHT_ERR_BAD_DIM;
     if (T == 0) return WHT_OK;
+    if (num_pages < 1) return WHT_ERR_BAD_DIM;
     if (!q || !k_cache || !v_cache || !summary || !out || !pages_out || !kv_lens || (table_width > 0 && !page_table)) return WHT_ERR_NULL;
     if (!strides_ok(q, q_stride_t, q_stride_h, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(summary) ||
         !aligned16(out) || !aligned16(workspace))
@@ -262,7 +274,7 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     set_parts(p, static_cast<unsigned char*>(workspace) + f.scores_bytes, T * Hq);
     p.page_table = page_table; p.kv_lens = kv_lens; p.q_start = q_start;
     p.table_width = table_width; p.B = B; p.max_q_len = max_q_len;
-    p.own_splits = f.splits; p.own_row_tiles = f.row_tiles; p.own_rw = f.rw;
+    p.own_splits = f.splits; p.own_row_tiles = f.row_tiles; p.own_nr = f.nr; p.own_wpu = f.wpu;
     p.chosen = pages_out; p.select = select;
     p.T = T; p.num_pages = num_pages;
     p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
@@ -286,10 +298,12 @@ int wht_attn_device_status(void) {
         if (rc != WHT_OK) return rc;
         any |= flag;
     }
-    unsigned waits = 0;
-    const int rc = take_device_error_attn_umma(&waits);
-    if (rc != WHT_OK) return rc;
-    if (waits) any |= wht::kAttnErrWait;
+    for (auto take : {take_device_error_attn_umma, take_device_error_attn_paged_bf16, take_device_error_attn_paged_f32}) {
+        unsigned waits = 0;
+        const int rc = take(&waits);
+        if (rc != WHT_OK) return rc;
+        if (waits) any |= wht::kAttnErrWait;
+    }
     return any & wht::kAttnErrIndex ? WHT_ERR_DEVICE_INDEX : any ? WHT_ERR_DEVICE_WAIT : WHT_OK;
 }
 
