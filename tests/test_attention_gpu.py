@@ -267,6 +267,27 @@ def test_shared_prefix_equals_its_parts_in_one(A):
     _check(shared, alone.double().cpu(), BF16, c["vc"].abs().max().item())
 
 
+@pytest.mark.parametrize("B,h,d,page", [(70, 16, 64, 64), (128, 16, 128, 128), (200, 8, 96, 32), (256, 8, 128, 16)])
+def test_long_prefix_by_both_kernels(A, B, h, d, page):
+    """Many key tiles per block of the tensor-core kernel, against the paged kernel on the prefix as everyone's own pages."""
+    prefix = 20011
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B)
+    n_pre = -(-prefix // page)
+    kc = torch.empty(n_pre, h, page, d, device="cuda", dtype=BF16).normal_(generator=g)
+    vc = torch.empty_like(kc).normal_(generator=g)
+    q = torch.empty(B, h, d, device="cuda", dtype=BF16).normal_(generator=g) * 3
+    pre = torch.randperm(n_pre, device="cuda", generator=g).to(torch.int32)
+    none = torch.zeros(B, dtype=torch.int32, device="cuda")
+    for _ in range(3):
+        shared = A.shared_prefix_attention(q, kc, vc, pre, prefix, pre[:1].expand(B, 1).contiguous(), none)
+        own = A.shared_prefix_attention(q, kc, vc, None, 0, pre[None].expand(B, -1).contiguous(), none + prefix)
+        # each is within the bound of the exact result
+        assert torch.isfinite(shared).all()
+        assert (shared.float() - own.float()).abs().max().item() <= 2 * R.tolerance(BF16, vc.abs().max().item())
+    A.device_status()
+
+
 def test_shared_prefix_reports_bad_pages_and_lengths(A):
     from paper_2603_08343_b200 import binding as B
     c = _paged(10, 2, 2, 1, 64, 16, BF16, 40, [1, 1], [20, 30], poison=False)
