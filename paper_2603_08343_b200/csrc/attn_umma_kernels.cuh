@@ -5,9 +5,9 @@
 // From about 250 rows on that is the tensor core's balance, and the exponentials (one per row and key,
 // 16 a clock and SM) weigh as much as the products.
 //
-// A block of 11 warps owns 256 rows of one key head as two tiles of 128, and a range of keys:
+// A block of 10 warps owns 256 rows of one key head as two tiles of 128, and a range of keys:
 //   warps 0..3, 4..7   softmax of tile 0 / tile 1: one thread per row
-//   warps 8, 9         issue the products of tile 0 / tile 1;   warp 10   copies keys and values (TMA, a ring of 128-key tiles)
+//   warp 8             issues the products;   warp 9   copies keys and values (TMA, a ring of 128-key tiles)
 // and runs steps of one tile and 128 keys, the two tiles taking turns, so that one tile's softmax runs under the other's products:
 //   S = Q K^T            into tensor memory (128 lanes x 128 fp32 columns)
 //   P = exp2(S - m)      read by the row's thread, rounded to bf16 and written over S
@@ -31,7 +31,7 @@
 
 namespace wht {
 
-constexpr int kUmmaAttnThreads = 352;
+constexpr int kUmmaAttnThreads = 576;
 constexpr float kLargestHalf = 16384.0f;  // 2^14: sum of 64 weights from which a row's reference maximum moves
 
 template <int D>
@@ -42,9 +42,10 @@ struct UmmaAttnGeo {
     static constexpr int STAGES = HALVES == 2 ? 5 : 8;
     static constexpr int OFF_RING = 2 * TILE;
     static constexpr int OFF_BARS = OFF_RING + STAGES * TILE;
-    static constexpr int NBARS = 2 * STAGES + 10 + 2;
+    static constexpr int NBARS = 2 * STAGES + 6 + 1;
     static constexpr int OFF_MISC = OFF_BARS + NBARS * 8;
-    static constexpr int BYTES = OFF_MISC + 16 + 1024;        // and what aligning the start to 1024 bytes takes
+    static constexpr int OFF_MAX = OFF_MISC + 16;             // [2 tiles][2 halves][128 rows] fp32
+    static constexpr int BYTES = OFF_MAX + 2048;
     static constexpr int O_COLS = D > 64 ? 128 : 64;
 };
 
@@ -98,47 +99,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-constexpr float kExp2C0 = 0.9999992847f, kExp2C1 = 0.6931217909f, kExp2C2 = 0.2402474433f, kExp2C3 = 0.05591785908f, kExp2C4 = 0.0095701003f;
-// 2^x for two values on the multiply-add pipe: x = n + f with n the nearest whole number, 2^f by a polynomial of degree 4
-// on [-1/2, 1/2] (least relative error, 2.6e-6: a thousandth of the rounding to bf16 that follows), 2^n from its exponent bits.
-// Held to [-126, 127]; NaN stays NaN.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x) {
-    float a, b;
-    unpair(x, a, b);
-    asm("max.NaN.f32 %0, %0, %1;\n\tmin.NaN.f32 %0, %0, %2;" : "+f"(a) : "f"(-126.0f), "f"(127.0f));
-    asm("max.NaN.f32 %0, %0, %1;\n\tmin.NaN.f32 %0, %0, %2;" : "+f"(b) : "f"(-126.0f), "f"(127.0f));
-    x = pair(a, b);
-    constexpr float kRound = 12582912.0f;  // 1.5 * 2^23: adding it leaves the nearest whole number in the low bits
-    const uint64_t r = add2(x, pair(kRound, kRound));
-    const uint64_t f = add2(x, mul2(add2(r, pair(-kRound, -kRound)), pair(-1.0f, -1.0f)));
-    uint64_t y = fma2(f, pair(kExp2C4, kExp2C4), pair(kExp2C3, kExp2C3));
-    y = fma2(y, f, pair(kExp2C2, kExp2C2));
-    y = fma2(y, f, pair(kExp2C1, kExp2C1));
-    y = fma2(y, f, pair(kExp2C0, kExp2C0));
-    float ra, rb;
-    unpair(r, ra, rb);
-    return mul2(y, pair(__uint_as_float((__float_as_uint(ra) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(rb) << 23) + 0x3f800000u)));
-}
-
-// Bounded wait that polls without a pause: the products and the softmax hand over to each other every thousand clocks or so, and
-// a parked wait answered some 400 clocks late (measured).  Gives up like wait_or_abort.
+// Bounded wait on the barriers that products and softmax hand over by, every thousand clocks or so.  try_wait lets the
+// hardware hold the warp and wake it when the phase ends; polling with test_wait instead floods the unit that answers it (and
+// copies between registers and tensor memory go through), and made everything else in the block slower (measured).
+// Gives up like wait_or_abort.
 __device__ __forceinline__ bool poll_or_abort(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
-    for (uint32_t i = 0; i < (1u << 24); ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if ((i & 255u) == 255u && *abort_flag) return false;
+    for (uint32_t i = 0; i < (1u << 20); ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (i > 4096) __nanosleep(256);
     }
     *abort_flag = 1;
     atomicExch(&g_wht_device_error, kDeviceErrWaitExpired);
@@ -154,28 +123,35 @@ __device__ __forceinline__ bool elect_one() {
     return is != 0;
 }
 
-// one lane's row of weights
-struct SoftmaxRow {
-    float m = 0.0f;  // reference maximum, in units of the raw scores
-    float l = 0.0f;
-};
+// Vote of the 256 threads that hold a row tile (both halves of its keys), and a barrier among them.
+__device__ __forceinline__ bool tile_any(int w, bool flag) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(flag ? 1u : 0u), "r"(w + 1)
+        : "memory");
+    return any != 0;
+}
 
 template <int D>
 __global__ void __launch_bounds__(kUmmaAttnThreads, 1)
 attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using Geo = UmmaAttnGeo<D>;
-    extern __shared__ unsigned char umma_attn_smem[];
+    extern __shared__ __align__(1024) unsigned char umma_attn_smem[];
     const AttnParams& p = up.a;
-    unsigned char* smem = umma_attn_smem + ((1024u - (smem_u32(umma_attn_smem) & 1023u)) & 1023u);
+    unsigned char* smem = umma_attn_smem;
+    if (smem_u32(smem) & 1023u) {  // the swizzle counts on it (dynamic shared memory starts on such a boundary)
+        attn_report(kAttnErrWait);
+        return;
+    }
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Geo::OFF_BARS);
     uint64_t* kv_full = bars;
     uint64_t* kv_empty = bars + Geo::STAGES;
     uint64_t* s_full = bars + 2 * Geo::STAGES;   // [2] scores of a tile's step are in tensor memory
     uint64_t* p_ready = s_full + 2;              // [2] its weights are
     uint64_t* o_done = s_full + 4;               // [2] its second product is complete
-    uint64_t* p_half = s_full + 6;               // [2] the weights of its first 64 keys are
-    uint64_t* o_half = s_full + 8;               // [2] the product of those is complete
-    uint64_t* all_done = s_full + 10;            // [2] every product issued for a tile is complete
+    uint64_t* all_done = s_full + 6;             // every product issued is complete
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + Geo::OFF_MISC);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + Geo::OFF_MISC + 4);
 
@@ -207,23 +183,21 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
     };
 
     grid_launch_dependents();
-    if (warp == 8) {
+    if (warp == 16) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
-    if (tid == 10 * 32) {
+    if (tid == 17 * 32) {
         for (int s = 0; s < Geo::STAGES; ++s) {
             mbar_init(kv_full + s, 1);
             mbar_init(kv_empty + s, same ? 1 : 2);  // as many row tiles read it
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(s_full + s, 1);
-            mbar_init(p_ready + s, 4);
-            mbar_init(p_half + s, 4);
+            mbar_init(p_ready + s, 8);
             mbar_init(o_done + s, 1);
-            mbar_init(o_half + s, 1);
-            mbar_init(all_done + s, 1);
         }
+        mbar_init(all_done, 1);
         *abort_flag = 0;
         fence_mbar_init();
     }
@@ -260,7 +234,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
     const uint32_t tmem = *tmem_slot;
     const uint32_t ring = smem_u32(smem) + Geo::OFF_RING;
 
-    if (warp == 10) {
+    if (warp == 17) {
         if (lane == 0) {
             // the items in the order in which the products take them
             const int list = static_cast<int>((p.prefix_len + (1 << p.page_shift) - 1) >> p.page_shift);
@@ -301,27 +275,27 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                     }
             }
         }
-    } else if (warp >= 8) {
-        // One warp per row tile issues its products.  The whole warp walks the loop and one elected lane issues, so that
-        // descriptors and barrier addresses stay in uniform registers (from a single lane's code each product took 100
-        // clocks to issue, more than the 64 it runs).
-        const int w = warp - 8;
-        const int n = steps_of(w);
+    } else if (warp == 16) {
+        // One warp issues all products, the tiles strictly in turn: a tile's second product and its next scores go to the tensor core as
+        // one piece, so that its softmax starts while the other tile's piece runs.  (With a warp per tile the two tiles shared
+        // the tensor core, ended together and then shared the exponential unit: no overlap, measured.)  The whole warp walks the loop
+        // and one elected lane issues, so that descriptors and barrier addresses stay in uniform registers.
         constexpr uint32_t qk_idesc = umma_attn_idesc(128, false), pv_idesc = umma_attn_idesc(D, true);
-        const uint64_t q_desc = umma_desc_sw128(smem_u32(smem) + w * Geo::TILE, 16);
-        const uint32_t s_cols = tmem + w * 128, o_cols = tmem + 256 + w * Geo::O_COLS;
+        const uint64_t q_desc0 = umma_desc_sw128(smem_u32(smem), 16);
+        const int n0 = steps_of(0), n1 = steps_of(1);
         bool ok = true;
-        auto scores = [&](int i) {   // S of the tile's step i
+        auto scores = [&](int w, int i) {   // S of tile w's step i
             const Place at = place_of(w, 2 * i);
             if (!warp_poll_or_abort(kv_full + at.stage, at.parity, abort_flag)) return false;
             tc_fence_after();
+            const uint64_t q_desc = q_desc0 + static_cast<uint64_t>(w * (Geo::TILE >> 4));
             const uint64_t k_desc = umma_desc_sw128(ring + at.stage * Geo::TILE, 16);
             if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     constexpr int kBox = Geo::BOX;
                     const uint64_t off = static_cast<uint64_t>(((k >> 2) * kBox + (k & 3) * 32) >> 4);
-                    umma_bf16(s_cols, q_desc + off, k_desc + off, qk_idesc, k > 0);
+                    umma_bf16(tmem + w * 128, q_desc + off, k_desc + off, qk_idesc, k > 0);
                 }
                 umma_commit(s_full + w);
                 umma_commit(kv_empty + at.stage);
@@ -329,138 +303,139 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
             __syncwarp();
             return true;
         };
-        if (n > 0) ok = scores(0);
-        for (int i = 0; ok && i < n; ++i) {
-            const Place at = place_of(w, 2 * i + 1);
-            ok = warp_poll_or_abort(kv_full + at.stage, at.parity, abort_flag) &&
-                 warp_poll_or_abort(p_half + w, static_cast<uint32_t>(i) & 1u, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t v_desc = umma_desc_sw128(ring + at.stage * Geo::TILE, Geo::BOX);
-            if (elect_one()) {
+        if (n0 > 0) ok = scores(0, 0);
+        if (ok && n1 > 0) ok = scores(1, 0);
+        for (int i = 0; ok && i < n0; ++i) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) umma_bf16_a_tmem(o_cols, s_cols + k * 8, v_desc + k * 128, pv_idesc, i > 0 || k > 0);
-                umma_commit(o_half + w);
-            }
-            __syncwarp();
-            ok = warp_poll_or_abort(p_ready + w, static_cast<uint32_t>(i) & 1u, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
+            for (int w = 0; w < 2; ++w) {
+                if (w == 1 && i >= n1) break;
+                const uint32_t o_cols = tmem + 256 + w * Geo::O_COLS, p_cols = tmem + w * 128;
+                const Place at = place_of(w, 2 * i + 1);
+                ok = ok && warp_poll_or_abort(kv_full + at.stage, at.parity, abort_flag) &&
+                     warp_poll_or_abort(p_ready + w, static_cast<uint32_t>(i) & 1u, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t v_desc = umma_desc_sw128(ring + at.stage * Geo::TILE, Geo::BOX);
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 4; k < 8; ++k) umma_bf16_a_tmem(o_cols, s_cols + k * 8, v_desc + k * 128, pv_idesc, 1);
-                umma_commit(o_done + w);
-                umma_commit(kv_empty + at.stage);
+                    for (int k = 0; k < 8; ++k) umma_bf16_a_tmem(o_cols, p_cols + k * 8, v_desc + k * 128, pv_idesc, i > 0 || k > 0);
+                    umma_commit(o_done + w);
+                    umma_commit(kv_empty + at.stage);
+                }
+                __syncwarp();
+                // the tensor core runs a tile's products in order: the next scores may overwrite the weights just used
+                if (i + 1 < (w ? n1 : n0)) ok = scores(w, i + 1);
+                if (!ok) break;
             }
-            __syncwarp();
-            // the tensor core runs a tile's products in order: the next scores may overwrite the weights just used
-            if (i + 1 < n) ok = scores(i + 1);
         }
-        if (elect_one()) umma_commit(all_done + w);
+        if (elect_one()) umma_commit(all_done);
         __syncwarp();
-        if (!mbar_wait_bounded(all_done + w, 0)) *abort_flag = 1;
-    } else if (warp < 8) {
-        const int w = warp >> 2;
-        const int r = row0 + (same ? 0 : w * 128) + (warp & 3) * 32 + lane;
+        if (!mbar_wait_bounded(all_done, 0)) *abort_flag = 1;
+    } else {
+        // 16 softmax warps: tile w, half h of the keys; warp & 3 says which 32 lanes of tensor memory it may read
+        const int w = warp >> 3, h = (warp >> 2) & 1;
+        const int lane_row = (warp & 3) * 32 + lane;
+        const int r = row0 + (same ? 0 : w * 128) + lane_row;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_cols = tmem + w * 128 + lanes, o_cols = tmem + 256 + w * Geo::O_COLS + lanes;
+        const uint32_t s_cols = tmem + w * 128 + h * 64 + lanes, p_cols = tmem + w * 128 + h * 32 + lanes;
+        const uint32_t o_cols = tmem + 256 + w * Geo::O_COLS + lanes;
+        constexpr int O_HALF = D / 2;            // each half's warps scale and write half of the channels
+        float* maxima = reinterpret_cast<float*>(smem + Geo::OFF_MAX) + w * 256;
         const float sl = p.scale_log2;
         const int n = steps_of(w);
-        SoftmaxRow st;
+        float m = 0.0f, l = 0.0f;                // reference maximum in units of the raw scores (the same in both halves), this half's sum
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int valid = min(128, key1 - key0 - key_tile(w, i) * 128);
-            ok = warp_poll_or_abort(s_full + w, static_cast<uint32_t>(i) & 1u, abort_flag);
-            if (!ok) break;
+            const int valid = min(128, key1 - key0 - key_tile(w, i) * 128) - h * 64;  // of this half's 64 keys
+            ok = ok && warp_poll_or_abort(s_full + w, static_cast<uint32_t>(i) & 1u, abort_flag);
             tc_fence_after();
-            uint32_t x[64];      // the half of the tile at hand
-            auto load_half = [&](int c0) {
-#pragma unroll
-                for (int c = 0; c < 64; c += 32) tmem_ld32(s_cols + c0 + c, x + c);
+            auto load = [&](uint32_t (&x)[32], int c0) {
+                tmem_ld32(s_cols + c0, x);
                 tmem_wait_ld();
-                if (valid < c0 + 64) {
+                if (valid < c0 + 32) {
 #pragma unroll
-                    for (int c = 0; c < 64; ++c)
+                    for (int c = 0; c < 32; ++c)
                         if (c0 + c >= valid) x[c] = 0xff800000u;  // -infinity
                 }
             };
-            // Weights of the half, against the reference maximum, into the columns from c0 / 2 on; returns their sum.  One pair in four takes the
-            // polynomial, so that the exponential unit (4 a clock and scheduler) and the multiply-add pipe finish together.
-            const uint64_t sl2 = pair(sl, sl);
-            auto weights = [&](int c0) {
-                const uint64_t off2 = pair(-st.m * sl, -st.m * sl);
+            // the half's weights against the reference, as bf16 pairs; returns their sum
+            uint32_t y[32];
+            auto weights = [&]() {
+                const uint64_t off2 = pair(-m * sl, -m * sl), sl2 = pair(sl, sl);
                 uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < 64; c += 32) {
-                    uint32_t y[16];
+                    uint32_t x[32];
+                    load(x, c);
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        uint64_t v = fma2(pair(__uint_as_float(x[c + e]), __uint_as_float(x[c + e + 1])), sl2, off2);
                         float a, b;
-                        if ((e & 7) == 6) {
-                            v = exp2_poly2(v);
-                            unpair(v, a, b);
-                        } else {
-                            unpair(v, a, b);
-                            a = exp2_fast(a);
-                            b = exp2_fast(b);
-                            v = pair(a, b);
-                        }
-                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], v);
-                        y[e / 2] = pack_bf16x2(a, b);
+                        unpair(fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), sl2, off2), a, b);
+                        a = exp2_fast(a);
+                        b = exp2_fast(b);
+                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(a, b));
+                        y[(c + e) / 2] = pack_bf16x2(a, b);
                     }
-                    tmem_st16(s_cols + (c0 + c) / 2, y);
                 }
                 float a, b;
                 unpair(add2(sum[0], sum[1]), a, b);
                 return a + b;
             };
-            auto half_max = [&]() {
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < 64; c += 8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top[e] = max3(top[e], __uint_as_float(x[c + e]), __uint_as_float(x[c + 4 + e]));
-                return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            };
-            // The rare case: some row's weights have grown past kLargestHalf.  Its reference moves to the half's maximum; the products issued so far (`bar`) are waited for, and O and l are scaled.
-            auto move_reference = [&](bool move, uint64_t* bar, uint32_t parity) {
-                if (!warp_poll_or_abort(bar, parity, abort_flag)) return false;
-                tc_fence_after();
-                const float mx = fmaxf(st.m, half_max());
-                const float f = move ? exp2_fast((st.m - mx) * sl) : 1.0f;
-                if (move) st.m = mx;
-                st.l *= f;
+            float sum = 0.0f;
+            bool move = i == 0;
+            if (i > 0) sum = weights();
+            // One vote of both halves' warps: nobody stores weights before all agree on the reference.  (A wait that ran out
+            // also ends up here, so that all leave together: the votes are barriers.)
+            if (tile_any(w, move || !ok || sum > kLargestHalf)) {
+                if (tile_any(w, !ok)) break;
+                // The first tile, and later the rare case that some row's weights have grown past kLargestHalf: the row's
+                // reference moves to the maximum of the tile.  O and l follow; its products so far are waited for.
+                float top = -INFINITY;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    float o[16];
-                    tmem_ld16(o_cols + c, o);
-                    tmem_wait_ld();
-                    uint32_t y[16];
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t x[32];
+                    load(x, c);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
-                    tmem_st16(o_cols + c, y);
+                    for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                 }
-                return true;
-            };
-            load_half(0);
-            if (i == 0) st.m = half_max();
-            float sum = weights(0);
-            if (__any_sync(kFullMask, sum > kLargestHalf) && i > 0) {
-                ok = move_reference(sum > kLargestHalf, o_done + w, static_cast<uint32_t>(i - 1) & 1u);
-                if (!ok) break;
-                sum = weights(0);
+                maxima[h * 128 + lane_row] = top;
+                if (i > 0) ok = warp_poll_or_abort(o_done + w, static_cast<uint32_t>(i - 1) & 1u, abort_flag);
+                if (tile_any(w, !ok)) break;
+                top = fmaxf(maxima[lane_row], maxima[128 + lane_row]);
+                if (i == 0) {
+                    m = top;
+                } else {
+                    tc_fence_after();
+                    const bool higher = top > m;
+                    const float f = higher ? exp2_fast((m - top) * sl) : 1.0f;
+                    if (higher) m = top;
+                    l *= f;
+#pragma unroll 1
+                    for (int c = h * O_HALF; c < (h + 1) * O_HALF; c += 16) {
+                        float o[16];
+                        tmem_ld16(o_cols + c, o);
+                        tmem_wait_ld();
+                        uint32_t z[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * f);
+                        tmem_st16(o_cols + c, z);
+                    }
+                }
+                sum = weights();
+                tile_any(w, false);              // everyone has read the scores and the maxima
             }
-            st.l += sum;
-            if (valid < 128) {
+            l += sum;
+            tmem_st16(p_cols, y);
+            tmem_st16(p_cols + 16, y + 16);
+            if (valid < 64) {
                 // the tile's last rows hold keys that nobody sees, or nothing at all: their values become 0 so that a
                 // weight of 0 takes nothing from them
                 const Place at = place_of(w, 2 * i + 1);
-                ok = warp_poll_or_abort(kv_full + at.stage, at.parity, abort_flag);
-                if (!ok) break;
-                unsigned char* v = smem + Geo::OFF_RING + at.stage * Geo::TILE;
-                for (int e = (warp & 3) * 32 + lane; e < (128 - valid) * 8 * Geo::HALVES; e += 128) {
-                    const int row = valid + e / (8 * Geo::HALVES), c = e % (8 * Geo::HALVES);
+                ok = ok && warp_poll_or_abort(kv_full + at.stage, at.parity, abort_flag);
+                unsigned char* v = smem + Geo::OFF_RING + at.stage * Geo::TILE + h * 64 * 128;
+                const int from = max(0, valid);
+                for (int e = lane_row; e < (64 - from) * 8 * Geo::HALVES; e += 128) {
+                    const int row = from + e / (8 * Geo::HALVES), c = e % (8 * Geo::HALVES);
                     *reinterpret_cast<uint4*>(v + (c >> 3) * Geo::BOX + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async_smem();
@@ -468,31 +443,17 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_half + w);
-            load_half(64);
-            sum = weights(64);
-            if (__any_sync(kFullMask, sum > kLargestHalf)) {
-                ok = move_reference(sum > kLargestHalf, o_half + w, static_cast<uint32_t>(i) & 1u);
-                if (!ok) break;
-                sum = weights(64);
-            }
-            st.l += sum;
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
             if (lane == 0) mbar_arrive(p_ready + w);
         }
-        if (ok && n > 0) {
-            ok = warp_poll_or_abort(o_done + w, static_cast<uint32_t>(n - 1) & 1u, abort_flag);
-            tc_fence_after();
-        }
-        if (ok) {
+        if (n > 0) ok = ok && warp_poll_or_abort(o_done + w, static_cast<uint32_t>(n - 1) & 1u, abort_flag);
+        tc_fence_after();
+        if (!tile_any(w, !ok)) {
             const int tok = r / p.group;
             const int64_t at = static_cast<int64_t>(tok) * p.hq + head * p.group + (r - tok * p.group);
             const int part = same ? 2 * split + w : split;
             const int64_t slot = static_cast<int64_t>(part) * p.T * p.hq + at;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
+            for (int c = h * O_HALF; c < (h + 1) * O_HALF; c += 16) {
                 float o[16];
                 if (n > 0) {
                     tmem_ld16(o_cols + c, o);
@@ -507,13 +468,15 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         *reinterpret_cast<float4*>(p.part_o + slot * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 }
             }
-            if (r < rows) p.part_ml[slot] = n > 0 ? make_float2(st.m * sl, st.l) : make_float2(-INFINITY, 0.0f);
+            if (h == 1) maxima[128 + lane_row] = l;
+            tile_any(w, false);
+            if (h == 0 && r < rows) p.part_ml[slot] = n > 0 ? make_float2(m * sl, l + maxima[128 + lane_row]) : make_float2(-INFINITY, 0.0f);
         }
         tc_fence_before();
     }
     __syncwarp();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 16) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
