@@ -19,7 +19,7 @@
 //     of a chunk, and a ring of chunks per warp keeps up to 24 KB in flight; no warp waits for another in the loop.
 //   - m moves only when a score passes it by more than 2^8, found by one vote: weights up to 2^8 are as exact as weights up to 1, and
 //     neither the reduction over lanes nor the scaling of o is in the common path.
-// A unit's keys are divided over 1, 2 or 4 warps of a block, which join their (m, l, o) through shared memory, and over
+// A unit's keys are divided over 1, 2, 4 or 8 warps of a block, which join their (m, l, o) through shared memory, and over
 // blocks where there are too few units to fill the machine (attn_join_kernel adds those parts up).
 //
 // fp32 tensors: both operands of each product are split in two tf32 terms (three products; what is dropped is below 2^-21
@@ -33,7 +33,6 @@
 
 namespace wht {
 
-constexpr int kAttnThreads = 128;
 constexpr int kChunk = 16;       // keys per chunk: they lie in one page
 constexpr float kSlack = 8.0f;   // log2 of how far a score may pass the reference maximum
 
@@ -53,6 +52,7 @@ struct AttnParams {
     const int32_t *page_table, *kv_lens, *q_start;
     int table_width, B, max_q_len;
     int own_splits, own_row_tiles, own_nr, own_wpu;
+    int joint;             // small calls: every sequence walks the prefix's pages before its own, and nothing is left to join
     // chosen pages: [T x Hkv x select] indices into the sequence's table
     const int32_t* chosen;
     int select;
@@ -69,17 +69,20 @@ struct UmmaAttnParams {
     int same_rows;   // 128 rows or fewer: both of a block's tiles hold them, each with every second key tile
 };
 
-template <typename T, int D>
+// W: warps per block.  Four, so that two blocks fit an SM; eight for small calls, where a unit is a block and all that counts is
+// how soon its last key is done.
+template <typename T, int D, int W>
 struct AttnGeo {
+    static constexpr int THREADS = 32 * W;
     static constexpr bool F32 = std::is_same<T, float>::value;
     static constexpr int BOX_CH = 128 / static_cast<int>(sizeof(T));    // channels per 128-byte box
     static constexpr int BOXES = (D + BOX_CH - 1) / BOX_CH;             // per key row (the last may reach over the row's end: zeros)
     static constexpr int BOX_BYTES = kChunk * 128;
     static constexpr int SIDE = BOXES * BOX_BYTES;                      // keys (or values) of a chunk
-    static constexpr int STAGES = 2 * SIDE >= 16384 ? 2 : 24576 / (2 * SIDE);
-    static constexpr int RING = STAGES * 2 * SIDE;                      // per warp
-    static constexpr int OFF_BARS = 4 * RING;
-    static constexpr int BYTES = OFF_BARS + 4 * STAGES * 8 + 1024;      // and what aligning the start to 1024 bytes takes
+    static constexpr int STAGES = 2 * SIDE >= 16384 ? (W > 4 ? 1 : 2) : 24576 / (2 * SIDE);
+    static constexpr int RING = STAGES * 2 * SIDE > 18432 ? STAGES * 2 * SIDE : 18432;  // per warp; holds the join buffer too
+    static constexpr int OFF_BARS = W * RING;
+    static constexpr int BYTES = OFF_BARS + W * STAGES * 8 + 1024;      // and what aligning the start to 1024 bytes takes
     static constexpr int JOIN_LD = D + 4;                               // floats per row of the join buffer: no bank conflicts
     static_assert(32 * (JOIN_LD + 2) * 4 <= RING, "the join buffer reuses the ring");
     // byte offset of 16-byte piece c of row r (the copy engine's 128-byte swizzle)
@@ -94,17 +97,19 @@ struct AttnUnit {
     int row0;            // first row of this unit
     const int32_t* ids;  // page list: physical pages, or (chosen) indices into `table`
     const int32_t* table;
-    int list;            // entries of the list
     int key0, key1;      // this part's keys, counted along the list; key0 a multiple of 16
-    int limit0, step;    // row r sees keys < min(key1, limit0 + (r / group) * step)
+    const int32_t* ids2; // (joint) the list goes on here after list1 entries
+    int list1;
+    int hole0, hole1;    // (joint) keys hole0 .. hole1 - 1 are the unused end of the prefix's last page; else 0
+    int limit0, step;    // row r sees keys < min(key1, max(hole1, limit0 + (r / group) * step)), but for the hole
     int part;            // where the partial result goes
     int nr, wpu;         // 8-row tiles, warps
 };
 
-template <typename T, int D, int NR>
+template <typename T, int D, int NR, int W>
 __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map,
                                           unsigned char* smem) {
-    using Geo = AttnGeo<T, D>;
+    using Geo = AttnGeo<T, D, W>;
     constexpr bool F32 = Geo::F32;
     constexpr int QS = D / (F32 ? 8 : 16);       // steps of the first product
     constexpr int DT = D / 16;                   // 16-channel tiles of the output
@@ -126,7 +131,8 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
         const int key = u.key0 + (wi + (j + lane) * u.wpu) * kChunk;
         int y = 0;
         if (j + lane < chunks) {
-            int pg = __ldg(u.ids + (key >> p.page_shift));
+            const int e = key >> p.page_shift;
+            int pg = __ldg(e < u.list1 ? u.ids + e : u.ids2 + (e - u.list1));
             if (u.table) pg = pg >= 0 ? __ldg(u.table + pg) : -1;
             if (pg < 0 || pg >= p.num_pages) {
                 attn_report(kAttnErrIndex);
@@ -183,10 +189,10 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int row = u.row0 + 8 * n + 2 * c4 + e;
-            limit[n][e] = min(u.key1, u.limit0 + (row / p.group) * u.step);
+            limit[n][e] = min(u.key1, max(u.hole1, u.limit0 + (row / p.group) * u.step));
             if (row >= u.rows) limit[n][e] = u.key1;
         }
-    least_limit = min(u.key1, u.limit0 + (u.row0 / p.group) * u.step);
+    least_limit = min(u.key1, max(u.hole1, u.limit0 + (u.row0 / p.group) * u.step));
 
     float o[NR][DT][4];
     float m[NR][2], l[NR][2];
@@ -256,10 +262,11 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
         const int s = j % Geo::STAGES;
         mbar_wait_bounded(full + s, static_cast<uint32_t>(j / Geo::STAGES) & 1u);
         const int base = u.key0 + (wi + j * u.wpu) * kChunk;
-        const bool mask = base + kChunk > least_limit;
-        if (base + kChunk > u.key1) {
+        const int end = base < u.hole1 ? min(u.hole0, u.key1) : u.key1;  // the first key from `base` on that nobody sees
+        const bool mask = base + kChunk > min(end, least_limit);
+        if (base + kChunk > end) {
             // keys that nobody sees: their values become 0, so that a weight of 0 takes nothing from whatever lies there
-            const int valid = u.key1 - base;
+            const int valid = max(0, end - base);
             unsigned char* v = ring + s * 2 * Geo::SIDE + Geo::SIDE;
             for (int i = lane; i < (kChunk - valid) * 8 * Geo::BOXES; i += 32) {
                 const int r = valid + i / (8 * Geo::BOXES), c = i % (8 * Geo::BOXES);
@@ -321,7 +328,8 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[n][i] *= p.scale_log2;
-                if (mask && base + r4 + 8 * (i >> 1) >= limit[n][i & 1]) x[n][i] = -INFINITY;
+                const int key = base + r4 + 8 * (i >> 1);
+                if (mask && (key >= limit[n][i & 1] || (key >= u.hole0 && key < u.hole1))) x[n][i] = -INFINITY;
                 passes = passes || x[n][i] > m[n][i & 1] + kSlack;
             }
         if (__any_sync(kFullMask, passes)) {
@@ -425,13 +433,13 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
     }
 }
 
-template <typename T, int D>
+template <typename T, int D, int W>
 __device__ __forceinline__ void attn_run(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map) {
     extern __shared__ unsigned char smem_attn[];
     unsigned char* smem = smem_attn + ((1024u - (smem_u32(smem_attn) & 1023u)) & 1023u);
-    if (u.nr == 1) attn_unit<T, D, 1>(p, u, k_map, v_map, smem);
-    else if (u.nr == 2) attn_unit<T, D, 2>(p, u, k_map, v_map, smem);
-    else attn_unit<T, D, 4>(p, u, k_map, v_map, smem);
+    if (u.nr == 1) attn_unit<T, D, 1, W>(p, u, k_map, v_map, smem);
+    else if (u.nr == 2) attn_unit<T, D, 2, W>(p, u, k_map, v_map, smem);
+    else attn_unit<T, D, 4, W>(p, u, k_map, v_map, smem);
 }
 
 // A length read on the device, held to what the tables can hold.
@@ -481,18 +489,20 @@ __device__ __forceinline__ void attn_part(int keys, int tile, int splits, int s,
 }
 
 // Prefix and own pages in one launch: blocks below prefix_blocks take the prefix.
-template <typename T, int D>
-__global__ void __launch_bounds__(kAttnThreads)
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(32 * W)
 attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     const int prefix_units = p.prefix_splits * p.prefix_row_tiles * p.hkv;
-    const int prefix_blocks = (prefix_units * p.prefix_wpu + 3) / 4;
+    const int prefix_blocks = (prefix_units * p.prefix_wpu + W - 1) / W;
     const int warp = threadIdx.x >> 5;
     const bool last_block = blockIdx.x == gridDim.x - 1;
     AttnUnit u;
     bool work;
+    u.list1 = 0x7fffffff;
+    u.hole0 = u.hole1 = 0;
     grid_launch_dependents();
     if (static_cast<int>(blockIdx.x) < prefix_blocks) {
-        int b = (blockIdx.x * 4 + warp) / p.prefix_wpu;
+        int b = (blockIdx.x * W + warp) / p.prefix_wpu;
         work = b < prefix_units;
         u.part = b % p.prefix_splits;
         b /= p.prefix_splits;
@@ -502,14 +512,13 @@ attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
         u.rows = static_cast<int>(p.T) * p.group;
         u.ids = p.prefix_pages;
         const int keys = static_cast<int>(p.prefix_len);
-        u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
         attn_part(keys, kChunk * 4, p.prefix_splits, u.part, u.key0, u.key1);
         u.limit0 = keys;
         u.step = 0;
         u.nr = p.prefix_nr;
         u.wpu = p.prefix_wpu;
     } else {
-        int b = ((blockIdx.x - prefix_blocks) * 4 + warp) / p.own_wpu;
+        int b = ((blockIdx.x - prefix_blocks) * W + warp) / p.own_wpu;
         const int split = b % p.own_splits;
         b /= p.own_splits;
         u.part = (p.parts - p.own_splits) + split;
@@ -528,18 +537,25 @@ attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
         }
         u.rows = count * p.group;
         work = u.row0 < u.rows;
-        u.list = (keys + (1 << p.page_shift) - 1) >> p.page_shift;
+        if (p.joint) {
+            u.ids2 = u.ids;
+            u.ids = p.prefix_pages;
+            u.hole0 = static_cast<int>(p.prefix_len);
+            u.list1 = (u.hole0 + (1 << p.page_shift) - 1) >> p.page_shift;
+            u.hole1 = u.list1 << p.page_shift;
+            keys += u.hole1;
+        }
         // the unit's last row sees the most: nothing beyond its place is read
         u.limit0 = keys - count + 1;
         u.step = 1;
         const int last_tok = (min(u.rows, u.row0 + 8 * p.own_nr) - 1) / p.group;
         attn_part(keys, kChunk * 4, p.own_splits, split, u.key0, u.key1);
-        u.key1 = max(u.key0, min(u.key1, u.limit0 + last_tok));
+        u.key1 = max(u.key0, min(u.key1, max(u.hole1, u.limit0 + last_tok)));
         u.nr = p.own_nr;
         u.wpu = p.own_wpu;
     }
     u.table = nullptr;
-    if (work) attn_run<T, D>(p, u, &k_map, &v_map);
+    if (work) attn_run<T, D, W>(p, u, &k_map, &v_map);
     // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
     // for this grid alone, so this grid does not end before that one has.
     if (last_block) grid_dependency_wait();
@@ -563,13 +579,13 @@ __device__ __forceinline__ int attn_sequence_of(const AttnParams& p, int64_t t) 
 }
 
 // Chosen pages: one token and key head (and a part of the list) per unit.
-template <typename T, int D>
-__global__ void __launch_bounds__(kAttnThreads)
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(32 * W)
 attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     AttnUnit u;
     grid_dependency_wait();  // the list comes from the kernel before
     grid_launch_dependents();
-    int64_t b = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5)) / p.own_wpu;
+    int64_t b = (static_cast<int64_t>(blockIdx.x) * W + (threadIdx.x >> 5)) / p.own_wpu;
     u.part = static_cast<int>(b % p.own_splits);
     b /= p.own_splits;
     u.row0 = static_cast<int>(b % p.own_row_tiles) * 8 * p.own_nr;
@@ -585,15 +601,16 @@ attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
     const int64_t place = attn_place(p, seq, u.token0, first, count);
     u.ids = p.chosen + (u.token0 * p.hkv + u.head) * p.select;
     u.table = p.page_table + static_cast<int64_t>(seq) * p.table_width;
-    const int page = static_cast<int>(place >> p.page_shift);
-    u.list = place < 0 ? 0 : min(p.select, page + 1);
-    const int keys = place < 0 ? 0 : ((u.list - 1) << p.page_shift) + static_cast<int>(place & ((1 << p.page_shift) - 1)) + 1;
+    u.list1 = 0x7fffffff;
+    u.hole0 = u.hole1 = 0;
+    const int list = place < 0 ? 0 : min(p.select, static_cast<int>(place >> p.page_shift) + 1);
+    const int keys = place < 0 ? 0 : ((list - 1) << p.page_shift) + static_cast<int>(place & ((1 << p.page_shift) - 1)) + 1;
     attn_part(keys, kChunk * 4, p.own_splits, u.part, u.key0, u.key1);
     u.limit0 = keys;
     u.step = 0;
     u.nr = p.own_nr;
     u.wpu = p.own_wpu;
-    attn_run<T, D>(p, u, &k_map, &v_map);
+    attn_run<T, D, W>(p, u, &k_map, &v_map);
 }
 
 // Joins the parts of each row: out = sum_s exp(m_s - m) o_s / sum_s exp(m_s - m) l_s.  One warp per row, lanes
@@ -619,14 +636,19 @@ attn_join_kernel(const float2* __restrict__ ml, const float* __restrict__ po, T*
         if (s0 + lane < parts) mine = ml[(s0 + lane) * rows + row];
         const float f = exp2_fast(mine.x - z);
         l += f * mine.y;
+        // eight parts' products in flight at a time: the rows are short and the wait is all latency
         const int n = min(32, parts - s0);
-#pragma unroll 4
-        for (int s = 0; s < n; ++s) {
-            const float w = __shfl_sync(kFullMask, f, s);
-            // a part that holds no key of this row has weight 0 and its product is 0
-            if (lane * PER < D) {
-                const float4 x = *reinterpret_cast<const float4*>(po + ((s0 + s) * rows + row) * D + lane * PER);
-                acc.x += w * x.x; acc.y += w * x.y; acc.z += w * x.z; acc.w += w * x.w;
+        for (int s1 = 0; s1 < n; s1 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s1 + s < n && lane * PER < D) x[s] = *reinterpret_cast<const float4*>(po + ((s0 + s1 + s) * rows + row) * D + lane * PER);
+            }
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const float w = __shfl_sync(kFullMask, f, s1 + s);  // (a part that holds no key of this row has weight 0)
+                acc.x += w * x[s].x; acc.y += w * x[s].y; acc.z += w * x[s].z; acc.w += w * x[s].w;
             }
         }
     }

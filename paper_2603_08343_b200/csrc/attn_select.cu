@@ -41,9 +41,40 @@ int pick(const SelectParams& p, cudaStream_t s) {
     return WHT_OK;
 }
 
+template <typename T, int D, int TQ>
+int select_one(SelectParams& p, cudaStream_t s) {
+    static int ready[kMaxDevices] = {};
+    p.token_tiles = static_cast<int>(ceil_div(p.a.max_q_len, TQ));
+    const size_t smem = static_cast<size_t>(TQ) * p.stride * sizeof(int32_t);
+    int dev = 0, sms = 0;
+    const int rc = device_info(&dev, &sms);
+    if (rc != WHT_OK) return rc;
+    if (!ready[dev]) {
+        WHT_CUDA_TRY(cudaFuncSetAttribute(attn_select_kernel<T, D, TQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024));
+        ready[dev] = 1;
+    }
+    const long long blocks = static_cast<long long>(p.a.B) * p.token_tiles * p.a.hkv;
+    if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
+    attn_select_kernel<T, D, TQ><<<static_cast<unsigned>(blocks), kSelectThreads, smem, s>>>(p);
+    WHT_CUDA_TRY(cudaGetLastError());
+    return WHT_OK;
+}
+
+template <typename T>
+int select_d(SelectParams& p, int d, cudaStream_t s) {
+    if (p.a.max_q_len == 1)
+        return d == 64 ? select_one<T, 64, 1>(p, s) : d == 96 ? select_one<T, 96, 1>(p, s) : select_one<T, 128, 1>(p, s);
+    return d == 64 ? select_one<T, 64, 16>(p, s) : d == 96 ? select_one<T, 96, 16>(p, s) : select_one<T, 128, 16>(p, s);
+}
+
 }  // namespace
 
 int launch_select(SelectParams& p, int dtype, int d, cudaStream_t s) {
+    // One kernel where its blocks' scores fit shared memory, unless a few blocks would have to read long tables alone.
+    const int tq = p.a.max_q_len == 1 ? 1 : 16;
+    const long long blocks = static_cast<long long>(p.a.B) * ceil_div(p.a.max_q_len, tq) * p.a.hkv;
+    if (static_cast<long long>(p.stride) * tq * 4 <= 96 * 1024 && (p.stride <= 512 || blocks >= 128))
+        return dtype == WHT_F32 ? select_d<float>(p, d, s) : select_d<__nv_bfloat16>(p, d, s);
     const int rc = dtype == WHT_F32 ? score_d<float>(p, d, s) : score_d<__nv_bfloat16>(p, d, s);
     if (rc != WHT_OK) return rc;
     // a thread holds a few of a row's candidates at most; long rows get a larger block

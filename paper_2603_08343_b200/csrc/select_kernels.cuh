@@ -5,6 +5,7 @@
 // so a page costs two products of length D whatever the group.  Sums of whole numbers have no order: the scores, and
 // so the selection, are the same for every batch shape and split.
 //
+// attn_select_kernel does both for a block's queries where their scores fit shared memory and there are blocks enough; else
 // attn_score_kernel: one thread per page, its summary (2 D bytes) in registers, the queries' sums in shared memory as
 // base-64 digits (two signed bytes each), four dp4a chains per query.  A block takes up to TQ tokens of a
 // sequence, so that prompts read each summary once per TQ queries; single tokens stream summaries at the rate of memory.
@@ -122,6 +123,226 @@ attn_score_kernel(const SelectParams sp) {
             lo = dot(*reinterpret_cast<const uint4*>(&digits[i][3][v * 16]), least[v], lo);
         }
         sp.scores[((t0 + i) * p.hkv + head) * sp.stride + page] = hi * 64 + lo;
+    }
+}
+
+// ---- scoring and picking in one kernel, where the candidates of a block's queries fit shared memory ----
+constexpr int kSelectThreads = 256;
+
+// The k best of n scores (n > k), ties to the lowest, ascending; then page n itself.  By one warp, scores in shared memory.
+__device__ __forceinline__ void warp_pick(const int32_t* score, int n, int k, int32_t* out) {
+    const int lane = threadIdx.x & 31;
+    int least = 0x7fffffff, most = -0x7fffffff - 1;
+    for (int i = lane; i < n; i += 32) {
+        least = min(least, score[i]);
+        most = max(most, score[i]);
+    }
+    least = __reduce_min_sync(kFullMask, least);
+    most = __reduce_max_sync(kFullMask, most);
+    // the largest threshold that at least k scores reach, bit by bit, counted from the least score
+    uint32_t cut = 0;
+    bool exact = k == n;
+    for (int bit = 31 - __clz(static_cast<int>((static_cast<uint32_t>(most) - static_cast<uint32_t>(least)) | 1u)); bit >= 0 && !exact; --bit) {
+        const uint32_t want = cut | (1u << bit);
+        int c = 0;
+        for (int i = lane; i < n; i += 32) c += static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) >= want;
+        c = __reduce_add_sync(kFullMask, c);
+        if (c >= k) {
+            cut = want;
+            exact = c == k;
+        }
+    }
+    int wanted = 0;  // of those that equal the threshold
+    if (!exact) {
+        int above = 0;
+        for (int i = lane; i < n; i += 32) above += static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) > cut;
+        wanted = k - __reduce_add_sync(kFullMask, above);
+    }
+    const unsigned before = (1u << lane) - 1u;
+    int written = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t v = i < n ? static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) : 0u;
+        const bool above = i < n && (exact ? v >= cut : v > cut), equal = i < n && !exact && v == cut;
+        const unsigned equals = __ballot_sync(kFullMask, equal);
+        const bool take = above || (equal && __popc(equals & before) < wanted);
+        wanted = max(0, wanted - __popc(equals));
+        const unsigned taken = __ballot_sync(kFullMask, take);
+        if (take) out[written + __popc(taken & before)] = i;
+        written += __popc(taken);
+    }
+    if (lane == 0) out[k] = n;
+}
+
+__device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// TQ = 1: single tokens, a thread per page and dp4a, the summaries on their way while the query is made whole numbers.
+// TQ = 16: prompts, 16 queries as the rows of an int8 matrix product with 8 pages, digits and summaries as they lie in memory
+// (the contraction index is permuted so that a lane's 16 bytes of a page are its operands of two instructions).
+template <typename T, int D, int TQ>
+__global__ void __launch_bounds__(kSelectThreads)
+attn_select_kernel(const SelectParams sp) {
+    constexpr int ROW = 2 * D + (TQ > 1 ? 64 : 0);           // bytes of a query's digits (most | least), padded against bank conflicts
+    __shared__ __align__(16) int8_t digits[2][TQ][ROW];      // [high, low]
+    extern __shared__ int32_t scores[];                      // [TQ][stride]
+    const AttnParams& p = sp.a;
+    grid_launch_dependents();
+    int64_t b = blockIdx.x;
+    const int head = static_cast<int>(b % p.hkv);
+    b /= p.hkv;
+    const int tile = static_cast<int>(b % sp.token_tiles), seq = static_cast<int>(b / sp.token_tiles);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t* table = p.page_table + static_cast<int64_t>(seq) * p.table_width;
+    int64_t first;
+    int count;
+    attn_tokens(p, seq, first, count);
+    const int n = min(TQ, count - tile * TQ);
+    if (n <= 0) return;
+    const int64_t t0 = first + tile * TQ;
+    const int64_t place0 = static_cast<int64_t>(attn_length(p, seq)) - count + tile * TQ;
+    const int64_t last = place0 + n - 1;
+    const int most = last < 0 ? 0 : static_cast<int>(last >> p.page_shift);  // candidates of the last token
+    const int k = p.select - 1;
+    auto physical = [&](int page) {
+        int phys = __ldg(table + page);
+        if (phys < 0 || phys >= p.num_pages) {
+            attn_report(kAttnErrIndex);
+            phys = 0;
+        }
+        return sp.summary + (static_cast<int64_t>(phys) * p.hkv + head) * 2 * D;
+    };
+    const bool scoring = most > k && k > 0;
+    constexpr int V = D / 16;
+    uint4 least[V], largest[V];
+    if (TQ == 1 && scoring && tid < most) {  // the first round's summaries
+        const uint4* row = reinterpret_cast<const uint4*>(physical(tid));
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            least[v] = __ldg(row + v);
+            largest[v] = __ldg(row + V + v);
+        }
+    }
+    if (scoring) {
+        constexpr int C = D / 32;
+        for (int i = warp; i < TQ; i += kSelectThreads / 32) {
+            if (i >= n) {
+                for (int c = lane; c < ROW; c += 32) digits[0][i][c] = digits[1][i][c] = 0;
+                continue;
+            }
+            const T* q = static_cast<const T*>(p.q) + (t0 + i) * p.q_st + static_cast<int64_t>(head) * p.group * p.q_sh;
+            float top = 0.0f;
+            for (int g = 0; g < p.group; ++g)
+#pragma unroll
+                for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(load_f32(q + g * p.q_sh + lane + 32 * c)));
+#pragma unroll
+            for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, s));
+            const float r = top > 1e-30f ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
+            int up[C], down[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) up[c] = down[c] = 0;
+            for (int g = 0; g < p.group; ++g)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    // (an infinite or NaN query gives no number: 0)
+                    const int v = max(-127, min(127, __float2int_rn(__fmul_rn(load_f32(q + g * p.q_sh + lane + 32 * c), r))));
+                    up[c] += max(v, 0);
+                    down[c] += min(v, 0);
+                }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                // base-64 digits; a summary is least | most, so that the digits of `down` come first
+                const int at = lane + 32 * c, uh = (up[c] + 32) >> 6, dh = (down[c] + 32) >> 6;
+                digits[0][i][at] = static_cast<int8_t>(dh);
+                digits[1][i][at] = static_cast<int8_t>(down[c] - dh * 64);
+                digits[0][i][D + at] = static_cast<int8_t>(uh);
+                digits[1][i][D + at] = static_cast<int8_t>(up[c] - uh * 64);
+            }
+        }
+        __syncthreads();
+        if constexpr (TQ == 1) {
+            for (int page = tid; page < most; page += kSelectThreads) {
+                int hi = 0, lo = 0;
+                auto dot = [](const uint4& x, const uint4& y, int acc) {
+                    acc = __dp4a(static_cast<int>(x.x), static_cast<int>(y.x), acc);
+                    acc = __dp4a(static_cast<int>(x.y), static_cast<int>(y.y), acc);
+                    acc = __dp4a(static_cast<int>(x.z), static_cast<int>(y.z), acc);
+                    return __dp4a(static_cast<int>(x.w), static_cast<int>(y.w), acc);
+                };
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    hi = dot(*reinterpret_cast<const uint4*>(&digits[0][0][v * 16]), least[v], hi);
+                    lo = dot(*reinterpret_cast<const uint4*>(&digits[1][0][v * 16]), least[v], lo);
+                    hi = dot(*reinterpret_cast<const uint4*>(&digits[0][0][D + v * 16]), largest[v], hi);
+                    lo = dot(*reinterpret_cast<const uint4*>(&digits[1][0][D + v * 16]), largest[v], lo);
+                }
+                scores[page] = hi * 64 + lo;
+                if (page + kSelectThreads < most) {
+                    const uint4* row = reinterpret_cast<const uint4*>(physical(page + kSelectThreads));
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        least[v] = __ldg(row + v);
+                        largest[v] = __ldg(row + V + v);
+                    }
+                }
+            }
+        } else {
+            const int r4 = lane >> 2, c4 = lane & 3;
+            constexpr int NG = 2;                            // 8-page groups at a time
+            for (int p0 = warp * 8 * NG; p0 < most; p0 += kSelectThreads / 32 * 8 * NG) {
+                const int8_t* row[NG];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) row[g] = physical(min(p0 + 8 * g + r4, most - 1)) + 16 * c4;
+                int hi[NG][4], lo[NG][4];
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) hi[g][i] = lo[g][i] = 0;
+                uint4 s[2 * D / 64][NG];
+#pragma unroll
+                for (int x = 0; x < 2 * D / 64; ++x)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) s[x][g] = __ldg(reinterpret_cast<const uint4*>(row[g] + 64 * x));
+#pragma unroll
+                for (int x = 0; x < 2 * D / 64; ++x) {
+                    const uint4 h0 = *reinterpret_cast<const uint4*>(&digits[0][r4][64 * x + 16 * c4]);
+                    const uint4 h1 = *reinterpret_cast<const uint4*>(&digits[0][r4 + 8][64 * x + 16 * c4]);
+                    const uint4 l0 = *reinterpret_cast<const uint4*>(&digits[1][r4][64 * x + 16 * c4]);
+                    const uint4 l1 = *reinterpret_cast<const uint4*>(&digits[1][r4 + 8][64 * x + 16 * c4]);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        mma_s8_16832(hi[g], h0.x, h1.x, h0.y, h1.y, s[x][g].x, s[x][g].y);
+                        mma_s8_16832(hi[g], h0.z, h1.z, h0.w, h1.w, s[x][g].z, s[x][g].w);
+                        mma_s8_16832(lo[g], l0.x, l1.x, l0.y, l1.y, s[x][g].x, s[x][g].y);
+                        mma_s8_16832(lo[g], l0.z, l1.z, l0.w, l1.w, s[x][g].z, s[x][g].w);
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int page = p0 + 8 * g + 2 * c4 + (i & 1);
+                        if (page < most) scores[(r4 + 8 * (i >> 1)) * sp.stride + page] = hi[g][i] * 64 + lo[g][i];
+                    }
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = warp; i < n; i += kSelectThreads / 32) {
+        const int64_t place = place0 + i;
+        const int own = place < 0 ? -1 : static_cast<int>(place >> p.page_shift);
+        int32_t* out = sp.pages + ((t0 + i) * p.hkv + head) * p.select;
+        if (own <= k) {
+            for (int e = lane; e < p.select; e += 32) out[e] = e <= own ? e : -1;
+        } else if (k == 0) {
+            if (lane == 0) out[0] = own;
+        } else {
+            warp_pick(scores + i * sp.stride, own, k, out);
+        }
     }
 }
 

@@ -60,27 +60,37 @@ Division divide(int64_t units, int64_t keys, int sms) {
 
 struct PrefixPlan {
     int prefix_nr, prefix_row_tiles, prefix_wpu, prefix_splits, own_nr, own_row_tiles, own_wpu, own_splits, parts;
+    bool joint;                                 // small: every sequence walks the prefix itself
     bool umma;                                  // the prefix on the tcgen05 kernel
     int umma_splits, umma_row_blocks, same_rows;
     size_t bytes;
 };
 
-constexpr int kUmmaMinRows = 65;   // rows per key head from which the tcgen05 kernel takes the prefix
+// Rows per key head from which the tcgen05 kernel takes the prefix.  Up to 32 rows are one unit of the paged kernel, which then reads
+// each key once as well (16 heads x 16384 keys: 32 rows 48 us, here 46); above, it reads them once per 32 rows (48 rows: 63 us, here 49).
+constexpr int kUmmaMinRows = 33;
 constexpr int kUmmaMinKeys = 256;
 
-// Key ranges of the tcgen05 kernel: the number that makes the longest SM's time least, in units of 128-key tiles, a block's set-up
-// and the join of its part counted as kSetUp tiles.
-int umma_splits_for(int64_t units, int64_t tiles, int sms) {
-    constexpr int64_t kSetUp = 4;
-    int64_t best = 1, best_cost = INT64_MAX;
+// Key ranges of the tcgen05 kernel: the number that makes the whole call shortest by a small model of it.  Its blocks take an
+// SM each; the sequences' own pages (own_bytes of keys and values) run beside it on the SMs that are left, then on all.
+// Measured at 1.5 GHz under load: 8 us for a block's set-up and result and 1.8 (D = 64) to 2.2 us per tile of 128 keys;
+// 54 GB/s per SM for the own pages next to it, 6000 GB/s alone.  256 x 32768 keys with 150 keys of their own, 32 heads: 3 ranges
+// (96 blocks) 209 us, 4 ranges (128 blocks) 219 us, 9 (two waves) 235 us; 64 x 8192 with 256, 8 key heads: 15 ranges 45 us, 18 53 us.
+int umma_splits_for(int64_t units, int64_t tiles, int tiles_per_step, int32_t D, double own_bytes, int sms) {
+    const double tile_us = (D > 64 ? 2.2 : 1.8) * tiles_per_step;
+    double best_us = 1e30;
+    int best = 1;
     for (int64_t n = 1; n <= tiles && n <= 64; ++n) {
-        const int64_t cost = ceil_div(units * n, sms) * (ceil_div(tiles, n) + kSetUp);
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = n;
+        const int64_t blocks = units * n, waves = ceil_div(blocks, sms);
+        const double umma_us = static_cast<double>(waves) * (8.0 + tile_us * static_cast<double>(ceil_div(tiles, n)));
+        const double beside = waves == 1 ? 54e3 * static_cast<double>(sms - blocks) * umma_us : 0.0;  // bytes
+        const double us = umma_us + (own_bytes > beside ? (own_bytes - beside) / 6e6 : 0.0);
+        if (us < best_us) {
+            best_us = us;
+            best = static_cast<int>(n);
         }
     }
-    return static_cast<int>(best);
+    return best;
 }
 
 PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv,
@@ -94,12 +104,27 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     f.own_wpu = own.wpu;
     f.own_splits = own.splits;
     f.prefix_nr = f.prefix_wpu = 1;
+    // Small calls are all latency: one launch in which eight warps per unit walk the prefix and then the sequence's own pages beats a
+    // prefix part and a join as long as no warp has more than 6 chunks (fp32, whose chunks take twice as long and more: 2) and the units
+    // fit the machine at once.  2 sequences x 16 heads, D = 64, 40 own keys: 512 prefix keys 8.2 us against 10.3, 1000 keys 10.3
+    // both, 2000 keys 14.4 against 11.3; fp32: 128 keys 8.3 against 12.3, 512 keys 14.4 against 12.3.
+    const int64_t own_units = static_cast<int64_t>(B) * Hkv * f.own_row_tiles;
+    const int64_t all_keys = prefix_len + static_cast<int64_t>(table_width) * page;
+    f.joint = prefix_len > 0 && own_units <= sms && all_keys <= 16 * 8 * (dtype == WHT_F32 ? 2 : 6);
+    if (f.joint) {
+        f.own_wpu = 8;
+        f.own_splits = f.parts = 1;
+        return f;
+    }
     f.umma = umma_allowed && dtype == WHT_BF16 && T * group >= kUmmaMinRows && prefix_len >= kUmmaMinKeys;
     if (f.umma) {
         f.same_rows = T * group <= 128;
         f.umma_row_blocks = static_cast<int>(ceil_div(T * group, 256));
         // with the same rows in both tiles a block takes two key tiles at a time
-        f.umma_splits = umma_splits_for(static_cast<int64_t>(Hkv) * f.umma_row_blocks, ceil_div(prefix_len, f.same_rows ? 256 : 128), sms);
+        // (the lengths are on the device: sequences are taken to fill 0.6 of their tables' width)
+        const double own_bytes = 0.6 * B * Hkv * static_cast<double>(table_width) * page * D * 4.0;
+        f.umma_splits = umma_splits_for(static_cast<int64_t>(Hkv) * f.umma_row_blocks, ceil_div(prefix_len, f.same_rows ? 256 : 128),
+                                        1, D, own_bytes, sms);
     } else if (prefix_len > 0) {
         f.prefix_nr = row_tiles(T * group);
         f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 8 * f.prefix_nr));
@@ -123,7 +148,10 @@ SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t H
     const int group = Hq / Hkv;
     f.nr = row_tiles(group);
     f.row_tiles = static_cast<int>(ceil_div(group, 8 * f.nr));
-    const Division d = divide(T * Hkv * f.row_tiles, static_cast<int64_t>(std::min(select, table_width)) * page, sms);
+    const int64_t units = T * Hkv * f.row_tiles, keys = static_cast<int64_t>(std::min(select, table_width)) * page;
+    Division d = divide(units, keys, sms);
+    // few units: eight warps each and no join, as long as that leaves no warp more than eight chunks
+    if (units <= sms && keys <= 16 * 8 * 8) d = Division{8, 1};
     f.wpu = d.wpu;
     f.splits = d.splits;
     f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
@@ -223,6 +251,7 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.page_table = page_table; p.kv_lens = kv_lens; p.q_start = q_start;
     p.table_width = table_width; p.B = B; p.max_q_len = max_q_len;
     p.own_splits = f.own_splits; p.own_row_tiles = f.own_row_tiles; p.own_nr = f.own_nr; p.own_wpu = f.own_wpu;
+    p.joint = f.joint;
     p.T = T; p.num_pages = num_pages;
     p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
     p.scale_log2 = scale * wht::kLog2e;
