@@ -129,7 +129,9 @@ attn_score_kernel(const SelectParams sp) {
 // ---- scoring and picking in one kernel, where the candidates of a block's queries fit shared memory ----
 constexpr int kSelectThreads = 256;
 
-// The k best of n scores (n > k), ties to the lowest, ascending; then page n itself.  By one warp, scores in shared memory.
+// The k best of n scores (n > k), ties to the lowest, ascending; then page n itself.  By one warp, scores in shared memory;
+// R: rounds of 32 that are held in registers (n <= 32 R), 0: read again in every step.
+template <int R>
 __device__ __forceinline__ void warp_pick(const int32_t* score, int n, int k, int32_t* out) {
     const int lane = threadIdx.x & 31;
     int least = 0x7fffffff, most = -0x7fffffff - 1;
@@ -139,37 +141,49 @@ __device__ __forceinline__ void warp_pick(const int32_t* score, int n, int k, in
     }
     least = __reduce_min_sync(kFullMask, least);
     most = __reduce_max_sync(kFullMask, most);
-    // the largest threshold that at least k scores reach, bit by bit, counted from the least score
-    uint32_t cut = 0;
-    bool exact = k == n;
-    for (int bit = 31 - __clz(static_cast<int>((static_cast<uint32_t>(most) - static_cast<uint32_t>(least)) | 1u)); bit >= 0 && !exact; --bit) {
-        const uint32_t want = cut | (1u << bit);
+    // scores counted from the least one, plus 1: what is no candidate is 0 and reaches no threshold
+    uint32_t held[R > 0 ? R : 1];
+#pragma unroll
+    for (int j = 0; j < R; ++j) held[j] = lane + 32 * j < n ? static_cast<uint32_t>(score[lane + 32 * j]) - static_cast<uint32_t>(least) + 1u : 0u;
+    auto value = [&](int i) { return i < n ? static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) + 1u : 0u; };
+    auto reached = [&](uint32_t want) {  // how many scores reach it
         int c = 0;
-        for (int i = lane; i < n; i += 32) c += static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) >= want;
-        c = __reduce_add_sync(kFullMask, c);
+        if constexpr (R > 0) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) c += held[j] >= want;
+        } else {
+            for (int i = lane; i < n; i += 32) c += value(i) >= want;
+        }
+        return __reduce_add_sync(kFullMask, c);
+    };
+    // the largest threshold that at least k scores reach, bit by bit
+    uint32_t cut = 0;
+    bool exact = false;
+    for (int bit = 31 - __clz(static_cast<int>(static_cast<uint32_t>(most) - static_cast<uint32_t>(least) + 1u)); bit >= 0 && !exact; --bit) {
+        const int c = reached(cut | (1u << bit));
         if (c >= k) {
-            cut = want;
+            cut |= 1u << bit;
             exact = c == k;
         }
     }
-    int wanted = 0;  // of those that equal the threshold
-    if (!exact) {
-        int above = 0;
-        for (int i = lane; i < n; i += 32) above += static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) > cut;
-        wanted = k - __reduce_add_sync(kFullMask, above);
-    }
+    int wanted = exact ? 0 : k - reached(cut + 1u);  // of those that equal the threshold
     const unsigned before = (1u << lane) - 1u;
     int written = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t v = i < n ? static_cast<uint32_t>(score[i]) - static_cast<uint32_t>(least) : 0u;
-        const bool above = i < n && (exact ? v >= cut : v > cut), equal = i < n && !exact && v == cut;
+    auto round = [&](int i0, uint32_t v) {
+        const bool above = exact ? v >= cut : v > cut, equal = !exact && v == cut;
         const unsigned equals = __ballot_sync(kFullMask, equal);
         const bool take = above || (equal && __popc(equals & before) < wanted);
         wanted = max(0, wanted - __popc(equals));
         const unsigned taken = __ballot_sync(kFullMask, take);
-        if (take) out[written + __popc(taken & before)] = i;
+        if (take) out[written + __popc(taken & before)] = i0 + lane;
         written += __popc(taken);
+    };
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+            if (32 * j < n) round(32 * j, held[j]);
+    } else {
+        for (int i0 = 0; i0 < n; i0 += 32) round(i0, value(i0 + lane));
     }
     if (lane == 0) out[k] = n;
 }
@@ -181,11 +195,11 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// TQ = 1: single tokens, a thread per page and dp4a, the summaries on their way while the query is made whole numbers.
+// TQ = 1: single tokens, four threads per page and dp4a, the summaries on their way while the query is made whole numbers.
 // TQ = 16: prompts, 16 queries as the rows of an int8 matrix product with 8 pages, digits and summaries as they lie in memory
 // (the contraction index is permuted so that a lane's 16 bytes of a page are its operands of two instructions).
 template <typename T, int D, int TQ>
-__global__ void __launch_bounds__(kSelectThreads)
+__global__ void __launch_bounds__(kSelectThreads, TQ > 1 ? 2 : 4)
 attn_select_kernel(const SelectParams sp) {
     constexpr int ROW = 2 * D + (TQ > 1 ? 64 : 0);           // bytes of a query's digits (most | least), padded against bank conflicts
     __shared__ __align__(16) int8_t digits[2][TQ][ROW];      // [high, low]
@@ -217,15 +231,24 @@ attn_select_kernel(const SelectParams sp) {
         return sp.summary + (static_cast<int64_t>(phys) * p.hkv + head) * 2 * D;
     };
     const bool scoring = most > k && k > 0;
-    constexpr int V = D / 16;
-    uint4 least[V], largest[V];
-    if (TQ == 1 && scoring && tid < most) {  // the first round's summaries
-        const uint4* row = reinterpret_cast<const uint4*>(physical(tid));
+    // Single tokens: four threads per page, a quarter of its summary each, two pages of a thread on their way at a time and
+    // the table's entries a round ahead of that.
+    constexpr int V = 2 * D / 64, PAGES = kSelectThreads / 4;
+    uint4 part[2][V];
+    const int8_t* next_row = nullptr;
+    auto locate = [&](int page) {
+        if (page < most) next_row = physical(page) + (tid & 3) * (D / 2);
+    };
+    auto fetch = [&](int page, uint4 (&to)[V]) {
+        if (page < most) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            least[v] = __ldg(row + v);
-            largest[v] = __ldg(row + V + v);
+            for (int v = 0; v < V; ++v) to[v] = __ldg(reinterpret_cast<const uint4*>(next_row) + v);
         }
+    };
+    if (TQ == 1 && scoring) {  // started before the query is made whole numbers
+        locate(tid >> 2);
+        fetch(tid >> 2, part[0]);
+        locate(PAGES + (tid >> 2));
     }
     if (scoring) {
         constexpr int C = D / 32;
@@ -235,24 +258,41 @@ attn_select_kernel(const SelectParams sp) {
                 continue;
             }
             const T* q = static_cast<const T*>(p.q) + (t0 + i) * p.q_st + static_cast<int64_t>(head) * p.group * p.q_sh;
-            float top = 0.0f;
-            for (int g = 0; g < p.group; ++g)
+            // eight heads' values at a time, all loads in flight; groups of up to eight are read once
+            constexpr int GB = 8;
+            float x[GB][C];
+            auto heads = [&](int g0) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(load_f32(q + g * p.q_sh + lane + 32 * c)));
+                for (int g = 0; g < GB; ++g)
+#pragma unroll
+                    for (int c = 0; c < C; ++c) x[g][c] = g0 + g < p.group ? load_f32(q + (g0 + g) * p.q_sh + lane + 32 * c) : 0.0f;
+            };
+            float top = 0.0f;
+            for (int g0 = 0; g0 < p.group; g0 += GB) {
+                heads(g0);
+#pragma unroll
+                for (int g = 0; g < GB; ++g)
+#pragma unroll
+                    for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(x[g][c]));
+            }
 #pragma unroll
             for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, s));
             const float r = top > 1e-30f ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
             int up[C], down[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) up[c] = down[c] = 0;
-            for (int g = 0; g < p.group; ++g)
+            for (int g0 = 0; g0 < p.group; g0 += GB) {
+                if (p.group > GB) heads(g0);
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    // (an infinite or NaN query gives no number: 0)
-                    const int v = max(-127, min(127, __float2int_rn(__fmul_rn(load_f32(q + g * p.q_sh + lane + 32 * c), r))));
-                    up[c] += max(v, 0);
-                    down[c] += min(v, 0);
-                }
+                for (int g = 0; g < GB; ++g)
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        // (an infinite or NaN query gives no number: 0)
+                        const int v = max(-127, min(127, __float2int_rn(__fmul_rn(x[g][c], r))));
+                        up[c] += max(v, 0);
+                        down[c] += min(v, 0);
+                    }
+            }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 // base-64 digits; a summary is least | most, so that the digits of `down` come first
@@ -265,30 +305,34 @@ attn_select_kernel(const SelectParams sp) {
         }
         __syncthreads();
         if constexpr (TQ == 1) {
-            for (int page = tid; page < most; page += kSelectThreads) {
+            const int8_t* high = &digits[0][0][(tid & 3) * (D / 2)];
+            const int8_t* low = &digits[1][0][(tid & 3) * (D / 2)];
+            auto dot = [](const uint4& x, const uint4& y, int acc) {
+                acc = __dp4a(static_cast<int>(x.x), static_cast<int>(y.x), acc);
+                acc = __dp4a(static_cast<int>(x.y), static_cast<int>(y.y), acc);
+                acc = __dp4a(static_cast<int>(x.z), static_cast<int>(y.z), acc);
+                return __dp4a(static_cast<int>(x.w), static_cast<int>(y.w), acc);
+            };
+            auto round = [&](int p0, const uint4 (&now)[V], uint4 (&next)[V]) {  // (all threads: a page's four exchange their sums)
+                const int page = p0 + (tid >> 2);
+                fetch(page + PAGES, next);
+                locate(page + 2 * PAGES);
                 int hi = 0, lo = 0;
-                auto dot = [](const uint4& x, const uint4& y, int acc) {
-                    acc = __dp4a(static_cast<int>(x.x), static_cast<int>(y.x), acc);
-                    acc = __dp4a(static_cast<int>(x.y), static_cast<int>(y.y), acc);
-                    acc = __dp4a(static_cast<int>(x.z), static_cast<int>(y.z), acc);
-                    return __dp4a(static_cast<int>(x.w), static_cast<int>(y.w), acc);
-                };
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    hi = dot(*reinterpret_cast<const uint4*>(&digits[0][0][v * 16]), least[v], hi);
-                    lo = dot(*reinterpret_cast<const uint4*>(&digits[1][0][v * 16]), least[v], lo);
-                    hi = dot(*reinterpret_cast<const uint4*>(&digits[0][0][D + v * 16]), largest[v], hi);
-                    lo = dot(*reinterpret_cast<const uint4*>(&digits[1][0][D + v * 16]), largest[v], lo);
-                }
-                scores[page] = hi * 64 + lo;
-                if (page + kSelectThreads < most) {
-                    const uint4* row = reinterpret_cast<const uint4*>(physical(page + kSelectThreads));
+                if (page < most) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        least[v] = __ldg(row + v);
-                        largest[v] = __ldg(row + V + v);
+                        hi = dot(*reinterpret_cast<const uint4*>(high + v * 16), now[v], hi);
+                        lo = dot(*reinterpret_cast<const uint4*>(low + v * 16), now[v], lo);
                     }
                 }
+                int sum = hi * 64 + lo;
+                sum += __shfl_xor_sync(kFullMask, sum, 1);
+                sum += __shfl_xor_sync(kFullMask, sum, 2);
+                if (page < most && !(tid & 3)) scores[page] = sum;
+            };
+            for (int p0 = 0; p0 < most; p0 += 2 * PAGES) {
+                round(p0, part[0], part[1]);
+                if (p0 + PAGES < most) round(p0 + PAGES, part[1], part[0]);
             }
         } else {
             const int r4 = lane >> 2, c4 = lane & 3;
@@ -341,7 +385,9 @@ attn_select_kernel(const SelectParams sp) {
         } else if (k == 0) {
             if (lane == 0) out[0] = own;
         } else {
-            warp_pick(scores + i * sp.stride, own, k, out);
+            if (own <= 8 * 32) warp_pick<8>(scores + i * sp.stride, own, k, out);
+            else if (TQ == 1 && own <= 16 * 32) warp_pick<16>(scores + i * sp.stride, own, k, out);
+            else warp_pick<0>(scores + i * sp.stride, own, k, out);
         }
     }
 }
