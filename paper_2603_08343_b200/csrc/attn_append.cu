@@ -29,12 +29,14 @@ int launch_append(AppendParams& p, int dtype, bool interleaved, int sms, cudaStr
     p.flat_y = static_cast<int>(ceil_div(static_cast<long long>(p.tile) * per_token, kAppendThreads));
     long long blocks = static_cast<long long>(p.flat_x) * p.flat_y;
     if (p.summary) {
-        // A block's eight warps take (run, head) pairs of a tile of tokens.  Few tokens (a decode step, where every token
-        // is a run): a block per token and eight heads.  Many (prompts, a run per page): wider tiles, or most blocks
-        // would find no run to own.
+        // A block's eight warps take the runs of a tile of tokens for eight heads: four tokens a tile in a decode step, where every
+        // token is a run; more in prompts (a run per page), where most tiles of a few tokens would find none to own.
         p.run_heads = p.hkv < 8 ? p.hkv : 8;
-        p.run_tile = p.T < 1024 ? 1 : p.T < 32 * 512 ? static_cast<int>(p.T / 512) : 32;
-        blocks += ceil_div(p.T, p.run_tile) * ceil_div(p.hkv, p.run_heads);
+        p.run_tile = p.T < 4 * 512 ? 4 : p.T < 32 * 512 ? static_cast<int>(p.T / 512) : 32;
+        const long long page_blocks = ceil_div(p.T, p.run_tile) * ceil_div(p.hkv, p.run_heads);
+        blocks += page_blocks;
+        if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
+        p.page_blocks = static_cast<int>(page_blocks);
     }
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     if (dtype == WHT_F32)

@@ -8,8 +8,8 @@
 // of a token and come from the caches.
 //
 // With page summaries the keys are walked by page instead: one warp takes the run of tokens that a call adds
-// to one page for one head, keeps the channels' least and largest whole values in registers as 16-bit pairs, folds
-// the rows of the warp by shuffles and joins the page's stored summary once.  No atomics: a run has one owner.
+// to one page for one head, keeps the channels' least and largest values in registers, folds the rows of the warp by
+// shuffles and joins the page's stored summary once.  No atomics: a run has one owner.
 #pragma once
 #include "attn_common.cuh"
 
@@ -31,16 +31,13 @@ struct AppendParams {
     int flat_x, flat_y;       // its thread blocks: token tiles, and blocks per tile
     int run_tile;             // tokens per block of the page part
     int run_heads;            // heads per block of the page part
+    int page_blocks;          // thread blocks of the page part
 };
 
 template <typename T>
 __device__ __forceinline__ T* row_of(void* base, int64_t off) { return static_cast<T*>(base) + off; }
 template <typename T>
 __device__ __forceinline__ const T* row_of(const void* base, int64_t off) { return static_cast<const T*>(base) + off; }
-
-// The value a stored element has: rounded to the type.
-__device__ __forceinline__ float stored(float x, const float*) { return x; }
-__device__ __forceinline__ float stored(float x, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(x)); }
 
 // One item of a row: 16 elements as two groups of eight, at lo and hi.  Items below rot/16 turn; the pairs are
 // (lo[i], hi[i]) (halves) or neighbours (interleaved); the others pass through.
@@ -109,6 +106,14 @@ struct Raw8 {
     __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
         for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void narrow(const float (&v)[8]) {  // rounded to the type
+        if constexpr (sizeof(T) == 4) {
+            w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        } else {
+            w[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+        }
     }
     __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
@@ -212,45 +217,119 @@ __device__ __forceinline__ void append_flat(const AppendParams& p, int block) {
     }
 }
 
-__device__ __forceinline__ unsigned pack_s16(int lo, int hi) {
-    return (static_cast<unsigned>(lo) & 0xffffu) | (static_cast<unsigned>(hi) << 16);
-}
+// ---- page part ----
+// The least and the largest of 16 channels' stored values.  c() is monotonic, so they can be found on the values themselves, for bf16
+// two to an instruction, and made whole numbers once per run (on whole numbers this part took 36 instructions per element and
+// a third of the kernel's time).
+template <typename T>
+struct Range {
+    static constexpr int N = 16;
+    float least[N], most[N];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            least[i] = INFINITY;
+            most[i] = -INFINITY;
+        }
+    }
+    __device__ __forceinline__ void join(const Raw8<T>& lo, const Raw8<T>& hi) {
+        float a[8], b[8];
+        lo.widen(a);
+        hi.widen(b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            least[i] = fminf(least[i], a[i]);
+            most[i] = fmaxf(most[i], a[i]);
+            least[8 + i] = fminf(least[8 + i], b[i]);
+            most[8 + i] = fmaxf(most[8 + i], b[i]);
+        }
+    }
+    __device__ __forceinline__ void fold(int lanes) {  // with the lane `lanes` further on
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            least[i] = fminf(least[i], __shfl_down_sync(kFullMask, least[i], lanes));
+            most[i] = fmaxf(most[i], __shfl_down_sync(kFullMask, most[i], lanes));
+        }
+    }
+    __device__ __forceinline__ void get(int i, float& lo, float& hi) const {
+        lo = least[i];
+        hi = most[i];
+    }
+};
+template <>
+struct Range<__nv_bfloat16> {
+    static constexpr int N = 8;  // pairs
+    __nv_bfloat162 least[N], most[N];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            least[i] = __halves2bfloat162(__ushort_as_bfloat16(0x7f80), __ushort_as_bfloat16(0x7f80));
+            most[i] = __halves2bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80));
+        }
+    }
+    __device__ __forceinline__ void join(const Raw8<__nv_bfloat16>& lo, const Raw8<__nv_bfloat16>& hi) {
+        const unsigned w[8] = {lo.w[0].x, lo.w[0].y, lo.w[0].z, lo.w[0].w, hi.w[0].x, hi.w[0].y, hi.w[0].z, hi.w[0].w};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+            least[i] = __hmin2(least[i], x);
+            most[i] = __hmax2(most[i], x);
+        }
+    }
+    __device__ __forceinline__ void fold(int lanes) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            least[i] = __hmin2(least[i], __shfl_down_sync(kFullMask, least[i], lanes));
+            most[i] = __hmax2(most[i], __shfl_down_sync(kFullMask, most[i], lanes));
+        }
+    }
+    __device__ __forceinline__ void get(int i, float& lo, float& hi) const {
+        lo = __bfloat162float(i & 1 ? least[i / 2].y : least[i / 2].x);
+        hi = __bfloat162float(i & 1 ? most[i / 2].y : most[i / 2].x);
+    }
+};
 
-// Page part: the warps of a block share the tile's runs and the block's heads.
+// The warps of a block share the tile's runs and the block's heads.
 template <typename T, bool INTERLEAVED>
 __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile0, int head0) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int per_row = p.d / 16;
-    int rows = 1;  // rows of a warp's step: a power of two, so that they fold by shuffles
-    while (rows * 2 * per_row <= 32) rows *= 2;
-    const int sub = lane / per_row;
-    const RowItem<T, INTERLEAVED> it(lane - sub * per_row, p.rot);
-    const bool active = sub < rows;
+    const int per_row = p.d / 16;                      // 4, 6 or 8 lanes
+    const int rows = per_row == 4 ? 8 : 4;             // rows of a warp's step: a power of two, so that they fold by shuffles
+    const int lane_row = lane / per_row;
+    const RowItem<T, INTERLEAVED> it(lane - lane_row * per_row, p.rot);
     const int heads = min(p.run_heads, p.hkv - head0);
-    // which of the tile's tokens begin a run
-    int64_t page = -1, before = -1;
+    // which of the tile's tokens begin a run, and which runs go on after their first token
+    int64_t page = -1, before = -1, after = -1;
     if (lane < p.run_tile && tile0 + lane < p.T) {
         const int64_t s = append_slot(p, tile0 + lane);
+        const int64_t s1 = tile0 + lane > 0 ? append_slot(p, tile0 + lane - 1) : -1;
+        const int64_t s2 = tile0 + lane + 1 < p.T ? append_slot(p, tile0 + lane + 1) : -1;
         if (s >= 0) page = s >> p.page_shift;
-        if (tile0 + lane > 0) {
-            const int64_t s1 = append_slot(p, tile0 + lane - 1);
-            if (s1 >= 0) before = s1 >> p.page_shift;
-        }
+        if (s1 >= 0) before = s1 >> p.page_shift;
+        if (s2 >= 0) after = s2 >> p.page_shift;
     }
     const unsigned leaders = __ballot_sync(kFullMask, page >= 0 && page != before);
-    const int pairs = __popc(leaders) * heads;
-    for (int pair = warp; pair < pairs; pair += warps) {
-        const int head = head0 + pair % heads;
-        const int l = __fns(leaders, 0, pair / heads + 1);
-        const float scale = __ldg(p.summary_scale + head);
+    const unsigned longer = __ballot_sync(kFullMask, page >= 0 && page != before && page == after);
+    // A warp's rows are tokens of one head, or, where every run is a single token (a decode step), heads of one token.
+    const int across = longer ? 1 : rows;              // heads of a warp
+    const int row_step = rows / across, sub = lane_row % row_step;
+    const int groups = (heads + across - 1) / across;
+    // (run, group) pairs are dealt to the warps in turn
+    unsigned left = leaders;
+    for (int group = warp; left; group += warps) {
+        while (group >= groups && left) {
+            group -= groups;
+            left &= left - 1;
+        }
+        if (!left) break;
+        const int l = __ffs(left) - 1;
+        const int hb = group * across + lane_row / row_step;
+        const bool mine = lane_row < rows && hb < heads;
+        const int head = head0 + (mine ? hb : 0);
         const int64_t first = tile0 + l;
         const int64_t run_page = __shfl_sync(kFullMask, page, l);
-        unsigned least[8], most[8];  // 16 channels as 16-bit pairs
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            least[i] = pack_s16(127, 127);
-            most[i] = pack_s16(-127, -127);
-        }
+        Range<T> range;
+        range.clear();
         int first_place = 0;
         const T* src = row_of<T>(p.k, head * p.k_sh);
         T* dst = row_of<T>(p.k_cache, cache_offset(p, run_page << p.page_shift, head));
@@ -260,86 +339,62 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
             int pos = 0;
             if (c0 + lane < p.T) {
                 const int64_t s = append_slot(p, c0 + lane);
-                if (s >= 0 && (s >> p.page_shift) == run_page) place = static_cast<int>(s & ((1 << p.page_shift) - 1));
                 pos = static_cast<int>(append_position(p, c0 + lane));
+                if (s >= 0 && (s >> p.page_shift) == run_page) place = static_cast<int>(s & ((1 << p.page_shift) - 1));
             }
             const unsigned other = ~__ballot_sync(kFullMask, place >= 0);
             const int n = other ? __ffs(other) - 1 : 32;
             if (c0 == first) first_place = __shfl_sync(kFullMask, place, 0);
+            const T* row = src + (c0 + sub) * p.k_st;
+            const int64_t next_row = row_step * p.k_st;
 #pragma unroll 2
-            for (int r0 = 0; r0 < n; r0 += rows) {
+            for (int r0 = 0; r0 < n; r0 += row_step, row += next_row) {
                 const int r = r0 + sub;
-                const int at = __shfl_sync(kFullMask, place, r & 31), ps = __shfl_sync(kFullMask, pos, r & 31);
-                if (!active || r >= n) continue;
-                const T* row = src + (c0 + r) * p.k_st;
+                const int to = __shfl_sync(kFullMask, place, r & 31), ps = __shfl_sync(kFullMask, pos, r & 31);
+                if (r >= n || !mine) continue;
                 Raw8<T> lo, hi;
                 lo.load(row + it.lo);
                 hi.load(row + it.hi);
-                float a[8], b[8];
                 if (it.angle >= 0) {
-                    float c[8], s[8];
+                    float c[8], s[8], a[8], b[8];
                     load8(p.cos_t + static_cast<int64_t>(ps) * (p.rot / 2) + it.angle, c);
                     load8(p.sin_t + static_cast<int64_t>(ps) * (p.rot / 2) + it.angle, s);
                     lo.widen(a);
                     hi.widen(b);
                     it.turn(a, b, c, s);
-                } else {
-                    lo.widen(a);
-                    hi.widen(b);
+                    lo.narrow(a);
+                    hi.narrow(b);
                 }
-                store8(dst + at * p.d + it.lo, a);
-                store8(dst + at * p.d + it.hi, b);
-                int w[16];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(a[i], src), scale))));
-                    w[8 + i] = max(-127, min(127, __float2int_rn(__fmul_rn(stored(b[i], src), scale))));
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const unsigned x = pack_s16(w[2 * i], w[2 * i + 1]);
-                    least[i] = __vmins2(least[i], x);
-                    most[i] = __vmaxs2(most[i], x);
-                }
+                lo.store(dst + to * p.d + it.lo);
+                hi.store(dst + to * p.d + it.hi);
+                range.join(lo, hi);
             }
             if (n < 32) break;
         }
-        for (int step = rows / 2; step >= 1; step >>= 1) {
+        for (int step = row_step / 2; step >= 1; step >>= 1) range.fold(step * per_row);
+        if (!mine || sub != 0) continue;
+        const bool anew = first_place == 0;
+        const float scale = __ldg(p.summary_scale + head);
+        int8_t* at = p.summary + ((run_page * p.hkv + head) * 2) * p.d;
+        auto whole = [&](float x) { return max(-127, min(127, __float2int_rn(__fmul_rn(x, scale)))); };
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                least[i] = __vmins2(least[i], __shfl_down_sync(kFullMask, least[i], step * per_row));
-                most[i] = __vmaxs2(most[i], __shfl_down_sync(kFullMask, most[i], step * per_row));
+        for (int w = 0; w < 4; ++w) {                  // four channels at a time
+            unsigned wl = 0, wh = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float lo, hi;
+                range.get(4 * w + i, lo, hi);
+                const int a = whole(lo), b = whole(hi);  // (a negative scale turns them round)
+                wl |= (static_cast<unsigned>(min(a, b)) & 0xffu) << (8 * i);
+                wh |= (static_cast<unsigned>(max(a, b)) & 0xffu) << (8 * i);
             }
-        }
-        if (lane < per_row) {
-            const bool anew = first_place == 0;
-            int8_t* at = p.summary + ((run_page * p.hkv + head) * 2) * p.d;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                int8_t* lo = at + (half ? it.hi : it.lo);
-                int8_t* hi = lo + p.d;
-                uint2 old_lo, old_hi, new_lo, new_hi;
-                if (!anew) {
-                    old_lo = *reinterpret_cast<const uint2*>(lo);
-                    old_hi = *reinterpret_cast<const uint2*>(hi);
-                }
-                unsigned wl[2], wh[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {  // four channels: two pairs to four bytes
-                    const unsigned l0 = least[half * 4 + 2 * j], l1 = least[half * 4 + 2 * j + 1];
-                    const unsigned h0 = most[half * 4 + 2 * j], h1 = most[half * 4 + 2 * j + 1];
-                    wl[j] = __byte_perm(l0, l1, 0x6420);
-                    wh[j] = __byte_perm(h0, h1, 0x6420);
-                }
-                new_lo = make_uint2(wl[0], wl[1]);
-                new_hi = make_uint2(wh[0], wh[1]);
-                if (!anew) {
-                    new_lo = make_uint2(__vmins4(new_lo.x, old_lo.x), __vmins4(new_lo.y, old_lo.y));
-                    new_hi = make_uint2(__vmaxs4(new_hi.x, old_hi.x), __vmaxs4(new_hi.y, old_hi.y));
-                }
-                *reinterpret_cast<uint2*>(lo) = new_lo;
-                *reinterpret_cast<uint2*>(hi) = new_hi;
+            unsigned* to = reinterpret_cast<unsigned*>(at + (w < 2 ? it.lo : it.hi) + 4 * (w & 1));
+            if (!anew) {
+                wl = __vmins4(wl, to[0]);
+                wh = __vmaxs4(wh, to[p.d / 4]);
             }
+            to[0] = wl;
+            to[p.d / 4] = wh;
         }
     }
 }
@@ -347,18 +402,22 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
 constexpr int kAppendThreads = 256;
 
 template <typename T, bool INTERLEAVED, bool SUMMARY>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, SUMMARY ? 3 : 4)
 kv_append_kernel(const AppendParams p) {
-    const int flat = p.flat_x * p.flat_y;
-    // (the page blocks come first: theirs is the longer work)
-    const int page_blocks = static_cast<int>(gridDim.x) - flat;
-    if (SUMMARY && static_cast<int>(blockIdx.x) < page_blocks) {
-        const int hb = (p.hkv + p.run_heads - 1) / p.run_heads;
-        const int tile = static_cast<int>(blockIdx.x) / hb;
-        append_pages<T, INTERLEAVED>(p, static_cast<int64_t>(tile) * p.run_tile, (static_cast<int>(blockIdx.x) - tile * hb) * p.run_heads);
-        return;
+    const int block = static_cast<int>(blockIdx.x);
+    if constexpr (SUMMARY) {
+        // Page blocks wait more than they move, flat blocks the other way round: spread evenly among each other they share the SMs.
+        const long long pages = p.page_blocks, total = gridDim.x;
+        const int before = static_cast<int>(block * pages / total), after = static_cast<int>((block + 1) * pages / total);
+        if (after > before) {
+            const int hb = (p.hkv + p.run_heads - 1) / p.run_heads, tile = before / hb;
+            append_pages<T, INTERLEAVED>(p, static_cast<int64_t>(tile) * p.run_tile, (before - tile * hb) * p.run_heads);
+            return;
+        }
+        append_flat<T, INTERLEAVED, true>(p, block - before);
+    } else {
+        append_flat<T, INTERLEAVED, false>(p, block);
     }
-    append_flat<T, INTERLEAVED, SUMMARY>(p, static_cast<int>(blockIdx.x) - page_blocks);
 }
 
 }  // namespace wht
