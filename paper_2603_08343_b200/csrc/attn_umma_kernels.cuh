@@ -45,7 +45,8 @@ struct UmmaAttnGeo {
     static constexpr int NBARS = 2 * STAGES + 6 + 1;
     static constexpr int OFF_MISC = OFF_BARS + NBARS * 8;
     static constexpr int OFF_MAX = OFF_MISC + 16;             // [2 tiles][2 halves][128 rows] fp32
-    static constexpr int BYTES = OFF_MAX + 2048;
+    static constexpr int OFF_IDS = OFF_MAX + 2048;            // page numbers on their way to the copies
+    static constexpr int BYTES = OFF_IDS + 64 * 4;
     static constexpr int O_COLS = D > 64 ? 128 : 64;
 };
 
@@ -134,6 +135,13 @@ __device__ __forceinline__ bool tile_any(int w, bool flag) {
     return any != 0;
 }
 
+// 32 bytes in one store: a thread's row is its own, so narrower stores would write half sectors
+__device__ __forceinline__ void store_sector(float* p, const float* v) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+                 "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
+}
+
 template <int D>
 __global__ void __launch_bounds__(kUmmaAttnThreads, 1)
 attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -189,6 +197,53 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
+    // The copies, by warp 17: the items in the order in which the products take them.  Page numbers come 32 at a time, one per lane,
+    // and the next 32 are on their way while these are used.  As many items as the ring holds are asked for before anything
+    // else is set up.
+    int item = 0, of = 0, loaded = 0;
+    const int list = static_cast<int>((p.prefix_len + (1 << p.page_shift) - 1) >> p.page_shift);
+    int filled = key0 >> p.page_shift, ahead = -1;  // list entries below `filled` have been put into `ids`; `ahead`: this lane's next one
+    int32_t* ids = reinterpret_cast<int32_t*>(smem + Geo::OFF_IDS);
+    auto fetch_ids = [&]() { ahead = filled + lane < list ? __ldg(p.prefix_pages + filled + lane) : 0; };
+    auto copy_items = [&](int until) {
+        const int page = 1 << p.page_shift;
+        for (; item < 2 * steps_of(0); ++item, of = 0) {
+            for (; of < (same ? 2 : 1); ++of) {
+                if (item >= 2 * steps_of(of)) break;
+                if (loaded >= until) return true;
+                const Place at = place_of(of, item);
+                const int first = (key0 + key_tile(of, item >> 1) * 128) >> p.page_shift;
+                const int n = min(128 >> p.page_shift, list - first);
+                while (filled < first + n) {
+                    int pg = ahead;
+                    if (pg < 0 || pg >= p.num_pages) {
+                        attn_report(kAttnErrIndex);
+                        pg = 0;
+                    }
+                    ids[(filled + lane) & 63] = pg;
+                    filled += 32;
+                    fetch_ids();
+                    __syncwarp();
+                }
+                if (!__all_sync(kFullMask, wait_or_abort(kv_empty + at.stage, at.parity ^ 1u, abort_flag))) return false;
+                const CUtensorMap* map = item & 1 ? &v_map : &k_map;
+                if (lane == 0) {
+                    mbar_expect_tx(kv_full + at.stage, static_cast<uint32_t>(n * page * 128 * Geo::HALVES));
+                    for (int i = 0; i < n; ++i) {
+                        const int y = (ids[(first + i) & 63] * p.hkv + head) << p.page_shift;
+#pragma unroll
+                        for (int h = 0; h < Geo::HALVES; ++h)
+                            tma_load_2d(smem_u32(smem) + Geo::OFF_RING + at.stage * Geo::TILE + h * Geo::BOX + i * page * 128, map, h * 64, y,
+                                        kv_full + at.stage);
+                    }
+                }
+                __syncwarp();
+                ++loaded;
+            }
+        }
+        return true;
+    };
+    if (warp == 17) fetch_ids();
     if (tid == 17 * 32) {
         for (int s = 0; s < Geo::STAGES; ++s) {
             mbar_init(kv_full + s, 1);
@@ -203,30 +258,30 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         *abort_flag = 0;
         fence_mbar_init();
     }
-    // queries: 128-byte rows of 64 channels, chunks permuted by the row as the copies' swizzle does
-    {
+    if (warp == 17) {
+        __syncwarp();
+        copy_items(same ? Geo::STAGES / 2 * 2 : Geo::STAGES);
+    }
+    // queries, by the softmax warps: 128-byte rows of 64 channels, chunks permuted by the row as the copies' swizzle does
+    if (warp < 16) {
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q);
-        constexpr int CH = Geo::HALVES * 8;
-        // eight chunks a thread at a time, all loads in flight
-        constexpr int BATCH = 8;
-        for (int i0 = tid; i0 < 256 * CH; i0 += BATCH * kUmmaAttnThreads) {
-            uint4 v[BATCH];
+        constexpr int CH = Geo::HALVES * 8, BATCH = 256 * CH / 512;   // chunks a row and a thread, all loads in flight
+        uint4 v[BATCH];
 #pragma unroll
-            for (int e = 0; e < BATCH; ++e) {
-                const int i = i0 + e * kUmmaAttnThreads, r = i / CH, c = i % CH;
-                const int row = row0 + (same ? r & 127 : r);
-                v[e] = make_uint4(0, 0, 0, 0);
-                if (i < 256 * CH && row < rows && c * 8 < D) {
-                    const int tok = row / p.group;
-                    v[e] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh) + c);
-                }
+        for (int e = 0; e < BATCH; ++e) {
+            const int i = tid + e * 512, r = i / CH, c = i % CH;
+            const int row = row0 + (same ? r & 127 : r);
+            v[e] = make_uint4(0, 0, 0, 0);
+            if (row < rows && c * 8 < D) {
+                const int tok = row / p.group;
+                v[e] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh) + c);
             }
+        }
 #pragma unroll
-            for (int e = 0; e < BATCH; ++e) {
-                const int i = i0 + e * kUmmaAttnThreads, r = i / CH, c = i % CH;
-                unsigned char* dst = smem + (r >> 7) * Geo::TILE + (c >> 3) * Geo::BOX + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-                if (i < 256 * CH) *reinterpret_cast<uint4*>(dst) = v[e];
-            }
+        for (int e = 0; e < BATCH; ++e) {
+            const int i = tid + e * 512, r = i / CH, c = i % CH;
+            unsigned char* dst = smem + (r >> 7) * Geo::TILE + (c >> 3) * Geo::BOX + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+            *reinterpret_cast<uint4*>(dst) = v[e];
         }
         fence_async_smem();
     }
@@ -237,45 +292,14 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
     const uint32_t ring = smem_u32(smem) + Geo::OFF_RING;
 
     if (warp == 17) {
-        if (lane == 0) {
-            // the items in the order in which the products take them
-            const int list = static_cast<int>((p.prefix_len + (1 << p.page_shift) - 1) >> p.page_shift);
-            const int page = 1 << p.page_shift;
-            bool ok = true;
-            int loaded = 0;
-            for (int item = 0; ok && item < 2 * steps_of(0); ++item) {
-                for (int w = 0; ok && w < (same ? 2 : 1); ++w) {
-                    if (item >= 2 * steps_of(w)) break;
-                    const Place at = place_of(w, item);
-                    ok = wait_or_abort(kv_empty + at.stage, at.parity ^ 1u, abort_flag);
-                    if (!ok) break;
-                    const CUtensorMap* map = item & 1 ? &v_map : &k_map;
-                    const int first = (key0 + key_tile(w, item >> 1) * 128) >> p.page_shift;
-                    const int n = min(128 >> p.page_shift, list - first);
-                    mbar_expect_tx(kv_full + at.stage, static_cast<uint32_t>(n * page * 128 * Geo::HALVES));
-                    for (int i = 0; i < n; ++i) {
-                        int pg = __ldg(p.prefix_pages + first + i);
-                        if (pg < 0 || pg >= p.num_pages) {
-                            attn_report(kAttnErrIndex);
-                            pg = 0;
-                        }
-                        const int y = (pg * p.hkv + head) << p.page_shift;
-#pragma unroll
-                        for (int h = 0; h < Geo::HALVES; ++h)
-                            tma_load_2d(ring + at.stage * Geo::TILE + h * Geo::BOX + i * page * 128, map, h * 64, y, kv_full + at.stage);
-                    }
-                    ++loaded;
+        if (!copy_items(0x7fffffff)) {  // given up: the copies in flight still write this block's memory
+            for (int k = 0, j = 0; k < loaded; ++j)
+                for (int w = 0; w < (same ? 2 : 1) && k < loaded; ++w) {
+                    if (j >= 2 * steps_of(w)) break;
+                    if (k++ < loaded - Geo::STAGES) continue;
+                    const Place at = place_of(w, j);
+                    mbar_wait_bounded(kv_full + at.stage, at.parity);
                 }
-            }
-            if (!ok) {  // given up: the copies in flight still write this block's memory
-                for (int k = 0, item = 0; k < loaded; ++item)
-                    for (int w = 0; w < (same ? 2 : 1) && k < loaded; ++w) {
-                        if (item >= 2 * steps_of(w)) break;
-                        if (k++ < loaded - Geo::STAGES) continue;
-                        const Place at = place_of(w, item);
-                        mbar_wait_bounded(kv_full + at.stage, at.parity);
-                    }
-            }
         }
     } else if (warp == 16) {
         // One warp issues all products, the tiles strictly in turn: a tile's second product and its next scores go to the tensor core as
@@ -383,13 +407,15 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                 unpair(add2(sum[0], sum[1]), a, b);
                 return a + b;
             };
+            // One vote of both halves' warps per round: nobody stores weights before all agree on the reference.  (A wait that ran
+            // out also ends up here, so that all leave together: the votes are barriers.)
             float sum = 0.0f;
-            bool move = i == 0;
-            if (i > 0) sum = weights();
-            // One vote of both halves' warps: nobody stores weights before all agree on the reference.  (A wait that ran out
-            // also ends up here, so that all leave together: the votes are barriers.)
-            if (tile_any(w, move || !ok || sum > kLargestHalf)) {
-                if (tile_any(w, !ok)) break;
+            bool unset = i == 0, gave_up = false;
+            for (;;) {
+                if (!unset) {
+                    sum = weights();
+                    if (!tile_any(w, !ok || sum > kLargestHalf)) break;
+                }
                 // The first tile, and later the rare case that some row's weights have grown past kLargestHalf: the row's
                 // reference moves to the maximum of the tile.  O and l follow; its products so far are waited for.
                 float top = -INFINITY;
@@ -402,7 +428,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                 }
                 maxima[h * 128 + lane_row] = top;
                 if (i > 0) ok = warp_poll_or_abort(o_done + w, static_cast<uint32_t>(i - 1) & 1u, abort_flag);
-                if (tile_any(w, !ok)) break;
+                if ((gave_up = tile_any(w, !ok))) break;
                 top = fmaxf(maxima[lane_row], maxima[128 + lane_row]);
                 if (i == 0) {
                     m = top;
@@ -423,9 +449,9 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         tmem_st16(o_cols + c, z);
                     }
                 }
-                sum = weights();
-                tile_any(w, false);              // everyone has read the scores and the maxima
+                unset = false;  // (the next vote also says that everyone has read the maxima)
             }
+            if (gave_up) break;
             l += sum;
             tmem_st16(p_cols, y);
             tmem_st16(p_cols + 16, y + 16);
@@ -466,8 +492,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                 }
                 if (r < rows) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        *reinterpret_cast<float4*>(p.part_o + slot * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    for (int e = 0; e < 16; e += 8) store_sector(p.part_o + slot * D + c + e, o + e);
                 }
             }
             if (h == 1) maxima[128 + lane_row] = l;
