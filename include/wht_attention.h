@@ -19,8 +19,9 @@
  *     wht_affine.h; no exception crosses this boundary and no kernel traps.
  *   - Storage types: WHT_F32 (queries, keys, values, caches, outputs float32) or WHT_BF16 (all bfloat16).
  *     Scores, softmax statistics and sums are fp32 whatever the type.  On bf16 tensors the softmax weights
- *     are rounded to bf16 where they enter the product with the values (the tensor core takes both operands in
- *     one type); on fp32 tensors both products take each operand as two terms, about 21 significant bits.
+ *     enter the product with the values as two bf16 terms (16 significant bits; the tensor core takes both operands
+ *     in one type), as one where many rows share a long prefix and that product is what the time goes to; on
+ *     fp32 tensors both products take each operand as two terms, about 21 significant bits.
  *   - Caches: k_cache, v_cache [num_pages x Hkv x page x D], contiguous.  page in {16, 32, 64, 128}; D in
  *     {64, 96, 128}; Hq = G*Hkv query heads, head h reading key head h / G, G <= 64.
  *   - Slots, page numbers, lengths and query offsets are read on the device.  A page number or slot outside
@@ -28,7 +29,8 @@
  *     position clamped) and the device status word is set; wht_attn_device_status() then reports
  *     WHT_ERR_DEVICE_INDEX, and the call's outputs are invalid.
  *   - Rows that see no key (a length of zero) get zeros.
- *   - Cache entries beyond a sequence's length are never used, whatever they hold (NaN and infinities included).
+ *   - Cache entries that a row does not see (beyond a sequence's length, at the places of later tokens) never
+ *     reach its result, whatever they hold (NaN and infinities included).
  */
 #ifndef WHT_ATTENTION_H_
 #define WHT_ATTENTION_H_

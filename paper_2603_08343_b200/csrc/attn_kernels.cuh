@@ -106,7 +106,8 @@ struct AttnUnit {
     int nr, wpu;         // 8-row tiles, warps
 };
 
-template <typename T, int D, int NR, int W>
+// TOKENS: a unit's rows may be of several tokens, which see different keys.
+template <typename T, int D, int NR, int W, bool TOKENS>
 __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map,
                                           unsigned char* smem) {
     using Geo = AttnGeo<T, D, W>;
@@ -242,20 +243,61 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
                 }
             }
         } else {
-            uint32_t b[NR][2];
+            // each weight as two bf16 terms: one term's 2^-9 would stand beside the rounding of the output in every result
+            uint32_t b[NR][2], low[NR][2];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                b[n][0] = transpose_8x8(pack_bf16x2(w[n][0], w[n][1]));
-                b[n][1] = transpose_8x8(pack_bf16x2(w[n][2], w[n][3]));
-            }
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t lead = pack_bf16x2(w[n][2 * i], w[n][2 * i + 1]);
+                    b[n][i] = transpose_8x8(lead);
+                    low[n][i] = transpose_8x8(pack_bf16x2(w[n][2 * i] - __uint_as_float(lead << 16), w[n][2 * i + 1] - __uint_as_float(lead & 0xffff0000u)));
+                }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 uint32_t a[4];
                 ldmatrix_x4_trans(vt + Geo::place((lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)), a);
 #pragma unroll
-                for (int n = 0; n < NR; ++n) mma_bf16_16816(o[n][d], a, b[n][0], b[n][1]);
+                for (int n = 0; n < NR; ++n) {
+                    mma_bf16_16816(o[n][d], a, b[n][0], b[n][1]);
+                    mma_bf16_16816(o[n][d], a, low[n][0], low[n][1]);
+                }
             }
         }
+    };
+
+    auto values_finite = [&](int s) {
+        const unsigned char* v = ring + s * 2 * Geo::SIDE + Geo::SIDE;
+        constexpr uint32_t kExp = F32 ? 0x7f800000u : 0x7f80u;
+        bool finite = true;
+        for (int i = lane; i < Geo::SIDE / 4; i += 32) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + i * 4);
+            finite = finite && (w & kExp) != kExp && (F32 || ((w >> 16) & kExp) != kExp);
+        }
+        return __all_sync(kFullMask, finite) != 0;
+    };
+    auto add_seen_values = [&](const float (&w)[NR][4], int s, int base) {
+        const unsigned char* v = ring + s * 2 * Geo::SIDE + Geo::SIDE;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+                float weight[NR][2];
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) weight[n][e] = __shfl_sync(kFullMask, w[n][2 * h + e], k * 4 + c4);
+#pragma unroll
+                for (int d = 0; d < 2 * DT; ++d) {
+                    const int ch = d * 8 + r4, bytes = ch * static_cast<int>(sizeof(T));
+                    const float value = static_cast<float>(*reinterpret_cast<const T*>(v + Geo::place(8 * h + k, bytes >> 4) + (bytes & 15)));
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (base + 8 * h + k < limit[n][e]) o[n][d >> 1][(d & 1) * 2 + e] += weight[n][e] * value;
+                }
+            }
     };
 
     for (int j = 0; j < chunks; ++j) {
@@ -361,7 +403,11 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
                 x[n][i] = exp2_fast(x[n][i] - z);
                 l[n][i & 1] += x[n][i];
             }
-        add_values(x, s);
+        // Rows that see different keys share each product, where a weight of 0 would turn an infinity or NaN among the values of a later
+        // token into NaN for the earlier ones: such a chunk (found by a look at the values of the few that straddle a row's end) is
+        // added up row by row.
+        if (TOKENS && least_limit < end && base + kChunk > least_limit && !values_finite(s)) add_seen_values(x, s, base);
+        else add_values(x, s);
         __syncwarp();                            // every lane has read the slot
         const int next = j + Geo::STAGES;
         if ((next & 31) == 0) {
@@ -433,13 +479,13 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
     }
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, bool TOKENS>
 __device__ __forceinline__ void attn_run(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map) {
     extern __shared__ unsigned char smem_attn[];
     unsigned char* smem = smem_attn + ((1024u - (smem_u32(smem_attn) & 1023u)) & 1023u);
-    if (u.nr == 1) attn_unit<T, D, 1, W>(p, u, k_map, v_map, smem);
-    else if (u.nr == 2) attn_unit<T, D, 2, W>(p, u, k_map, v_map, smem);
-    else attn_unit<T, D, 4, W>(p, u, k_map, v_map, smem);
+    if (u.nr == 1) attn_unit<T, D, 1, W, TOKENS>(p, u, k_map, v_map, smem);
+    else if (u.nr == 2) attn_unit<T, D, 2, W, TOKENS>(p, u, k_map, v_map, smem);
+    else attn_unit<T, D, 4, W, TOKENS>(p, u, k_map, v_map, smem);
 }
 
 // A length read on the device, held to what the tables can hold.
@@ -555,7 +601,7 @@ attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
         u.wpu = p.own_wpu;
     }
     u.table = nullptr;
-    if (work) attn_run<T, D, W>(p, u, &k_map, &v_map);
+    if (work) attn_run<T, D, W, true>(p, u, &k_map, &v_map);
     // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
     // for this grid alone, so this grid does not end before that one has.
     if (last_block) grid_dependency_wait();
@@ -610,7 +656,7 @@ attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
     u.step = 0;
     u.nr = p.own_nr;
     u.wpu = p.own_wpu;
-    attn_run<T, D, W>(p, u, &k_map, &v_map);
+    attn_run<T, D, W, false>(p, u, &k_map, &v_map);
 }
 
 // Joins the parts of each row: out = sum_s exp(m_s - m) o_s / sum_s exp(m_s - m) l_s.  One warp per row, lanes

@@ -237,6 +237,24 @@ def test_shared_prefix_large_scores(A, dtype, B):
     assert (got - want).abs().max().item() <= R.tolerance(BF16, 5.0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("d,prefix,lens", [(64, 0, [20, 37]), (128, 21, [18, 300]), (96, 700, [40, 18])])
+def test_later_tokens_values_stay_out_of_earlier_ones(A, dtype, d, prefix, lens):
+    """Values that are infinite or NaN at a token's place do not reach the tokens of the same call that do not see it."""
+    q_lens = [18, 18]
+    c = _paged(12, 2, 6, 2, d, 16, dtype, prefix, q_lens, lens)
+    clean = _run_prefix(A, c, prefix, None).cpu()
+    bad = [int(n) - 7 for n in lens]                    # seen by the last seven tokens of each sequence only
+    for b, (j, value) in enumerate(zip(bad, (float("inf"), float("nan")))):
+        c["vc"][int(c["table"][b, j // 16]), :, j % 16] = value
+    got = _run_prefix(A, c, prefix, None).cpu()
+    for b in range(2):
+        first, last = 18 * b, 18 * (b + 1) - 7
+        assert not torch.isfinite(got[last:18 * (b + 1)].float()).any()
+        assert (got[first:last].double() - clean[first:last].double()).abs().max() <= 2 * R.tolerance(dtype, 6.0)
+    A.device_status()
+
+
 def test_shared_prefix_strides_out_and_stream(A):
     c = _paged(8, 6, 4, 2, 64, 16, BF16, 100, [1] * 6, [9, 1, 30, 4, 5, 6])
     wide = torch.zeros(6, 9, 64, dtype=BF16).cuda()
