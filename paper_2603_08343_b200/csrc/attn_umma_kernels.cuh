@@ -198,19 +198,17 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         tmem_relinquish();
     }
     // The copies, by warp 17: the items in the order in which the products take them.  Page numbers come 32 at a time, one per lane,
-    // and the next 32 are on their way while these are used.  As many items as the ring holds are asked for before anything
-    // else is set up.
+    // and the next 32 are on their way while these are used.
     int item = 0, of = 0, loaded = 0;
     const int list = static_cast<int>((p.prefix_len + (1 << p.page_shift) - 1) >> p.page_shift);
     int filled = key0 >> p.page_shift, ahead = -1;  // list entries below `filled` have been put into `ids`; `ahead`: this lane's next one
     int32_t* ids = reinterpret_cast<int32_t*>(smem + Geo::OFF_IDS);
     auto fetch_ids = [&]() { ahead = filled + lane < list ? __ldg(p.prefix_pages + filled + lane) : 0; };
-    auto copy_items = [&](int until) {
+    auto copy_items = [&]() {
         const int page = 1 << p.page_shift;
         for (; item < 2 * steps_of(0); ++item, of = 0) {
             for (; of < (same ? 2 : 1); ++of) {
                 if (item >= 2 * steps_of(of)) break;
-                if (loaded >= until) return true;
                 const Place at = place_of(of, item);
                 const int first = (key0 + key_tile(of, item >> 1) * 128) >> p.page_shift;
                 const int n = min(128 >> p.page_shift, list - first);
@@ -258,41 +256,55 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         *abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == 17) {
-        __syncwarp();
-        copy_items(same ? Geo::STAGES / 2 * 2 : Geo::STAGES);
-    }
     // queries, by the softmax warps: 128-byte rows of 64 channels, chunks permuted by the row as the copies' swizzle does
     if (warp < 16) {
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q);
         constexpr int CH = Geo::HALVES * 8, BATCH = 256 * CH / 512;   // chunks a row and a thread, all loads in flight
+        constexpr int STEP = 512 / CH;           // rows from one chunk of a thread to its next
+        const int c = tid % CH, step_tok = STEP / p.group, step_in = STEP % p.group;
+        int row = row0 + tid / CH, tok = row / p.group, in = row - tok * p.group;
         uint4 v[BATCH];
 #pragma unroll
         for (int e = 0; e < BATCH; ++e) {
-            const int i = tid + e * 512, r = i / CH, c = i % CH;
-            const int row = row0 + (same ? r & 127 : r);
+            if (same && e == BATCH / 2) {        // the second tile has the first one's rows
+                row -= 128;
+                tok = row / p.group;
+                in = row - tok * p.group;
+            }
             v[e] = make_uint4(0, 0, 0, 0);
-            if (row < rows && c * 8 < D) {
-                const int tok = row / p.group;
-                v[e] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh) + c);
+            if (row < rows && c * 8 < D)
+                v[e] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q_st + (static_cast<int64_t>(head) * p.group + in) * p.q_sh) + c);
+            row += STEP;
+            tok += step_tok;
+            in += step_in;
+            if (in >= p.group) {
+                in -= p.group;
+                ++tok;
             }
         }
 #pragma unroll
         for (int e = 0; e < BATCH; ++e) {
-            const int i = tid + e * 512, r = i / CH, c = i % CH;
+            const int r = tid / CH + e * STEP;
             unsigned char* dst = smem + (r >> 7) * Geo::TILE + (c >> 3) * Geo::BOX + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
             *reinterpret_cast<uint4*>(dst) = v[e];
         }
         fence_async_smem();
     }
+    // The copying warp needs nothing from the others: it says that the barriers are set up and goes on.  (Waiting here as well, after
+    // it had filled the ring, held the first scores up by 3600 clocks.)
     tc_fence_before();
-    __syncthreads();
+    if (warp == 17) {
+        __syncwarp();
+        asm volatile("bar.arrive 0, %0;" ::"n"(kUmmaAttnThreads) : "memory");
+    } else {
+        asm volatile("bar.sync 0, %0;" ::"n"(kUmmaAttnThreads) : "memory");
+    }
     tc_fence_after();
-    const uint32_t tmem = __shfl_sync(kFullMask, *tmem_slot, 0);
+    const uint32_t tmem = warp == 17 ? 0u : __shfl_sync(kFullMask, *tmem_slot, 0);
     const uint32_t ring = smem_u32(smem) + Geo::OFF_RING;
 
     if (warp == 17) {
-        if (!copy_items(0x7fffffff)) {  // given up: the copies in flight still write this block's memory
+        if (!copy_items()) {  // given up: the copies in flight still write this block's memory
             for (int k = 0, j = 0; k < loaded; ++j)
                 for (int w = 0; w < (same ? 2 : 1) && k < loaded; ++w) {
                     if (j >= 2 * steps_of(w)) break;
