@@ -32,6 +32,7 @@
 namespace wht {
 
 constexpr int kUmmaAttnThreads = 576;
+constexpr int kStartBarrier = 3;  // (0: the whole block at its end; 1, 2: the two tiles' votes)
 constexpr float kLargestHalf = 16384.0f;  // 2^14: sum of 64 weights from which a row's reference maximum moves
 
 template <int D>
@@ -291,13 +292,15 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         fence_async_smem();
     }
     // The copying warp needs nothing from the others: it says that the barriers are set up and goes on.  (Waiting here as well, after
-    // it had filled the ring, held the first scores up by 3600 clocks.)
+    // it had filled the ring, held the first scores up by 3600 clocks.)  The barrier has a number of its own: where the ring takes all
+    // copies of a block at once, this warp comes to the block's last barrier while others are still here.
     tc_fence_before();
     if (warp == 17) {
+        __threadfence_block();
         __syncwarp();
-        asm volatile("bar.arrive 0, %0;" ::"n"(kUmmaAttnThreads) : "memory");
+        asm volatile("bar.arrive %0, %1;" ::"n"(kStartBarrier), "n"(kUmmaAttnThreads) : "memory");
     } else {
-        asm volatile("bar.sync 0, %0;" ::"n"(kUmmaAttnThreads) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"n"(kStartBarrier), "n"(kUmmaAttnThreads) : "memory");
     }
     tc_fence_after();
     const uint32_t tmem = warp == 17 ? 0u : __shfl_sync(kFullMask, *tmem_slot, 0);

@@ -209,6 +209,9 @@ PREFIX = [
     (128, 1, 1, 128, 64, 5000, [1] * 128, [3] * 128),
     (129, 2, 2, 128, 128, 4096, [1] * 129, [2] * 129),
     (2, 16, 1, 64, 32, 600, [40, 3], [41, 3]),
+    # key ranges of one tile: all copies of a block are asked for before its queries are loaded
+    (140, 1, 1, 128, 64, 300, [1] * 140, [2] * 140),
+    (300, 2, 2, 64, 128, 640, [1] * 300, [1] * 300),
 ]
 
 
