@@ -73,16 +73,17 @@ constexpr int kUmmaMinKeys = 256;
 
 // Key ranges of the tcgen05 kernel: the number that makes the whole call shortest by a small model of it.  Its blocks take an
 // SM each; the sequences' own pages (own_bytes of keys and values) run beside it on the SMs that are left, then on all.
-// Measured at 1.5 GHz under load: 8 us for a block's set-up and result and 1.8 (D = 64) to 2.2 us per tile of 128 keys;
+// Measured at 1.5 GHz under load: 6 us for a block's set-up and result and 1.8 (D = 64) to 2.2 us per tile of 128 keys;
 // 54 GB/s per SM for the own pages next to it, 6000 GB/s alone.  256 x 32768 keys with 150 keys of their own, 32 heads: 3 ranges
-// (96 blocks) 209 us, 4 ranges (128 blocks) 219 us, 9 (two waves) 235 us; 64 x 8192 with 256, 8 key heads: 15 ranges 45 us, 18 53 us.
+// (96 blocks) are best, 4 (128 blocks) take 5% more, 9 (two waves) 12% more; 64 x 8192 with 256, 8 key heads: 10 ranges 40.5 us,
+// 11 42.7 us, 15 45 us, 18 53 us.
 int umma_splits_for(int64_t units, int64_t tiles, int tiles_per_step, int32_t D, double own_bytes, int sms) {
     const double tile_us = (D > 64 ? 2.2 : 1.8) * tiles_per_step;
     double best_us = 1e30;
     int best = 1;
     for (int64_t n = 1; n <= tiles && n <= 64; ++n) {
         const int64_t blocks = units * n, waves = ceil_div(blocks, sms);
-        const double umma_us = static_cast<double>(waves) * (8.0 + tile_us * static_cast<double>(ceil_div(tiles, n)));
+        const double umma_us = static_cast<double>(waves) * (6.0 + tile_us * static_cast<double>(ceil_div(tiles, n)));
         const double beside = waves == 1 ? 54e3 * static_cast<double>(sms - blocks) * umma_us : 0.0;  // bytes
         const double us = umma_us + (own_bytes > beside ? (own_bytes - beside) / 6e6 : 0.0);
         if (us < best_us) {
