@@ -58,6 +58,18 @@ Division divide(int64_t units, int64_t keys, int sms) {
     return d;
 }
 
+// Whether each unit gets a block of eight warps, so that nothing is left to join: short lists, and few enough units that fill the
+// machine at a block each.  us, against the division above, 8 key heads of 4 rows, D = 128:
+//   own pages  bf16  1 x 512 keys 8.5 (12.8), 1 x 2048 18.5 (12.4), 4 x 4096 30.8 (21.8), 9 x 2048 20.5 (22.7), 18 x 8192 97 (102)
+//              fp32  1 x 1024 32.9 (18.5), 9 x 8192 237 (180), 18 x 512 27 (37), 18 x 8192 243 (342), 40 tokens of 2 x 512 (80 units) 61 (102)
+//   selection  bf16  1 x 1024 16.4 (20.5), 1 x 2048 23.5 (18.8), 9 x 2048 27.1 (31.8), 18 x 2048 39.0 (43.4)
+//              fp32  1 x 256 18.6 (21.2), 1 x 512 25.4 (24.7), 1 x 1024 37.3 (25.9), 18 x 1024 47.8 (63.9)
+bool block_each(int64_t units, int64_t keys, int dtype, int sms) {
+    const bool f32 = dtype == WHT_F32;
+    const int64_t chunks = ceil_div(keys, 16 * 8);  // of a warp
+    return units <= sms && (chunks <= (f32 ? 3 : 8) || (f32 ? 2 : 3) * units > sms);
+}
+
 struct PrefixPlan {
     int prefix_nr, prefix_row_tiles, prefix_wpu, prefix_splits, own_nr, own_row_tiles, own_wpu, own_splits, parts;
     bool joint;                                 // small: every sequence walks the prefix itself
@@ -105,6 +117,10 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     f.own_wpu = own.wpu;
     f.own_splits = own.splits;
     f.prefix_nr = f.prefix_wpu = 1;
+    if (prefix_len == 0 && block_each(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, dtype, sms)) {
+        f.own_wpu = 8;
+        f.own_splits = 1;
+    }
     // Small calls are all latency: one launch in which eight warps per unit walk the prefix and then the sequence's own pages beats a
     // prefix part and a join as long as no warp has more than 6 chunks (fp32, whose chunks take twice as long and more: 2) and the units
     // fit the machine at once.  2 sequences x 16 heads, D = 64, 40 own keys: 512 prefix keys 8.2 us against 10.3, 1000 keys 10.3
@@ -151,8 +167,7 @@ SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t H
     f.row_tiles = static_cast<int>(ceil_div(group, 8 * f.nr));
     const int64_t units = T * Hkv * f.row_tiles, keys = static_cast<int64_t>(std::min(select, table_width)) * page;
     Division d = divide(units, keys, sms);
-    // few units: eight warps each and no join, as long as that leaves no warp more than eight chunks
-    if (units <= sms && keys <= 16 * 8 * 8) d = Division{8, 1};
+    if (block_each(units, keys, dtype, sms)) d = Division{8, 1};
     f.wpu = d.wpu;
     f.splits = d.splits;
     f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));

@@ -337,6 +337,10 @@ SELECT = [
     (2, 4, 2, 64, 16, 4, [40, 7], [200, 7]),                          # prompts
     (1, 6, 2, 128, 16, 3, [33], [20]),                                # tokens before the first key
     (1, 2, 1, 64, 16, 40, [1], [3000]),                               # more pages than a block scores at once
+    (1, 2, 1, 64, 16, 5, [18], [24700]),                              # a prompt whose scores no block holds: two kernels
+    (1, 2, 2, 64, 16, 600, [1], [20000]),                             # a long list out of a long table
+    (2, 4, 2, 64, 16, 1024, [1, 3], [90, 500]),                       # room for more pages than there are
+    (20, 8, 8, 64, 16, 20, [1] * 20, [(37 * i) % 700 for i in range(20)]),  # units beyond one block an SM
 ]
 
 
