@@ -69,9 +69,10 @@ struct UmmaAttnParams {
     int same_rows;   // 128 rows or fewer: both of a block's tiles hold them, each with every second key tile
 };
 
-// W: warps per block.  Four, so that two blocks fit an SM; eight for small calls, where a unit is a block and all that counts is
-// how soon its last key is done.
-template <typename T, int D, int W>
+// W: warps per block.  Four, so that two or three blocks fit an SM; eight for small calls, where a unit is a block and all that counts
+// is how soon its last key is done.  N: the most 8-row tiles a unit has, 1 or 4.  Units of one tile (bf16) need fewer registers and a
+// shorter ring, so that three blocks fit: with eight warps an SM the wait is for the results of products, not for memory.
+template <typename T, int D, int W, int N>
 struct AttnGeo {
     static constexpr int THREADS = 32 * W;
     static constexpr bool F32 = std::is_same<T, float>::value;
@@ -79,12 +80,14 @@ struct AttnGeo {
     static constexpr int BOXES = (D + BOX_CH - 1) / BOX_CH;             // per key row (the last may reach over the row's end: zeros)
     static constexpr int BOX_BYTES = kChunk * 128;
     static constexpr int SIDE = BOXES * BOX_BYTES;                      // keys (or values) of a chunk
-    static constexpr int STAGES = 2 * SIDE >= 16384 ? (W > 4 ? 1 : 2) : 24576 / (2 * SIDE);
-    static constexpr int RING = STAGES * 2 * SIDE > 18432 ? STAGES * 2 * SIDE : 18432;  // per warp; holds the join buffer too
+    static constexpr bool SLIM = N == 1 && W == 4 && !F32;
+    static constexpr int BLOCKS = SLIM ? 3 : 1;                         // on an SM, at least
+    static constexpr int STAGES = SLIM ? 16384 / (2 * SIDE) : 2 * SIDE >= 16384 ? (W > 4 ? 1 : 2) : 24576 / (2 * SIDE);
+    static constexpr int RING = SLIM ? 16384 : STAGES * 2 * SIDE > 18432 ? STAGES * 2 * SIDE : 18432;  // per warp; holds the join buffer too
     static constexpr int OFF_BARS = W * RING;
     static constexpr int BYTES = OFF_BARS + W * STAGES * 8 + 1024;      // and what aligning the start to 1024 bytes takes
     static constexpr int JOIN_LD = D + 4;                               // floats per row of the join buffer: no bank conflicts
-    static_assert(32 * (JOIN_LD + 2) * 4 <= RING, "the join buffer reuses the ring");
+    static_assert(8 * N * (JOIN_LD + 2) * 4 <= RING, "the join buffer reuses the ring");
     // byte offset of 16-byte piece c of row r (the copy engine's 128-byte swizzle)
     __device__ __forceinline__ static int place(int r, int c) { return (c >> 3) * BOX_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 };
@@ -107,10 +110,10 @@ struct AttnUnit {
 };
 
 // TOKENS: a unit's rows may be of several tokens, which see different keys.
-template <typename T, int D, int NR, int W, bool TOKENS>
+template <typename T, int D, int NR, int W, int N, bool TOKENS>
 __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map,
                                           unsigned char* smem) {
-    using Geo = AttnGeo<T, D, W>;
+    using Geo = AttnGeo<T, D, W, N>;
     constexpr bool F32 = Geo::F32;
     constexpr int QS = D / (F32 ? 8 : 16);       // steps of the first product
     constexpr int DT = D / 16;                   // 16-channel tiles of the output
@@ -427,7 +430,7 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
     // the unit's warps store (m, l, o) over their rings and add them up together
     {
         float* jo = reinterpret_cast<float*>(ring);
-        float2* jm = reinterpret_cast<float2*>(jo + 32 * Geo::JOIN_LD);
+        float2* jm = reinterpret_cast<float2*>(jo + 8 * N * Geo::JOIN_LD);
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -450,13 +453,13 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
         const int r = i / (D / PER), d = (i % (D / PER)) * PER;
         float mm = -INFINITY;
         for (int w = 0; w < u.wpu; ++w)
-            mm = fmaxf(mm, reinterpret_cast<const float2*>(first + w * Geo::RING + 32 * Geo::JOIN_LD * 4)[r].x);
+            mm = fmaxf(mm, reinterpret_cast<const float2*>(first + w * Geo::RING + 8 * N * Geo::JOIN_LD * 4)[r].x);
         const float z = mm == -INFINITY ? 0.0f : mm;
         float ll = 0.0f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = 0; w < u.wpu; ++w) {
             const float* wo = reinterpret_cast<const float*>(first + w * Geo::RING);
-            const float2 ml = reinterpret_cast<const float2*>(wo + 32 * Geo::JOIN_LD)[r];
+            const float2 ml = reinterpret_cast<const float2*>(wo + 8 * N * Geo::JOIN_LD)[r];
             const float f = exp2_fast(ml.x - z);
             ll += f * ml.y;
             const float4 v = *reinterpret_cast<const float4*>(wo + r * Geo::JOIN_LD + d);
@@ -479,13 +482,17 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
     }
 }
 
-template <typename T, int D, int W, bool TOKENS>
+template <typename T, int D, int W, int N, bool TOKENS>
 __device__ __forceinline__ void attn_run(const AttnParams& p, const AttnUnit& u, const CUtensorMap* k_map, const CUtensorMap* v_map) {
     extern __shared__ unsigned char smem_attn[];
     unsigned char* smem = smem_attn + ((1024u - (smem_u32(smem_attn) & 1023u)) & 1023u);
-    if (u.nr == 1) attn_unit<T, D, 1, W, TOKENS>(p, u, k_map, v_map, smem);
-    else if (u.nr == 2) attn_unit<T, D, 2, W, TOKENS>(p, u, k_map, v_map, smem);
-    else attn_unit<T, D, 4, W, TOKENS>(p, u, k_map, v_map, smem);
+    if constexpr (N == 1) {
+        attn_unit<T, D, 1, W, N, TOKENS>(p, u, k_map, v_map, smem);
+    } else {
+        if (u.nr == 1) attn_unit<T, D, 1, W, N, TOKENS>(p, u, k_map, v_map, smem);
+        else if (u.nr == 2) attn_unit<T, D, 2, W, N, TOKENS>(p, u, k_map, v_map, smem);
+        else attn_unit<T, D, 4, W, N, TOKENS>(p, u, k_map, v_map, smem);
+    }
 }
 
 // A length read on the device, held to what the tables can hold.
@@ -535,8 +542,8 @@ __device__ __forceinline__ void attn_part(int keys, int tile, int splits, int s,
 }
 
 // Prefix and own pages in one launch: blocks below prefix_blocks take the prefix.
-template <typename T, int D, int W>
-__global__ void __launch_bounds__(32 * W)
+template <typename T, int D, int W, int N>
+__global__ void __launch_bounds__(32 * W, AttnGeo<T, D, W, N>::BLOCKS)
 attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     const int prefix_units = p.prefix_splits * p.prefix_row_tiles * p.hkv;
     const int prefix_blocks = (prefix_units * p.prefix_wpu + W - 1) / W;
@@ -601,7 +608,7 @@ attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
         u.wpu = p.own_wpu;
     }
     u.table = nullptr;
-    if (work) attn_run<T, D, W, true>(p, u, &k_map, &v_map);
+    if (work) attn_run<T, D, W, N, true>(p, u, &k_map, &v_map);
     // Launched next to the tensor-core kernel of the prefix, these blocks run while it runs; the join that follows waits
     // for this grid alone, so this grid does not end before that one has.
     if (last_block) grid_dependency_wait();
@@ -625,8 +632,8 @@ __device__ __forceinline__ int attn_sequence_of(const AttnParams& p, int64_t t) 
 }
 
 // Chosen pages: one token and key head (and a part of the list) per unit.
-template <typename T, int D, int W>
-__global__ void __launch_bounds__(32 * W)
+template <typename T, int D, int W, int N>
+__global__ void __launch_bounds__(32 * W, AttnGeo<T, D, W, N>::BLOCKS)
 attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     AttnUnit u;
     grid_dependency_wait();  // the list comes from the kernel before
@@ -656,7 +663,7 @@ attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
     u.step = 0;
     u.nr = p.own_nr;
     u.wpu = p.own_wpu;
-    attn_run<T, D, W, false>(p, u, &k_map, &v_map);
+    attn_run<T, D, W, N, false>(p, u, &k_map, &v_map);
 }
 
 // Joins the parts of each row: out = sum_s exp(m_s - m) o_s / sum_s exp(m_s - m) l_s.  One warp per row, lanes

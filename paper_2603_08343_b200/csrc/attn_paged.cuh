@@ -22,12 +22,12 @@ int attn_prepare(Kernel kernel, int smem, int dev, int* cache) {
 template <typename T>
 constexpr int attn_code() { return sizeof(T) == 4 ? WHT_F32 : WHT_BF16; }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, int N>
 int attn_prefix_w(const AttnParams& p, int dev, bool overlapped, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnGeo<T, D, W>;
+    using Geo = AttnGeo<T, D, W, N>;
     static_assert(Geo::BYTES <= 227 * 1024, "shared memory");
-    int rc = attn_prepare(attn_prefix_kernel<T, D, W>, Geo::BYTES, dev, ready);
+    int rc = attn_prepare(attn_prefix_kernel<T, D, W, N>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     const long long prefix_units = static_cast<long long>(p.prefix_splits) * p.prefix_row_tiles * p.hkv;
     const long long own_units = static_cast<long long>(p.B) * p.hkv * p.own_row_tiles * p.own_splits;
@@ -37,30 +37,34 @@ int attn_prefix_w(const AttnParams& p, int dev, bool overlapped, cudaStream_t s)
     rc = cache_maps(&k_map, &v_map, p, D, attn_code<T>(), kChunk);
     if (rc != WHT_OK) return rc;
     if (overlapped)
-        launch_overlapped(attn_prefix_kernel<T, D, W>, dim3(static_cast<unsigned>(blocks)), Geo::THREADS, Geo::BYTES, s, p, k_map, v_map);
+        launch_overlapped(attn_prefix_kernel<T, D, W, N>, dim3(static_cast<unsigned>(blocks)), Geo::THREADS, Geo::BYTES, s, p, k_map, v_map);
     else
-        attn_prefix_kernel<T, D, W><<<static_cast<unsigned>(blocks), Geo::THREADS, Geo::BYTES, s>>>(p, k_map, v_map);
+        attn_prefix_kernel<T, D, W, N><<<static_cast<unsigned>(blocks), Geo::THREADS, Geo::BYTES, s>>>(p, k_map, v_map);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }
 
 template <typename T, int D>
 int attn_prefix_d(const AttnParams& p, int dev, bool overlapped, cudaStream_t s) {
-    return p.own_wpu == 8 ? attn_prefix_w<T, D, 8>(p, dev, overlapped, s) : attn_prefix_w<T, D, 4>(p, dev, overlapped, s);
+    if (p.own_wpu == 8) return attn_prefix_w<T, D, 8, 4>(p, dev, overlapped, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p.own_nr == 1 && (p.prefix_splits == 0 || p.prefix_nr == 1)) return attn_prefix_w<T, D, 4, 1>(p, dev, overlapped, s);
+    }
+    return attn_prefix_w<T, D, 4, 4>(p, dev, overlapped, s);
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, int N>
 int attn_chosen_w(const AttnParams& p, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = AttnGeo<T, D, W>;
-    int rc = attn_prepare(attn_chosen_kernel<T, D, W>, Geo::BYTES, dev, ready);
+    using Geo = AttnGeo<T, D, W, N>;
+    int rc = attn_prepare(attn_chosen_kernel<T, D, W, N>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     const long long units = static_cast<long long>(p.T) * p.hkv * p.own_row_tiles * p.own_splits;
     if (units > 0x0fffffffll) return WHT_ERR_BAD_T;
     CUtensorMap k_map, v_map;
     rc = cache_maps(&k_map, &v_map, p, D, attn_code<T>(), kChunk);
     if (rc != WHT_OK) return rc;
-    launch_overlapped(attn_chosen_kernel<T, D, W>, dim3(static_cast<unsigned>(ceil_div(units * p.own_wpu, W))), Geo::THREADS, Geo::BYTES, s,
+    launch_overlapped(attn_chosen_kernel<T, D, W, N>, dim3(static_cast<unsigned>(ceil_div(units * p.own_wpu, W))), Geo::THREADS, Geo::BYTES, s,
                       p, k_map, v_map);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
@@ -68,7 +72,11 @@ int attn_chosen_w(const AttnParams& p, int dev, cudaStream_t s) {
 
 template <typename T, int D>
 int attn_chosen_d(const AttnParams& p, int dev, cudaStream_t s) {
-    return p.own_wpu == 8 ? attn_chosen_w<T, D, 8>(p, dev, s) : attn_chosen_w<T, D, 4>(p, dev, s);
+    if (p.own_wpu == 8) return attn_chosen_w<T, D, 8, 4>(p, dev, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p.own_nr == 1) return attn_chosen_w<T, D, 4, 1>(p, dev, s);
+    }
+    return attn_chosen_w<T, D, 4, 4>(p, dev, s);
 }
 
 template <typename T, int D>

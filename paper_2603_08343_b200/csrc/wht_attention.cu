@@ -44,15 +44,28 @@ int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, in
 // 8-row tiles per unit of the paged kernel
 int row_tiles(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
-// How the paged kernel divides a set of units of up to `keys` keys: warps per unit, and key ranges (splits).  Eight warps an SM are
-// resident.  Many units: a warp each, which needs no join and no waiting; fewer: more warps per unit, then more
-// ranges, but no warp with fewer than four 16-key chunks (its own set-up and the join would cost more than they save).
+// How the paged kernel divides a set of units of up to `keys` keys: warps per unit, and key ranges (splits).
+// No warp gets fewer than four 16-key chunks: its own set-up and the join would cost more than they save.
 struct Division {
     int wpu, splits;
 };
-Division divide(int64_t units, int64_t keys, int sms) {
-    const int64_t slots = 8ll * sms, chunks = ceil_div(keys, 16);
+// bf16 units of one 8-row tile: twelve warps an SM can be resident, seven or eight take all that memory gives, and a second wave that
+// the units do not fill costs more than it brings.  So as many warps per unit, then ranges, as stay within one wave of up to
+// 8.75 warps an SM.  D = 128, 8 key heads, us for (warps . ranges): 64 sequences x 2048 keys 98 (1.1) 82.6 (2.1) 94 (4.1) 90.6 (4.2); 8 x 16384
+// 180 (4.1) 98.6 (4.2) 85.6 (4.4) 89.4 (4.6); 32 x 4096 96.5 (2.1) 82.2 (4.1) 98 (4.2); 128 x 1024 86.5 (1.1) 96 (2.1).  Beyond
+// one wave long lists take four warps (200 x 2048: 237, with one 247), short ones a warp each (no join, no waiting).
+// More rows or fp32: eight (four) warps are resident, bound by products as well.
+Division divide(int64_t units, int64_t keys, int nr, int dtype, int sms) {
+    const int64_t chunks = ceil_div(keys, 16);
     Division d{1, 1};
+    if (nr == 1 && dtype == WHT_BF16) {
+        const int64_t wave = 35ll * sms / 4;
+        if (units > wave) return Division{chunks >= 32 && units <= 24 * sms ? 4 : 1, 1};
+        while (d.wpu < 4 && units * d.wpu * 2 <= wave && chunks >= 4 * 2 * d.wpu) d.wpu *= 2;
+        if (d.wpu == 4) d.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(8ll * sms / (units * 4), chunks / 16)));
+        return d;
+    }
+    const int64_t slots = 8ll * sms;
     while (d.wpu < 4 && units * d.wpu < 3 * slots && chunks >= 4 * 2 * d.wpu) d.wpu *= 2;
     if (d.wpu == 4) d.splits = static_cast<int>(std::max<int64_t>(1, std::min(slots / (units * 4), chunks / 16)));
     return d;
@@ -67,7 +80,7 @@ Division divide(int64_t units, int64_t keys, int sms) {
 bool block_each(int64_t units, int64_t keys, int dtype, int sms) {
     const bool f32 = dtype == WHT_F32;
     const int64_t chunks = ceil_div(keys, 16 * 8);  // of a warp
-    return units <= sms && (chunks <= (f32 ? 3 : 8) || (f32 ? 2 : 3) * units > sms);
+    return units <= sms && (chunks <= (f32 ? 3 : 8) || (f32 ? 2 * units > sms : 4 * units > 3 * sms));
 }
 
 struct PrefixPlan {
@@ -113,7 +126,7 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
     f.own_nr = row_tiles(own_rows);
     f.own_row_tiles = static_cast<int>(ceil_div(own_rows, 8 * f.own_nr));
-    const Division own = divide(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, sms);
+    const Division own = divide(static_cast<int64_t>(B) * Hkv * f.own_row_tiles, static_cast<int64_t>(table_width) * page, f.own_nr, dtype, sms);
     f.own_wpu = own.wpu;
     f.own_splits = own.splits;
     f.prefix_nr = f.prefix_wpu = 1;
@@ -145,7 +158,7 @@ PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32
     } else if (prefix_len > 0) {
         f.prefix_nr = row_tiles(T * group);
         f.prefix_row_tiles = static_cast<int>(ceil_div(T * group, 8 * f.prefix_nr));
-        const Division pre = divide(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, sms);
+        const Division pre = divide(static_cast<int64_t>(f.prefix_row_tiles) * Hkv, prefix_len, f.prefix_nr, dtype, sms);
         f.prefix_wpu = pre.wpu;
         f.prefix_splits = pre.splits;
     }
@@ -166,7 +179,7 @@ SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t H
     f.nr = row_tiles(group);
     f.row_tiles = static_cast<int>(ceil_div(group, 8 * f.nr));
     const int64_t units = T * Hkv * f.row_tiles, keys = static_cast<int64_t>(std::min(select, table_width)) * page;
-    Division d = divide(units, keys, sms);
+    Division d = divide(units, keys, f.nr, dtype, sms);
     if (block_each(units, keys, dtype, sms)) d = Division{8, 1};
     f.wpu = d.wpu;
     f.splits = d.splits;
