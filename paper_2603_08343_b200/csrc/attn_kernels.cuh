@@ -16,14 +16,19 @@
 //   - Products are taken transposed, S^T = K Q^T and O^T = V^T P^T: keys and channels fill the 16-row operand and the rows sit
 //     on the 8-column one, so 8 rows waste nothing.  P^T changes from accumulator to operand layout by one 8x8 transposition.
 //   - Each warp streams its own chunks: one lane asks the copy engine (TMA, 128-byte swizzle) for the key and value boxes
-//     of a chunk, and a ring of chunks per warp keeps up to 24 KB in flight; no warp waits for another in the loop.
+//     of a chunk, and a ring of chunks per warp keeps 16 to 24 KB in flight; no warp waits for another in the loop.
 //   - m moves only when a score passes it by more than 2^8, found by one vote: weights up to 2^8 are as exact as weights up to 1, and
 //     neither the reduction over lanes nor the scaling of o is in the common path.
 // A unit's keys are divided over 1, 2, 4 or 8 warps of a block, which join their (m, l, o) through shared memory, and over
 // blocks where there are too few units to fill the machine (attn_join_kernel adds those parts up).
 //
+// Measured, bf16, D = 128: 64 sequences x 2048 keys, 8 key heads of 4 rows 82.6 us (6.5 TB/s, all that memory gives); 256 x 150 keys, 32 heads
+// 103 us (6.1 TB/s).  Pages out of the L2 cache (2048 prompt tokens of 4 key heads with 16 pages of 64 each) 275 us for 4.3 GB, 15.6 TB/s: there
+// eight warps an SM waited for the results of products (371 us), twelve wait for the cache.
+//
 // fp32 tensors: both operands of each product are split in two tf32 terms (three products; what is dropped is below 2^-21
-// relative), contraction indices paired so that a thread's two values are neighbours.
+// relative), contraction indices paired so that a thread's two values are neighbours.  Bound by those products: 64 x 2048 keys as above
+// 240 us (4.5 TB/s).
 #pragma once
 #include <cuda.h>
 

@@ -5,18 +5,23 @@
 // From about 250 rows on that is the tensor core's balance, and the exponentials (one per row and key,
 // 16 a clock and SM) weigh as much as the products.
 //
-// A block of 10 warps owns 256 rows of one key head as two tiles of 128, and a range of keys:
-//   warps 0..3, 4..7   softmax of tile 0 / tile 1: one thread per row
-//   warp 8             issues the products;   warp 9   copies keys and values (TMA, a ring of 128-key tiles)
-// and runs steps of one tile and 128 keys, the two tiles taking turns, so that one tile's softmax runs under the other's products:
+// A block of 18 warps owns 256 rows of one key head as two tiles of 128, and a range of keys:
+//   warps 0..7, 8..15  softmax of tile 0 / tile 1: a row's 128 keys of a step belong to two threads, 64 each
+//   warp 16            issues the products;   warp 17   copies keys and values (TMA, a ring of 128-key tiles)
+// and runs steps of one tile and 128 keys, the two tiles strictly in turn, so that one tile's softmax runs under the other's products:
 //   S = Q K^T            into tensor memory (128 lanes x 128 fp32 columns)
-//   P = exp2(S - m)      read by the row's thread, rounded to bf16 and written over S
+//   P = exp2(S - m)      read by the row's threads, rounded to bf16 and written over S
 //   O += P V             P from tensor memory, V from shared memory, O stays in tensor memory (D columns)
-// The reference maximum m of a row is that of its first 64 keys and moves only when 64 weights add up to more than 2^14: large
+// The reference maximum m of a row is that of its first tile and moves only when a half's 64 weights add up to more than 2^14: large
 // weights are as exact in bf16 and fp32 as weights up to 1, O, which sits in tensor memory, is rescaled a few times per row at
-// most instead of once per tile, and the common path needs no maximum at all.  The weights are handed over in halves of 64 keys, so that
-// the second product of the first half runs under the exponentials of the second.  With 128 rows or fewer both tiles hold the SAME rows and take alternate key tiles; they
-// leave as two parts.
+// most instead of once per tile, and the common path needs no maximum at all.  The weights are one bf16 term here: a second
+// product for the second term would cost what the first does.  With 128 rows or fewer both tiles hold the SAME rows and take alternate
+// key tiles; they leave as two parts.
+//
+// Measured, 256 rows x 32768 keys x 32 heads, D = 128: 128 to 145 us (1.07 to 0.95 PFLOP/s, with the SM clock), 178 in the first form; eight
+// softmax warps instead of sixteen 191, warp numbers not known to be uniform 163 (a product then takes 100 clocks to issue, not
+// 30).  A step takes 3400 clocks, 1600 of them a tile's weights, which is what bounds it: exponentials, multiply-adds and tensor-memory
+// reads of 256 x 128 scores.  Short ranges (512 keys a block) spend 5.9k clocks before the first scores and 5k on the result.
 //
 // Keys and values arrive as page-high boxes of 64 channels in the 128-byte swizzle; K is the K-major operand of the
 // first product and V, the same way in memory, the MN-major operand of the second.  For D = 96 the second box reaches over

@@ -72,7 +72,7 @@ Division divide(int64_t units, int64_t keys, int nr, int dtype, int sms) {
 }
 
 // Whether each unit gets a block of eight warps, so that nothing is left to join: short lists, and few enough units that fill the
-// machine at a block each.  us, against the division above, 8 key heads of 4 rows, D = 128:
+// machine at a block each.  us, in brackets with four warps a unit and ranges, 8 key heads of 4 rows, D = 128:
 //   own pages  bf16  1 x 512 keys 8.5 (12.8), 1 x 2048 18.5 (12.4), 4 x 4096 30.8 (21.8), 9 x 2048 20.5 (22.7), 18 x 8192 97 (102)
 //              fp32  1 x 1024 32.9 (18.5), 9 x 8192 237 (180), 18 x 512 27 (37), 18 x 8192 243 (342), 40 tokens of 2 x 512 (80 units) 61 (102)
 //   selection  bf16  1 x 1024 16.4 (20.5), 1 x 2048 23.5 (18.8), 9 x 2048 27.1 (31.8), 18 x 2048 39.0 (43.4)
