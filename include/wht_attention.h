@@ -31,6 +31,7 @@
  *   - Rows that see no key (a length of zero) get zeros.
  *   - Cache entries that a row does not see (beyond a sequence's length, at the places of later tokens) never
  *     reach its result, whatever they hold (NaN and infinities included).
+ *   - In a -DWHT_DEBUG build these calls run as they do otherwise, without guarded buffers.
  */
 #ifndef WHT_ATTENTION_H_
 #define WHT_ATTENTION_H_
