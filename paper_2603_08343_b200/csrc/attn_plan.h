@@ -16,7 +16,7 @@ constexpr size_t kPartStats = 2 * sizeof(float);  // a partial result's maximum 
 // 8-row tiles per unit of the paged kernel
 inline int row_tiles(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
-// How the paged kernel divides a set of units of up to `keys` keys: warps per unit, and key ranges (splits).
+// How the paged kernel divides a set of units (one at least) of up to `keys` keys: warps per unit, and key ranges (splits).
 // No warp gets fewer than four 16-key chunks: its own set-up and the join would cost more than they save.
 struct Division {
     int wpu, splits;
@@ -92,8 +92,9 @@ inline int umma_splits_for(int64_t units, int64_t tiles, int tiles_per_step, int
 }
 
 inline PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv,
-                       int32_t D, int32_t page, int dtype, bool umma_allowed, int sms) {
+                              int32_t D, int32_t page, int dtype, bool umma_allowed, int sms) {
     PrefixPlan f{};
+    if (T == 0) return f;  // nothing is launched
     const int group = Hq / Hkv;
     const int64_t own_rows = static_cast<int64_t>(max_q_len) * group;
     f.own_nr = row_tiles(own_rows);
@@ -147,6 +148,7 @@ struct SelectPlan {
 
 inline SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int dtype, int sms) {
     SelectPlan f{};
+    if (T == 0) return f;  // nothing is launched
     const int group = Hq / Hkv;
     f.nr = row_tiles(group);
     f.row_tiles = static_cast<int>(div_up(group, 8 * f.nr));

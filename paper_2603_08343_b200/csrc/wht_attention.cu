@@ -38,7 +38,7 @@ int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages
 
 int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, int32_t page, bool ragged) {
     if (B < 0 || max_q_len < 1 || table_width < 0 || static_cast<int64_t>(table_width) * page > 0x7fffffff) return WHT_ERR_BAD_DIM;
-    if (max_q_len > (1 << 20) || (!ragged && (T != B || max_q_len != 1))) return WHT_ERR_BAD_T;
+    if (max_q_len > (1 << 20) || (!ragged && (T != B || max_q_len != 1)) || (T > 0 && B == 0)) return WHT_ERR_BAD_T;
     return WHT_OK;
 }
 

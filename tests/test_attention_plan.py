@@ -1,0 +1,63 @@
+"""How the serving attention divides its work (csrc/attn_plan.h), without a GPU: the header is host arithmetic alone and is
+compiled here with the host compiler, for 148 SMs."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BF16, F32 = 1, 0
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("plan") / "probe")
+    proc = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", os.path.join(ROOT, "tests", "attn_plan_probe.cpp"), "-o", exe],
+                          capture_output=True, text=True)
+    assert proc.returncode == 0, proc.stderr
+
+    def run(kind, *numbers):
+        line = " ".join([kind, *map(str, numbers)] + ["0"] * (11 - len(numbers)))
+        proc = subprocess.run([exe], input=line + "\n", capture_output=True, text=True)
+        assert proc.returncode == 0, f"{line}: ended with {proc.returncode}"
+        return {k: int(v) for k, v in (word.split("=") for word in proc.stdout.split())}
+    return run
+
+
+EMPTY_PREFIX = [
+    # prefix_len, width, T, B, max_q_len, Hq, Hkv, D, page, dtype, tcgen05
+    (0, 8, 0, 0, 1, 32, 8, 128, 64, BF16, 1),
+    (8192, 8, 0, 0, 1, 32, 8, 128, 64, BF16, 1),
+    (8192, 8, 0, 4, 16, 32, 8, 128, 64, BF16, 1),
+    (8192, 8, 0, 4, 16, 32, 8, 128, 64, BF16, 0),
+    (1000, 4, 0, 0, 1, 12, 12, 64, 16, F32, 0),
+    (0, 512, 0, 0, 1, 32, 1, 128, 128, F32, 0),
+    (40, 1, 0, 0, 1, 2, 2, 64, 16, BF16, 1),
+]
+
+
+@pytest.mark.parametrize("call", EMPTY_PREFIX)
+def test_a_prefix_call_of_no_tokens_needs_nothing(plan, call):
+    assert plan("prefix", *call)["bytes"] == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("width,select,hq", [(512, 32, 32), (8, 1024, 8), (2048, 600, 64), (0, 4, 8)])
+def test_a_selection_of_no_tokens_needs_nothing(plan, width, select, hq, dtype):
+    assert plan("select", width, select, 0, 0, 1, hq, 8, 128, 64, dtype)["bytes"] == 0
+
+
+def test_tokens_without_a_sequence_are_refused():
+    """Through the C entry points, which check before any CUDA work: T = 3 tokens, B = 0 sequences, q_start given."""
+    import ctypes
+    from paper_2603_08343_b200 import build
+    build.build()
+    from paper_2603_08343_b200 import binding
+    lib = binding.lib()
+    buf = (ctypes.c_char * 4096)()
+    p = ctypes.c_void_p((ctypes.addressof(buf) + 15) & ~15)
+    rest = (3, 0, 1, 4, 2, 64, 9, 16, 0.125, BF16, p, 0, None)
+    assert lib.wht_attn_prefix(p, 256, 64, p, p, p, 100, p, 4, p, p, p, *rest) == -3
+    assert lib.wht_attn_select(p, 256, 64, p, p, p, p, 4, p, p, 2, p, p, *rest) == -3
+    assert lib.wht_attn_prefix_workspace_bytes(1000, 64, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
+    assert lib.wht_attn_select_workspace_bytes(64, 32, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
