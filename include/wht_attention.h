@@ -28,7 +28,8 @@
  *     the cache, or a position outside the table, is never used as an address: the access is skipped (or the
  *     position clamped) and the device status word is set; wht_attn_device_status() then reports
  *     WHT_ERR_DEVICE_INDEX, and the call's outputs are invalid.
- *   - Rows that see no key (a length of zero) get zeros.
+ *   - Rows that see no key (a length of zero) get zeros.  So do rows of tokens that no sequence covers (before q_start[0], from q_start[B]
+ *     on); these are reported like an index out of range, and their entries of pages_out are -1.
  *   - Cache entries that a row does not see (beyond a sequence's length, at the places of later tokens) never
  *     reach its result, whatever they hold (NaN and infinities included).
  *   - In a -DWHT_DEBUG build these calls run as they do otherwise, without guarded buffers.

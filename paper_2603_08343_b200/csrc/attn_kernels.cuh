@@ -537,6 +537,30 @@ __device__ __forceinline__ int64_t attn_place(const AttnParams& p, int b, int64_
     return static_cast<int64_t>(attn_length(p, b)) - count + (t - first);
 }
 
+// The tokens that the sequences cover are first .. last - 1; says whether that is all of them.  (q_start is not NULL.)
+__device__ __forceinline__ bool attn_covered(const AttnParams& p, int64_t& first, int64_t& last) {
+    const int64_t a = __ldg(p.q_start), e = __ldg(p.q_start + p.B);
+    first = a < 0 ? 0 : (a > p.T ? p.T : a);
+    last = e < first ? first : (e > p.T ? p.T : e);
+    return first == 0 && last == p.T;
+}
+// Tokens of no sequence are reported.  Nobody's keys are theirs: one warp per key head sets their rows to zero (those of several parts
+// are left to the join).
+template <typename T, int D>
+__device__ __forceinline__ void attn_uncovered(const AttnParams& p, int head) {
+    int64_t first, last;
+    if (attn_covered(p, first, last)) return;
+    attn_report(kAttnErrIndex);
+    if (p.parts > 1) return;
+    const int pieces = p.group * D * static_cast<int>(sizeof(T)) / 16;
+    for (int64_t t = 0; t < p.T; ++t) {
+        if (t == first) t = last;
+        if (t >= p.T) break;
+        uint4* row = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + (t * p.hq + static_cast<int64_t>(head) * p.group) * D);
+        for (int i = threadIdx.x & 31; i < pieces; i += 32) row[i] = make_uint4(0, 0, 0, 0);
+    }
+}
+
 // keys [key0, key1) of part `s` of `splits`, in whole tiles
 __device__ __forceinline__ void attn_part(int keys, int tile, int splits, int s, int& key0, int& key1) {
     const int tiles = (keys + tile - 1) / tile;
@@ -592,6 +616,7 @@ attn_prefix_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
             if (ahead < p.table_width) asm volatile("prefetch.global.L1 [%0];" ::"l"(u.ids + ahead));
             attn_tokens(p, seq, u.token0, count);
             keys = attn_length(p, seq);
+            if (p.q_start != nullptr && seq == 0 && u.row0 == 0 && split == 0 && warp % p.own_wpu == 0) attn_uncovered<T, D>(p, u.head);
         }
         u.rows = count * p.group;
         work = u.row0 < u.rows;
@@ -672,15 +697,22 @@ attn_chosen_kernel(const AttnParams p, const __grid_constant__ CUtensorMap k_map
 }
 
 // Joins the parts of each row: out = sum_s exp(m_s - m) o_s / sum_s exp(m_s - m) l_s.  One warp per row, lanes
-// over the channels; the parts' statistics are read by the lanes at once.
+// over the channels; the parts' statistics are read by the lanes at once.  q_start (or NULL): rows of tokens that no sequence covers
+// have parts that nobody wrote, and get zeros.
 template <typename T, int D>
 __global__ void __launch_bounds__(128)
-attn_join_kernel(const float2* __restrict__ ml, const float* __restrict__ po, T* __restrict__ out, int64_t rows, int parts) {
+attn_join_kernel(const float2* __restrict__ ml, const float* __restrict__ po, T* __restrict__ out, int64_t rows, int parts,
+                 const int32_t* __restrict__ q_start, int B, int hq) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int lane = threadIdx.x & 31;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
     if (row >= rows) return;
+    bool covered = true;
+    if (q_start != nullptr) {
+        const int t = static_cast<int>(row) / hq;
+        covered = t >= __ldg(q_start) && t < __ldg(q_start + B);
+    }
     float m = -INFINITY;
     for (int s = lane; s < parts; s += 32) m = fmaxf(m, ml[s * rows + row].x);
 #pragma unroll
@@ -713,6 +745,7 @@ attn_join_kernel(const float2* __restrict__ ml, const float* __restrict__ po, T*
 #pragma unroll
     for (int i = 16; i; i >>= 1) l += __shfl_xor_sync(kFullMask, l, i);
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (!covered) acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (lane * PER < D) {
         T* dst = out + row * D + lane * PER;
         if constexpr (std::is_same<T, float>::value)

@@ -90,7 +90,7 @@ template <typename T, int D>
 int attn_join_d(const AttnParams& p, cudaStream_t s) {
     const long long rows = static_cast<long long>(p.T) * p.hq;
     launch_overlapped(attn_join_kernel<T, D>, dim3(static_cast<unsigned>(ceil_div(rows, 4))), 128, 0, s, p.part_ml, p.part_o,
-                      static_cast<T*>(p.out), static_cast<int64_t>(rows), p.parts);
+                      static_cast<T*>(p.out), static_cast<int64_t>(rows), p.parts, p.chosen ? nullptr : p.q_start, p.B, p.hq);
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }

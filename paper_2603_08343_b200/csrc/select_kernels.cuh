@@ -220,6 +220,16 @@ attn_select_kernel(const SelectParams sp) {
     int count;
     attn_tokens(p, seq, first, count);
     const int n = min(TQ, count - tile * TQ);
+    if (p.q_start != nullptr && seq == 0 && tile == 0) {  // tokens of no sequence read no page (the attention reports them)
+        int64_t from, to;
+        if (!attn_covered(p, from, to)) {
+            for (int64_t t = 0; t < p.T; ++t) {
+                if (t == from) t = to;
+                if (t >= p.T) break;
+                for (int e = tid; e < p.select; e += kSelectThreads) sp.pages[(t * p.hkv + head) * p.select + e] = -1;
+            }
+        }
+    }
     if (n <= 0) return;
     const int64_t t0 = first + tile * TQ;
     const int64_t place0 = static_cast<int64_t>(attn_length(p, seq)) - count + tile * TQ;

@@ -68,3 +68,93 @@ def test_tokens_without_a_sequence_are_refused(A):
     with pytest.raises(B.WhtError) as e:
         A.selected_page_attention(q, kc, kc, summary, table, lens, 4, q_start=_ints(0), max_q_len=3)
     assert e.value.status == -3
+
+
+# ---------------------------------------------------------------- tokens that no sequence covers
+
+def _paged(seed, B, hq, hkv, d, page, dtype, prefix, lead, q_lens, tail, kv_lens, width=None):
+    """`lead` tokens before the first sequence's and `tail` after the last one's; keys that no token may see are NaN, values infinite."""
+    g = _gen(seed)
+    width = max([1] + [-(-n // page) for n in kv_lens]) if width is None else width
+    n_pre = -(-prefix // page)
+    pages = n_pre + sum(-(-n // page) for n in kv_lens) + 1
+    perm = torch.randperm(pages, generator=g).to(torch.int32)
+    pre, rest = perm[:n_pre].contiguous(), perm[n_pre:].tolist()
+    table = torch.full((B, width), -1, dtype=torch.int32)       # beyond a sequence's length: no page at all
+    kc, vc = _randn((pages, hkv, page, d), dtype, g), _randn((pages, hkv, page, d), dtype, g)
+    seen = torch.zeros(pages, page, dtype=torch.bool)
+    for i in range(prefix):
+        seen[int(pre[i // page]), i % page] = True
+    for b, n in enumerate(kv_lens):
+        for j in range(-(-n // page)):
+            table[b, j] = rest.pop()
+        for i in range(n):
+            seen[int(table[b, i // page]), i % page] = True
+    dead = ~seen[:, None, :, None].expand_as(kc)
+    kc[dead] = float("nan")
+    vc[dead] = float("inf")
+    T = lead + sum(q_lens) + tail
+    starts = torch.tensor([lead] + q_lens).cumsum(0).to(torch.int32)
+    return dict(T=T, q=_randn((T, hq, d), dtype, g, 1.5), kc=kc, vc=vc, pre=pre, table=table, lens=torch.tensor(kv_lens, dtype=torch.int32),
+                starts=starts, max_q=max(q_lens), vmax=vc[torch.isfinite(vc)].abs().max().item())
+
+
+def _poison_workspace(nbytes):
+    """The next block of this size from the allocator is full of NaN."""
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    if nbytes:
+        junk = torch.full((-(-nbytes // 4),), float("nan"), device="cuda")
+        torch.cuda.synchronize()
+        del junk
+
+
+UNCOVERED = [
+    # B, hq, hkv, d, page, prefix, lead, q_lens, tail, kv_lens
+    (2, 4, 2, 64, 16, 0, 2, [1, 1], 3, [20, 5]),                  # own pages alone, nothing to join
+    (2, 4, 2, 128, 64, 0, 1, [3, 2], 2, [2000, 900]),             # key ranges, joined
+    (2, 4, 2, 64, 16, 40, 0, [2, 1], 1, [9, 30]),                 # one walk over prefix and own pages
+    (3, 4, 1, 96, 32, 2000, 3, [1, 4, 2], 0, [50, 4, 70]),        # prefix ranges, own pages, a join
+    (4, 16, 2, 128, 64, 1500, 5, [1, 6, 2, 8], 9, [50, 6, 70, 33]),  # the prefix on tcgen05 (bf16)
+    (2, 4, 2, 64, 16, 0, 1, [1, 40], 6, [30, 200]),               # prompts
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("B,hq,hkv,d,page,prefix,lead,q_lens,tail,kv_lens", UNCOVERED)
+def test_tokens_of_no_sequence_get_zeros_and_are_reported(A, B, hq, hkv, d, page, prefix, lead, q_lens, tail, kv_lens, dtype):
+    from paper_2603_08343_b200 import binding
+    c = _paged(30 + B, B, hq, hkv, d, page, dtype, prefix, lead, q_lens, tail, kv_lens)
+    q, kc, vc, pre, table, lens, starts = _cuda(c["q"], c["kc"], c["vc"], c["pre"], c["table"], c["lens"], c["starts"])
+    code = 0 if dtype == F32 else 1
+    out = torch.full_like(q, 7.0)
+    _poison_workspace(binding.lib().wht_attn_prefix_workspace_bytes(prefix, table.shape[1], c["T"], B, c["max_q"], hq, hkv, d, page, code))
+    A.shared_prefix_attention(q, kc, vc, pre, prefix, table, lens, q_start=starts, max_q_len=c["max_q"], out=out)
+    with pytest.raises(binding.WhtError) as e:
+        A.device_status()
+    assert e.value.status == -11
+    want = R.prefix_attention(c["q"], c["kc"], c["vc"], c["pre"], prefix, c["table"], c["lens"], c["starts"], d ** -0.5)
+    covered = torch.zeros(c["T"], dtype=torch.bool)
+    covered[lead:c["T"] - tail] = True
+    assert torch.all(out.cpu()[~covered] == 0)
+    assert torch.isfinite(out).all() and (out.cpu().double() - want).abs().max().item() <= R.tolerance(dtype, c["vmax"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("select,width", [(3, None), (3, 700), (40, None)])
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 1, 1], [200, 17, 90]), ([30, 1, 7], [200, 17, 90])])
+def test_a_selection_s_tokens_of_no_sequence(A, q_lens, kv_lens, select, width, dtype):
+    from paper_2603_08343_b200 import binding
+    c = _paged(40, 3, 4, 2, 64, 16, dtype, 0, 2, q_lens, 4, kv_lens, width)
+    summary = R.page_summary(torch.nan_to_num(c["kc"].float(), nan=0.0), torch.full((2,), 30.0))
+    want, want_pages = R.select_attention(c["q"], c["kc"], c["vc"], summary, c["table"], c["lens"], select, c["starts"], 0.125)
+    q, kc, vc, sm, table, lens, starts = _cuda(c["q"], c["kc"], c["vc"], summary, c["table"], c["lens"], c["starts"])
+    out = torch.full_like(q, 7.0)
+    pages = torch.full((c["T"], 2, select), 99, dtype=torch.int32, device="cuda")
+    A.selected_page_attention(q, kc, vc, sm, table, lens, select, q_start=starts, max_q_len=c["max_q"], out=out, pages_out=pages)
+    with pytest.raises(binding.WhtError) as e:
+        A.device_status()
+    assert e.value.status == -11
+    assert torch.equal(pages.cpu(), want_pages)
+    assert torch.all(out.cpu()[:2] == 0) and torch.all(out.cpu()[-4:] == 0)
+    assert torch.isfinite(out).all() and (out.cpu().double() - want).abs().max().item() <= R.tolerance(dtype, c["vmax"])
