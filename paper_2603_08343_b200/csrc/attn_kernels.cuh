@@ -322,6 +322,8 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
                 const int r = valid + i / (8 * Geo::BOXES), c = i % (8 * Geo::BOXES);
                 *reinterpret_cast<uint4*>(v + Geo::place(r, c)) = make_uint4(0, 0, 0, 0);
             }
+            // (behind a hole the list goes on, and the copy engine writes this slot again: ordinary stores come before it)
+            fence_before_copies();
             __syncwarp();
         }
 

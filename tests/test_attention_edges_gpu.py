@@ -158,3 +158,25 @@ def test_a_selection_s_tokens_of_no_sequence(A, q_lens, kv_lens, select, width, 
     assert torch.equal(pages.cpu(), want_pages)
     assert torch.all(out.cpu()[:2] == 0) and torch.all(out.cpu()[-4:] == 0)
     assert torch.isfinite(out).all() and (out.cpu().double() - want).abs().max().item() <= R.tolerance(dtype, c["vmax"])
+
+
+# ---------------------------------------------------------------- one walk over the prefix and the own pages
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("d,page,prefix,kv_lens", [
+    (128, 128, 20, [128, 77, 1]),       # fp32: one stage a warp; slots zeroed for the hole are copied into again at once
+    (128, 128, 130, [128, 5, 64]),
+    (64, 64, 33, [190, 64, 129]),
+    (96, 128, 257, [380, 300, 126]),
+])
+def test_slots_behind_the_prefix_s_hole_are_used_again(A, d, page, prefix, kv_lens, dtype):
+    """The unused end of the prefix's last page lies inside the list; what it holds (NaN and infinities) and the zeros put in its place
+    must not reach the chunks that follow in the same shared memory.  Same bits every time."""
+    c = _paged(60 + d, 3, 8, 4, d, page, dtype, prefix, 0, [1, 1, 1], 0, kv_lens)
+    q, kc, vc, pre, table, lens = _cuda(c["q"], c["kc"], c["vc"], c["pre"], c["table"], c["lens"])
+    want = R.prefix_attention(c["q"], c["kc"], c["vc"], c["pre"], prefix, c["table"], c["lens"], None, d ** -0.5)
+    outs = [A.shared_prefix_attention(q, kc, vc, pre, prefix, table, lens) for _ in range(20)]
+    assert torch.isfinite(outs[0]).all()
+    assert (outs[0].cpu().double() - want).abs().max().item() <= R.tolerance(dtype, c["vmax"])
+    assert all(torch.equal(o, outs[0]) for o in outs)
+    A.device_status()
