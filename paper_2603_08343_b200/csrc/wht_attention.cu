@@ -201,6 +201,8 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
 }
 
 int wht_attn_device_status(void) {
+    // the words are copied on the default stream, which other streams need not wait for, nor it for them
+    WHT_CUDA_TRY(cudaDeviceSynchronize());
     unsigned any = 0;
     for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select,
                       take_attn_error_umma}) {

@@ -180,3 +180,23 @@ def test_slots_behind_the_prefix_s_hole_are_used_again(A, d, page, prefix, kv_le
     assert (outs[0].cpu().double() - want).abs().max().item() <= R.tolerance(dtype, c["vmax"])
     assert all(torch.equal(o, outs[0]) for o in outs)
     A.device_status()
+
+
+# ---------------------------------------------------------------- the status of work on other streams
+
+def test_the_status_waits_for_other_streams(A):
+    """An error on a side stream (torch's do not wait for the default stream, nor it for them) behind some tenths of a second of work."""
+    from paper_2603_08343_b200 import binding
+    kc = torch.zeros(4, 1, 16, 64, dtype=BF16, device="cuda")
+    k = torch.zeros(1, 1, 64, dtype=BF16, device="cuda")
+    past = torch.tensor([4 * 16], device="cuda")                # the first slot behind the cache
+    A.kv_append(k, k, kc, kc, torch.tensor([0], device="cuda"))
+    A.device_status()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+        A.kv_append(k, k, kc, kc, past)
+    with pytest.raises(binding.WhtError) as e:
+        A.device_status()
+    assert e.value.status == -11
+    A.device_status()
