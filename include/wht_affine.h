@@ -292,8 +292,8 @@ int wht_copy_rows(const void* src, void* dst, int64_t T, int32_t d, int dtype, v
  * The kernels that stream rows through shared memory (the tcgen05 family and the
  * streamed mma.sync family) wait for their async copies, tensor-core products and
  * hand-overs between warps with a bound; a wait that expires does not hang or trap, it sets a flag on the device and the launch's
- * results are invalid.  This call synchronises with the current device's work
- * (it copies the flag back), returns WHT_ERR_DEVICE_WAIT if the flag was set
+ * results are invalid.  This call synchronises with the current device's work on
+ * every stream, copies the flag back, returns WHT_ERR_DEVICE_WAIT if the flag was set
  * since the last query and clears it, else WHT_OK.  Never expected in normal
  * operation; meant for tests and for debugging after a suspicious result.
  */

@@ -646,6 +646,8 @@ int wht_copy_rows(const void* src, void* dst, int64_t T, int32_t d, int dtype, v
 }
 
 int wht_affine_device_status(void) {
+    // the words are copied on the default stream, which other streams need not wait for, nor it for them
+    WHT_CUDA_TRY(cudaDeviceSynchronize());
     // one status word per translation unit that holds waiting kernels: read and clear them all
     unsigned any = 0;
     for (auto take : {take_device_error_mma, take_device_error_umma_fwd, take_device_error_umma_bwd,

@@ -200,3 +200,18 @@ def test_the_status_waits_for_other_streams(A):
         A.device_status()
     assert e.value.status == -11
     A.device_status()
+
+
+def test_the_older_status_waits_for_other_streams():
+    """An expired wait (the library's self-test, 100 ms) on a side stream."""
+    from paper_2603_08343_b200 import binding
+    torch.cuda.synchronize()
+    binding.wht_affine_device_status()
+    out = torch.zeros(3, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    binding.wht_affine_selftest_wait_expiry(100_000, out, stream=side)
+    with pytest.raises(binding.WhtError) as e:
+        binding.wht_affine_device_status()
+    assert e.value.status == -9
+    binding.wht_affine_device_status()
