@@ -25,8 +25,8 @@ template <typename T> int launch_attn_chosen(const wht::AttnParams& p, int d, in
 template <typename T> int launch_attn_join(const wht::AttnParams& p, int d, cudaStream_t s);
 // attn_umma.cu
 int launch_attn_umma_prefix(const wht::UmmaAttnParams& p, int d, int dev, cudaStream_t s);
-// attn_select.cu
-int launch_select(wht::SelectParams& p, int dtype, int d, cudaStream_t s);
+// attn_select.cu; one_kernel: scores stay in shared memory, and p.scores is not used
+int launch_select(wht::SelectParams& p, bool one_kernel, int dtype, int d, cudaStream_t s);
 
 int take_attn_error_append(unsigned* flag);
 int take_attn_error_paged_bf16(unsigned* flag);

@@ -143,10 +143,12 @@ inline PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T
 
 struct SelectPlan {
     int nr, row_tiles, wpu, splits;
+    bool one_kernel;       // scores and picks in one kernel, which needs no memory for the scores
     size_t scores_bytes, bytes;
 };
 
-inline SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int dtype, int sms) {
+inline SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv,
+                              int32_t D, int32_t page, int dtype, int sms) {
     SelectPlan f{};
     if (T == 0) return f;  // nothing is launched
     const int group = Hq / Hkv;
@@ -157,7 +159,13 @@ inline SelectPlan plan_select(int32_t table_width, int32_t select, int64_t T, in
     if (block_each(units, keys, dtype, sms)) d = Division{8, 1};
     f.wpu = d.wpu;
     f.splits = d.splits;
-    f.scores_bytes = up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
+    // One kernel where its blocks' scores fit shared memory, unless a few blocks would have to read long tables alone.  Whole call, 8 key
+    // heads, pages of 16, one kernel against two: 1 x 256 pages 15.9 us (17.2), 1 x 512 18.6 (18.2), 1 x 1024 29.5 (20.6), 1 x 2048 43.0 (21.3), 4 x 2048
+    // 42.5 (32.3), 16 x 2048 57.0 (51.1), 64 x 2048 100.7 (105.3), 300 prompt tokens of 1500 pages 110 (163).
+    const int tq = max_q_len == 1 ? 1 : 16;  // queries of a block
+    const int64_t blocks = static_cast<int64_t>(B) * div_up(max_q_len, tq) * Hkv;
+    f.one_kernel = static_cast<int64_t>(table_width) * tq * 4 <= 96 * 1024 && (table_width <= 512 || blocks >= 128);
+    f.scores_bytes = f.one_kernel ? 0 : up256(static_cast<size_t>(T) * Hkv * table_width * sizeof(int32_t));
     const size_t rows = static_cast<size_t>(T) * Hq;
     f.bytes = f.scores_bytes + (f.splits > 1 ? up256(rows * f.splits * kPartStats) + rows * f.splits * D * sizeof(float) : 0);
     return f;

@@ -69,14 +69,8 @@ int select_d(SelectParams& p, int d, cudaStream_t s) {
 
 }  // namespace
 
-int launch_select(SelectParams& p, int dtype, int d, cudaStream_t s) {
-    // One kernel where its blocks' scores fit shared memory, unless a few blocks would have to read long tables alone.  Whole call, 8 key
-    // heads, pages of 16, one kernel against two: 1 x 256 pages 15.9 us (17.2), 1 x 512 18.6 (18.2), 1 x 1024 29.5 (20.6), 1 x 2048 43.0 (21.3), 4 x 2048
-    // 42.5 (32.3), 16 x 2048 57.0 (51.1), 64 x 2048 100.7 (105.3), 300 prompt tokens of 1500 pages 110 (163).
-    const int tq = p.a.max_q_len == 1 ? 1 : 16;
-    const long long blocks = static_cast<long long>(p.a.B) * ceil_div(p.a.max_q_len, tq) * p.a.hkv;
-    if (static_cast<long long>(p.stride) * tq * 4 <= 96 * 1024 && (p.stride <= 512 || blocks >= 128))
-        return dtype == WHT_F32 ? select_d<float>(p, d, s) : select_d<__nv_bfloat16>(p, d, s);
+int launch_select(SelectParams& p, bool one_kernel, int dtype, int d, cudaStream_t s) {
+    if (one_kernel) return dtype == WHT_F32 ? select_d<float>(p, d, s) : select_d<__nv_bfloat16>(p, d, s);
     const int rc = dtype == WHT_F32 ? score_d<float>(p, d, s) : score_d<__nv_bfloat16>(p, d, s);
     if (rc != WHT_OK) return rc;
     // a thread holds a few of a row's candidates at most; long rows get a larger block

@@ -24,7 +24,7 @@ namespace wht {
 struct SelectParams {
     AttnParams a;           // queries, tables, lengths
     const int8_t* summary;  // [num_pages x Hkv x 2 x D]
-    int32_t* scores;        // [T x Hkv x stride]
+    int32_t* scores;        // [T x Hkv x stride], for the two kernels
     int32_t* pages;         // [T x Hkv x select]
     int stride;             // candidates a row has room for (the table's width)
     int token_tiles;        // token tiles per sequence

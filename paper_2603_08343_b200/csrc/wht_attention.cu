@@ -153,7 +153,7 @@ size_t wht_attn_select_workspace_bytes(int32_t table_width, int32_t select, int6
     if (check_shape(T, Hq, Hkv, D, 0, page, dtype) != WHT_OK || check_batch(T, B, max_q_len, table_width, page, true) != WHT_OK ||
         select < 1 || select > 1024 || device_info(&dev, &sms) != WHT_OK)
         return 0;
-    return plan_select(table_width, select, T, Hq, Hkv, D, page, dtype, sms).bytes;
+    return plan_select(table_width, select, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms).bytes;
 }
 
 int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k_cache, const void* v_cache,
@@ -174,7 +174,7 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     int dev = 0, sms = 0;
     rc = device_info(&dev, &sms);
     if (rc != WHT_OK) return rc;
-    const SelectPlan f = plan_select(table_width, select, T, Hq, Hkv, D, page, dtype, sms);
+    const SelectPlan f = plan_select(table_width, select, T, B, max_q_len, Hq, Hkv, D, page, dtype, sms);
     if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return WHT_ERR_WORKSPACE;
     SelectParams sp{};
     AttnParams& p = sp.a;
@@ -191,11 +191,11 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.hq = Hq; p.hkv = Hkv; p.group = Hq / Hkv; p.page_shift = page_shift_of(page);
     p.scale_log2 = scale * wht::kLog2e;
     sp.summary = summary;
-    sp.scores = static_cast<int32_t*>(workspace);
+    sp.scores = f.one_kernel ? nullptr : static_cast<int32_t*>(workspace);
     sp.pages = pages_out;
     sp.stride = table_width;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    rc = launch_select(sp, dtype, D, s);
+    rc = launch_select(sp, f.one_kernel, dtype, D, s);
     if (rc == WHT_OK) rc = dtype == WHT_F32 ? launch_attn_chosen<float>(p, D, dev, s) : launch_attn_chosen<__nv_bfloat16>(p, D, dev, s);
     return rc != WHT_OK ? rc : join(p, dtype, D, s);
 }

@@ -16,8 +16,8 @@ int main() {
             std::printf("joint=%d umma=%d umma_splits=%d prefix_wpu=%d prefix_splits=%d own_wpu=%d own_splits=%d parts=%d bytes=%zu\n", f.joint, f.umma,
                         f.umma_splits, f.prefix_wpu, f.prefix_splits, f.own_wpu, f.own_splits, f.parts, f.bytes);
         } else {  // width select T B max_q_len Hq Hkv D page dtype -
-            const wht_plan::SelectPlan f = wht_plan::plan_select(i(0), i(1), n[2], i(5), i(6), i(7), i(8), i(9), 148);
-            std::printf("wpu=%d splits=%d scores_bytes=%zu bytes=%zu\n", f.wpu, f.splits, f.scores_bytes, f.bytes);
+            const wht_plan::SelectPlan f = wht_plan::plan_select(i(0), i(1), n[2], i(3), i(4), i(5), i(6), i(7), i(8), i(9), 148);
+            std::printf("wpu=%d splits=%d one_kernel=%d scores_bytes=%zu bytes=%zu\n", f.wpu, f.splits, f.one_kernel, f.scores_bytes, f.bytes);
         }
         std::fflush(stdout);
     }

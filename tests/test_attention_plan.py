@@ -61,3 +61,22 @@ def test_tokens_without_a_sequence_are_refused():
     assert lib.wht_attn_select(p, 256, 64, p, p, p, p, 4, p, p, 2, p, p, *rest) == -3
     assert lib.wht_attn_prefix_workspace_bytes(1000, 64, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
     assert lib.wht_attn_select_workspace_bytes(64, 32, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
+
+
+@pytest.mark.parametrize("width,select,T,B,max_q,hkv,page", [
+    (1500, 32, 32768, 1, 32768, 8, 16),     # a long prompt: 1.5 GB of scores that nobody would read
+    (512, 32, 64, 64, 1, 8, 64),
+    (64, 16, 1, 1, 1, 8, 64),
+    (2048, 32, 64, 64, 1, 8, 16),
+])
+def test_scores_that_stay_in_shared_memory_need_no_workspace(plan, width, select, T, B, max_q, hkv, page):
+    f = plan("select", width, select, T, B, max_q, 4 * hkv, hkv, 128, page, BF16)
+    assert f["scores_bytes"] == 0
+    parts = f["splits"] * T * 4 * hkv * (128 * 4 + 8) if f["splits"] > 1 else 0
+    assert f["bytes"] <= parts + 256
+
+
+@pytest.mark.parametrize("width,T,B,max_q", [(1024, 1, 1, 1), (2048, 4, 4, 1), (1600, 300, 1, 300), (49152, 200, 200, 1)])
+def test_scores_of_the_two_kernels_do(plan, width, T, B, max_q):
+    f = plan("select", width, 32, T, B, max_q, 32, 8, 128, 16, BF16)
+    assert f["scores_bytes"] >= T * 8 * width * 4
