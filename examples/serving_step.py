@@ -32,6 +32,8 @@ class Block:
     def __init__(self, batch, heads, kv_heads, head_dim, page, prefix, own, dtype=torch.bfloat16, summary_scale=28.0, a=None, b=None):
         if prefix % page:
             raise ValueError("the shared prefix takes whole pages")
+        if own < 1:
+            raise ValueError("a sequence needs room for one token of its own at least")
         self.batch, self.heads, self.kv_heads, self.head_dim, self.page, self.prefix = batch, heads, kv_heads, head_dim, page, prefix
         n_prefix, n_own = prefix // page, -(-own // page)
         pages = n_prefix + batch * n_own
@@ -44,7 +46,8 @@ class Block:
         self.own_pages = order[n_prefix:].reshape(batch, n_own).contiguous()
         self.all_pages = torch.cat([self.prefix_pages.expand(batch, -1), self.own_pages], 1).contiguous()
         self.own_lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
-        self.cos, self.sin = rope_tables(prefix + own, head_dim)
+        self.capacity = n_own * page                                       # tokens of its own that a sequence has room for
+        self.cos, self.sin = rope_tables(prefix + self.capacity, head_dim)
         self.a = torch.ones(heads * head_dim, device="cuda") if a is None else a
         self.b = torch.zeros(heads * head_dim, device="cuda") if b is None else b
 
@@ -59,6 +62,8 @@ class Block:
     def write_prefix(self, qkv):
         """The shared document, once: qkv [prefix, heads + 2 kv_heads, head_dim]; returns its tokens' block outputs."""
         n = qkv.shape[0]
+        if n != self.prefix:
+            raise ValueError(f"{n} tokens for a document of {self.prefix}")
         place = torch.arange(n, device="cuda")
         slots = self.prefix_pages.long()[place // self.page] * self.page + place % self.page
         q = self._append(qkv, slots, place.int())
@@ -68,9 +73,13 @@ class Block:
 
     def step(self, qkv, select=0):
         """One token per sequence: qkv [batch, heads + 2 kv_heads, head_dim] -> [batch, heads * head_dim].  select: 0 reads all keys,
-        the shared ones once for the whole batch; otherwise each token reads that many pages."""
+        the shared ones once for the whole batch; otherwise each token reads that many pages.  A token that finds its sequence's pages
+        full is dropped, and the attention reports the length (`device_status`)."""
+        if qkv.shape[0] != self.batch:
+            raise ValueError(f"{qkv.shape[0]} tokens for {self.batch} sequences")
         place = self.own_lens.long()
-        slots = self.own_pages.gather(1, (place // self.page)[:, None])[:, 0].long() * self.page + place % self.page
+        page = self.own_pages.gather(1, (place // self.page).clamp(max=self.own_pages.shape[1] - 1)[:, None])[:, 0].long()
+        slots = torch.where(place < self.capacity, page * self.page + place % self.page, -1)
         q = self._append(qkv, slots, self.own_lens + self.prefix)
         self.own_lens += 1
         if select:
@@ -86,6 +95,8 @@ def main():
                         ("steps", 32), ("select", 32)):
         ap.add_argument(f"--{name}", type=int, default=value)
     o = ap.parse_args()
+    if not 1 <= o.steps <= o.own:
+        ap.error(f"--steps {o.steps}: the sequences have room for 1 to --own {o.own} tokens")
     torch.manual_seed(0)
     rows = o.heads + 2 * o.kv_heads
     block = Block(o.batch, o.heads, o.kv_heads, o.head_dim, o.page, o.prefix, o.own)

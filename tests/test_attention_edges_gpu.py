@@ -215,3 +215,36 @@ def test_the_older_status_waits_for_other_streams():
         binding.wht_affine_device_status()
     assert e.value.status == -9
     binding.wht_affine_device_status()
+
+
+# ---------------------------------------------------------------- the example at the end of its pages
+
+@pytest.mark.parametrize("select", [0, 2])
+def test_a_step_past_the_example_s_pages_is_reported(select):
+    """The own pages are looked up in range (an index past them would be a device assertion), the token is dropped, the length reported."""
+    import importlib.util
+    import os
+    from paper_2603_08343_b200 import binding
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serving_step.py")
+    spec = importlib.util.spec_from_file_location("serving_step", path)
+    E = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(E)
+    block = E.Block(2, 4, 2, 64, 16, 16, 20)          # room for 32
+    rows = 4 + 2 * 2
+    block.write_prefix(torch.zeros(16, rows, 64, dtype=BF16, device="cuda"))
+    block.own_lens.fill_(31)
+    block.step(torch.ones(2, rows, 64, dtype=BF16, device="cuda"), select)
+    E.A.device_status()
+    before = block.k_cache.clone()
+    block.step(torch.ones(2, rows, 64, dtype=BF16, device="cuda"), select)
+    with pytest.raises(binding.WhtError) as e:
+        E.A.device_status()
+    assert e.value.status == -11
+    assert torch.equal(block.k_cache, before)
+    for bad in (15, 17):
+        with pytest.raises(ValueError):
+            block.write_prefix(torch.zeros(bad, rows, 64, dtype=BF16, device="cuda"))
+    with pytest.raises(ValueError):
+        block.step(torch.ones(3, rows, 64, dtype=BF16, device="cuda"), select)
+    with pytest.raises(ValueError):
+        E.Block(2, 4, 2, 64, 16, 16, 0)

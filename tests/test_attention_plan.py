@@ -80,3 +80,12 @@ def test_scores_that_stay_in_shared_memory_need_no_workspace(plan, width, select
 def test_scores_of_the_two_kernels_do(plan, width, T, B, max_q):
     f = plan("select", width, 32, T, B, max_q, 32, 8, 128, 16, BF16)
     assert f["scores_bytes"] >= T * 8 * width * 4
+
+
+def test_the_example_refuses_more_steps_than_it_has_pages_for():
+    """(On the host: an index past the own pages would be a device assertion.)"""
+    import sys
+    for steps, own in ((513, 512), (0, 512), (1, 0)):
+        proc = subprocess.run([sys.executable, os.path.join(ROOT, "examples", "serving_step.py"), "--steps", str(steps), "--own", str(own)],
+                              capture_output=True, text=True, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""})
+        assert proc.returncode == 2 and "--steps" in proc.stderr, proc.stderr
