@@ -137,9 +137,9 @@ __device__ __forceinline__ void attn_unit(const AttnParams& p, const AttnUnit& u
     }
     // cache rows of 32 of this warp's chunks, one per lane, and of the next 32
     auto rows_of = [&](int j) {
-        const int key = u.key0 + (wi + (j + lane) * u.wpu) * kChunk;
         int y = 0;
         if (j + lane < chunks) {
+            const int key = u.key0 + (wi + (j + lane) * u.wpu) * kChunk;
             const int e = key >> p.page_shift;
             int pg = __ldg(e < u.list1 ? u.ids + e : u.ids2 + (e - u.list1));
             if (u.table) pg = pg >= 0 ? __ldg(u.table + pg) : -1;

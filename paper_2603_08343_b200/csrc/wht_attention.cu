@@ -36,8 +36,11 @@ int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages
     return WHT_OK;
 }
 
+// Keys of a list are counted in 31 bits, and the kernels round counts up to whole tiles: some room is left above the longest list.
+constexpr int64_t kMostKeys = 0x7fffff00;
+
 int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, int32_t page, bool ragged) {
-    if (B < 0 || max_q_len < 1 || table_width < 0 || static_cast<int64_t>(table_width) * page > 0x7fffffff) return WHT_ERR_BAD_DIM;
+    if (B < 0 || max_q_len < 1 || table_width < 0 || static_cast<int64_t>(table_width) * page > kMostKeys) return WHT_ERR_BAD_DIM;
     if (max_q_len > (1 << 20) || (!ragged && (T != B || max_q_len != 1)) || (T > 0 && B == 0)) return WHT_ERR_BAD_T;
     return WHT_OK;
 }
@@ -94,7 +97,7 @@ size_t wht_attn_prefix_workspace_bytes(int64_t prefix_len, int32_t table_width, 
                                        int32_t Hkv, int32_t D, int32_t page, int dtype) {
     int dev = 0, sms = 0;
     if (check_shape(T, Hq, Hkv, D, 0, page, dtype) != WHT_OK || check_batch(T, B, max_q_len, table_width, page, true) != WHT_OK ||
-        prefix_len < 0 || device_info(&dev, &sms) != WHT_OK)
+        prefix_len < 0 || prefix_len > kMostKeys || device_info(&dev, &sms) != WHT_OK)
         return 0;
     // either form of the prefix may be taken (the tcgen05 one has conditions that are not known here)
     return std::max(plan_prefix(prefix_len, table_width, T, B, max_q_len, Hq, Hkv, D, page, dtype, true, sms).bytes,
@@ -109,7 +112,7 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     int rc = check_shape(T, Hq, Hkv, D, num_pages, page, dtype);
     if (rc == WHT_OK) rc = check_batch(T, B, max_q_len, table_width, page, q_start != nullptr);
     if (rc != WHT_OK) return rc;
-    if (prefix_len < 0 || prefix_len > 0x7fffff00) return WHT_ERR_BAD_T;
+    if (prefix_len < 0 || prefix_len > kMostKeys) return WHT_ERR_BAD_T;
     if (T == 0) return WHT_OK;
     if (!q || !k_cache || !v_cache || !out || !kv_lens || (table_width > 0 && !page_table) || (prefix_len > 0 && !prefix_pages))
         return WHT_ERR_NULL;

@@ -47,20 +47,38 @@ def test_a_selection_of_no_tokens_needs_nothing(plan, width, select, hq, dtype):
     assert plan("select", width, select, 0, 0, 1, hq, 8, 128, 64, dtype)["bytes"] == 0
 
 
-def test_tokens_without_a_sequence_are_refused():
-    """Through the C entry points, which check before any CUDA work: T = 3 tokens, B = 0 sequences, q_start given."""
-    import ctypes
+@pytest.fixture(scope="module")
+def lib():
     from paper_2603_08343_b200 import build
     build.build()
     from paper_2603_08343_b200 import binding
-    lib = binding.lib()
+    return binding.lib()
+
+
+@pytest.fixture(scope="module")
+def p():
+    import ctypes
     buf = (ctypes.c_char * 4096)()
-    p = ctypes.c_void_p((ctypes.addressof(buf) + 15) & ~15)
+    yield ctypes.c_void_p((ctypes.addressof(buf) + 15) & ~15)
+    del buf
+
+
+def test_tokens_without_a_sequence_are_refused(lib, p):
+    """Through the C entry points, which check before any CUDA work: T = 3 tokens, B = 0 sequences, q_start given."""
     rest = (3, 0, 1, 4, 2, 64, 9, 16, 0.125, BF16, p, 0, None)
     assert lib.wht_attn_prefix(p, 256, 64, p, p, p, 100, p, 4, p, p, p, *rest) == -3
     assert lib.wht_attn_select(p, 256, 64, p, p, p, p, 4, p, p, 2, p, p, *rest) == -3
     assert lib.wht_attn_prefix_workspace_bytes(1000, 64, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
     assert lib.wht_attn_select_workspace_bytes(64, 32, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_lists_whose_rounded_length_passes_31_bits_are_refused(lib, p, page):
+    """A list's keys are rounded up to whole tiles of 128 in 31 bits."""
+    for width in ((2 ** 31 - 1) // page, (2 ** 31 - 128) // page):
+        rest = (3, 3, 1, 4, 2, 64, 9, page, 0.125, BF16, p, 0, None)
+        assert lib.wht_attn_prefix(p, 256, 64, p, p, p, 100, p, width, p, None, p, *rest) == -2
+    assert lib.wht_attn_prefix(p, 256, 64, p, p, p, 2 ** 31 - 128, p, 4, p, None, p, *rest) == -3
 
 
 @pytest.mark.parametrize("width,select,T,B,max_q,hkv,page", [
