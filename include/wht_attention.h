@@ -49,7 +49,7 @@ extern "C" {
  *            between heads (multiples of 16 bytes; channels contiguous), so slices of a fused projection serve as they are.
  *   q_out    [T x Hq x D] contiguous; may be q itself if that is contiguous; NULL exactly when q is NULL.
  *   slots    [T] int64: page * page_size + place in the page; negative = the token is padding, its keys and
- *            values are dropped (its query is still rotated).
+ *            values are dropped (its query is still rotated; without q its position is not looked at).
  *   positions[T] int32, cos_table, sin_table [max_pos x rot/2] float32.  rot: how many leading channels turn,
  *            a multiple of 16 up to D; 0 = none (positions and tables may be NULL).  Channel pairs are (i, i + rot/2), or
  *            (2i, 2i + 1) with interleaved = 1.  Each product and each sum is rounded to fp32 on its own and the

@@ -81,12 +81,12 @@ struct RowItem {
     }
 };
 
-__device__ __forceinline__ int64_t append_position(const AppendParams& p, int64_t t) {
-    if (p.rot == 0) return 0;
-    const int64_t pos = __ldg(p.positions + t);
-    if (pos < 0 || pos >= p.max_pos) {
+__device__ __forceinline__ int append_position(const AppendParams& p, int64_t t) { return p.rot == 0 ? 0 : __ldg(p.positions + t); }
+// The position held to the table: for tokens that use theirs (a dropped token's may be anything).
+__device__ __forceinline__ int checked_position(const AppendParams& p, int pos) {
+    if (p.rot != 0 && (pos < 0 || pos >= p.max_pos)) {
         attn_report(kAttnErrIndex);
-        return pos < 0 ? 0 : p.max_pos - 1;
+        return pos < 0 ? 0 : static_cast<int>(p.max_pos - 1);
     }
     return pos;
 }
@@ -165,8 +165,7 @@ __device__ __forceinline__ void append_flat(const AppendParams& p, int block) {
     int64_t step, out_step;  // from head to head
     int heads;
     bool turns = it.angle >= 0;
-    int64_t pos = 0;
-    if (turns) pos = append_position(p, t);
+    int pos = turns ? append_position(p, t) : 0;  // (asked for beside the slot, checked once it is known to be used)
     if (rb < p.q_blocks) {
         const int h = rb * HB;
         heads = p.hq - h;
@@ -206,9 +205,10 @@ __device__ __forceinline__ void append_flat(const AppendParams& p, int block) {
         }
         return;
     }
+    pos = checked_position(p, pos);
     float c[8], s[8];
-    load8(p.cos_t + pos * (p.rot / 2) + it.angle, c);
-    load8(p.sin_t + pos * (p.rot / 2) + it.angle, s);
+    load8(p.cos_t + static_cast<int64_t>(pos) * (p.rot / 2) + it.angle, c);
+    load8(p.sin_t + static_cast<int64_t>(pos) * (p.rot / 2) + it.angle, s);
 #pragma unroll
     for (int i = 0; i < HB; ++i) {
         if (i < heads) {
@@ -344,8 +344,11 @@ __device__ __forceinline__ void append_pages(const AppendParams& p, int64_t tile
             int pos = 0;
             if (c0 + lane < p.T) {
                 const int64_t s = append_slot(p, c0 + lane);
-                pos = static_cast<int>(append_position(p, c0 + lane));
-                if (s >= 0 && (s >> p.page_shift) == run_page) place = static_cast<int>(s & ((1 << p.page_shift) - 1));
+                pos = append_position(p, c0 + lane);
+                if (s >= 0 && (s >> p.page_shift) == run_page) {
+                    place = static_cast<int>(s & ((1 << p.page_shift) - 1));
+                    pos = checked_position(p, pos);
+                }
             }
             const unsigned other = ~__ballot_sync(kFullMask, place >= 0);
             const int n = other ? __ffs(other) - 1 : 32;

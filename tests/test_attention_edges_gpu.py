@@ -248,3 +248,31 @@ def test_a_step_past_the_example_s_pages_is_reported(select):
         block.step(torch.ones(3, rows, 64, dtype=BF16, device="cuda"), select)
     with pytest.raises(ValueError):
         E.Block(2, 4, 2, 64, 16, 16, 0)
+
+
+# ---------------------------------------------------------------- append: what is not used is not checked
+
+@pytest.mark.parametrize("with_summary", [False, True])
+def test_positions_of_dropped_tokens_are_not_looked_at(A, with_summary):
+    """Padding tokens without a query use no position: one outside the table is no error."""
+    g = _gen(50)
+    T, page = 70, 16
+    kc, vc = (torch.zeros(9, 2, page, 64, dtype=BF16, device="cuda") for _ in range(2))
+    k, v = _randn((T, 2, 64), BF16, g), _randn((T, 2, 64), BF16, g)
+    slots = torch.arange(T) + 5
+    positions = torch.arange(T, dtype=torch.int32)
+    slots[[0, 33]], positions[[0, 33]] = -1, torch.tensor([-1, 10 ** 6], dtype=torch.int32)
+    slots[40:], positions[40:] = -1, 10 ** 9
+    cos, sin = R.inverse_frequencies(64, 50)
+    summary = torch.zeros(9, 2, 2, 64, dtype=torch.int8, device="cuda") if with_summary else None
+    if with_summary:   # (a dropped token inside a page's tokens would part them)
+        slots[33], positions[33] = 38, 33
+    kd, vd, sd, pd, cd, nd = _cuda(k, v, slots, positions, cos, sin)
+    A.kv_append(kd, vd, kc, vc, sd, positions=pd, cos=cd, sin=nd, summary=summary, summary_scale=torch.full((2,), 30.0, device="cuda"))
+    A.device_status()
+    live = slots >= 0
+    want_k, want_v = torch.zeros(9 * page, 2, 64, dtype=BF16), torch.zeros(9 * page, 2, 64, dtype=BF16)
+    want_k[slots[live]] = R.rotate32(k[live], positions[live], cos, sin, False)
+    want_v[slots[live]] = v[live]
+    assert torch.equal(kc.cpu().transpose(1, 2).reshape(9 * page, 2, 64), want_k)
+    assert torch.equal(vc.cpu().transpose(1, 2).reshape(9 * page, 2, 64), want_v)
