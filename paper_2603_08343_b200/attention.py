@@ -13,7 +13,8 @@ Caches are [num_pages, kv_heads, page, head_dim] (page 16, 32, 64 or 128; head_d
 [tokens, heads, head_dim]; all tensors of a call are bf16 or all are fp32.  Query, key and value tensors may be slices of a
 fused projection.  Argument checks and marshalling only: the work is the library's (include/wht_attention.h).
 The calls run on the current stream of the tensors' device, or on `stream`; they do not synchronise.  Page
-numbers, slots and lengths are checked on the device: device_status() reports what was out of range.
+numbers, slots and lengths are checked on the device: device_status() reports what was out of range.  There is no backward:
+tensors that require a gradient are refused unless gradients are off.
 """
 from __future__ import annotations
 

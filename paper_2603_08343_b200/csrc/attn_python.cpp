@@ -4,6 +4,7 @@
 // checking and boxing some thirty arguments in Python takes 12 to 15.  This module does the same checks on the
 // tensors' metadata directly and calls the C ABI (about 2 us on top of the launches).  It computes nothing.
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -49,6 +50,12 @@ int64_t integer(PyObject* o, const char* name) {
     return v;
 }
 
+// These operators have no backward: rather than cut a graph without a word they refuse to be part of one.
+void no_gradient(const at::Tensor& t, const char* name) {
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        refuse(std::string(name) + " requires a gradient and the serving attention has no backward: call it under torch.no_grad() or detach it");
+}
+
 struct Caches {
     const at::Tensor &k, &v;
     at::Device device;
@@ -65,6 +72,8 @@ Caches caches(PyObject* ko, PyObject* vo) {
         refuse("unsupported storage types: the caches must both be bf16 or both fp32");
     if (!k.is_cuda() || v.device() != k.device() || !k.is_contiguous() || !v.is_contiguous())
         refuse("caches must be contiguous tensors on one CUDA device");
+    no_gradient(k, "k_cache");
+    no_gradient(v, "v_cache");
     if (k.device().index() != c10::cuda::current_device()) refuse("all tensors must live on the current CUDA device");
     const int64_t page = k.size(2), dim = k.size(3);
     if ((page != 16 && page != 32 && page != 64 && page != 128) || (dim != 64 && dim != 96 && dim != 128))
@@ -78,6 +87,7 @@ void rows(const at::Tensor& t, const char* name, int64_t tokens, int64_t heads, 
         refuse(std::string(name) + " must be [tokens, heads, head_dim] and match the other tensors, got " + shape_of(t));
     if (t.scalar_type() != c.type || t.device() != c.device) refuse(std::string(name) + " must have the caches' type and device");
     if (t.stride(2) != 1) refuse(std::string(name) + " must have contiguous channels");
+    no_gradient(t, name);
 }
 
 void* vec(const at::Tensor& t, const char* name, at::ScalarType type, const Caches& c, at::IntArrayRef sizes) {

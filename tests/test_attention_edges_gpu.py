@@ -276,3 +276,23 @@ def test_positions_of_dropped_tokens_are_not_looked_at(A, with_summary):
     want_v[slots[live]] = v[live]
     assert torch.equal(kc.cpu().transpose(1, 2).reshape(9 * page, 2, 64), want_k)
     assert torch.equal(vc.cpu().transpose(1, 2).reshape(9 * page, 2, 64), want_v)
+
+
+# ---------------------------------------------------------------- refusals of the Python calls
+
+def test_tensors_that_want_a_gradient_are_refused(A):
+    """These operators have no backward: a graph that would end in them without a word is refused, and not under no_grad."""
+    kc, summary = torch.zeros(4, 1, 16, 64, dtype=BF16, device="cuda"), torch.zeros(4, 1, 2, 64, dtype=torch.int8, device="cuda")
+    k, slots = torch.zeros(1, 1, 64, dtype=BF16, device="cuda"), torch.tensor([0], device="cuda")
+    wants = torch.zeros(1, 1, 64, dtype=BF16, device="cuda", requires_grad=True)
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), _ints(1)
+    calls = [lambda x: A.kv_append(x, k, kc, kc, slots), lambda x: A.kv_append(k, x, kc, kc, slots),
+             lambda x: A.kv_append(k, k, kc, kc, slots, q=x), lambda x: A.shared_prefix_attention(x, kc, kc, None, 0, table, lens),
+             lambda x: A.selected_page_attention(x, kc, kc, summary, table, lens, 1)]
+    for call in calls:
+        with pytest.raises(ValueError, match="no_grad"):
+            call(wants)
+        with torch.no_grad():
+            call(wants)
+        call(wants.detach())
+    A.device_status()
