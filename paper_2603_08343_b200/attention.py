@@ -47,6 +47,8 @@ _native = _load()
 def _raw(stream):
     if stream is None:
         return None
+    if stream.device_index != torch.cuda.current_device():
+        raise ValueError(f"the stream is on device {stream.device_index}, the call on the current one, {torch.cuda.current_device()}")
     # outputs and scratch come from the current stream's pool, which may hand out memory that stream still uses
     stream.wait_stream(torch.cuda.current_stream())
     return stream.cuda_stream

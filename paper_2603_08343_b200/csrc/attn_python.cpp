@@ -223,11 +223,13 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
             sum_p = vec(*summary, "summary", at::kChar, c, {c.pages, c.hkv, 2, c.dim});
             scale_p = vec(required(a[11], "summary_scale"), "summary_scale", at::kFloat, c, {c.hkv});
         }
+        const int interleaved = PyObject_IsTrue(a[12]);
+        if (interleaved < 0) return nullptr;  // (no truth value: the error is set)
         const int rc = wht_kv_append(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), q_p, q_st, q_sh, out_p,
                                      static_cast<const int64_t*>(slots), static_cast<const int32_t*>(pos_p), static_cast<const float*>(cos_p),
                                      static_cast<const float*>(sin_p), c.k.data_ptr(), c.v.data_ptr(), static_cast<int8_t*>(sum_p),
                                      static_cast<const float*>(scale_p), tokens, static_cast<int32_t>(hq), static_cast<int32_t>(c.hkv),
-                                     static_cast<int32_t>(c.dim), static_cast<int32_t>(rot), PyObject_IsTrue(a[12]), max_pos, c.pages,
+                                     static_cast<int32_t>(c.dim), static_cast<int32_t>(rot), interleaved, max_pos, c.pages,
                                      static_cast<int32_t>(c.page), c.code, s.raw);
         if (!ok(rc, "wht_kv_append")) return nullptr;
         if (!q) return keep(Py_None);

@@ -296,3 +296,20 @@ def test_tensors_that_want_a_gradient_are_refused(A):
             call(wants)
         call(wants.detach())
     A.device_status()
+
+
+def test_arguments_of_no_use_are_refused(A):
+    """A truth value that is none, and a stream of another device (a stand-in: nothing is launched on it)."""
+    kc = torch.zeros(4, 1, 16, 64, dtype=BF16, device="cuda")
+    k, slots = torch.zeros(1, 1, 64, dtype=BF16, device="cuda"), torch.tensor([0], device="cuda")
+    with pytest.raises(RuntimeError):
+        A.kv_append(k, k, kc, kc, slots, interleaved=torch.tensor([True, False]))
+
+    class Elsewhere:
+        device_index, cuda_stream = torch.cuda.current_device() + 1, 0
+    with pytest.raises(ValueError, match="device"):
+        A.kv_append(k, k, kc, kc, slots, stream=Elsewhere())
+    side = torch.cuda.Stream()
+    A.kv_append(k, k, kc, kc, slots, stream=side)
+    A.kv_append(k, k, kc, kc, slots, stream=torch.cuda.default_stream())
+    A.device_status()
