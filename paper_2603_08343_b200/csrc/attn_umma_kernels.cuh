@@ -404,7 +404,8 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         if (c0 + c >= valid) x[c] = 0xff800000u;  // -infinity
                 }
             };
-            // the half's weights against the reference, as bf16 pairs; returns their sum
+            // The half's weights against the reference, as bf16 pairs.  Returns the sum of what the pairs hold: the result is then a mean with
+            // just these weights, and that of a row with one key that counts is its value.
             uint32_t y[32];
             auto weights = [&]() {
                 const uint64_t off2 = pair(-m * sl, -m * sl), sl2 = pair(sl, sl);
@@ -419,8 +420,9 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         unpair(fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), sl2, off2), a, b);
                         a = exp2_fast(a);
                         b = exp2_fast(b);
-                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(a, b));
-                        y[(c + e) / 2] = pack_bf16x2(a, b);
+                        const uint32_t ab = pack_bf16x2(a, b);
+                        y[(c + e) / 2] = ab;
+                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(__uint_as_float(ab << 16), __uint_as_float(ab & 0xffff0000u)));
                     }
                 }
                 float a, b;

@@ -313,3 +313,40 @@ def test_arguments_of_no_use_are_refused(A):
     A.kv_append(k, k, kc, kc, slots, stream=side)
     A.kv_append(k, k, kc, kc, slots, stream=torch.cuda.default_stream())
     A.device_status()
+
+
+# ---------------------------------------------------------------- scores of any size
+
+@pytest.mark.parametrize("size", [30.0, 300.0])
+@pytest.mark.parametrize("B,d,page,grow", [(9, 128, 16, True), (70, 128, 64, False), (70, 96, 32, True), (300, 64, 16, True)])
+def test_scores_of_any_size(A, size, B, d, page, grow):
+    """Queries and keys of up to some hundreds, scores of up to 10^6: one key takes all the weight (the two best scores of a row lie much
+    further apart than fp32 rounds them), so the result is its value, within one rounding."""
+    prefix = 700
+    g = _gen(70 + B)
+    c = _paged(70 + B, B, 2, 1, d, page, BF16, prefix, 0, [1] * B, 0, [1 + i % 3 for i in range(B)])
+    scale_of_page = torch.ones(c["kc"].shape[0], 1, 1, 1)
+    if grow:   # the best key of a row comes late: its reference moves again and again
+        scale_of_page[c["pre"].long()] = (0.1 + torch.arange(len(c["pre"])) / len(c["pre"])).reshape(-1, 1, 1, 1)
+    kc = (torch.randn(c["kc"].shape, generator=g) * size * scale_of_page).to(BF16)
+    kc[c["kc"].isnan()] = float("nan")
+    qs = (torch.randn(c["q"].shape, generator=g) * size).to(BF16)
+    want = torch.zeros(c["q"].shape, dtype=torch.float64)
+    clear = torch.zeros(B, 2, dtype=torch.bool)
+    for b in range(B):
+        n = int(c["lens"][b])
+        k = torch.cat([R.keys_of(kc, c["pre"], 0, prefix), R.keys_of(kc, c["table"][b], 0, n)]).double()
+        v = torch.cat([R.keys_of(c["vc"], c["pre"], 0, prefix), R.keys_of(c["vc"], c["table"][b], 0, n)]).double()
+        s = qs[b].double() @ k.T * d ** -0.5
+        top = s.topk(2).values
+        # fp32: a sum of d products (2^-22 of their magnitudes at most) and a few roundings of the score; 40 = more than any weight that counts
+        slack = 2.0 ** -20 * (qs[b].double().abs() @ k.abs().T * d ** -0.5).max(-1).values
+        clear[b] = top[:, 0] - top[:, 1] > 40 + 2 * slack
+        want[b] = v[s.argmax(-1)]
+    if size >= 300:
+        assert clear.float().mean() > 0.9
+    qd, kd, vd, pre, table, lens = _cuda(qs, kc, c["vc"], c["pre"], c["table"], c["lens"])
+    got = A.shared_prefix_attention(qd, kd, vd, pre, prefix, table, lens).cpu()
+    assert torch.isfinite(got).all()
+    assert torch.equal(got[clear].double(), want[clear])
+    A.device_status()
