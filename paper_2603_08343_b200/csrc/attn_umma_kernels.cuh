@@ -12,7 +12,7 @@
 //   S = Q K^T            into tensor memory (128 lanes x 128 fp32 columns)
 //   P = exp2(S - m)      read by the row's threads, rounded to bf16 and written over S
 //   O += P V             P from tensor memory, V from shared memory, O stays in tensor memory (D columns)
-// The reference maximum m of a row is that of its first tile and moves only when a half's 64 weights add up to more than 2^14: large
+// The reference maximum m of a row is that of its first tile and moves (once a step at most) only when a half's 64 weights add up to more than 2^14: large
 // weights are as exact in bf16 and fp32 as weights up to 1, O, which sits in tensor memory, is rescaled a few times per row at
 // most instead of once per tile, and the common path needs no maximum at all.  The weights are one bf16 term here: a second
 // product for the second term would cost what the first does.  With 128 rows or fewer both tiles hold the SAME rows and take alternate
@@ -39,6 +39,9 @@ namespace wht {
 constexpr int kUmmaAttnThreads = 576;
 constexpr int kStartBarrier = 3;  // (0: the whole block at its end; 1, 2: the two tiles' votes)
 constexpr float kLargestHalf = 16384.0f;  // 2^14: sum of 64 weights from which a row's reference maximum moves
+// 2^29: largest reference in the exponents.  Beyond, a row's two largest scores, if they differ at all, are 32 or more apart in its units: all weight
+// is the largest one's under any scale that leaves them so, and with this one the rounding of m * scale (below 64) cannot take it to 0.
+constexpr float kLargestReference = 536870912.0f;
 
 template <int D>
 struct UmmaAttnGeo {
@@ -390,6 +393,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
         const float sl = p.scale_log2;
         const int n = steps_of(w);
         float m = 0.0f, l = 0.0f;                // reference maximum in units of the raw scores (the same in both halves), this half's sum
+        float slope = sl;                        // the row's scale in the exponents
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int valid = min(128, key1 - key0 - key_tile(w, i) * 128) - h * 64;  // of this half's 64 keys
@@ -404,11 +408,12 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         if (c0 + c >= valid) x[c] = 0xff800000u;  // -infinity
                 }
             };
-            // The half's weights against the reference, as bf16 pairs.  Returns the sum of what the pairs hold: the result is then a mean with
-            // just these weights, and that of a row with one key that counts is its value.
+            // The half's weights against the reference m slope, rounded up so that none passes 1, as bf16 pairs.  Returns the sum of what the
+            // pairs hold: the result is then a mean with just these weights, and that of a row with one key that counts is its value.
             uint32_t y[32];
             auto weights = [&]() {
-                const uint64_t off2 = pair(-m * sl, -m * sl), sl2 = pair(sl, sl);
+                const float off = -__fmul_ru(m, slope);
+                const uint64_t off2 = pair(off, off), sl2 = pair(slope, slope);
                 uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < 64; c += 32) {
@@ -430,13 +435,14 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                 return a + b;
             };
             // One vote of both halves' warps per round: nobody stores weights before all agree on the reference.  (A wait that ran
-            // out also ends up here, so that all leave together: the votes are barriers.)
+            // out also ends up here, so that all leave together: the votes are barriers.)  The reference moves once per step at most: it is
+            // the tile's maximum then, whatever the sum that follows.
             float sum = 0.0f;
-            bool unset = i == 0, gave_up = false;
-            for (;;) {
-                if (!unset) {
+            bool gave_up = false;
+            for (bool moved = false;; moved = true) {
+                if (i > 0 || moved) {
                     sum = weights();
-                    if (!tile_any(w, !ok || sum > kLargestHalf)) break;
+                    if (!tile_any(w, !ok || (!moved && sum > kLargestHalf))) break;
                 }
                 // The first tile, and later the rare case that some row's weights have grown past kLargestHalf: the row's
                 // reference moves to the maximum of the tile.  O and l follow; its products so far are waited for.
@@ -449,7 +455,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                     for (int e = 0; e < 32; e += 2) top = max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                 }
                 maxima[h * 128 + lane_row] = top;
-                if (i > 0) ok = warp_poll_or_abort(o_done + w, static_cast<uint32_t>(i - 1) & 1u, abort_flag);
+                if (i > 0) ok = ok && warp_poll_or_abort(o_done + w, static_cast<uint32_t>(i - 1) & 1u, abort_flag);
                 if ((gave_up = tile_any(w, !ok))) break;
                 top = fmaxf(maxima[lane_row], maxima[128 + lane_row]);
                 if (i == 0) {
@@ -457,7 +463,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                 } else {
                     tc_fence_after();
                     const bool higher = top > m;
-                    const float f = higher ? exp2_fast((m - top) * sl) : 1.0f;
+                    const float f = higher ? exp2_fast(__fsub_rn(__fmul_ru(m, sl), __fmul_ru(top, sl))) : 1.0f;
                     if (higher) m = top;
                     l *= f;
 #pragma unroll 1
@@ -471,8 +477,8 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
                         tmem_st16(o_cols + c, z);
                     }
                 }
-                unset = false;  // (the next vote also says that everyone has read the maxima)
-            }
+                slope = fabsf(m * sl) > kLargestReference ? kLargestReference / fabsf(m) : sl;
+            }                   // (the next vote also says that everyone has read the maxima)
             if (gave_up) break;
             l += sum;
             tmem_st16(p_cols, y);
@@ -519,7 +525,7 @@ attn_umma_prefix_kernel(const UmmaAttnParams up, const __grid_constant__ CUtenso
             }
             if (h == 1) maxima[128 + lane_row] = l;
             tile_any(w, false);
-            if (h == 0 && r < rows) p.part_ml[slot] = n > 0 ? make_float2(m * sl, l + maxima[128 + lane_row]) : make_float2(-INFINITY, 0.0f);
+            if (h == 0 && r < rows) p.part_ml[slot] = n > 0 ? make_float2(__fmul_ru(m, sl), l + maxima[128 + lane_row]) : make_float2(-INFINITY, 0.0f);
         }
         tc_fence_before();
     }

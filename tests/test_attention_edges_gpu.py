@@ -317,10 +317,10 @@ def test_arguments_of_no_use_are_refused(A):
 
 # ---------------------------------------------------------------- scores of any size
 
-@pytest.mark.parametrize("size", [30.0, 300.0])
+@pytest.mark.parametrize("size", [30.0, 300.0, 5e3, 2e4, 1e6])
 @pytest.mark.parametrize("B,d,page,grow", [(9, 128, 16, True), (70, 128, 64, False), (70, 96, 32, True), (300, 64, 16, True)])
 def test_scores_of_any_size(A, size, B, d, page, grow):
-    """Queries and keys of up to some hundreds, scores of up to 10^6: one key takes all the weight (the two best scores of a row lie much
+    """Queries and keys of up to 10^6, scores of up to 10^13: one key takes all the weight (the two best scores of a row lie much
     further apart than fp32 rounds them), so the result is its value, within one rounding."""
     prefix = 700
     g = _gen(70 + B)
