@@ -20,18 +20,22 @@
  *   - Storage types: WHT_F32 (queries, keys, values, caches, outputs float32) or WHT_BF16 (all bfloat16).
  *     Scores, softmax statistics and sums are fp32 whatever the type.  On bf16 tensors the softmax weights
  *     enter the product with the values as two bf16 terms (16 significant bits; the tensor core takes both operands
- *     in one type), as one where many rows share a long prefix and that product is what the time goes to; on
- *     fp32 tensors both products take each operand as two terms, about 21 significant bits.
+ *     in one type), as one (8 bits, the softmax sum taken of the same terms) where 33 and more rows of a key head share a prefix
+ *     of 256 and more keys and that product is what the time goes to; on fp32 tensors both products take each operand as
+ *     two terms, about 21 significant bits.
  *   - Caches: k_cache, v_cache [num_pages x Hkv x page x D], contiguous.  page in {16, 32, 64, 128}; D in
  *     {64, 96, 128}; Hq = G*Hkv query heads, head h reading key head h / G, G <= 64.
  *   - Slots, page numbers, lengths and query offsets are read on the device.  A page number or slot outside
- *     the cache, or a position outside the table, is never used as an address: the access is skipped (or the
- *     position clamped) and the device status word is set; wht_attn_device_status() then reports
- *     WHT_ERR_DEVICE_INDEX, and the call's outputs are invalid.
+ *     the cache, or a position outside the table, is never used as an address: nothing is written for such a slot, page 0
+ *     is read for such a page, positions, lengths and offsets are clamped, and the device status word is set;
+ *     wht_attn_device_status() then reports WHT_ERR_DEVICE_INDEX, and the call's outputs are invalid.
+ *   - Lengths being on the device, the division of the work goes by table_width: with a table much wider than its sequences
+ *     a call is right but can take several times as long as with one that is as wide as the longest of them.
  *   - Rows that see no key (a length of zero) get zeros.  So do rows of tokens that no sequence covers (before q_start[0], from q_start[B]
  *     on); these are reported like an index out of range, and their entries of pages_out are -1.
  *   - Cache entries that a row does not see (beyond a sequence's length, at the places of later tokens) never
- *     reach its result, whatever they hold (NaN and infinities included).
+ *     reach its result, whatever they hold (NaN and infinities included).  An infinity among the values that it does see
+ *     may come out as NaN, in that channel.
  *   - In a -DWHT_DEBUG build these calls run as they do otherwise, without guarded buffers.
  */
 #ifndef WHT_ATTENTION_H_
@@ -74,7 +78,8 @@ int wht_kv_append(const void* k, int64_t k_stride_t, int64_t k_stride_h,
  * keys have been appended before):   out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j.
  *   q [T x Hq x D] with strides as above; out [T x Hq x D] contiguous (rows of the head mixing).
  *   prefix_pages [ceil(prefix_len / page)] int32 (may be NULL when prefix_len == 0).
- *   page_table   [B x table_width] int32: a sequence's own pages in order; kv_lens [B] int32: its own keys.
+ *   page_table   [B x table_width] int32: a sequence's own pages in order (at most 2^31 - 256 keys; entries beyond its length are
+ *                not looked at); kv_lens [B] int32: its own keys.  B >= 1 where T > 0.
  *   q_start      [B + 1] int32: sequence b's tokens are q_start[b] .. q_start[b+1]-1, at most max_q_len of them;
  *                NULL = one token per sequence (T == B).
  *   workspace    at least wht_attn_prefix_workspace_bytes(...) bytes of device memory, 16-byte aligned.
@@ -98,6 +103,7 @@ size_t wht_attn_prefix_workspace_bytes(int64_t prefix_len, int32_t table_width, 
  * -- an upper bound of what any key of the page can score, in whole numbers, so that the selection does not depend on
  * the order of a sum.  The G heads of a key head read the same pages.  Keys after p are not seen.
  *   select       pages per query and key head, 1 .. 1024.
+ *   table_width  up to 49152 (a row's scores are picked from in shared memory).
  *   pages_out    [T x Hkv x select] int32: the pages read (index in the sequence), ascending, then -1.
  *   workspace    at least wht_attn_select_workspace_bytes(...) bytes.
  */
@@ -113,7 +119,7 @@ size_t wht_attn_select_workspace_bytes(int32_t table_width, int32_t select, int6
 /*
  * Synchronises with the current device and reports what the kernels of this header recorded since the last query:
  * WHT_ERR_DEVICE_INDEX (a page number, slot, position or length out of range), WHT_ERR_DEVICE_WAIT (a bounded wait
- * expired; never expected), else WHT_OK.  Clears the record.
+ * expired; never expected), else WHT_OK.  Clears the record (what another thread's call records meanwhile may go with it).
  */
 int wht_attn_device_status(void);
 

@@ -74,8 +74,9 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len: int, 
     sequence's own keys up to itself.  Returns [tokens, heads, head_dim].
 
     page_table [batch, pages] int32 and kv_lens [batch] int32: the sequences' own pages and how many keys they hold, this
-    call's tokens included.  q_start [batch + 1] int32: sequence b's tokens are q_start[b]..q_start[b+1]-1, at most
-    max_q_len; None = one token per sequence.  prefix_len = 0 gives plain attention over the own pages.  scale: 1/sqrt(head_dim).
+    call's tokens included (the work is divided by the table's width: one about as wide as the longest sequence is fastest).
+    q_start [batch + 1] int32: sequence b's tokens are q_start[b]..q_start[b+1]-1, at most max_q_len; None = one token per
+    sequence.  prefix_len = 0 gives plain attention over the own pages.  scale: 1/sqrt(head_dim).
     """
     return _native.shared_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, kv_lens, q_start, max_q_len, scale,
                                            out, _raw(stream))
@@ -85,11 +86,13 @@ def selected_page_attention(q, k_cache, v_cache, summary, page_table, kv_lens, s
                             scale: float | None = None, out=None, pages_out=None, stream=None):
     """Attention of each query to its own page and to the `select` - 1 earlier pages of its sequence that score highest
     by their summaries (the summary that kv_append keeps).  Returns (out [tokens, heads, head_dim], pages [tokens, kv_heads,
-    select] int32: the pages read, ascending, then -1).  The other arguments are those of shared_prefix_attention."""
+    select] int32: the pages read, ascending, then -1).  Tables of up to 49152 pages; the other arguments are those of
+    shared_prefix_attention."""
     return _native.selected_page_attention(q, k_cache, v_cache, summary, page_table, kv_lens, select, q_start, max_q_len, scale, out,
                                            pages_out, _raw(stream))
 
 
 def device_status() -> None:
-    """Synchronises and raises WhtError if a kernel met an index out of range since the last query."""
+    """Synchronises with the device, all streams, and raises WhtError if a kernel met an index out of range (a token that no
+    sequence covers included) since the last query."""
     _B._check(_B.lib().wht_attn_device_status(), "wht_attn_device_status")

@@ -18,8 +18,7 @@ void launch(const AppendParams& p, int blocks, cudaStream_t s) {
 }
 }  // namespace
 
-int launch_append(AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s) {
-    (void)sms;
+int launch_append(AppendParams& p, int dtype, bool interleaved, cudaStream_t s) {
     const int hb = dtype == WHT_F32 ? kHeadBlock<float> : kHeadBlock<__nv_bfloat16>;
     p.q_blocks = static_cast<int>(ceil_div(p.hq, hb));
     p.kv_blocks = static_cast<int>(ceil_div(p.hkv, hb));

@@ -17,7 +17,7 @@ namespace wht_host {
 // attn_tma.cu: the caches as [num_pages * Hkv * page] rows of d channels, copied in boxes of box_rows rows by 128 bytes
 int cache_maps(CUtensorMap* k_map, CUtensorMap* v_map, const wht::AttnParams& p, int d, int dtype, int box_rows);
 // attn_append.cu
-int launch_append(wht::AppendParams& p, int dtype, bool interleaved, int sms, cudaStream_t s);
+int launch_append(wht::AppendParams& p, int dtype, bool interleaved, cudaStream_t s);
 // attn_paged.cuh, instantiated per storage type in attn_paged_bf16.cu and attn_paged_f32.cu
 // overlapped: launched right after the tensor-core kernel of the prefix, to run next to it
 template <typename T> int launch_attn_prefix(const wht::AttnParams& p, int d, int dev, bool overlapped, cudaStream_t s);

@@ -74,8 +74,8 @@ constexpr int kUmmaMinKeys = 256;
 // 54 GB/s per SM for the own pages next to it, 6000 GB/s alone.  256 x 32768 keys with 150 keys of their own, 32 heads: 3 ranges
 // (96 blocks) are best, 4 (128 blocks) take 5% more, 9 (two waves) 12% more; 64 x 8192 with 256, 8 key heads: 10 ranges 40.5 us,
 // 11 42.7 us, 15 45 us, 18 53 us.
-inline int umma_splits_for(int64_t units, int64_t tiles, int tiles_per_step, int32_t D, double own_bytes, int sms) {
-    const double tile_us = (D > 64 ? 2.2 : 1.8) * tiles_per_step;
+inline int umma_splits_for(int64_t units, int64_t tiles, int32_t D, double own_bytes, int sms) {
+    const double tile_us = D > 64 ? 2.2 : 1.8;
     double best_us = 1e30;
     int best = 1;
     for (int64_t n = 1; n <= tiles && n <= 64; ++n) {
@@ -127,7 +127,7 @@ inline PrefixPlan plan_prefix(int64_t prefix_len, int32_t table_width, int64_t T
         // (the lengths are on the device: sequences are taken to fill 0.6 of their tables' width)
         const double own_bytes = 0.6 * B * Hkv * static_cast<double>(table_width) * page * D * 4.0;
         f.umma_splits = umma_splits_for(static_cast<int64_t>(Hkv) * f.umma_row_blocks, div_up(prefix_len, f.same_rows ? 256 : 128),
-                                        1, D, own_bytes, sms);
+                                        D, own_bytes, sms);
     } else if (prefix_len > 0) {
         f.prefix_nr = row_tiles(T * group);
         f.prefix_row_tiles = static_cast<int>(div_up(T * group, 8 * f.prefix_nr));

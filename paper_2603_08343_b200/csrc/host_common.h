@@ -124,7 +124,9 @@ int resident_ctas(Kernel kernel, int threads, size_t smem, int dev, int* cache) 
 
 // Launch with the programmatic-stream-serialization attribute: the kernel may be scheduled
 // while its predecessor in the stream drains.  Only for kernels that call
-// grid_dependency_wait() before they touch global memory.
+// grid_dependency_wait() before they touch what the predecessor writes, or memory that it reads
+// and they write; one that shares nothing with it (the own pages beside the tcgen05 prefix kernel) calls
+// it before it ends, so that what follows can wait for it alone.
 template <typename... KArgs, typename... Args>
 void launch_overlapped(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t s, Args... args) {
     cudaLaunchConfig_t cfg = {};

@@ -90,7 +90,7 @@ int wht_kv_append(const void* k, int64_t k_stride_t, int64_t k_stride_h, const v
     p.summary = summary; p.summary_scale = summary_scale;
     p.T = T; p.max_pos = max_pos; p.num_slots = num_pages * page;
     p.hq = q ? Hq : 0; p.hkv = Hkv; p.d = D; p.rot = rot; p.page_shift = page_shift_of(page);
-    return launch_append(p, dtype, interleaved != 0, sms, static_cast<cudaStream_t>(stream));
+    return launch_append(p, dtype, interleaved != 0, static_cast<cudaStream_t>(stream));
 }
 
 size_t wht_attn_prefix_workspace_bytes(int64_t prefix_len, int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq,
