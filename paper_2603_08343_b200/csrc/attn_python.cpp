@@ -104,7 +104,7 @@ at::Tensor output(const at::Tensor* given, const at::Tensor& like, const char* n
 }
 
 // Scratch of one call, taken from the caching allocator on the current stream.  When the call runs on another
-// stream, the allocator is told, so that the block is not handed out before that stream is done with it.
+// stream, the allocator is told of all its tensors, so that no block is handed out before that stream is done with it.
 struct Scratch {
     c10::DataPtr mem;
     void* take(size_t bytes) {
@@ -126,6 +126,12 @@ struct Stream {
         if (other && p) c10::cuda::CUDACachingAllocator::recordStream(p, c10::cuda::getStreamFromExternal(raw, device));
     }
     void uses(const at::Tensor& t) const { uses(t.storage().data_ptr()); }
+    // every tensor among the arguments of a call
+    void uses(PyObject* const* a, Py_ssize_t n) const {
+        if (!other) return;
+        for (Py_ssize_t i = 0; i < n; ++i)
+            if (THPVariable_Check(a[i])) uses(THPVariable_Unpack(a[i]));
+    }
 };
 
 struct Batch {
@@ -231,6 +237,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                      static_cast<const float*>(scale_p), tokens, static_cast<int32_t>(hq), static_cast<int32_t>(c.hkv),
                                      static_cast<int32_t>(c.dim), static_cast<int32_t>(rot), interleaved, max_pos, c.pages,
                                      static_cast<int32_t>(c.page), c.code, s.raw);
+        s.uses(a, n);
         if (!ok(rc, "wht_kv_append")) return nullptr;
         if (!q) return keep(Py_None);
         if (q_given) return keep(a[9]);
@@ -280,6 +287,7 @@ PyObject* shared_prefix_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                        static_cast<const int32_t*>(b.start), out.data_ptr(), tokens, i32(b.size), i32(max_q), i32(hq), i32(c.hkv),
                                        i32(c.dim), c.pages, i32(c.page), scale, c.code, ws, need, s.raw);
         s.uses(work.mem);
+        s.uses(a, n);
         if (!ok(rc, "wht_attn_prefix")) return nullptr;
         if (given) return keep(a[10]);
         s.uses(out);
@@ -316,6 +324,7 @@ PyObject* selected_page_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                        static_cast<const int32_t*>(b.start), i32(select), out.data_ptr(), static_cast<int32_t*>(pages_p), tokens,
                                        i32(b.size), i32(max_q), i32(hq), i32(c.hkv), i32(c.dim), c.pages, i32(c.page), scale, c.code, ws, need, s.raw);
         s.uses(work.mem);
+        s.uses(a, n);
         if (!ok(rc, "wht_attn_select")) return nullptr;
         if (!given) s.uses(out);
         if (!given_pages) s.uses(pages);

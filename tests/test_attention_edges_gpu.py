@@ -350,3 +350,36 @@ def test_scores_of_any_size(A, size, B, d, page, grow):
     assert torch.isfinite(got).all()
     assert torch.equal(got[clear].double(), want[clear])
     A.device_status()
+
+
+# ---------------------------------------------------------------- calls on another stream
+
+def test_inputs_freed_after_a_call_on_another_stream(A):
+    """The call waits on a side stream behind some tenths of a second; its inputs are dropped at once and their memory asked for again."""
+    c = _paged(90, 4, 4, 2, 64, 16, BF16, 300, 0, [1] * 4, 0, [40, 3, 17, 60])
+    args = _cuda(c["q"], c["kc"], c["vc"], c["pre"], c["table"], c["lens"])
+    want = A.shared_prefix_attention(args[0], args[1], args[2], args[3], 300, args[4], args[5])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+    got = A.shared_prefix_attention(args[0], args[1], args[2], args[3], 300, args[4], args[5], stream=side)
+    shapes = [(a.shape, a.dtype) for a in args]
+    del args
+    junk = [torch.zeros(s, dtype=t, device="cuda") for s, t in shapes for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    del junk
+    # and an append: rows and slots
+    kc, vc = (torch.zeros(4, 2, 16, 64, dtype=BF16, device="cuda") for _ in range(2))
+    k, slots = _cuda(_randn((50, 2, 64), BF16, _gen(91)), torch.arange(50))
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+    A.kv_append(k, k, kc, vc, slots, stream=side)
+    keep = k.cpu()
+    del k, slots
+    junk = [torch.zeros(50, 2, 64, dtype=BF16, device="cuda") for _ in range(4)] + [torch.zeros(50, dtype=torch.int64, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(kc.cpu().transpose(1, 2).reshape(64, 2, 64)[:50], keep)
+    del junk
+    A.device_status()
