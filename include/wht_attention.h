@@ -50,7 +50,7 @@ extern "C" {
 /*
  * Append with the position rotation.
  *   k, v     [T x Hkv x D], q [T x Hq x D] or NULL: element strides *_stride_t between tokens and *_stride_h
- *            between heads (multiples of 16 bytes; channels contiguous), so slices of a fused projection serve as they are.
+ *            between heads (multiples of 16 bytes where there are several; channels contiguous), so slices of a fused projection serve as they are.
  *   q_out    [T x Hq x D] contiguous; may be q itself if that is contiguous; NULL exactly when q is NULL.
  *   slots    [T] int64: page * page_size + place in the page; negative = the token is padding, its keys and
  *            values are dropped (its query is still rotated; without q its position is not looked at).

@@ -20,10 +20,10 @@ size_t elem(int dtype) { return dtype == WHT_F32 ? 4 : 2; }
 
 int page_shift_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : -1; }
 
-// Rows of a strided [T x H x D] tensor start on 16-byte boundaries.
-bool strides_ok(const void* p, int64_t st, int64_t sh, int dtype) {
+// Rows of a strided [T x H x D] tensor start on 16-byte boundaries.  (The stride of a dimension of one may be anything.)
+bool strides_ok(const void* p, int64_t st, int64_t sh, int64_t T, int32_t H, int dtype) {
     const int64_t unit = 16 / static_cast<int64_t>(elem(dtype));
-    return aligned16(p) && st % unit == 0 && sh % unit == 0;
+    return aligned16(p) && (T == 1 || st % unit == 0) && (H == 1 || sh % unit == 0);
 }
 
 int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages, int32_t page, int dtype) {
@@ -73,8 +73,8 @@ int wht_kv_append(const void* k, int64_t k_stride_t, int64_t k_stride_h, const v
     if (!k || !v || !slots || !k_cache || !v_cache) return WHT_ERR_NULL;
     if (rot > 0 && (!positions || !cos_table || !sin_table)) return WHT_ERR_NULL;
     if (summary && !summary_scale) return WHT_ERR_NULL;
-    if (!strides_ok(k, k_stride_t, k_stride_h, dtype) || !strides_ok(v, v_stride_t, v_stride_h, dtype) ||
-        (q && !strides_ok(q, q_stride_t, q_stride_h, dtype)) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache) ||
+    if (!strides_ok(k, k_stride_t, k_stride_h, T, Hkv, dtype) || !strides_ok(v, v_stride_t, v_stride_h, T, Hkv, dtype) ||
+        (q && !strides_ok(q, q_stride_t, q_stride_h, T, Hq, dtype)) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache) ||
         !aligned16(summary) || !aligned16(cos_table) || !aligned16(sin_table))
         return WHT_ERR_MISALIGNED;
     int dev = 0, sms = 0;
@@ -116,7 +116,7 @@ int wht_attn_prefix(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     if (T == 0) return WHT_OK;
     if (!q || !k_cache || !v_cache || !out || !kv_lens || (table_width > 0 && !page_table) || (prefix_len > 0 && !prefix_pages))
         return WHT_ERR_NULL;
-    if (!strides_ok(q, q_stride_t, q_stride_h, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
+    if (!strides_ok(q, q_stride_t, q_stride_h, T, Hq, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
         return WHT_ERR_MISALIGNED;
     int dev = 0, sms = 0;
     rc = device_info(&dev, &sms);
@@ -171,7 +171,7 @@ int wht_attn_select(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     if (T == 0) return WHT_OK;
     if (num_pages < 1) return WHT_ERR_BAD_DIM;
     if (!q || !k_cache || !v_cache || !summary || !out || !pages_out || !kv_lens || (table_width > 0 && !page_table)) return WHT_ERR_NULL;
-    if (!strides_ok(q, q_stride_t, q_stride_h, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(summary) ||
+    if (!strides_ok(q, q_stride_t, q_stride_h, T, Hq, dtype) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(summary) ||
         !aligned16(out) || !aligned16(workspace))
         return WHT_ERR_MISALIGNED;
     int dev = 0, sms = 0;

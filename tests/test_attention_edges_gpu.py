@@ -383,3 +383,19 @@ def test_inputs_freed_after_a_call_on_another_stream(A):
     assert torch.equal(kc.cpu().transpose(1, 2).reshape(64, 2, 64)[:50], keep)
     del junk
     A.device_status()
+
+
+def test_strides_of_dimensions_of_one(A):
+    """[tokens, 1, head_dim] out of [tokens, head_dim, 1], and one token out of a tensor with odd strides."""
+    c = _paged(95, 3, 1, 1, 64, 16, BF16, 40, 0, [1] * 3, 0, [4, 30, 17])
+    q, kc, vc, pre, table, lens = _cuda(c["q"], c["kc"], c["vc"], c["pre"], c["table"], c["lens"])
+    odd = q.reshape(3, 64, 1).transpose(1, 2)
+    assert odd.stride(1) == 1
+    want = A.shared_prefix_attention(q, kc, vc, pre, 40, table, lens)
+    assert torch.equal(A.shared_prefix_attention(odd, kc, vc, pre, 40, table, lens), want)
+    one = torch.as_strided(q, (1, 1, 64), (3, 5, 1))
+    assert torch.equal(A.shared_prefix_attention(one, kc, vc, pre, 40, table[:1], lens[:1]), want[:1])
+    cache = torch.zeros_like(kc)
+    A.kv_append(one, one, cache, cache, torch.tensor([17], device="cuda"), q=odd[:1])
+    assert torch.equal(cache[1, 0, 1], q[0, 0])
+    A.device_status()

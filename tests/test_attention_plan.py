@@ -72,6 +72,21 @@ def test_tokens_without_a_sequence_are_refused(lib, p):
     assert lib.wht_attn_select_workspace_bytes(64, 32, 3, 0, 1, 4, 2, 64, 16, BF16) == 0
 
 
+def test_the_stride_of_a_dimension_of_one_may_be_anything(lib, p):
+    """(Without a GPU the calls then end at the device query.)"""
+    def append(T, hkv, st, sh):
+        return lib.wht_kv_append(p, st, sh, p, st, sh, p, st, sh, p, p, p, p, p, p, p, None, None, T, hkv, hkv, 64, 64, 0, 10, 5, 16, BF16, None)
+
+    def prefix(T, hkv, st, sh):
+        return lib.wht_attn_prefix(p, st, sh, p, p, p, 100, p, 4, p, None, p, T, T, 1, hkv, hkv, 64, 9, 16, 0.125, BF16, p, 0, None)
+    import torch
+    if not torch.cuda.is_available():   # (host memory stands in for tensors: nothing may run)
+        for call in (append, prefix):
+            assert call(1, 2, 3, 64) != -5 and call(3, 1, 64, 1) != -5 and call(1, 1, 7, 9) != -5
+    for call in (append, prefix):
+        assert call(2, 1, 100, 1) == -5 and call(1, 2, 128, 9) == -5
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 def test_lists_whose_rounded_length_passes_31_bits_are_refused(lib, p, page):
     """A list's keys are rounded up to whole tiles of 128 in 31 bits."""
