@@ -23,8 +23,9 @@
 // blocks where there are too few units to fill the machine (attn_join_kernel adds those parts up).
 //
 // Measured, bf16, D = 128: 64 sequences x 2048 keys, 8 key heads of 4 rows 82.6 us (6.5 TB/s, all that memory gives); 256 x 150 keys, 32 heads
-// 103 us (6.1 TB/s).  Pages out of the L2 cache (2048 prompt tokens of 4 key heads with 16 pages of 64 each) 275 us for 4.3 GB, 15.6 TB/s: there
-// eight warps an SM waited for the results of products (371 us), twelve wait for the cache.
+// 103 us (6.1 TB/s).  Pages out of the L2 cache (2048 prompt tokens of 4 key heads with 16 pages of 64 each) 275 us for 4.3 GB, 15.6 TB/s: with
+// eight warps an SM (371 us) and with twelve the first wait is for the results of products and the arithmetic between them (3.0 of 6.5 clocks a warp
+// and instruction); the cache is at 57 %, the tensor pipe at 34 %.
 //
 // fp32 tensors: both operands of each product are split in two tf32 terms (three products; what is dropped is below 2^-21
 // relative), contraction indices paired so that a thread's two values are neighbours.  Bound by those products: 64 x 2048 keys as above

@@ -12,7 +12,7 @@
 // shuffles and joins the page's stored summary once.  No atomics: a run has one owner.
 //
 // Measured: 16384 tokens, 16 heads of 64 and as many key heads, bf16: 38 us without summaries (5.4 TB/s), 54 with them, where a warp's walk
-// of its run is a chain of waits; one token 6.1 us, 256 tokens of 32 heads 5.1 us, both the launch; 3001 fp32 tokens 22.8 us.
+// of its run is a chain of waits; one token 6.1 us, 256 tokens of 32 heads 4.9 us, both the launch; 3001 fp32 tokens 22.5 us.
 // Slower: a team of warps per run (57), the ranges in a second kernel that reads the stored keys back (55, and 16.5 instead of 7.5
 // for 256 tokens).
 #pragma once
