@@ -92,6 +92,51 @@ def selected_page_attention(q, k_cache, v_cache, summary, page_table, kv_lens, s
                                            pages_out, _raw(stream))
 
 
+def cache4(num_pages: int, kv_heads: int, page: int, head_dim: int, device="cuda"):
+    """An empty cache in 4 bits: uint8 [num_pages, kv_heads, page / 16, 16 * head_dim + 128] (keys and values of 16 keys in one piece)."""
+    if page not in PAGE_SIZES or head_dim not in HEAD_DIMS:
+        raise ValueError(f"page must be one of {PAGE_SIZES} and head_dim one of {HEAD_DIMS}, got {page} and {head_dim}")
+    return torch.zeros(num_pages, kv_heads, page // 16, 16 * head_dim + 128, dtype=torch.uint8, device=device)
+
+
+def kv_append4(k, v, cache, slots, positions=None, cos=None, sin=None, q=None, q_out=None, interleaved: bool = False, stream=None):
+    """kv_append for a cache in 4 bits (`cache4`): rotates queries and keys, writes each key and value row of a head as 4-bit codes with a
+    least value and a step; returns the rotated queries, or None without q.  Arguments as for kv_append."""
+    return _native.kv_append4(k, v, cache, slots, positions, cos, sin, q, q_out, interleaved, _raw(stream))
+
+
+def kv_read4(cache, slots, dtype=torch.float32, stream=None):
+    """The keys and values that the cache holds at `slots` [n] int64: two tensors [n, kv_heads, head_dim] of `dtype` (fp32 or bf16);
+    zeros where a slot is negative."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
+    return _native.kv_read4(cache, slots, dtype == torch.float32, _raw(stream))
+
+
+def paged_attention4(q, cache, page_table, kv_lens, q_start=None, max_q_len: int = 1, scale: float | None = None, out=None, weights=None,
+                     weights_out=None, stream=None):
+    """Attention of each token to its sequence's keys up to itself, over a cache in 4 bits.  Returns [tokens, heads, head_dim].
+
+    page_table, kv_lens, q_start, max_q_len, scale as for shared_prefix_attention (a table wider than its sequences costs nothing here).
+    weights [batch, kv_heads, table pages * page] fp32: what each key has received so far.  With it (or with weights_out alone, starting from nothing)
+    the call returns (out, weights_out): weights_out (allocated if None; may be weights itself) = weights + the softmax weights of
+    this call's tokens, summed over them and the heads of each key head; 0 from a sequence's length on.
+    """
+    return _native.paged_attention4(q, cache, page_table, kv_lens, q_start, max_q_len, scale, out, weights, weights_out, _raw(stream))
+
+
+def kv_evict4(cache, page_table, kv_lens, weights, out_table, budget: int, keep_first: int = 0, keep_last: int = 0, stream=None):
+    """Keeps min(length, budget) keys of each sequence and key head (the first `keep_first`, the last `keep_last`, and the heaviest
+    of those between by `weights`, ties to the lowest) and moves them, in their order, into the pages of out_table [batch, pages]
+    int32, which no sequence of the call reads.  The pages of page_table are left as they are.
+
+    weights [batch, kv_heads, table pages * page] fp32, as paged_attention4 keeps it.  Returns (kv_lens [batch] int32, kept [batch, kv_heads,
+    budget] int32: which keys stayed, ascending, then -1; weights [batch, kv_heads, out_table pages * page]).  A key's position is in its
+    rotation: new tokens go on counting from the length before the eviction.
+    """
+    return _native.kv_evict4(cache, page_table, kv_lens, weights, out_table, budget, keep_first, keep_last, _raw(stream))
+
+
 def device_status() -> None:
     """Synchronises with the device, all streams, and raises WhtError if a kernel met an index out of range (a token that no
     sequence covers included) since the last query."""

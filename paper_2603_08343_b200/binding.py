@@ -35,6 +35,9 @@ ATTENTION_EXPORTS = (
     "wht_attn_select", "wht_attn_select_workspace_bytes", "wht_attn_device_status",
 )
 
+# the 4-bit cache of include/wht_cache4.h (wrapped by attention.py)
+CACHE4_EXPORTS = ("wht_kv_append4", "wht_kv_read4", "wht_attn_paged4", "wht_attn_paged4_workspace_bytes", "wht_kv_evict4")
+
 
 class WhtError(RuntimeError):
     def __init__(self, status: int, where: str):
@@ -97,7 +100,15 @@ def _load(path: str | None = None) -> ctypes.CDLL:
     lib.wht_attn_select_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32, i32, i32, i32, ci]
     lib.wht_attn_select_workspace_bytes.restype = sz
     lib.wht_attn_device_status.argtypes = []
-    for name in EXPORTS + ATTENTION_EXPORTS:
+    lib.wht_kv_append4.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp,
+                                   i64, i32, i32, i32, i32, i32, i64, i64, i32, ci, vp]
+    lib.wht_kv_read4.argtypes = [vp, vp, vp, vp, i64, i32, i32, i64, i32, ci, vp]
+    lib.wht_attn_paged4.argtypes = [vp, i64, i64, vp, vp, i32, vp, vp, vp, vp, vp,
+                                    i64, i32, i32, i32, i32, i32, i64, i32, f32, ci, vp, sz, vp]
+    lib.wht_attn_paged4_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, i32, i32, ci, i32]
+    lib.wht_attn_paged4_workspace_bytes.restype = sz
+    lib.wht_kv_evict4.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, i64, i32, i32, i32, i32, vp]
+    for name in EXPORTS + ATTENTION_EXPORTS + CACHE4_EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int or fn.restype is None:
             fn.restype = ctypes.c_int

@@ -14,7 +14,7 @@
 #include <cmath>
 #include <string>
 
-#include "../../include/wht_attention.h"
+#include "../../include/wht_cache4.h"
 
 namespace {
 
@@ -79,6 +79,20 @@ Caches caches(PyObject* ko, PyObject* vo) {
     if ((page != 16 && page != 32 && page != 64 && page != 128) || (dim != 64 && dim != 96 && dim != 128))
         refuse("page must be 16, 32, 64 or 128 and head_dim 64, 96 or 128, got " + std::to_string(page) + " and " + std::to_string(dim));
     return {k, v, k.device(), type, type == at::kFloat ? WHT_F32 : WHT_BF16, k.size(0), k.size(1), page, dim};
+}
+
+// The 4-bit cache, which has no type of its own: the call's type is that of `like`.
+Caches cache4(PyObject* o, at::ScalarType type, const char* what) {
+    const at::Tensor& t = required(o, "cache");
+    if (t.dim() != 4 || t.scalar_type() != at::kByte) refuse("cache must be a uint8 tensor [num_pages, kv_heads, page / 16, 16 * head_dim + 128]");
+    if (type != at::kBFloat16 && type != at::kFloat) refuse(std::string("unsupported storage type: ") + what + " must be bf16 or fp32");
+    if (!t.is_cuda() || !t.is_contiguous()) refuse("cache must be a contiguous tensor on a CUDA device");
+    if (t.device().index() != c10::cuda::current_device()) refuse("all tensors must live on the current CUDA device");
+    const int64_t page = t.size(2) * 16, dim = (t.size(3) - 128) / 16;
+    if ((page != 16 && page != 32 && page != 64 && page != 128) || (dim != 64 && dim != 96 && dim != 128) || dim * 16 + 128 != t.size(3))
+        refuse("cache must be [num_pages, kv_heads, page / 16, 16 * head_dim + 128] with pages of 16, 32, 64 or 128 keys and head_dim 64, 96 or 128, got " +
+               shape_of(t));
+    return {t, t, t.device(), type, type == at::kFloat ? WHT_F32 : WHT_BF16, t.size(0), t.size(1), page, dim};
 }
 
 // A [tokens, heads, head_dim] tensor with any token and head strides; heads or tokens < 0: any.
@@ -185,6 +199,26 @@ bool count(Py_ssize_t got, Py_ssize_t want) {
     return false;
 }
 
+struct Rotation {
+    int64_t rot = 0, max_pos = 0;
+    const int32_t* positions = nullptr;
+    const float *cos = nullptr, *sin = nullptr;
+};
+Rotation rotation(PyObject* pos_o, PyObject* cos_o, PyObject* sin_o, int64_t tokens, const Caches& c) {
+    const at::Tensor *pos = tensor(pos_o, "positions"), *cos = tensor(cos_o, "cos"), *sin = tensor(sin_o, "sin");
+    Rotation r;
+    if (!pos && !cos && !sin) return r;
+    if (!pos || !cos || !sin || cos->dim() != 2) refuse("positions, cos and sin [max_pos, rot/2] come together");
+    r.max_pos = cos->size(0);
+    r.rot = 2 * cos->size(1);
+    if (r.rot % 16 || r.rot > c.dim || r.max_pos < 1)
+        refuse("rot = " + std::to_string(r.rot) + " must be a multiple of 16 up to head_dim, with at least one position");
+    r.cos = static_cast<const float*>(vec(*cos, "cos", at::kFloat, c, {r.max_pos, r.rot / 2}));
+    r.sin = static_cast<const float*>(vec(*sin, "sin", at::kFloat, c, {r.max_pos, r.rot / 2}));
+    r.positions = static_cast<const int32_t*>(vec(*pos, "positions", at::kInt, c, {tokens}));
+    return r;
+}
+
 // kv_append(k, v, k_cache, v_cache, slots, positions, cos, sin, q, q_out, summary, summary_scale, interleaved, stream)
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!count(n, 14)) return nullptr;
@@ -195,19 +229,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t tokens = k.size(0);
         rows(v, "v", tokens, c.hkv, c);
         void* slots = vec(required(a[4], "slots"), "slots", at::kLong, c, {tokens});
-        const at::Tensor *pos = tensor(a[5], "positions"), *cos = tensor(a[6], "cos"), *sin = tensor(a[7], "sin");
-        int64_t rot = 0, max_pos = 0;
-        void *pos_p = nullptr, *cos_p = nullptr, *sin_p = nullptr;
-        if (pos || cos || sin) {
-            if (!pos || !cos || !sin || cos->dim() != 2) refuse("positions, cos and sin [max_pos, rot/2] come together");
-            max_pos = cos->size(0);
-            rot = 2 * cos->size(1);
-            if (rot % 16 || rot > c.dim || max_pos < 1)
-                refuse("rot = " + std::to_string(rot) + " must be a multiple of 16 up to head_dim, with at least one position");
-            cos_p = vec(*cos, "cos", at::kFloat, c, {max_pos, rot / 2});
-            sin_p = vec(*sin, "sin", at::kFloat, c, {max_pos, rot / 2});
-            pos_p = vec(*pos, "positions", at::kInt, c, {tokens});
-        }
+        const Rotation r = rotation(a[5], a[6], a[7], tokens, c);
         const at::Tensor *q = tensor(a[8], "q"), *q_given = tensor(a[9], "q_out");
         const Stream s(a[13], c);
         at::Tensor q_out;
@@ -232,10 +254,9 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int interleaved = PyObject_IsTrue(a[12]);
         if (interleaved < 0) return nullptr;  // (no truth value: the error is set)
         const int rc = wht_kv_append(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), q_p, q_st, q_sh, out_p,
-                                     static_cast<const int64_t*>(slots), static_cast<const int32_t*>(pos_p), static_cast<const float*>(cos_p),
-                                     static_cast<const float*>(sin_p), c.k.data_ptr(), c.v.data_ptr(), static_cast<int8_t*>(sum_p),
+                                     static_cast<const int64_t*>(slots), r.positions, r.cos, r.sin, c.k.data_ptr(), c.v.data_ptr(), static_cast<int8_t*>(sum_p),
                                      static_cast<const float*>(scale_p), tokens, static_cast<int32_t>(hq), static_cast<int32_t>(c.hkv),
-                                     static_cast<int32_t>(c.dim), static_cast<int32_t>(rot), interleaved, max_pos, c.pages,
+                                     static_cast<int32_t>(c.dim), static_cast<int32_t>(r.rot), interleaved, r.max_pos, c.pages,
                                      static_cast<int32_t>(c.page), c.code, s.raw);
         s.uses(a, n);
         if (!ok(rc, "wht_kv_append")) return nullptr;
@@ -336,6 +357,166 @@ PyObject* selected_page_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// kv_append4(k, v, cache, slots, positions, cos, sin, q, q_out, interleaved, stream)
+PyObject* kv_append4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 11)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor &k = required(a[0], "k"), &v = required(a[1], "v");
+        const Caches c = cache4(a[2], k.scalar_type(), "k");
+        rows(k, "k", -1, c.hkv, c);
+        const int64_t tokens = k.size(0);
+        rows(v, "v", tokens, c.hkv, c);
+        void* slots = vec(required(a[3], "slots"), "slots", at::kLong, c, {tokens});
+        const Rotation r = rotation(a[4], a[5], a[6], tokens, c);
+        const at::Tensor *q = tensor(a[7], "q"), *q_given = tensor(a[8], "q_out");
+        const Stream s(a[10], c);
+        at::Tensor q_out;
+        int64_t hq = c.hkv, q_st = 0, q_sh = 0;
+        void *q_p = nullptr, *out_p = nullptr;
+        if (q) {
+            rows(*q, "q", tokens, -1, c);
+            hq = q->size(1);
+            q_st = q->stride(0);
+            q_sh = q->stride(1);
+            q_out = output(q_given, *q, "q_out", c);
+            q_p = q->data_ptr();
+            out_p = q_out.data_ptr();
+        } else if (q_given) {
+            refuse("q_out without q");
+        }
+        const int interleaved = PyObject_IsTrue(a[9]);
+        if (interleaved < 0) return nullptr;  // (no truth value: the error is set)
+        const int rc = wht_kv_append4(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), q_p, q_st, q_sh, out_p,
+                                      static_cast<const int64_t*>(slots), r.positions, r.cos, r.sin, c.k.data_ptr(), tokens,
+                                      static_cast<int32_t>(hq), static_cast<int32_t>(c.hkv), static_cast<int32_t>(c.dim),
+                                      static_cast<int32_t>(r.rot), interleaved, r.max_pos, c.pages, static_cast<int32_t>(c.page), c.code, s.raw);
+        s.uses(a, n);
+        if (!ok(rc, "wht_kv_append4")) return nullptr;
+        if (!q) return keep(Py_None);
+        if (q_given) return keep(a[8]);
+        s.uses(q_out);
+        return THPVariable_Wrap(std::move(q_out));
+    });
+}
+
+// kv_read4(cache, slots, fp32, stream)
+PyObject* kv_read4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 4)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const int fp32 = PyObject_IsTrue(a[2]);
+        if (fp32 < 0) return nullptr;
+        const Caches c = cache4(a[0], fp32 ? at::kFloat : at::kBFloat16, "dtype");
+        const at::Tensor& slots = required(a[1], "slots");
+        const int64_t count = slots.numel();
+        void* slots_p = vec(slots, "slots", at::kLong, c, {count});
+        const Stream s(a[3], c);
+        at::Tensor k = at::detail::empty_cuda({count, c.hkv, c.dim}, c.type, c.device, std::nullopt);
+        at::Tensor v = at::detail::empty_cuda({count, c.hkv, c.dim}, c.type, c.device, std::nullopt);
+        const int rc = wht_kv_read4(c.k.data_ptr(), static_cast<const int64_t*>(slots_p), k.data_ptr(), v.data_ptr(), count,
+                                    static_cast<int32_t>(c.hkv), static_cast<int32_t>(c.dim), c.pages, static_cast<int32_t>(c.page), c.code, s.raw);
+        s.uses(a, n);
+        if (!ok(rc, "wht_kv_read4")) return nullptr;
+        s.uses(k);
+        s.uses(v);
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(std::move(k)));
+        PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(std::move(v)));
+        return r;
+    });
+}
+
+// paged_attention4(q, cache, page_table, kv_lens, q_start, max_q_len, scale, out, weights, weights_out, stream)
+PyObject* paged_attention4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 11)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor& q = required(a[0], "q");
+        const Caches c = cache4(a[1], q.scalar_type(), "q");
+        rows(q, "q", -1, -1, c);
+        const int64_t tokens = q.size(0), hq = q.size(1), max_q = integer(a[5], "max_q_len");
+        const Batch b = batch(a[2], a[3], a[4], tokens, max_q, c);
+        const float scale = scale_of(a[6], c);
+        const Stream s(a[10], c);
+        const at::Tensor *given = tensor(a[7], "out"), *weights = tensor(a[8], "weights"), *given_weights = tensor(a[9], "weights_out");
+        at::Tensor out = output(given, q, "out", c), received;
+        const int64_t width = b.width * c.page;
+        void *weights_p = nullptr, *received_p = nullptr;
+        if (weights) {
+            no_gradient(*weights, "weights");
+            weights_p = vec(*weights, "weights", at::kFloat, c, {b.size, c.hkv, width});
+        }
+        if (weights || given_weights) {
+            if (given_weights) received = *given_weights;
+            else received = at::detail::empty_cuda({b.size, c.hkv, width}, at::kFloat, c.device, std::nullopt);
+            no_gradient(received, "weights_out");
+            received_p = vec(received, "weights_out", at::kFloat, c, {b.size, c.hkv, width});
+        }
+        const bool weigh = weights || given_weights;
+        const auto i32 = [](int64_t v) { return static_cast<int32_t>(v > 0x7fffffff ? 0x7fffffff : v); };
+        const size_t need = wht_attn_paged4_workspace_bytes(i32(b.width), tokens, i32(b.size), i32(max_q), i32(hq), i32(c.hkv), i32(c.dim),
+                                                            i32(c.page), c.code, weigh);
+        Scratch work;
+        void* ws = work.take(need);
+        const int rc = wht_attn_paged4(q.data_ptr(), q.stride(0), q.stride(1), c.k.data_ptr(), static_cast<const int32_t*>(b.table), i32(b.width),
+                                       static_cast<const int32_t*>(b.lens), static_cast<const int32_t*>(b.start), out.data_ptr(),
+                                       static_cast<const float*>(weights_p), static_cast<float*>(received_p), tokens, i32(b.size), i32(max_q),
+                                       i32(hq), i32(c.hkv), i32(c.dim), c.pages, i32(c.page), scale, c.code, ws, need, s.raw);
+        s.uses(work.mem);
+        s.uses(a, n);
+        if (!ok(rc, "wht_attn_paged4")) return nullptr;
+        if (!given) s.uses(out);
+        PyObject* result = given ? keep(a[7]) : THPVariable_Wrap(std::move(out));
+        if (!result || !weigh) return result;
+        if (!given_weights) s.uses(received);
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, result);
+        PyTuple_SET_ITEM(r, 1, given_weights ? keep(a[9]) : THPVariable_Wrap(std::move(received)));
+        return r;
+    });
+}
+
+// kv_evict4(cache, page_table, kv_lens, weights, out_table, budget, keep_first, keep_last, stream)
+PyObject* kv_evict4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 9)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const Caches c = cache4(a[0], at::kBFloat16, "cache");
+        const at::Tensor &table = required(a[1], "page_table"), &out_table = required(a[4], "out_table"), &weights = required(a[3], "weights");
+        if (table.dim() != 2 || out_table.dim() != 2) refuse("page_table and out_table must be [batch, pages]");
+        const int64_t batch = table.size(0), width = table.size(1), out_width = out_table.size(1);
+        const int64_t budget = integer(a[5], "budget"), first = integer(a[6], "keep_first"), last = integer(a[7], "keep_last");
+        if (first < 0 || last < 0 || first > budget || last > budget - first || budget < 1 || budget > out_width * c.page || budget > 0x7fffffff)
+            refuse("keep_first " + std::to_string(first) + " and keep_last " + std::to_string(last) + " must fit the budget of " + std::to_string(budget) +
+                   " keys, and that the " + std::to_string(out_width) + " pages of out_table");
+        void* table_p = vec(table, "page_table", at::kInt, c, {batch, width});
+        void* out_p = vec(out_table, "out_table", at::kInt, c, {batch, out_width});
+        void* lens_p = vec(required(a[2], "kv_lens"), "kv_lens", at::kInt, c, {batch});
+        void* weights_p = vec(weights, "weights", at::kFloat, c, {batch, c.hkv, width * c.page});
+        no_gradient(weights, "weights");
+        const Stream s(a[8], c);
+        at::Tensor lens = at::detail::empty_cuda({batch}, at::kInt, c.device, std::nullopt);
+        at::Tensor kept = at::detail::empty_cuda({batch, c.hkv, budget}, at::kInt, c.device, std::nullopt);
+        at::Tensor received = at::detail::empty_cuda({batch, c.hkv, out_width * c.page}, at::kFloat, c.device, std::nullopt);
+        const auto i32 = [](int64_t v) { return static_cast<int32_t>(v > 0x7fffffff ? 0x7fffffff : v); };
+        const int rc = wht_kv_evict4(c.k.data_ptr(), static_cast<const int32_t*>(table_p), i32(width), static_cast<const int32_t*>(lens_p),
+                                     static_cast<const float*>(weights_p), static_cast<const int32_t*>(out_p), i32(out_width),
+                                     static_cast<int32_t*>(lens.data_ptr()), static_cast<float*>(received.data_ptr()),
+                                     static_cast<int32_t*>(kept.data_ptr()), i32(batch), i32(c.hkv), i32(c.dim), c.pages, i32(c.page), i32(budget),
+                                     i32(first), i32(last), s.raw);
+        s.uses(a, n);
+        if (!ok(rc, "wht_kv_evict4")) return nullptr;
+        s.uses(lens);
+        s.uses(kept);
+        s.uses(received);
+        PyObject* r = PyTuple_New(3);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(std::move(lens)));
+        PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(std::move(kept)));
+        PyTuple_SET_ITEM(r, 2, THPVariable_Wrap(std::move(received)));
+        return r;
+    });
+}
+
 PyObject* raise_with(PyObject*, PyObject* f) {
     Py_INCREF(f);
     Py_XDECREF(g_raise);
@@ -347,6 +528,10 @@ PyMethodDef methods[] = {
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_append)), METH_FASTCALL, nullptr},
     {"shared_prefix_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(shared_prefix_attention)), METH_FASTCALL, nullptr},
     {"selected_page_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(selected_page_attention)), METH_FASTCALL, nullptr},
+    {"kv_append4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_append4)), METH_FASTCALL, nullptr},
+    {"kv_read4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_read4)), METH_FASTCALL, nullptr},
+    {"paged_attention4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_attention4)), METH_FASTCALL, nullptr},
+    {"kv_evict4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_evict4)), METH_FASTCALL, nullptr},
     {"raise_with", raise_with, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -1,0 +1,241 @@
+// Eviction: for each sequence and key head the first keys, the last ones and the heaviest of those between move into pages of their own.
+//
+// Two kernels.  The choice, a block per sequence and key head: the weights as ordered whole numbers; the spare-th largest found by
+// three counts of 11, 11 and 10 bits; then one walk in the order of the keys that lists what stays (above the threshold, or at it while there is
+// room: the lowest first).  Its bytes are 4 a key; what it costs is the chain of counts and scans.
+// The move, a warp per 16 kept keys: a tile is gathered from wherever its rows lie and written as one piece, 2 (D + 8) bytes a row
+// moved, which memory bounds.
+#pragma once
+#include "cache4_common.cuh"
+
+namespace wht {
+
+struct Evict4Params {
+    AttnParams a;            // page_table, table_width, kv_lens, B, hkv, page_shift, num_pages
+    unsigned char* cache;
+    const int32_t* out_table;
+    int out_width;           // pages
+    const float* weights;    // [B x Hkv x table_width * page]
+    float* weights_out;      // [B x Hkv x out_width * page]
+    int32_t *lens_out, *kept;  // [B], [B x Hkv x budget]
+    int budget, first, last;
+    int cached;              // weights that the block's shared memory holds
+};
+
+constexpr int kEvictBins = 2048;
+
+// Ordered whole numbers: NaN the least, -0 as 0.
+__device__ __forceinline__ unsigned ordered4(float x) {
+    if (x != x) return 0;
+    const unsigned u = __float_as_uint(x == 0.0f ? 0.0f : x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Sum over the threads before this one, and over all (two barriers).
+template <int THREADS>
+__device__ __forceinline__ unsigned block_scan4(unsigned x, unsigned* warp_sums, unsigned& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned upto = x;
+#pragma unroll
+    for (int i = 1; i < 32; i <<= 1) {
+        const unsigned y = __shfl_up_sync(kFullMask, upto, i);
+        if (lane >= i) upto += y;
+    }
+    if (lane == 31) warp_sums[warp] = upto;
+    __syncthreads();
+    unsigned before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const unsigned s = warp_sums[w];
+        before += w < warp ? s : 0;
+        all += s;
+    }
+    __syncthreads();
+    return before + upto - x;
+}
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+kv_evict4_choose_kernel(const Evict4Params p) {
+    extern __shared__ __align__(16) unsigned evict_smem[];
+    __shared__ unsigned bins[kEvictBins];
+    __shared__ unsigned warp_sums[THREADS / 32];
+    __shared__ unsigned found[2];                      // the bin that holds the threshold, and what is above it
+    const AttnParams& a = p.a;
+    const int tid = threadIdx.x;
+    const int b = blockIdx.x / a.hkv, head = blockIdx.x % a.hkv;
+    grid_launch_dependents();
+    const int n = attn_length(a, b);
+    const int keep = min(p.budget, n);
+    const int from = min(p.first, n), to = max(from, n - p.last);    // the keys between, of which the heaviest `spare` stay
+    const int spare = keep - (n - (to - from));
+    const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
+    const float* w = p.weights + (static_cast<int64_t>(b) * a.hkv + head) * width;
+    const int64_t out_keys = static_cast<int64_t>(p.out_width) << a.page_shift;
+    float* w_out = p.weights_out + (static_cast<int64_t>(b) * a.hkv + head) * out_keys;
+    int32_t* kept = p.kept + (static_cast<int64_t>(b) * a.hkv + head) * p.budget;
+    if (head == 0 && tid == 0) p.lens_out[b] = keep;
+
+    const bool chosen = spare < to - from;             // (otherwise all stay)
+    const bool in_smem = chosen && n <= p.cached;
+    unsigned threshold = 0, ties = 0;
+    if (chosen && spare > 0) {
+        unsigned known = 0, mask = 0, want = static_cast<unsigned>(spare);
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, count = pass == 2 ? 1024 : 2048;
+            for (int i = tid; i < count; i += THREADS) bins[i] = 0;
+            __syncthreads();
+            for (int i = from + tid; i < to; i += THREADS) {
+                unsigned key;
+                if (pass == 0 || !in_smem) {
+                    key = ordered4(__ldg(w + i));
+                    if (in_smem) evict_smem[i] = key;
+                } else {
+                    key = evict_smem[i];
+                }
+                if ((key & mask) == known) atomicAdd(&bins[(key >> shift) & (count - 1)], 1u);
+            }
+            __syncthreads();
+            // from the top: each thread four (two) bins, the highest first
+            const int per = count / THREADS, top = count - 1 - tid * per;
+            unsigned mine = 0;
+            for (int i = 0; i < per; ++i) mine += bins[top - i];
+            unsigned all;
+            unsigned above = block_scan4<THREADS>(mine, warp_sums, all);
+            if (above < want && above + mine >= want) {
+                for (int i = 0; i < per; ++i) {
+                    const unsigned c = bins[top - i];
+                    if (above + c >= want) {
+                        found[0] = static_cast<unsigned>(top - i);
+                        found[1] = above;
+                        break;
+                    }
+                    above += c;
+                }
+            }
+            __syncthreads();
+            known |= found[0] << shift;
+            mask |= static_cast<unsigned>(count - 1) << shift;
+            want -= found[1];
+        }
+        threshold = known;
+        ties = want;                                   // of the keys at the threshold, this many stay
+    }
+
+    // the walk: four neighbouring keys a thread and step
+    unsigned written = 0, tied = 0;
+    for (int base = 0; base < n; base += 4 * THREADS) {
+        const int i0 = base + 4 * tid;
+        float x[4];
+        unsigned above = 0, at = 0;                    // bits: stays in any case; at the threshold
+        if (i0 + 3 < n) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(w + i0));
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = i0 + e < n ? __ldg(w + i0 + e) : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + e;
+            if (i >= n) continue;
+            if (!chosen || i < from || i >= to) {
+                above |= 1u << e;
+            } else if (spare > 0) {
+                const unsigned key = ordered4(x[e]);
+                if (key > threshold) above |= 1u << e;
+                else if (key == threshold) at |= 1u << e;
+            }
+        }
+        unsigned all;
+        const unsigned before = block_scan4<THREADS>(static_cast<unsigned>(__popc(above)) | static_cast<unsigned>(__popc(at)) << 16, warp_sums, all);
+        unsigned rank = tied + (before >> 16);         // of this thread's first key at the threshold
+        unsigned place = written + (before & 0xffffu) + (min(rank, ties) - min(tied, ties));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            bool stays = above >> e & 1u;
+            if (at >> e & 1u) stays = rank++ < ties;
+            if (!stays) continue;
+            kept[place] = i0 + e;
+            w_out[place] = x[e];
+            ++place;
+        }
+        written += (all & 0xffffu) + (min(tied + (all >> 16), ties) - min(tied, ties));
+        tied += all >> 16;
+    }
+    for (int64_t i = keep + tid; i < p.budget; i += THREADS) kept[i] = -1;
+    for (int64_t i = keep + tid; i < out_keys; i += THREADS) w_out[i] = 0.0f;
+}
+
+// A row of a tile in pieces that lie together: its codes of the key and of the value, then (step, lo).
+template <int D>
+__device__ __forceinline__ void move_row4(const unsigned char* from, int j, unsigned char* to, int i, int piece) {
+    constexpr int KEY = D / 32;                        // 16-byte pieces of a key's codes
+    if (piece < KEY) {
+        *reinterpret_cast<uint4*>(to + i * (D / 2) + piece * 16) = __ldg(reinterpret_cast<const uint4*>(from + j * (D / 2) + piece * 16));
+    } else if constexpr (D == 128) {
+        const int u = piece - KEY;                     // eight pieces of 8 bytes, then (step, lo)
+        const int src = u < 8 ? 8 * D + value4_place(j) * 64 + ((u ^ (j & 4)) << 3) : tile4_rows(D) + j * 8;
+        const int dst = u < 8 ? 8 * D + value4_place(i) * 64 + ((u ^ (i & 4)) << 3) : tile4_rows(D) + i * 8;
+        *reinterpret_cast<uint2*>(to + dst) = __ldg(reinterpret_cast<const uint2*>(from + src));
+    } else if (piece < KEY + KEY) {                    // two pieces of 16 bytes, D = 96: one more from the section behind
+        const int u = piece - KEY;
+        const int src = u < 2 ? 8 * D + value4_place(j) * 32 + u * 16 : 8 * D + 512 + value4_place(j) * 16;
+        const int dst = u < 2 ? 8 * D + value4_place(i) * 32 + u * 16 : 8 * D + 512 + value4_place(i) * 16;
+        *reinterpret_cast<uint4*>(to + dst) = __ldg(reinterpret_cast<const uint4*>(from + src));
+    } else {
+        *reinterpret_cast<uint2*>(to + tile4_rows(D) + i * 8) = __ldg(reinterpret_cast<const uint2*>(from + tile4_rows(D) + j * 8));
+    }
+}
+
+constexpr int kMove4Warps = 4;
+
+template <int D>
+__global__ void __launch_bounds__(32 * kMove4Warps)
+kv_evict4_move_kernel(const Evict4Params p) {
+    constexpr int PIECES = D / 32 + (D == 128 ? 8 : D / 32) + 1;
+    const AttnParams& a = p.a;
+    const int lane = threadIdx.x & 31;
+    const int tiles = (p.budget + kTileKeys - 1) / kTileKeys;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kMove4Warps + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int64_t bh = unit / tiles;
+    const int tile = static_cast<int>(unit - bh * tiles);
+    const int b = static_cast<int>(bh / a.hkv), head = static_cast<int>(bh - static_cast<int64_t>(b) * a.hkv);
+    if (b >= a.B) return;
+    const int shift = a.page_shift - 4, in_page = (1 << shift) - 1;
+    // lanes 0 .. 15: where each row comes from
+    int64_t from = -1;                                 // tile of the cache * 16 + row
+    const int at = tile * kTileKeys + lane;
+    if (lane < kTileKeys && at < p.budget) {
+        const int key = __ldcg(p.kept + bh * p.budget + at);
+        if (key >= 0) {
+            const int t = key >> 4;
+            int pg = __ldg(a.page_table + static_cast<int64_t>(b) * a.table_width + (t >> shift));
+            if (pg < 0 || pg >= a.num_pages) {
+                attn_report(kAttnErrIndex);
+                pg = 0;
+            }
+            from = ((((static_cast<int64_t>(pg) * a.hkv + head) << shift) + (t & in_page)) << 4) + (key & 15);
+        }
+    }
+    if (!__any_sync(kFullMask, from >= 0)) return;
+    const int out = __ldg(p.out_table + static_cast<int64_t>(b) * p.out_width + (tile >> shift));
+    if (out < 0 || out >= a.num_pages) {
+        attn_report(kAttnErrIndex);
+        return;
+    }
+    unsigned char* to = p.cache + (((static_cast<int64_t>(out) * a.hkv + head) << shift) + (tile & in_page)) * tile4_bytes(D);
+#pragma unroll 4
+    for (int i = lane; i < (kTileKeys * PIECES + 31) / 32 * 32; i += 32) {
+        const int row = i / PIECES, piece = i - row * PIECES;
+        const int64_t src = __shfl_sync(kFullMask, from, row & 15);
+        if (row >= kTileKeys || src < 0) continue;
+        move_row4<D>(p.cache + (src >> 4) * tile4_bytes(D), static_cast<int>(src & 15), to, row, piece);
+    }
+}
+
+}  // namespace wht

@@ -1,8 +1,9 @@
 // C ABI of the serving attention (see include/wht_attention.h): argument checks and launches.
 #include <algorithm>
 
-#include "attn_host.h"
+#include "attn_checks.h"
 #include "attn_plan.h"
+#include "cache4_host.h"
 #include "kv_append_kernels.cuh"
 #include "select_kernels.cuh"
 
@@ -14,36 +15,6 @@ using wht::AppendParams;
 using wht::AttnParams;
 using wht::SelectParams;
 using wht::UmmaAttnParams;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-size_t elem(int dtype) { return dtype == WHT_F32 ? 4 : 2; }
-
-int page_shift_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : -1; }
-
-// Rows of a strided [T x H x D] tensor start on 16-byte boundaries.  (The stride of a dimension of one may be anything.)
-bool strides_ok(const void* p, int64_t st, int64_t sh, int64_t T, int32_t H, int dtype) {
-    const int64_t unit = 16 / static_cast<int64_t>(elem(dtype));
-    return aligned16(p) && (T == 1 || st % unit == 0) && (H == 1 || sh % unit == 0);
-}
-
-int check_shape(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t num_pages, int32_t page, int dtype) {
-    if (dtype != WHT_F32 && dtype != WHT_BF16) return WHT_ERR_BAD_DTYPE;
-    if (D != 64 && D != 96 && D != 128) return WHT_ERR_BAD_DIM;
-    if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 64 || Hq > 65536) return WHT_ERR_BAD_DIM;
-    // (tiled copies count a cache's rows in 31 bits; one of more rows would not fit the device's memory)
-    if (page_shift_of(page) < 0 || num_pages < 0 || num_pages > 0x7fffffff / page / Hkv) return WHT_ERR_BAD_DIM;
-    if (T < 0 || T * Hq > 0x7fffffff) return WHT_ERR_BAD_T;
-    return WHT_OK;
-}
-
-// Keys of a list are counted in 31 bits, and the kernels round counts up to whole tiles: some room is left above the longest list.
-constexpr int64_t kMostKeys = 0x7fffff00;
-
-int check_batch(int64_t T, int32_t B, int32_t max_q_len, int32_t table_width, int32_t page, bool ragged) {
-    if (B < 0 || max_q_len < 1 || table_width < 0 || static_cast<int64_t>(table_width) * page > kMostKeys) return WHT_ERR_BAD_DIM;
-    if (max_q_len > (1 << 20) || (!ragged && (T != B || max_q_len != 1)) || (T > 0 && B == 0)) return WHT_ERR_BAD_T;
-    return WHT_OK;
-}
 
 void set_parts(AttnParams& p, unsigned char* at, int64_t rows) {
     if (p.parts <= 1) return;
@@ -208,13 +179,14 @@ int wht_attn_device_status(void) {
     WHT_CUDA_TRY(cudaDeviceSynchronize());
     unsigned any = 0;
     for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select,
-                      take_attn_error_umma}) {
+                      take_attn_error_umma, take_attn_error_append4, take_attn_error_attend4_bf16, take_attn_error_attend4_f32, take_attn_error_evict4}) {
         unsigned flag = 0;
         const int rc = take(&flag);
         if (rc != WHT_OK) return rc;
         any |= flag;
     }
-    for (auto take : {take_device_error_attn_umma, take_device_error_attn_paged_bf16, take_device_error_attn_paged_f32}) {
+    for (auto take : {take_device_error_attn_umma, take_device_error_attn_paged_bf16, take_device_error_attn_paged_f32,
+                      take_device_error_attend4_bf16, take_device_error_attend4_f32}) {
         unsigned waits = 0;
         const int rc = take(&waits);
         if (rc != WHT_OK) return rc;
