@@ -19,15 +19,15 @@ int prepare4(Kernel kernel, int smem, int dev, int* cache) {
     return WHT_OK;
 }
 
-template <typename T, int D, int HR, int NT>
+template <typename T, int D, int NR>
 int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = Attn4Geo<T, D, HR, NT>;
-    static_assert(Geo::BLOCKS == wht_plan::resident4(HR, NT, Geo::F32), "the plan's blocks per SM");
+    using Geo = Attn4Geo<T, D, NR>;
+    static_assert(Geo::BLOCKS == wht_plan::resident4(NR, Geo::F32), "the plan's blocks per SM");
     static_assert(Geo::BLOCKS * (Geo::BYTES + 1024) <= 228 * 1024, "shared memory");
-    int rc = prepare4(attn4_kernel<T, D, HR, NT>, Geo::BYTES, dev, ready);
+    int rc = prepare4(attn4_kernel<T, D, NR>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
-    attn4_kernel<T, D, HR, NT><<<static_cast<unsigned>(p.warps), 32, Geo::BYTES, s>>>(p);
+    attn4_kernel<T, D, NR><<<static_cast<unsigned>(p.warps), 32, Geo::BYTES, s>>>(p);
     WHT_CUDA_TRY(cudaGetLastError());
     const long long rows = static_cast<long long>(p.a.T) * p.a.hq;
     launch_overlapped(attn4_join_kernel<T, D>, dim3(static_cast<unsigned>(ceil_div(rows, 4))), 128, 0, s, p, static_cast<int>(Geo::ROWS));
@@ -36,44 +36,42 @@ int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
 }
 
 template <typename T, int D>
-int attend4_d(const Attn4Params& p, const wht_plan::Unit4& unit, int dev, cudaStream_t s) {
-    if constexpr (std::is_same<T, float>::value) {
-        return unit.operands == 1 ? attend4<T, D, 1, 1>(p, dev, s) : attend4<T, D, 1, 2>(p, dev, s);
-    } else {
-        if (unit.halves == 1) return attend4<T, D, 1, 1>(p, dev, s);
-        return unit.operands == 1 ? attend4<T, D, 2, 1>(p, dev, s) : attend4<T, D, 2, 2>(p, dev, s);
-    }
+int attend4_d(const Attn4Params& p, int row_tiles, int dev, cudaStream_t s) {
+    if (row_tiles == 1) return attend4<T, D, 1>(p, dev, s);
+    if constexpr (!std::is_same<T, float>::value)
+        if (row_tiles == 4) return attend4<T, D, 4>(p, dev, s);
+    return attend4<T, D, 2>(p, dev, s);
 }
 
-template <typename T, int D, int HR>
+template <typename T, int D, int NR>
 int weigh4(const Attn4Params& p, bool after, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
-    using Geo = Weigh4Geo<T, D, HR>;
-    int rc = prepare4(attn4_weigh_kernel<T, D, HR>, Geo::BYTES, dev, ready);
+    using Geo = Weigh4Geo<T, D, NR>;
+    int rc = prepare4(attn4_weigh_kernel<T, D, NR>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     const long long keys = static_cast<long long>(p.a.table_width) << p.a.page_shift;
     const long long chunks = ceil_div(keys, kWeightTiles * kTileKeys), blocks = chunks * p.a.hkv * p.a.B;
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     if (blocks == 0) return WHT_OK;
     if (after)
-        launch_overlapped(attn4_weigh_kernel<T, D, HR>, dim3(static_cast<unsigned>(blocks)), 32, Geo::BYTES, s, p, static_cast<int>(chunks));
+        launch_overlapped(attn4_weigh_kernel<T, D, NR>, dim3(static_cast<unsigned>(blocks)), 32, Geo::BYTES, s, p, static_cast<int>(chunks));
     else
-        attn4_weigh_kernel<T, D, HR><<<static_cast<unsigned>(blocks), 32, Geo::BYTES, s>>>(p, static_cast<int>(chunks));
+        attn4_weigh_kernel<T, D, NR><<<static_cast<unsigned>(blocks), 32, Geo::BYTES, s>>>(p, static_cast<int>(chunks));
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }
 
 template <typename T, int D>
 int weigh4_d(const Attn4Params& p, bool few_rows, bool after, int dev, cudaStream_t s) {
-    if constexpr (std::is_same<T, float>::value) return weigh4<T, D, 1>(p, after, dev, s);
+    if constexpr (std::is_same<T, float>::value) return weigh4<T, D, 1>(p, after, dev, s);  // (two terms: registers for one tile)
     else return few_rows ? weigh4<T, D, 1>(p, after, dev, s) : weigh4<T, D, 2>(p, after, dev, s);
 }
 
 }  // namespace
 
 template <typename T>
-int launch_attend4(const Attn4Params& p, const wht_plan::Unit4& unit, int d, int dev, cudaStream_t s) {
-    return d == 64 ? attend4_d<T, 64>(p, unit, dev, s) : d == 96 ? attend4_d<T, 96>(p, unit, dev, s) : attend4_d<T, 128>(p, unit, dev, s);
+int launch_attend4(const Attn4Params& p, int row_tiles, int d, int dev, cudaStream_t s) {
+    return d == 64 ? attend4_d<T, 64>(p, row_tiles, dev, s) : d == 96 ? attend4_d<T, 96>(p, row_tiles, dev, s) : attend4_d<T, 128>(p, row_tiles, dev, s);
 }
 template <typename T>
 int launch_weigh4(const Attn4Params& p, bool few_rows, bool after, int d, int dev, cudaStream_t s) {

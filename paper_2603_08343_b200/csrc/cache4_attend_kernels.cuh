@@ -13,9 +13,10 @@
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
 //
 // What bounds it: memory, 2 (D / 2 + 4) bytes a key and key head.  At 23 B a clock and SM a tile of 16 keys of 128 channels has 378 clocks of an SM's
-// quarter; its 170 mask, select and shift instructions take two clocks each.
-// Hence products with the rows on the 16-row operand: the weights leave the first product in the layout in which the second wants
-// them; codes of keys and of values are the 8-column operand.
+// quarter; its 100 or so mask, select and shift instructions take two clocks each.  So instructions count, and products are taken
+// transposed, S^T = C Q^T and O^T = C'^T P^T: codes of 16 keys (channels) fill the 16-row operand and the rows sit on the 8-column one, so that 8 rows
+// waste nothing, a key's step and least value are wanted by the four lanes that hold its scores, and P^T changes from accumulator to operand layout by
+// one 8x8 transposition.  (With the rows on the 16-row operand, half of it empty: 364 instructions a tile, 242 us for 64 x 16384 keys of 8 key heads.)
 //
 // The division of work goes by the lengths themselves, which are on the device: the tiles of all units (sequence, key head, row tile)
 // are counted one after the other, and each warp (a block of its own) takes an equal run of them, whatever units it touches.  A unit that lies in one
@@ -37,22 +38,22 @@ struct Attn4Params {
     float* weights_out;
 };
 
-// HR: rows of a lane.  1: a 16-row operand holds 8 rows, the upper half being their second terms (fp32) or nothing.  2: 16 rows.
-// NT: 16-row operands of a unit.
-template <typename T, int D, int HR, int NT>
+// NR: 8-row tiles of a unit.
+template <typename T, int D, int NR>
 struct Attn4Geo {
     static constexpr bool F32 = std::is_same<T, float>::value;
-    static_assert(!F32 || HR == 1, "fp32 queries are two terms");
     static constexpr int NG = D / 32;
-    static constexpr int ROWS = 8 * HR * NT;
+    static constexpr int ROWS = 8 * NR;
+    static constexpr int TERMS = F32 ? 2 : 1;                   // of queries and of weights
     static constexpr int TILE = tile4_bytes(D);
-    static constexpr int STAGES = 4;
-    static constexpr bool Q_SHARED = NT > 1;                    // query operands in shared memory
-    static constexpr int Q_BYTES = Q_SHARED ? NT * 2 * NG * 512 : 0;
-    static constexpr int OFF_Q = STAGES * TILE;
+    static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
+    static constexpr int STAGES = U == 2 ? 3 : 4;               // steps of the ring
+    static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
+    static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;
+    static constexpr int OFF_Q = STAGES * U * TILE;
     static constexpr int OFF_BARS = OFF_Q + Q_BYTES;
     static constexpr int BYTES = OFF_BARS + STAGES * 8;
-    static constexpr int BLOCKS = NT > 1 ? 8 : HR > 1 || F32 ? 12 : 16;  // on an SM
+    static constexpr int BLOCKS = NR * TERMS > 2 ? 8 : NR * TERMS > 1 ? 12 : 16;  // on an SM
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -79,12 +80,23 @@ __device__ __forceinline__ float quad_max(float x) {
     x = fmaxf(x, __shfl_xor_sync(kFullMask, x, 1));
     return fmaxf(x, __shfl_xor_sync(kFullMask, x, 2));
 }
+// over the eight lanes that hold one row's accumulators
+__device__ __forceinline__ float column_max(float x) {
+#pragma unroll
+    for (int i = 4; i < 32; i <<= 1) x = fmaxf(x, __shfl_xor_sync(kFullMask, x, i));
+    return x;
+}
+__device__ __forceinline__ float column_sum(float x) {
+#pragma unroll
+    for (int i = 4; i < 32; i <<= 1) x += __shfl_xor_sync(kFullMask, x, i);
+    return x;
+}
 __device__ __forceinline__ float quad_sum(float x) {
     x += __shfl_xor_sync(kFullMask, x, 1);
     return x + __shfl_xor_sync(kFullMask, x, 2);
 }
 
-// A row of queries: this lane's channels 32 g + 8 c4 .. + 7 as operands of the steps 2 g and 2 g + 1; a[g][step][0]: contraction indices
+// A row of queries: this lane's channels 32 g + 8 c4 .. + 7 as operands of the steps 2 g and 2 g + 1; [g][step][0]: contraction indices
 // 2 c4, + 1, [1]: + 8.  They stand for the channels whose codes lie there (the odd ones with codes times 16, hence queries / 16).
 template <typename T, int NG>
 struct Query4 {
@@ -141,141 +153,205 @@ struct Query4 {
     }
 };
 
-// The rows of a unit as the products take them, and what belongs to each.
-template <typename T, int D, int HR, int NT>
+// The rows of a unit as the products take them (row 8 n + r4 as operand), and what belongs to rows 8 n + 2 c4 + e, whose accumulators a lane holds.
+template <typename T, int D, int NR>
 struct Rows4 {
-    using Geo = Attn4Geo<T, D, HR, NT>;
-    uint32_t q[Geo::Q_SHARED ? 1 : NT][Geo::NG][2][4];
-    float factor[NT][HR], sum[NT][HR];
-    float first[NT][2];                                              // (fp32) what the products of the two terms begin with
+    using Geo = Attn4Geo<T, D, NR>;
+    static constexpr int TERMS = Geo::TERMS;
+    uint32_t q[Geo::Q_SHARED ? 1 : NR][TERMS][Geo::NG][2][2];
+    float factor[NR][2], sum[NR][2];
+    float first[NR][TERMS][2];                                       // (fp32) what the products of each term begin with
     __device__ __forceinline__ void load(const AttnParams& p, int64_t token0, int head, int row0, int rows, unsigned char* smem) {
-        const int lane = threadIdx.x & 31, r4 = lane >> 2;
+        const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            uint32_t f[Geo::NG][2][4];
+        for (int n = 0; n < NR; ++n) {
+            const int row = row0 + n * 8 + r4, tok = row / p.group;
+            const T* src = static_cast<const T*>(p.q) + (token0 + tok) * p.q_st +
+                           (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh;
+            Query4<T, Geo::NG> x;
+            x.load(src, row < rows, p.scale_log2);
 #pragma unroll
-            for (int h = 0; h < HR; ++h) {
-                const int row = row0 + (n * HR + h) * 8 + r4, tok = row / p.group;
-                const T* src = static_cast<const T*>(p.q) + (token0 + tok) * p.q_st +
-                               (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh;
-                Query4<T, Geo::NG> x;
-                x.load(src, row < rows, p.scale_log2);
-                factor[n][h] = x.factor;
-                sum[n][h] = x.sum;
-                first[n][0] = Geo::F32 ? x.lead0 : 0.0f;
-                first[n][1] = Geo::F32 ? x.rest0 : 0.0f;
-#pragma unroll
-                for (int g = 0; g < Geo::NG; ++g)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            f[g][s][2 * i + h] = x.lead[g][s][i];
-                            if (HR == 1) f[g][s][2 * i + 1] = x.rest[g][s][i];
-                        }
+            for (int e = 0; e < 2; ++e) {
+                const int from = (2 * c4 + e) * 4;
+                factor[n][e] = __shfl_sync(kFullMask, x.factor, from);
+                sum[n][e] = __shfl_sync(kFullMask, x.sum, from);
+                if constexpr (Geo::F32) {
+                    first[n][0][e] = __shfl_sync(kFullMask, x.lead0, from);
+                    first[n][1][e] = __shfl_sync(kFullMask, x.rest0, from);
+                }
             }
 #pragma unroll
             for (int g = 0; g < Geo::NG; ++g)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
+                for (int t = 0; t < TERMS; ++t) {
+                    auto& f = t ? x.rest[g] : x.lead[g];
                     if constexpr (Geo::Q_SHARED) {
-                        *reinterpret_cast<uint4*>(smem + ((n * Geo::NG + g) * 2 + s) * 512 + lane * 16) =
-                            make_uint4(f[g][s][0], f[g][s][1], f[g][s][2], f[g][s][3]);
+                        *reinterpret_cast<uint4*>(smem + ((n * TERMS + t) * Geo::NG + g) * 512 + lane * 16) =
+                            make_uint4(f[0][0], f[0][1], f[1][0], f[1][1]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) q[n][g][s][i] = f[g][s][i];
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) q[n][t][g][s][i] = f[s][i];
                     }
                 }
         }
     }
-    __device__ __forceinline__ void get(int n, int g, int s, const unsigned char* smem, uint32_t (&f)[4]) const {
+    __device__ __forceinline__ void get(int n, int t, int g, const unsigned char* smem, uint32_t (&f)[2][2]) const {
         if constexpr (Geo::Q_SHARED) {
-            const uint4 w = *reinterpret_cast<const uint4*>(smem + ((n * Geo::NG + g) * 2 + s) * 512 + (threadIdx.x & 31) * 16);
-            f[0] = w.x; f[1] = w.y; f[2] = w.z; f[3] = w.w;
+            const uint4 w = *reinterpret_cast<const uint4*>(smem + ((n * TERMS + t) * Geo::NG + g) * 512 + (threadIdx.x & 31) * 16);
+            f[0][0] = w.x; f[0][1] = w.y; f[1][0] = w.z; f[1][1] = w.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = q[n][g][s][i];
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) f[s][i] = q[n][t][g][s][i];
         }
     }
 };
 
-// One row against the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4 of a tile: log2 scores.
+// (step, lo) of the keys r4 and r4 + 8 of a tile and of their values.
 struct Params4 {
-    uint4 lower, upper;      // (step, lo) of key and value, of the keys 2 c4 and 2 c4 + 1, of 8 + 2 c4 and 9 + 2 c4
-    __device__ __forceinline__ void load(const unsigned char* tile, int rows_at) {
-        const int c4 = threadIdx.x & 3;
-        lower = *reinterpret_cast<const uint4*>(tile + rows_at + c4 * 16);
-        upper = *reinterpret_cast<const uint4*>(tile + rows_at + 64 + c4 * 16);
+    uint2 lower, upper;
+    __device__ __forceinline__ void load(const unsigned char* rows) {
+        const int r4 = (threadIdx.x & 31) >> 2;
+        lower = *reinterpret_cast<const uint2*>(rows + r4 * 8);
+        upper = *reinterpret_cast<const uint2*>(rows + 64 + r4 * 8);
     }
-    __device__ __forceinline__ uint32_t key(int j) const { return j == 0 ? lower.x : j == 1 ? lower.z : j == 2 ? upper.x : upper.z; }
-    __device__ __forceinline__ uint32_t value(int j) const { return j == 0 ? lower.y : j == 1 ? lower.w : j == 2 ? upper.y : upper.w; }
+    __device__ __forceinline__ uint32_t key(int k) const { return k ? upper.x : lower.x; }
+    __device__ __forceinline__ uint32_t value(int k) const { return k ? upper.y : lower.y; }
 };
-
-// S = Q C^T of a tile: s[n][t][e], e < 2 rows r4, keys 8 t + 2 c4 + e, e >= 2 the upper half of the operand (fp32: added to the lower).
-// fp32 rows: the tensor core's accumulation truncates to about 24 bits of the largest product.  The first term of a query is therefore a
-// whole number of eighths of 2^-10 of the row's range: products with codes and sums of 128 of them take 22 bits, so nothing is lost.
-template <typename T, int D, int HR, int NT>
-__device__ __forceinline__ void scores4(const Rows4<T, D, HR, NT>& rows, const unsigned char* tile, const unsigned char* q_smem,
-                                        float (&s)[NT][2][4]) {
-    constexpr int NG = D / 32;
-    constexpr bool F32 = std::is_same<T, float>::value;
-    const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
-    uint32_t w[2][NG];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const unsigned char* at = tile + (r4 + 8 * t) * (D / 2) + c4 * (D / 8);
-        if constexpr (NG == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(at);
-            w[t][0] = x.x; w[t][1] = x.y; w[t][2] = x.z; w[t][3] = x.w;
-        } else if constexpr (NG == 2) {
-            const uint2 x = *reinterpret_cast<const uint2*>(at);
-            w[t][0] = x.x; w[t][1] = x.y;
-        } else {
-#pragma unroll
-            for (int g = 0; g < NG; ++g) w[t][g] = reinterpret_cast<const uint32_t*>(at)[g];
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[n][t][0] = s[n][t][1] = F32 ? rows.first[n][0] : 0.0f;
-            s[n][t][2] = s[n][t][3] = F32 ? rows.first[n][1] : 0.0f;
-        }
-#pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            uint32_t b[2][2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t x = st ? w[t][g] >> 8 : w[t][g];
-                b[t][0] = x & 0x000f000fu;
-                b[t][1] = x & 0x00f000f0u;
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                uint32_t a[4];
-                rows.get(n, g, st, q_smem, a);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) mma_f16_16816(s[n][t], a, b[t][0], b[t][1]);
-            }
-        }
-    if constexpr (F32) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) s[n][t][e] += s[n][t][2 + e];
-    }
-}
 
 // A row's base: its least value; for fp32 what code 8 stands for, since lo and the sum of codes, all positive, are several times what they weigh
 // together in the end.
 template <typename T>
 __device__ __forceinline__ float base4_of(unsigned word) {
     return std::is_same<T, float>::value ? fmaf(8.0f, step4_of(word), lo4_of(word)) : lo4_of(word);
+}
+
+// S^T = C Q^T of a tile: s[n][2 k + e] = key r4 + 8 k, row 8 n + 2 c4 + e.
+// fp32 rows: the tensor core's accumulation truncates to about 24 bits of the largest product.  The first term of a query is therefore a
+// whole number of eighths of 2^-10 of the row's range: products with codes and sums of 128 of them take 22 bits, so nothing is lost.
+template <typename T, int D, int NR>
+__device__ __forceinline__ void scores4(const Rows4<T, D, NR>& rows, const unsigned char* tile, const unsigned char* q_smem,
+                                        float (&s)[NR][4]) {
+    constexpr int NG = D / 32, TERMS = Rows4<T, D, NR>::TERMS;
+    const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
+    uint32_t w[2][NG];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const unsigned char* at = tile + (r4 + 8 * k) * (D / 2) + c4 * (D / 8);
+        if constexpr (NG == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(at);
+            w[k][0] = x.x; w[k][1] = x.y; w[k][2] = x.z; w[k][3] = x.w;
+        } else if constexpr (NG == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
+            w[k][0] = x.x; w[k][1] = x.y;
+        } else {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) w[k][g] = reinterpret_cast<const uint32_t*>(at)[g];
+        }
+    }
+    float acc[TERMS][NR][4];
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][n][i] = TERMS == 2 ? rows.first[n][t][i & 1] : 0.0f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        uint32_t a[2][4];
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t x = st ? w[k][g] >> 8 : w[k][g];
+                a[st][k] = x & 0x000f000fu;
+                a[st][2 + k] = x & 0x00f000f0u;
+            }
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+                uint32_t b[2][2];
+                rows.get(n, t, g, q_smem, b);
+#pragma unroll
+                for (int st = 0; st < 2; ++st) mma_f16_16816(acc[t][n], a[st], b[st][0], b[st][1]);
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = TERMS == 2 ? acc[0][n][i] + acc[TERMS - 1][n][i] : acc[0][n][i];
+}
+
+// O^T += C'^T P^T of a tile; b[n][t]: the weights times the values' steps as operands (row r4; keys 2 c4, + 1 and 8 + 2 c4, + 1).
+// o[n][2 g + i][2 j + e]: channel 32 g + 4 r4 + 2 i + j, row 8 n + 2 c4 + e.
+template <typename T, int D, int NR>
+__device__ __forceinline__ void add_values4(const unsigned char* tile, const uint32_t (&b)[NR][Attn4Geo<T, D, NR>::TERMS][2], float (&o)[NR][D / 16][4]) {
+    constexpr int NG = D / 32;
+    constexpr bool F32 = std::is_same<T, float>::value;
+    const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
+    // this lane's codes of the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4, halves u = r4; two neighbouring keys side by side
+    const unsigned char* vt = tile + 8 * D;
+    uint32_t pair[NG][2];
+    if constexpr (NG == 4) {
+        uint2 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2*>(vt + (c4 + 4 * i) * 64 + ((r4 ^ ((c4 & 2) << 1)) << 3));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            pair[0][i] = __byte_perm(v[2 * i].x, v[2 * i + 1].x, 0x5410);
+            pair[1][i] = __byte_perm(v[2 * i].x, v[2 * i + 1].x, 0x7632);
+            pair[2][i] = __byte_perm(v[2 * i].y, v[2 * i + 1].y, 0x5410);
+            pair[3][i] = __byte_perm(v[2 * i].y, v[2 * i + 1].y, 0x7632);
+        }
+    } else {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(vt + (c4 + 4 * i) * 32 + r4 * 4);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            pair[0][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
+            pair[1][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x7632);
+        }
+        if constexpr (NG == 3) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const unsigned short*>(vt + 512 + (c4 + 4 * i) * 16 + r4 * 2);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pair[2][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            uint32_t a[4];                                           // channels j = 0, 1 of keys 0 .. 7, then of 8 .. 15
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t x = st ? pair[g][k] >> 8 : pair[g][k];
+                a[2 * k] = x & 0x000f000fu;
+                a[2 * k + 1] = x & 0x00f000f0u;
+                if (F32) {                                           // code - 8, exactly, as ordinary numbers
+                    a[2 * k] = minus_half2(a[2 * k] | 0x64006400u, 0x64086408u);
+                    a[2 * k + 1] = minus_half2(a[2 * k + 1] | 0x64006400u, 0x64806480u);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                if constexpr (F32) {
+                    // (the tensor core's accumulation truncates: one tile at a time, added up with rounding)
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    mma_f16_16816(sum, a, b[n][1][0], b[n][1][1]);
+                    mma_f16_16816(sum, a, b[n][0][0], b[n][0][1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][2 * g + st][e] += sum[e];
+                } else {
+                    mma_f16_16816(o[n][2 * g + st], a, b[n][0][0], b[n][0][1]);
+                }
+            }
+        }
 }
 
 // The tiles of one unit in one run.
@@ -307,11 +383,14 @@ __device__ __forceinline__ int tiles4_of(const AttnParams& p, const int32_t* tab
     return ((pg * p.hkv + head) << shift) + (t & ((1 << shift) - 1));
 }
 
-template <typename T, int D, int HR, int NT>
+// How far a weight times a value's step, and a weight itself, may go before the row's reference moves.
+constexpr float kMostProduct4 = 16384.0f, kMostWeight4 = 0x1p100f;
+
+template <typename T, int D, int NR>
 __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segment4& u, Ring4& ring, unsigned char* smem) {
-    using Geo = Attn4Geo<T, D, HR, NT>;
+    using Geo = Attn4Geo<T, D, NR>;
     constexpr bool F32 = Geo::F32;
-    constexpr int NG = Geo::NG, STAGES = Geo::STAGES;
+    constexpr int NG = Geo::NG, STAGES = Geo::STAGES, U = Geo::U, TERMS = Geo::TERMS;
     const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
     const int rows = u.count * a.group;
@@ -319,234 +398,210 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
     const int last_row = min(rows, u.row0 + Geo::ROWS) - 1;
     const int first_limit = u.keys - u.count + 1;                    // keys that the sequence's first token sees
     const int end = min(u.tile1 * kTileKeys, first_limit + last_row / a.group);
-    const int least_limit = first_limit + u.row0 / a.group;
+    const int least_limit = min(end, first_limit + u.row0 / a.group);
     const int tiles = max(0, (end - u.tile0 * kTileKeys + kTileKeys - 1) / kTileKeys);
+    const int steps = (tiles + U - 1) / U;
 
     int now = tiles4_of(a, u.table, u.head, u.tile0, u.tile0 + tiles);
     int next = tiles > 32 ? tiles4_of(a, u.table, u.head, u.tile0 + 32, u.tile0 + tiles) : 0;
-    auto ask = [&](int j, int tile) {                                // lane 0
-        const unsigned s = (ring.taken + j) % STAGES;
-        mbar_expect_tx(ring.full + s, Geo::TILE);
-        bulk_load(ring.base + s * Geo::TILE, p.cache + static_cast<int64_t>(tile) * Geo::TILE, Geo::TILE, ring.full + s);
+    auto ask = [&](unsigned stage, int j, const int (&tile)[U]) {    // lane 0: step j
+        const int there = min(U, tiles - j * U);
+        mbar_expect_tx(ring.full + stage, there * Geo::TILE);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (i < there)
+                bulk_load(ring.base + (stage * U + i) * Geo::TILE, p.cache + static_cast<int64_t>(tile[i]) * Geo::TILE, Geo::TILE, ring.full + stage);
     };
 #pragma unroll
     for (int j = 0; j < STAGES; ++j) {
-        const int tile = __shfl_sync(kFullMask, now, j);
-        if (lane == 0 && j < tiles) ask(j, tile);
+        int tile[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) tile[i] = __shfl_sync(kFullMask, now, j * U + i);
+        if (lane == 0 && j < steps) ask((ring.taken + j) % STAGES, j, tile);
     }
     unsigned char* q_smem = smem + Geo::OFF_Q;
-    Rows4<T, D, HR, NT> rw;
+    Rows4<T, D, NR> rw;
     rw.load(a, u.token0, u.head, u.row0, rows, q_smem);
     if constexpr (Geo::Q_SHARED) __syncwarp();
 
-    int limit[NT][HR];
-    float m[NT][HR], l[NT][HR], r[NT][HR], most[NT][HR];             // most: the largest p step' so far, which sets the weights' range
-    float range[NT][HR];                                             // weights enter times this power of two
-    float o[NT][4 * NG][4];
+    // m: the reference of a row's weights exp2(score - m), which it shares with its products (weight times step): the largest product so far is 2^6 or
+    // a little more, at most 2^14, so that products are fp16 numbers of full precision, whatever the values' size.
+    float m[NR][2], l[NR][2], r[NR][2];
+    float o[NR][D / 16][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NR; ++n) {
 #pragma unroll
-        for (int h = 0; h < HR; ++h) {
-            const int row = u.row0 + (n * HR + h) * 8 + r4;
-            limit[n][h] = row < rows ? first_limit + row / a.group : 0x7fffffff;   // (rows that are not there see zeros)
-            m[n][h] = -INFINITY;
-            l[n][h] = r[n][h] = most[n][h] = 0.0f;
-            range[n][h] = 1.0f;
+        for (int e = 0; e < 2; ++e) {
+            m[n][e] = -INFINITY;
+            l[n][e] = r[n][e] = 0.0f;
         }
 #pragma unroll
-        for (int d = 0; d < 4 * NG; ++d) o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
+        for (int d = 0; d < D / 16; ++d) o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
     }
+    // keys that row 8 n + 2 c4 + e sees of these (rows that are not there see zeros); a step's second tile may lie behind the end
+    auto limit = [&](int n, int e) {
+        const int row = u.row0 + n * 8 + 2 * c4 + e;
+        return row < rows ? min(end, first_limit + row / a.group) : end;
+    };
 
-    for (int j = 0; j < tiles; ++j) {
-        const unsigned stage = ring.taken % STAGES;
-        mbar_wait_bounded(ring.full + stage, (ring.taken / STAGES) & 1u);
-        const unsigned char* tile = ring.base + stage * Geo::TILE;
-        const int base = (u.tile0 + j) * kTileKeys;
-        const bool mask = base + kTileKeys > least_limit;
+    unsigned stage = ring.taken % STAGES, parity = (ring.taken / STAGES) & 1u;
+    ring.taken += steps;
+    for (int j = 0; j < steps; ++j) {
+        mbar_wait_bounded(ring.full + stage, parity);
+        const unsigned char* tile = ring.base + stage * U * Geo::TILE;
+        const int base = (u.tile0 + j * U) * kTileKeys;
+        const bool mask = base + U * kTileKeys > least_limit;
 
-        float s[NT][2][4];
-        scores4<T, D, HR, NT>(rw, tile, q_smem, s);
-        Params4 w;
-        w.load(tile, tile4_rows(D));
-        // log2 scores, weights, and weights times the values' steps, of the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4
-        float x[NT][HR][4], y[NT][HR][4];
-        bool passes = false;
-        auto hidden = [&](int n, int h, int i) { return mask && base + 8 * (i >> 1) + 2 * c4 + (i & 1) >= limit[n][h]; };
+        float s[U][NR][4], x[U][NR][4], y[U][NR][4];                 // scores, then weights, and products
+        Params4 w[U];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int t = 0; t < U; ++t) {
+            scores4<T, D, NR>(rw, tile + t * Geo::TILE, q_smem, s[t]);
+            w[t].load(tile + t * Geo::TILE + tile4_rows(D));
+        }
+        float all_x = 0.0f, all_y = 0.0f;
 #pragma unroll
-            for (int h = 0; h < HR; ++h) {
+        for (int t = 0; t < U; ++t)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[n][h][i] = fmaf(step4_of(w.key(i)) * s[n][i >> 1][(i & 1) + 2 * h], rw.factor[n][h], base4_of<T>(w.key(i)) * rw.sum[n][h]);
-                    float weight = exp2_fast(x[n][h][i] - m[n][h]);
-                    y[n][h][i] = weight * step4_of(w.value(i)) * range[n][h];
-                    if (hidden(n, h, i)) weight = y[n][h][i] = 0.0f;
-                    passes = passes || !(weight <= 256.0f) || !(y[n][h][i] <= 16384.0f);
-                    s[n][i >> 1][(i & 1) + 2 * (HR - 1) * h] = weight;   // (the scores of this key are done with)
+                    const int k = i >> 1, e = i & 1;
+                    const float z = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -m[n][e]));
+                    x[t][n][i] = exp2_fast(z);
+                    y[t][n][i] = x[t][n][i] * step4_of(w[t].value(k));
+                    if (!mask) {
+                        all_x += x[t][n][i];
+                        all_y += y[t][n][i];
+                    }
                 }
-            }
-        if (__any_sync(kFullMask, passes)) {
-            // a new maximum, or weights that leave the range of fp16: the references move
+        auto hidden = [&](int t, int n, int i) { return base + t * kTileKeys + 8 * (i >> 1) + r4 >= limit(n, i & 1); };
+        if (mask) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int t = 0; t < U; ++t)
 #pragma unroll
-                for (int h = 0; h < HR; ++h) {
-                    // (a row moves its references by its own scores alone: its result does not depend on the rows beside it)
-                    float top = -INFINITY;
-                    int moves = 0;
+                for (int n = 0; n < NR; ++n)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (!hidden(n, h, i)) top = fmaxf(top, x[n][h][i]);
-                        moves |= !(s[n][i >> 1][(i & 1) + 2 * (HR - 1) * h] <= 256.0f) || !(y[n][h][i] <= 16384.0f);
+                        if (hidden(t, n, i)) x[t][n][i] = y[t][n][i] = 0.0f;
+                        all_x += x[t][n][i];
+                        all_y += y[t][n][i];
                     }
-                    moves |= __shfl_xor_sync(kFullMask, moves, 1);
-                    moves |= __shfl_xor_sync(kFullMask, moves, 2);
-                    top = fmaxf(quad_max(top), m[n][h]);
-                    if (!__any_sync(kFullMask, moves)) continue;
-                    if (!moves) top = m[n][h];
-                    const float f = top > m[n][h] ? exp2_fast(m[n][h] - top) : 1.0f;
-                    m[n][h] = top;
-                    l[n][h] *= f;
-                    r[n][h] *= f;
-                    float heavy = 0.0f;
+        }
+        // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
+        if (!__all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float weight = hidden(n, h, i) ? 0.0f : exp2_fast(x[n][h][i] - top);
-                        if (moves) s[n][i >> 1][(i & 1) + 2 * (HR - 1) * h] = weight;
-                        heavy = fmaxf(heavy, hidden(n, h, i) ? 0.0f : weight * step4_of(w.value(i)));
-                    }
-                    heavy = fmaxf(quad_max(heavy), most[n][h] * f);
-                    if (!moves) heavy = most[n][h];
-                    most[n][h] = heavy;
-                    // the largest becomes 2^6: 2^8 above it before the range moves, 2^-31 of it below before bits are lost
-                    const int to = heavy > 0.0f ? max(-120, min(120, 6 - exponent_of(heavy))) : 100;
-                    const int by = to - exponent_of(range[n][h]);
-                    range[n][h] = power_of_two(to);
-                    const float f1 = f * power_of_two(by / 2), f2 = power_of_two(by - by / 2);
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-                    for (int d = 0; d < 4 * NG; ++d)
+                for (int e = 0; e < 2; ++e) {
+                    // (a row moves its reference by its own scores alone: its result does not depend on the rows beside it)
+                    float top = -INFINITY, heavy = -INFINITY;        // the largest score, and score plus log2 of the step
+                    float row_x = 0.0f, row_y = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            o[n][d][e + 2 * (HR - 1) * h] = o[n][d][e + 2 * (HR - 1) * h] * f1 * f2;
-                            if (HR == 1) o[n][d][e + 2] = o[n][d][e + 2] * f1 * f2;
+                    for (int t = 0; t < U; ++t)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int i = 2 * k + e;
+                            if (mask && hidden(t, n, i)) continue;
+                            const float score = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], base4_of<T>(w[t].key(k)) * rw.sum[n][e]);
+                            top = fmaxf(top, score);
+                            heavy = fmaxf(heavy, score + __log2f(step4_of(w[t].value(k))));
+                            row_x += x[t][n][i];
+                            row_y += y[t][n][i];
                         }
+                    int moves = !(row_x <= kMostWeight4 && row_y <= kMostProduct4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        y[n][h][i] = hidden(n, h, i) ? 0.0f : s[n][i >> 1][(i & 1) + 2 * (HR - 1) * h] * step4_of(w.value(i)) * range[n][h];
-                }
-        }
-        uint32_t pa[NT][4];
+                    for (int i = 4; i < 32; i <<= 1) moves |= __shfl_xor_sync(kFullMask, moves, i);
+                    if (!__any_sync(kFullMask, moves)) continue;
+                    top = column_max(top);
+                    heavy = column_max(heavy);
+                    // (without a step above 0 there are no products)
+                    float to = heavy > -INFINITY ? fmaxf(heavy - 6.0f, top - 90.0f) : top;
+                    to = moves ? fmaxf(to, m[n][e]) : m[n][e];
+                    const float f = to > m[n][e] ? exp2_fast(m[n][e] - to) : 1.0f;
+                    m[n][e] = to;
+                    l[n][e] *= f;
+                    r[n][e] *= f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int h = 0; h < HR; ++h) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float weight = s[n][i >> 1][(i & 1) + 2 * (HR - 1) * h];
-                    l[n][h] += weight;
-                    if (!hidden(n, h, i)) r[n][h] = fmaf(weight, base4_of<T>(w.value(i)), r[n][h]);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t lead = pack_half2(y[n][h][2 * i], y[n][h][2 * i + 1]);
-                    pa[n][2 * i + h] = lead;
-                    if (HR == 1) pa[n][2 * i + 1] = F32 ? pack_half2(y[n][h][2 * i] - half_lo(lead), y[n][h][2 * i + 1] - half_hi(lead)) : 0u;
-                }
-            }
-
-        // O += (P step') C': this lane's codes of the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4, halves u = r4
-        const unsigned char* vt = tile + 8 * D;
-        uint32_t pair[NG][2];
-        if constexpr (NG == 4) {
-            uint2 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2*>(vt + (c4 + 4 * i) * 64 + ((r4 ^ ((c4 & 2) << 1)) << 3));
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                pair[0][i] = __byte_perm(v[2 * i].x, v[2 * i + 1].x, 0x5410);
-                pair[1][i] = __byte_perm(v[2 * i].x, v[2 * i + 1].x, 0x7632);
-                pair[2][i] = __byte_perm(v[2 * i].y, v[2 * i + 1].y, 0x5410);
-                pair[3][i] = __byte_perm(v[2 * i].y, v[2 * i + 1].y, 0x7632);
-            }
-        } else {
-            uint32_t v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(vt + (c4 + 4 * i) * 32 + r4 * 4);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                pair[0][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
-                pair[1][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x7632);
-            }
-            if constexpr (NG == 3) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const unsigned short*>(vt + 512 + (c4 + 4 * i) * 16 + r4 * 2);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) pair[2][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
-            }
-        }
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t pick = i & 1 ? 0x00f000f0u : 0x000f000fu;
-                uint32_t b0 = (i >= 2 ? pair[g][0] >> 8 : pair[g][0]) & pick, b1 = (i >= 2 ? pair[g][1] >> 8 : pair[g][1]) & pick;
-                if (F32) {                                           // code - 8, exactly, as ordinary numbers
-                    b0 = minus_half2(b0 | 0x64006400u, i & 1 ? 0x64806480u : 0x64086408u);
-                    b1 = minus_half2(b1 | 0x64006400u, i & 1 ? 0x64806480u : 0x64086408u);
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if constexpr (F32) {
-                        // (the tensor core's accumulation truncates: one tile at a time, added up with rounding)
-                        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_f16_16816(sum, pa[n], b0, b1);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n][4 * g + i][e] += sum[e];
-                    } else {
-                        mma_f16_16816(o[n][4 * g + i], pa[n], b0, b1);
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[n][d][e] *= f;
+                        o[n][d][2 + e] *= f;
                     }
+#pragma unroll
+                    for (int t = 0; t < U; ++t)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int i = 2 * k + e;
+                            const float z = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -to));
+                            const bool seen = !(mask && hidden(t, n, i));
+                            x[t][n][i] = seen ? exp2_fast(z) : 0.0f;
+                            y[t][n][i] = seen ? x[t][n][i] * step4_of(w[t].value(k)) : 0.0f;
+                        }
                 }
-            }
-        __syncwarp();                                                // every lane has read the slot
-        const int ahead = j + STAGES;
-        if ((ahead & 31) == 0) {
-            now = next;
-            next = ahead + 32 < tiles ? tiles4_of(a, u.table, u.head, u.tile0 + ahead + 32, u.tile0 + tiles) : 0;
         }
-        const int t = __shfl_sync(kFullMask, now, ahead & 31);
-        if (lane == 0 && ahead < tiles) ask(STAGES, t);
-        ++ring.taken;
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            uint32_t b[NR][TERMS][2];
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        l[n][e] += x[t][n][2 * k + e];
+                        float v = base4_of<T>(w[t].value(k));
+                        if (mask && hidden(t, n, 2 * k + e)) v = 0.0f;
+                        r[n][e] = fmaf(x[t][n][2 * k + e], v, r[n][e]);
+                    }
+                    const uint32_t lead = pack_half2(y[t][n][2 * k], y[t][n][2 * k + 1]);
+                    b[n][0][k] = transpose_8x8(lead);
+                    if constexpr (F32)
+                        b[n][1][k] = transpose_8x8(pack_half2(y[t][n][2 * k] - half_lo(lead), y[t][n][2 * k + 1] - half_hi(lead)));
+                }
+            add_values4<T, D, NR>(tile + t * Geo::TILE, b, o);
+        }
+        __syncwarp();                                                // every lane has read the slot
+        const int ahead = (j + STAGES) * U;                          // (a multiple of U, which divides 32)
+        if (ahead < tiles) {
+            if ((ahead & 31) == 0) {
+                now = next;
+                next = ahead + 32 < tiles ? tiles4_of(a, u.table, u.head, u.tile0 + ahead + 32, u.tile0 + tiles) : 0;
+            }
+            int to[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) to[i] = __shfl_sync(kFullMask, now, (ahead + i) & 31);
+            if (lane == 0) ask(stage, j + STAGES, to);
+        }
+        if (++stage == STAGES) {
+            stage = 0;
+            parity ^= 1u;
+        }
     }
 
-    // the results, eight channels of a row at a time
+    // the results, four channels of a row at a time
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int h = 0; h < HR; ++h) {
-            const int local = (n * HR + h) * 8 + r4, row = u.row0 + local, tok = row / a.group;
-            const float ll = quad_sum(l[n][h]), rr = quad_sum(r[n][h]);
+        for (int e = 0; e < 2; ++e) {
+            const int local = n * 8 + 2 * c4 + e, row = u.row0 + local, tok = row / a.group;
+            const float ll = column_sum(l[n][e]), rr = column_sum(r[n][e]);
             if (row >= rows) continue;
-            const float unit = power_of_two(-exponent_of(range[n][h]));
             const int64_t at = (u.token0 + tok) * a.hq + static_cast<int64_t>(u.head) * a.group + (row - tok * a.group);
             const float inv = u.slot >= 0 ? 1.0f : ll > 0.0f ? 1.0f / ll : 0.0f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float c = o[n][4 * g + i][e + 2 * (HR - 1) * h];
-                        if (F32) c += o[n][4 * g + i][e + 2];
-                        v[4 * e + i] = (c * (F32 ? (i & 1 ? 0.0625f : 1.0f) : i & 1 ? 1048576.0f : 16777216.0f) * unit + rr) * inv;
-                    }
-                if (u.slot >= 0) store8(a.part_o + (u.slot * Geo::ROWS + local) * D + g * 32 + c4 * 8, v);
-                else store8(static_cast<T*>(a.out) + at * D + g * 32 + c4 * 8, v);
+                constexpr float even = F32 ? 1.0f : 0x1p24f, odd = even * 0.0625f;
+                const float4 v = make_float4((o[n][2 * g][e] * even + rr) * inv, (o[n][2 * g][2 + e] * odd + rr) * inv,
+                                             (o[n][2 * g + 1][e] * even + rr) * inv, (o[n][2 * g + 1][2 + e] * odd + rr) * inv);
+                const int ch = g * 32 + r4 * 4;
+                if (F32 || u.slot >= 0)
+                    *reinterpret_cast<float4*>(u.slot >= 0 ? a.part_o + (u.slot * Geo::ROWS + local) * D + ch : static_cast<float*>(a.out) + at * D + ch) = v;
+                else
+                    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + ch) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
             }
-            if (c4 != 0) continue;
-            if (u.slot >= 0) a.part_ml[u.slot * Geo::ROWS + local] = make_float2(m[n][h], ll);
-            else if (p.lse) p.lse[at] = ll > 0.0f || ll != ll ? m[n][h] + log2f(ll) : INFINITY;
+            if (r4 != 0) continue;
+            if (u.slot >= 0) a.part_ml[u.slot * Geo::ROWS + local] = make_float2(m[n][e], ll);
+            else if (p.lse) p.lse[at] = ll > 0.0f || ll != ll ? m[n][e] + log2f(ll) : INFINITY;
         }
 }
 
@@ -584,10 +639,10 @@ __device__ __forceinline__ int64_t run4_tiles(int64_t total, int warps, int leas
     return even > least ? even : least;
 }
 
-template <typename T, int D, int HR, int NT>
-__global__ void __launch_bounds__(32, (Attn4Geo<T, D, HR, NT>::BLOCKS))
+template <typename T, int D, int NR>
+__global__ void __launch_bounds__(32, (Attn4Geo<T, D, NR>::BLOCKS))
 attn4_kernel(const Attn4Params p) {
-    using Geo = Attn4Geo<T, D, HR, NT>;
+    using Geo = Attn4Geo<T, D, NR>;
     extern __shared__ __align__(128) unsigned char smem4[];
     const AttnParams& a = p.a;
     const int lane = threadIdx.x;
@@ -641,7 +696,7 @@ attn4_kernel(const Attn4Params p) {
             u.tile1 = static_cast<int>(min(stop - start, static_cast<int64_t>(s.tiles)));
             // a unit that began in an earlier run leaves its part in this one's first place, one that goes on in its second
             u.slot = u.tile0 > 0 ? 2ll * blockIdx.x : u.tile1 < s.tiles ? 2ll * blockIdx.x + 1 : -1;
-            attn4_segment<T, D, HR, NT>(p, u, ring, smem4);
+            attn4_segment<T, D, NR>(p, u, ring, smem4);
             __syncwarp();
             f = start + u.tile1;
         }
@@ -727,8 +782,8 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
 // one order.  Places from the sequence's length on become 0.
 constexpr int kWeightTiles = 32;
 
-template <typename T, int D, int HR>
-struct Weigh4Geo : Attn4Geo<T, D, HR, 1> {
+template <typename T, int D, int NR>
+struct Weigh4Geo {
     static constexpr int STAGE = 8 * D + 128;                        // codes of the keys, then (step, lo)
     static constexpr int STAGES = 4;
     static constexpr int OFF_SUMS = STAGES * STAGE;
@@ -736,10 +791,10 @@ struct Weigh4Geo : Attn4Geo<T, D, HR, 1> {
     static constexpr int BYTES = OFF_BARS + STAGES * 8;
 };
 
-template <typename T, int D, int HR>
+template <typename T, int D, int NR>
 __global__ void __launch_bounds__(32, 16)
 attn4_weigh_kernel(const Attn4Params p, int chunks) {
-    using Geo = Weigh4Geo<T, D, HR>;
+    using Geo = Weigh4Geo<T, D, NR>;
     constexpr int STAGES = Geo::STAGES;
     extern __shared__ __align__(128) unsigned char smem4[];
     const AttnParams& a = p.a;
@@ -774,9 +829,9 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
         bulk_load(smem4 + s * Geo::STAGE, src, 8 * D, full + s);
         bulk_load(smem4 + s * Geo::STAGE + 8 * D, src + tile4_rows(D), 128, full + s);
     };
-    for (int row0 = 0; row0 < rows; row0 += 8 * HR) {
+    for (int row0 = 0; row0 < rows; row0 += 8 * NR) {
         // rows that see nothing here are passed over: the last of these rows sees the most
-        const int end = first_limit + (min(rows, row0 + 8 * HR) - 1) / a.group;
+        const int end = first_limit + (min(rows, row0 + 8 * NR) - 1) / a.group;
         const int n = min(tiles, max(0, (end - key0 + kTileKeys - 1) / kTileKeys));
         if (n == 0) continue;
 #pragma unroll
@@ -784,44 +839,39 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
             const int tile = __shfl_sync(kFullMask, tile_no, j);
             if (lane == 0 && j < n) ask((taken + j) % STAGES, tile);
         }
-        Rows4<T, D, HR, 1> rw;
+        Rows4<T, D, NR> rw;
         rw.load(a, token0, head, row0, rows, nullptr);
-        int limit[HR];
-        float lse[HR];
+        int limit[NR][2];
+        float lse[NR][2];
 #pragma unroll
-        for (int h = 0; h < HR; ++h) {
-            const int row = row0 + h * 8 + r4, tok = row / a.group;
-            limit[h] = row < rows ? first_limit + tok : 0;           // (rows that are not there weigh nothing)
-            lse[h] = row < rows ? __ldcg(p.lse + (token0 + tok) * a.hq + static_cast<int64_t>(head) * a.group + (row - tok * a.group)) : INFINITY;
-        }
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = row0 + i * 8 + 2 * c4 + e, tok = row / a.group;
+                limit[i][e] = row < rows ? first_limit + tok : 0;    // (rows that are not there weigh nothing)
+                lse[i][e] = row < rows ? __ldcg(p.lse + (token0 + tok) * a.hq + static_cast<int64_t>(head) * a.group + (row - tok * a.group)) : INFINITY;
+            }
         for (int j = 0; j < n; ++j, ++taken) {
             const unsigned stage = taken % STAGES;
             mbar_wait_bounded(full + stage, (taken / STAGES) & 1u);
             const unsigned char* tile = smem4 + stage * Geo::STAGE;
-            float s[1][2][4];
-            scores4<T, D, HR, 1>(rw, tile, nullptr, s);
+            float s[NR][4];
+            scores4<T, D, NR>(rw, tile, nullptr, s);
             Params4 w;
-            w.load(tile, 8 * D);
-            float sum[4];
+            w.load(tile + 8 * D);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = key0 + j * kTileKeys + 8 * (i >> 1) + 2 * c4 + (i & 1);
-                sum[i] = 0.0f;
+            for (int k = 0; k < 2; ++k) {
+                const int key = key0 + j * kTileKeys + 8 * k + r4;
+                float sum = 0.0f;
 #pragma unroll
-                for (int h = 0; h < HR; ++h) {
-                    const float x = fmaf(step4_of(w.key(i)) * s[0][i >> 1][(i & 1) + 2 * h], rw.factor[0][h], base4_of<T>(w.key(i)) * rw.sum[0][h]);
-                    if (key < limit[h]) sum[i] += exp2_fast(x - lse[h]);
-                }
+                for (int i = 0; i < NR; ++i)
 #pragma unroll
-                for (int d = 4; d < 32; d <<= 1) sum[i] += __shfl_xor_sync(kFullMask, sum[i], d);
-            }
-            if (r4 == 0) {
-                float2* to = reinterpret_cast<float2*>(sums + j * kTileKeys + 2 * c4);
-                float2 lower = to[0], upper = to[4];
-                lower.x += sum[0]; lower.y += sum[1];
-                upper.x += sum[2]; upper.y += sum[3];
-                to[0] = lower;
-                to[4] = upper;
+                    for (int e = 0; e < 2; ++e) {
+                        const float z = fmaf(step4_of(w.key(k)) * s[i][2 * k + e], rw.factor[i][e], fmaf(base4_of<T>(w.key(k)), rw.sum[i][e], -lse[i][e]));
+                        if (key < limit[i][e]) sum += exp2_fast(z);
+                    }
+                sum = quad_sum(sum);
+                if (c4 == 0) sums[j * kTileKeys + 8 * k + r4] += sum;
             }
             __syncwarp();
             const int tile_next = __shfl_sync(kFullMask, tile_no, (j + STAGES) & 31);

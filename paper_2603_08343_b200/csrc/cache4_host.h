@@ -16,7 +16,7 @@ namespace wht_host {
 int launch_append4(wht::Append4Params& p, int dtype, bool interleaved, int d, cudaStream_t s);
 int launch_read4(const wht::Read4Params& p, int dtype, int d, cudaStream_t s);
 // cache4_attend.cuh, instantiated per storage type in cache4_attend_bf16.cu and cache4_attend_f32.cu
-template <typename T> int launch_attend4(const wht::Attn4Params& p, const wht_plan::Unit4& unit, int d, int dev, cudaStream_t s);
+template <typename T> int launch_attend4(const wht::Attn4Params& p, int row_tiles, int d, int dev, cudaStream_t s);
 template <typename T> int launch_weigh4(const wht::Attn4Params& p, bool few_rows, bool after, int d, int dev, cudaStream_t s);
 // cache4_evict.cu
 int launch_evict4(wht::Evict4Params& p, int d, cudaStream_t s);

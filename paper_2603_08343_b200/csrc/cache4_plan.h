@@ -5,24 +5,15 @@
 
 namespace wht_plan {
 
-// Rows of a unit: halves (rows of a lane in a 16-row operand; 1: the operand's upper half holds second terms or nothing) and operands.
-struct Unit4 {
-    int halves, operands;
-    int rows() const { return 8 * halves * operands; }
-};
-inline Unit4 unit4(int64_t rows, int dtype) {
-    if (rows <= 8) return {1, 1};
-    if (dtype == WHT_F32) return {1, 2};
-    return rows <= 16 ? Unit4{2, 1} : Unit4{2, 2};
-}
+// 8-row tiles of a unit (fp32 rows are two terms: half as many).
+inline int row_tiles4(int64_t rows, int dtype) { return rows <= 8 ? 1 : rows <= 16 || dtype == WHT_F32 ? 2 : 4; }
 // One-warp blocks that an SM holds at once.
-constexpr int resident4(int halves, int operands, bool f32) { return operands > 1 ? 8 : halves > 1 || f32 ? 12 : 16; }
+constexpr int resident4(int row_tiles, bool f32) { return row_tiles * (f32 ? 2 : 1) > 2 ? 8 : row_tiles * (f32 ? 2 : 1) > 1 ? 12 : 16; }
 
 constexpr int kLeastRun4 = 8;  // tiles of 16 keys: a shorter run would not pay for its start and its part of the join
 
 struct Attend4Plan {
-    Unit4 unit;
-    int warps;
+    int row_tiles, warps;
     size_t ml_bytes, o_bytes, lse_bytes, bytes;
 };
 
@@ -31,15 +22,16 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     Attend4Plan f{};
     if (T == 0) return f;
     const int group = Hq / Hkv;
-    f.unit = unit4(static_cast<int64_t>(max_q_len) * group, dtype);
+    f.row_tiles = row_tiles4(static_cast<int64_t>(max_q_len) * group, dtype);
+    const int rows = 8 * f.row_tiles;
     // as many runs as fit the machine at once, unless the tables hold too few keys for that
-    const double units = static_cast<double>(B) * Hkv * div_up(static_cast<int64_t>(max_q_len) * group, f.unit.rows());
+    const double units = static_cast<double>(B) * Hkv * div_up(static_cast<int64_t>(max_q_len) * group, rows);
     const double tiles = units * static_cast<double>(std::max<int64_t>(1, static_cast<int64_t>(table_width) * page / 16));
     const double runs = std::max(1.0, tiles / kLeastRun4 + 1.0);
-    const int most = sms * resident4(f.unit.halves, f.unit.operands, dtype == WHT_F32);
+    const int most = sms * resident4(f.row_tiles, dtype == WHT_F32);
     f.warps = runs < most ? static_cast<int>(runs) : most;
-    f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * f.unit.rows() * kPartStats);
-    f.o_bytes = static_cast<size_t>(2) * f.warps * f.unit.rows() * D * sizeof(float);
+    f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * rows * kPartStats);
+    f.o_bytes = static_cast<size_t>(2) * f.warps * rows * D * sizeof(float);
     f.lse_bytes = weigh ? static_cast<size_t>(T) * Hq * sizeof(float) : 0;
     f.bytes = f.ml_bytes + f.o_bytes + f.lse_bytes;
     return f;
