@@ -32,7 +32,8 @@ struct Attn4Params {
     AttnParams a;            // queries, output, tables, lengths, sizes; part_ml, part_o: [2 * warps][rows of a unit]
     const unsigned char* cache;
     int warps;               // runs
-    int least;               // tiles of a run, at least
+    int least;               // grains of a run, at least
+    int grain;               // log2 of a grain's tiles: work is counted in grains, in 32 bits
     float* lse;              // [T * Hq] log2 of a row's softmax sum, or NULL
     const float* weights;    // [B x Hkv x table_width * page]: received so far
     float* weights_out;
@@ -46,7 +47,7 @@ struct Attn4Geo {
     static constexpr int ROWS = 8 * NR;
     static constexpr int TERMS = F32 ? 2 : 1;                   // of queries and of weights
     static constexpr int TILE = tile4_bytes(D);
-    static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
+        static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
     static constexpr int STAGES = U == 2 ? 3 : 4;               // steps of the ring
     static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
     static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;
@@ -397,7 +398,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
     // the unit's last row sees the most keys, its first row the fewest
     const int last_row = min(rows, u.row0 + Geo::ROWS) - 1;
     const int first_limit = u.keys - u.count + 1;                    // keys that the sequence's first token sees
-    const int end = min(u.tile1 * kTileKeys, first_limit + last_row / a.group);
+    const int end = static_cast<int>(min(static_cast<int64_t>(u.tile1) * kTileKeys, static_cast<int64_t>(first_limit + last_row / a.group)));
     const int least_limit = min(end, first_limit + u.row0 / a.group);
     const int tiles = max(0, (end - u.tile0 * kTileKeys + kTileKeys - 1) / kTileKeys);
     const int steps = (tiles + U - 1) / U;
@@ -452,67 +453,81 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         const int base = (u.tile0 + j * U) * kTileKeys;
         const bool mask = base + U * kTileKeys > least_limit;
 
-        float s[U][NR][4], x[U][NR][4], y[U][NR][4];                 // scores, then weights, and products
+        float s[U][NR][4];
         Params4 w[U];
 #pragma unroll
         for (int t = 0; t < U; ++t) {
             scores4<T, D, NR>(rw, tile + t * Geo::TILE, q_smem, s[t]);
             w[t].load(tile + t * Geo::TILE + tile4_rows(D));
         }
-        float all_x = 0.0f, all_y = 0.0f;
-#pragma unroll
-        for (int t = 0; t < U; ++t)
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = i >> 1, e = i & 1;
-                    const float z = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -m[n][e]));
-                    x[t][n][i] = exp2_fast(z);
-                    y[t][n][i] = x[t][n][i] * step4_of(w[t].value(k));
-                    if (!mask) {
-                        all_x += x[t][n][i];
-                        all_y += y[t][n][i];
-                    }
-                }
         auto hidden = [&](int t, int n, int i) { return base + t * kTileKeys + 8 * (i >> 1) + r4 >= limit(n, i & 1); };
-        if (mask) {
+        // One score against the row's reference: its weight, and that times its value's step.
+        auto weigh = [&](int t, int n, int i, float& x, float& y) {
+            const int k = i >> 1, e = i & 1;
+            x = exp2_fast(fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -m[n][e])));
+            y = x * step4_of(w[t].value(k));
+        };
+        // This lane's sums of a row: weights, weights times base values, products; and the products as operands, before their transposition.
+        float sx[NR][2], sr[NR][2], sy[NR][2];
+        uint32_t b[U][NR][TERMS][2];
+        auto add_up = [&](auto masked) {
 #pragma unroll
-            for (int t = 0; t < U; ++t)
+            for (int n = 0; n < NR; ++n) {
+                sx[n][0] = sx[n][1] = sr[n][0] = sr[n][1] = sy[n][0] = sy[n][1] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < NR; ++n)
+                for (int t = 0; t < U; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (hidden(t, n, i)) x[t][n][i] = y[t][n][i] = 0.0f;
-                        all_x += x[t][n][i];
-                        all_y += y[t][n][i];
+                    for (int k = 0; k < 2; ++k) {
+                        const float base_value = base4_of<T>(w[t].value(k));
+                        float y[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float x;
+                            weigh(t, n, 2 * k + e, x, y[e]);
+                            bool seen = true;
+                            if constexpr (masked.value) seen = !hidden(t, n, 2 * k + e);
+                            if (!seen) y[e] = x = 0.0f;
+                            sx[n][e] += x;
+                            sy[n][e] += y[e];
+                            sr[n][e] = fmaf(x, seen ? base_value : 0.0f, sr[n][e]);
+                        }
+                        b[t][n][0][k] = pack_half2(y[0], y[1]);
+                        if constexpr (F32) b[t][n][1][k] = pack_half2(y[0] - half_lo(b[t][n][0][k]), y[1] - half_hi(b[t][n][0][k]));
                     }
-        }
-        // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
-        if (!__all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) {
+            }
+        };
+        bool moved = false;                                          // (once a step: what is NaN stays NaN)
+        for (bool careful = mask;; careful = true) {
+            if (careful) add_up(std::true_type{});
+            else add_up(std::false_type{});
+            float all_x = 0.0f, all_y = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                all_x += sx[n][0] + sx[n][1];
+                all_y += sy[n][0] + sy[n][1];
+            }
+            // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
+            if (moved || __all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) break;
+            moved = true;
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     // (a row moves its reference by its own scores alone: its result does not depend on the rows beside it)
+                    int moves = !(sx[n][e] <= kMostWeight4 && sy[n][e] <= kMostProduct4);
+#pragma unroll
+                    for (int i = 4; i < 32; i <<= 1) moves |= __shfl_xor_sync(kFullMask, moves, i);
+                    if (!__any_sync(kFullMask, moves)) continue;
                     float top = -INFINITY, heavy = -INFINITY;        // the largest score, and score plus log2 of the step
-                    float row_x = 0.0f, row_y = 0.0f;
 #pragma unroll
                     for (int t = 0; t < U; ++t)
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            const int i = 2 * k + e;
-                            if (mask && hidden(t, n, i)) continue;
-                            const float score = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], base4_of<T>(w[t].key(k)) * rw.sum[n][e]);
+                            if (mask && hidden(t, n, 2 * k + e)) continue;
+                            const float score = fmaf(step4_of(w[t].key(k)) * s[t][n][2 * k + e], rw.factor[n][e], base4_of<T>(w[t].key(k)) * rw.sum[n][e]);
                             top = fmaxf(top, score);
                             heavy = fmaxf(heavy, score + __log2f(step4_of(w[t].value(k))));
-                            row_x += x[t][n][i];
-                            row_y += y[t][n][i];
                         }
-                    int moves = !(row_x <= kMostWeight4 && row_y <= kMostProduct4);
-#pragma unroll
-                    for (int i = 4; i < 32; i <<= 1) moves |= __shfl_xor_sync(kFullMask, moves, i);
-                    if (!__any_sync(kFullMask, moves)) continue;
                     top = column_max(top);
                     heavy = column_max(heavy);
                     // (without a step above 0 there are no products)
@@ -527,38 +542,24 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                         o[n][d][e] *= f;
                         o[n][d][2 + e] *= f;
                     }
-#pragma unroll
-                    for (int t = 0; t < U; ++t)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int i = 2 * k + e;
-                            const float z = fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -to));
-                            const bool seen = !(mask && hidden(t, n, i));
-                            x[t][n][i] = seen ? exp2_fast(z) : 0.0f;
-                            y[t][n][i] = seen ? x[t][n][i] * step4_of(w[t].value(k)) : 0.0f;
-                        }
                 }
         }
 #pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                l[n][e] += sx[n][e];
+                r[n][e] += sr[n][e];
+            }
+#pragma unroll
         for (int t = 0; t < U; ++t) {
-            uint32_t b[NR][TERMS][2];
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int i = 0; i < TERMS; ++i)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        l[n][e] += x[t][n][2 * k + e];
-                        float v = base4_of<T>(w[t].value(k));
-                        if (mask && hidden(t, n, 2 * k + e)) v = 0.0f;
-                        r[n][e] = fmaf(x[t][n][2 * k + e], v, r[n][e]);
-                    }
-                    const uint32_t lead = pack_half2(y[t][n][2 * k], y[t][n][2 * k + 1]);
-                    b[n][0][k] = transpose_8x8(lead);
-                    if constexpr (F32)
-                        b[n][1][k] = transpose_8x8(pack_half2(y[t][n][2 * k] - half_lo(lead), y[t][n][2 * k + 1] - half_hi(lead)));
-                }
-            add_values4<T, D, NR>(tile + t * Geo::TILE, b, o);
+                    for (int k = 0; k < 2; ++k) b[t][n][i][k] = transpose_8x8(b[t][n][i][k]);
+            add_values4<T, D, NR>(tile + t * Geo::TILE, b[t], o);
         }
         __syncwarp();                                                // every lane has read the slot
         const int ahead = (j + STAGES) * U;                          // (a multiple of U, which divides 32)
@@ -607,36 +608,69 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
 
 // ---- the division of the work
 
-// Tiles of sequence b: units (key heads times row tiles) times tiles of its keys, one at least where it has tokens.
+// Grains of sequence b: units (key heads times row tiles) times grains of its keys, one at least where it has tokens.
 struct Share4 {
     int64_t token0;
-    int count, keys, row_tiles, tiles;
-    __device__ __forceinline__ Share4(const AttnParams& p, int b, int unit_rows) : token0(0), count(0), keys(0), row_tiles(0), tiles(1) {
+    int count, keys;
+    unsigned row_tiles, grains;
+    __device__ __forceinline__ Share4(const AttnParams& p, int b, int unit_rows, int grain) : token0(0), count(0), keys(0), row_tiles(0), grains(1) {
         if (b >= p.B) return;
         attn_tokens(p, b, token0, count);
-        if (count == 0) return;
         keys = attn_length(p, b);
-        row_tiles = (count * p.group + unit_rows - 1) / unit_rows;
-        tiles = max(1, (keys + kTileKeys - 1) / kTileKeys);
+        row_tiles = (static_cast<unsigned>(count) * p.group + unit_rows - 1) / unit_rows;
+        const unsigned keys_of_grain = static_cast<unsigned>(kTileKeys) << grain;
+        grains = max(1u, (static_cast<unsigned>(keys) + keys_of_grain - 1) / keys_of_grain);
     }
-    __device__ __forceinline__ int64_t cost(int hkv) const { return static_cast<int64_t>(hkv) * row_tiles * tiles; }
+    __device__ __forceinline__ unsigned cost(int hkv) const { return hkv * row_tiles * grains; }
 };
 
-__device__ __forceinline__ int64_t warp_sum64(int64_t x) {
+// Where a run (or a unit) lies among all grains: the sequence that holds grain `at`, the grains before that sequence, and all of them.
+struct Place4 {
+    int b;
+    unsigned before, total;
+};
+__device__ __forceinline__ unsigned run4_grains(unsigned total, int warps, int least) {
+    return max((total + warps - 1) / warps, static_cast<unsigned>(least));
+}
+__device__ __forceinline__ unsigned upto_lane(unsigned x) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 16; i; i >>= 1) x += __shfl_xor_sync(kFullMask, x, i);
+    for (int i = 1; i < 32; i <<= 1) {
+        const unsigned y = __shfl_up_sync(kFullMask, x, i);
+        if (lane >= i) x += y;
+    }
     return x;
 }
-// tiles of the sequences below `upto` (all lanes of a warp together)
-__device__ __forceinline__ int64_t tiles4_before(const AttnParams& p, int upto, int unit_rows) {
+// The place of run `run_no`; b = B where it has nothing to do.
+__device__ __forceinline__ Place4 find_run4(const Attn4Params& p, int unit_rows, unsigned run_no, unsigned& run) {
+    const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31;
-    int64_t sum = 0;
-    for (int b = lane; b < upto; b += 32) sum += Share4(p, b, unit_rows).cost(p.hkv);
-    return warp_sum64(sum);
-}
-__device__ __forceinline__ int64_t run4_tiles(int64_t total, int warps, int least) {
-    const int64_t even = (total + warps - 1) / warps;
-    return even > least ? even : least;
+    unsigned upto = upto_lane(Share4(a, lane, unit_rows, p.grain).cost(a.hkv));
+    unsigned total = __shfl_sync(kFullMask, upto, 31);
+    if (a.B > 32) {
+        unsigned more = 0;
+#pragma unroll 4
+        for (int b = 32 + lane; b < a.B; b += 32) more += Share4(a, b, unit_rows, p.grain).cost(a.hkv);
+        total += __reduce_add_sync(kFullMask, more);
+    }
+    run = run4_grains(total, p.warps, p.least);
+    Place4 at{0, 0, total};
+    const unsigned f = run * run_no;                   // (run * warps < 2^32: the host sees to it)
+    if (f >= total) return Place4{a.B, total, total};
+    for (;;) {
+        const unsigned past = __ballot_sync(kFullMask, at.before + upto > f);
+        if (past) {
+            const int i = __ffs(past) - 1;
+            const unsigned skipped = __shfl_sync(kFullMask, upto, max(i - 1, 0));
+            at.b += i;
+            at.before += i > 0 ? skipped : 0;
+            return at;
+        }
+        at.before += __shfl_sync(kFullMask, upto, 31);
+        at.b += 32;
+        if (at.b >= a.B) return at;                    // (lengths that changed meanwhile)
+        upto = upto_lane(Share4(a, at.b + lane, unit_rows, p.grain).cost(a.hkv));
+    }
 }
 
 template <typename T, int D, int NR>
@@ -655,50 +689,30 @@ attn4_kernel(const Attn4Params p) {
     grid_launch_dependents();
     if (a.q_start != nullptr)
         for (int head = blockIdx.x; head < a.hkv; head += gridDim.x) attn_uncovered<T, D>(a, head);
-    const int64_t total = tiles4_before(a, a.B, Geo::ROWS);
-    const int64_t run = run4_tiles(total, p.warps, p.least);
-    int64_t f = run * blockIdx.x;
-    const int64_t stop = min(f + run, total);
-    if (f >= stop) return;
-    // the sequence in which the run begins
-    int b = 0;
-    int64_t before = 0;
-    for (; b < a.B; b += 32) {
-        int64_t upto = Share4(a, b + lane, Geo::ROWS).cost(a.hkv);
-#pragma unroll
-        for (int i = 1; i < 32; i <<= 1) {
-            const int64_t x = __shfl_up_sync(kFullMask, upto, i);
-            if (lane >= i) upto += x;
-        }
-        const unsigned past = __ballot_sync(kFullMask, before + upto > f);
-        if (past) {
-            const int at = __ffs(past) - 1;
-            const int64_t skipped = __shfl_sync(kFullMask, upto, at > 0 ? at - 1 : 0);
-            before += at > 0 ? skipped : 0;
-            b += at;
-            break;
-        }
-        before += __shfl_sync(kFullMask, upto, 31);
-    }
-    for (; f < stop && b < a.B; ++b) {
-        const Share4 s(a, b, Geo::ROWS);
-        const int64_t cost = s.cost(a.hkv);
-        while (f < stop && f < before + cost) {
-            const int64_t unit = (f - before) / s.tiles, start = before + unit * s.tiles;
+    unsigned run;
+    const Place4 at = find_run4(p, Geo::ROWS, blockIdx.x, run);
+    unsigned f = run * blockIdx.x, before = at.before;
+    const unsigned stop = min(f + run, at.total);
+    for (int b = at.b; f < stop && b < a.B; ++b) {
+        const Share4 s(a, b, Geo::ROWS, p.grain);
+        const unsigned cost = s.cost(a.hkv);
+        while (f < stop && f - before < cost) {
+            const unsigned unit = (f - before) / s.grains, start = before + unit * s.grains;
             Segment4 u;
             u.token0 = s.token0;
             u.count = s.count;
             u.keys = s.keys;
             u.table = a.page_table + static_cast<int64_t>(b) * a.table_width;
             u.head = static_cast<int>(unit / s.row_tiles);
-            u.row0 = static_cast<int>(unit - static_cast<int64_t>(u.head) * s.row_tiles) * Geo::ROWS;
-            u.tile0 = static_cast<int>(f - start);
-            u.tile1 = static_cast<int>(min(stop - start, static_cast<int64_t>(s.tiles)));
+            u.row0 = static_cast<int>(unit - u.head * s.row_tiles) * Geo::ROWS;
+            const unsigned g0 = f - start, g1 = min(stop - start, s.grains);
+            u.tile0 = static_cast<int>(g0 << p.grain);
+            u.tile1 = static_cast<int>(g1 << p.grain);
             // a unit that began in an earlier run leaves its part in this one's first place, one that goes on in its second
-            u.slot = u.tile0 > 0 ? 2ll * blockIdx.x : u.tile1 < s.tiles ? 2ll * blockIdx.x + 1 : -1;
+            u.slot = g0 > 0 ? 2ll * blockIdx.x : g1 < s.grains ? 2ll * blockIdx.x + 1 : -1;
             attn4_segment<T, D, NR>(p, u, ring, smem4);
             __syncwarp();
-            f = start + u.tile1;
+            f = start + g1;
         }
         before += cost;
     }
@@ -709,30 +723,36 @@ attn4_kernel(const Attn4Params p) {
 template <typename T, int D>
 __global__ void __launch_bounds__(128)
 attn4_join_kernel(const Attn4Params p, int unit_rows) {
-    grid_dependency_wait();
     grid_launch_dependents();
     const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    if (row >= a.T * a.hq) return;
-    const int64_t t = row / a.hq;
-    const int h = static_cast<int>(row - t * a.hq), head = h / a.group;
-    const int b = attn_sequence_of(a, t);
-    const Share4 s(a, b, unit_rows);
-    if (t < s.token0 || t >= s.token0 + s.count) return;             // a token of no sequence
-    const int local = static_cast<int>(t - s.token0) * a.group + (h - head * a.group), rt = local / unit_rows;
-    int64_t before = 0, total = 0;
-    for (int i = lane; i < a.B; i += 32) {
-        const int64_t c = Share4(a, i, unit_rows).cost(a.hkv);
-        total += c;
-        before += i < b ? c : 0;
+    // where the row's parts lie follows from the call's inputs alone: found before the parts are there
+    int64_t w0 = 0;
+    int parts = 1, local = 0, rt = 0;
+    if (row < a.T * a.hq) {
+        const int64_t t = row / a.hq;
+        const int h = static_cast<int>(row - t * a.hq), head = h / a.group;
+        const int b = attn_sequence_of(a, t);
+        const Share4 s(a, b, unit_rows, p.grain);
+        unsigned total = 0, before = 0;
+#pragma unroll 4
+        for (int i = lane; i < a.B; i += 32) {
+            const unsigned c = Share4(a, i, unit_rows, p.grain).cost(a.hkv);
+            total += c;
+            before += i < b ? c : 0;
+        }
+        total = __reduce_add_sync(kFullMask, total);
+        before = __reduce_add_sync(kFullMask, before);
+        if (t >= s.token0 && t < s.token0 + s.count) {  // (else a token of no sequence)
+            local = static_cast<int>(t - s.token0) * a.group + (h - head * a.group);
+            rt = local / unit_rows;
+            const unsigned run = run4_grains(total, p.warps, p.least), start = before + (head * s.row_tiles + rt) * s.grains;
+            w0 = start / run;
+            parts = static_cast<int>((start + s.grains - 1) / run - w0) + 1;
+        }
     }
-    before = warp_sum64(before);
-    total = warp_sum64(total);
-    const int64_t run = run4_tiles(total, p.warps, p.least);
-    const int64_t start = before + (static_cast<int64_t>(head) * s.row_tiles + rt) * s.tiles;
-    const int64_t w0 = start / run;
-    const int parts = static_cast<int>((start + s.tiles - 1) / run - w0) + 1;
+    grid_dependency_wait();
     if (parts == 1) return;
     const int at = local - rt * unit_rows;
     auto slot = [&](int i) { return ((2 * (w0 + i) + (i == 0 ? 1 : 0)) * unit_rows + at); };

@@ -11,9 +11,10 @@ inline int row_tiles4(int64_t rows, int dtype) { return rows <= 8 ? 1 : rows <= 
 constexpr int resident4(int row_tiles, bool f32) { return row_tiles * (f32 ? 2 : 1) > 2 ? 8 : row_tiles * (f32 ? 2 : 1) > 1 ? 12 : 16; }
 
 constexpr int kLeastRun4 = 8;  // tiles of 16 keys: a shorter run would not pay for its start and its part of the join
+constexpr int kGrain4 = 1;     // log2 of the tiles in which work is counted: a step of the kernel takes two
 
 struct Attend4Plan {
-    int row_tiles, warps;
+    int row_tiles, warps, grain, least;
     size_t ml_bytes, o_bytes, lse_bytes, bytes;
 };
 
@@ -30,6 +31,10 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     const double runs = std::max(1.0, tiles / kLeastRun4 + 1.0);
     const int most = sms * resident4(f.row_tiles, dtype == WHT_F32);
     f.warps = runs < most ? static_cast<int>(runs) : most;
+    // grains are counted in 32 bits, with room for a run's worth beyond the last (wide tables of many sequences take larger ones)
+    f.grain = kGrain4;
+    while (units * static_cast<double>(div_up(static_cast<int64_t>(table_width) * page, 16ll << f.grain) + 1) > 2147483647.0 && f.grain < 26) ++f.grain;
+    f.least = std::max(1, kLeastRun4 >> f.grain);
     f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * rows * kPartStats);
     f.o_bytes = static_cast<size_t>(2) * f.warps * rows * D * sizeof(float);
     f.lse_bytes = weigh ? static_cast<size_t>(T) * Hq * sizeof(float) : 0;

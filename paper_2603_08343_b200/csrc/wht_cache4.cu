@@ -99,7 +99,8 @@ int wht_attn_paged4(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     a.scale_log2 = scale * wht::kLog2e;
     p.cache = static_cast<const unsigned char*>(cache);
     p.warps = f.warps;
-    p.least = kLeastRun4;
+    p.least = f.least;
+    p.grain = f.grain;
     p.lse = weights_out ? reinterpret_cast<float*>(ws + f.ml_bytes + f.o_bytes) : nullptr;
     p.weights = weights;
     p.weights_out = weights_out;
