@@ -28,11 +28,12 @@ void read(const Read4Params& p, int d, unsigned blocks, cudaStream_t s) {
 
 int launch_append4(Append4Params& p, int dtype, bool interleaved, int d, cudaStream_t s) {
     const int hb = dtype == WHT_F32 ? kHeads4<float> : kHeads4<__nv_bfloat16>;
-    p.q_groups = static_cast<int>(ceil_div(p.a.hq, hb));
-    p.kv_groups = static_cast<int>(ceil_div(p.a.hkv, hb));
-    p.per_token = p.q_groups + 2 * p.kv_groups;
-    const long long blocks = ceil_div(p.a.T * p.per_token * (d == 64 ? 4 : 8), kAppend4Threads);
+    p.a.q_blocks = static_cast<int>(ceil_div(p.a.hq, hb));
+    p.a.kv_blocks = static_cast<int>(ceil_div(p.a.hkv, hb));
+    const long long q_grid = ceil_div(p.a.T * p.a.q_blocks * (d / 16), kAppend4Threads);
+    const long long blocks = q_grid + ceil_div(p.a.T * 2 * p.a.kv_blocks * (d == 64 ? 4 : 8), kAppend4Threads);
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
+    p.q_grid = static_cast<int>(q_grid);
     const unsigned n = static_cast<unsigned>(blocks);
     if (dtype == WHT_F32) interleaved ? append<float, true>(p, d, n, s) : append<float, false>(p, d, n, s);
     else interleaved ? append<__nv_bfloat16, true>(p, d, n, s) : append<__nv_bfloat16, false>(p, d, n, s);
@@ -41,7 +42,7 @@ int launch_append4(Append4Params& p, int dtype, bool interleaved, int d, cudaStr
 }
 
 int launch_read4(const Read4Params& p, int dtype, int d, cudaStream_t s) {
-    const long long blocks = ceil_div(p.n * p.hkv * (d / 8), 256);
+    const long long blocks = ceil_div(p.n * ceil_div(p.hkv, kReadHeads4) * (d / 8), 256);
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     dtype == WHT_F32 ? read<float>(p, d, static_cast<unsigned>(blocks), s) : read<__nv_bfloat16>(p, d, static_cast<unsigned>(blocks), s);
     WHT_CUDA_TRY(cudaGetLastError());

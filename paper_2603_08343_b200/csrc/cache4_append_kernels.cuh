@@ -3,9 +3,9 @@
 //     q' = rotation(q)     row k' = rotation(k), row v: lo, step and codes (cache4_common.cuh)
 //
 // A pass over memory: each element is read once; queries are written as they came, keys and values in a quarter of the bytes or less.
-// Four lanes (D = 64) or eight own a row, 16 channels each as two groups of eight, so that a rotation's pairs never cross
-// lanes, the row's extremes take two or three shuffles, and each group of eight channels is one word of codes.  A thread takes the same channels of
-// several heads, all loads in flight at once; they share the angles.
+// Blocks take either queries or keys and values.  Four lanes (D = 64) or eight own a row of keys or values, 16 channels each as two groups of eight, so
+// that a rotation's pairs never cross lanes, the row's extremes take two or three shuffles, and each group of eight channels is one word of
+// codes.  A thread takes the same channels of several heads, all loads in flight at once; they share the angles.
 #pragma once
 #include "cache4_common.cuh"
 #include "kv_append_kernels.cuh"
@@ -13,10 +13,9 @@
 namespace wht {
 
 struct Append4Params {
-    AppendParams a;          // k_cache, v_cache, summary unused
+    AppendParams a;          // k_cache, v_cache, summary unused; q_blocks, kv_blocks: groups of heads that a thread takes
     unsigned char* cache;
-    int q_groups, kv_groups; // groups of heads that a thread takes
-    int per_token;           // q_groups + 2 * kv_groups
+    int q_grid;              // thread blocks of the queries, which come first
 };
 
 // where the tile of a slot's row lies, and its place in the tile
@@ -30,44 +29,74 @@ template <typename T>
 constexpr int kHeads4 = sizeof(T) == 4 ? 2 : 4;
 constexpr int kAppend4Threads = 256;
 
+// Queries: rotated and written; D / 16 lanes a row.
+template <typename T, bool INTERLEAVED, int D>
+__device__ __forceinline__ void append4_queries(const AppendParams& a, int64_t i) {
+    constexpr int HB = kHeads4<T>, PER = D / 16;
+    const int64_t job = i / PER, t = job / a.q_blocks;
+    const RowItem<T, INTERLEAVED> it(static_cast<int>(i - job * PER), a.rot);
+    if (t >= a.T) return;
+    const int h0 = static_cast<int>(job - t * a.q_blocks) * HB, heads = a.hq - h0;
+    const T* src = row_of<T>(a.q, t * a.q_st + h0 * a.q_sh);
+    T* dst = row_of<T>(a.q_out, (t * a.hq + h0) * D);
+    Raw8<T> lo[HB], hi[HB];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+        if (h < heads) {
+            lo[h].load(src + h * a.q_sh + it.lo);
+            hi[h].load(src + h * a.q_sh + it.hi);
+        }
+    }
+    if (it.angle < 0) {
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+            if (h < heads) {
+                lo[h].store(dst + h * D + it.lo);
+                hi[h].store(dst + h * D + it.hi);
+            }
+        }
+        return;
+    }
+    const int pos = checked_position(a, append_position(a, t));
+    float c[8], s[8];
+    load8(a.cos_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, c);
+    load8(a.sin_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, s);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+        if (h < heads) {
+            float x[8], y[8];
+            lo[h].widen(x);
+            hi[h].widen(y);
+            it.turn(x, y, c, s);
+            store8(dst + h * D + it.lo, x);
+            store8(dst + h * D + it.hi, y);
+        }
+    }
+}
+
 template <typename T, bool INTERLEAVED, int D>
 __global__ void __launch_bounds__(kAppend4Threads)
 kv_append4_kernel(const Append4Params p) {
     constexpr int HB = kHeads4<T>;
     constexpr int LANES = D == 64 ? 4 : 8;             // of a row
     const AppendParams& a = p.a;
-    const int64_t job = (static_cast<int64_t>(blockIdx.x) * kAppend4Threads + threadIdx.x) / LANES;
+    if (static_cast<int>(blockIdx.x) < p.q_grid) {
+        append4_queries<T, INTERLEAVED, D>(a, static_cast<int64_t>(blockIdx.x) * kAppend4Threads + threadIdx.x);
+        return;
+    }
+    const int64_t job = (static_cast<int64_t>(blockIdx.x - p.q_grid) * kAppend4Threads + threadIdx.x) / LANES;
     const int item = threadIdx.x % LANES;
-    const int64_t t = job / p.per_token;
-    int group = static_cast<int>(job - t * p.per_token);
+    const int64_t t = job / (2 * a.kv_blocks);
+    int group = static_cast<int>(job - t * 2 * a.kv_blocks);
+    const bool is_k = group < a.kv_blocks;
+    if (!is_k) group -= a.kv_blocks;
     const bool there = t < a.T && item < D / 16;       // (no lane leaves: rows fold by shuffles)
     const RowItem<T, INTERLEAVED> it(item < D / 16 ? item : 0, a.rot);
-    const bool is_q = group < p.q_groups;
-    bool turns = there && it.angle >= 0;
-    int pos = turns ? append_position(a, t) : 0;
-    int64_t slot = 0;
-    const T* src = nullptr;
-    int64_t step = 0;
-    int h0 = 0, heads = 0;
-    bool is_k = false;
-    if (there) {
-        if (is_q) {
-            h0 = group * HB;
-            heads = a.hq - h0;
-            src = row_of<T>(a.q, t * a.q_st + h0 * a.q_sh);
-            step = a.q_sh;
-        } else {
-            group -= p.q_groups;
-            is_k = group < p.kv_groups;
-            if (!is_k) group -= p.kv_groups;
-            slot = append_slot(a, t);
-            h0 = group * HB;
-            heads = slot < 0 ? 0 : a.hkv - h0;
-            src = is_k ? row_of<T>(a.k, t * a.k_st + h0 * a.k_sh) : row_of<T>(a.v, t * a.v_st + h0 * a.v_sh);
-            step = is_k ? a.k_sh : a.v_sh;
-            turns = turns && is_k && slot >= 0;
-        }
-    }
+    const int64_t slot = there ? append_slot(a, t) : -1;
+    int pos = there && it.angle >= 0 ? append_position(a, t) : 0;
+    const int h0 = group * HB, heads = slot < 0 ? 0 : a.hkv - h0;
+    const T* src = is_k ? row_of<T>(a.k, t * a.k_st + h0 * a.k_sh) : row_of<T>(a.v, t * a.v_st + h0 * a.v_sh);
+    const int64_t step = is_k ? a.k_sh : a.v_sh;
     Raw8<T> lo[HB], hi[HB];
 #pragma unroll
     for (int i = 0; i < HB; ++i) {
@@ -76,6 +105,7 @@ kv_append4_kernel(const Append4Params p) {
             hi[i].load(src + i * step + it.hi);
         }
     }
+    const bool turns = is_k && slot >= 0 && it.angle >= 0;
     float c[8], s[8];
     if (turns) {
         pos = checked_position(a, pos);
@@ -85,37 +115,29 @@ kv_append4_kernel(const Append4Params p) {
     const int place = static_cast<int>(slot & 15);
 #pragma unroll
     for (int i = 0; i < HB; ++i) {
+        if (__all_sync(kFullMask, i >= heads)) continue;
         float x[8], y[8];
-        bool finite = true;
-        float least = INFINITY, most = -INFINITY;
+        float least = INFINITY, most = -INFINITY, nought = 0.0f;   // nought: NaN as soon as a channel is not finite
         const bool mine = i < heads;
         if (mine) {
             lo[i].widen(x);
             hi[i].widen(y);
             if (turns) it.turn(x, y, c, s);
-            if (is_q) {
-                T* dst = row_of<T>(a.q_out, (t * a.hq + h0 + i) * D);
-                store8(dst + it.lo, x);
-                store8(dst + it.hi, y);
-            } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    least = fminf(least, fminf(x[e], y[e]));
-                    most = fmaxf(most, fmaxf(x[e], y[e]));
-                    finite = finite && fabsf(x[e]) < INFINITY && fabsf(y[e]) < INFINITY;
-                }
+            for (int e = 0; e < 8; ++e) {
+                least = fminf(least, fminf(x[e], y[e]));
+                most = fmaxf(most, fmaxf(x[e], y[e]));
+                nought = fmaf(x[e], 0.0f, fmaf(y[e], 0.0f, nought));
             }
         }
 #pragma unroll
         for (int n = 1; n < LANES; n <<= 1) {
             least = fminf(least, __shfl_xor_sync(kFullMask, least, n));
             most = fmaxf(most, __shfl_xor_sync(kFullMask, most, n));
+            nought += __shfl_xor_sync(kFullMask, nought, n);
         }
-        bool bad = !finite;
-#pragma unroll
-        for (int n = 1; n < LANES; n <<= 1) bad = bad || __shfl_xor_sync(kFullMask, static_cast<int>(bad), n);
-        if (!mine || is_q) continue;
-        const Hold4 hold(least, most, !bad);
+        if (!mine) continue;
+        const Hold4 hold(least, most, nought == 0.0f);
         unsigned char* tile = tile4_of(p.cache, slot, h0 + i, a.hkv, a.page_shift, D);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -142,41 +164,52 @@ struct Read4Params {
     int hkv, page_shift;
 };
 
-// A thread: eight channels of a key and of the value beside it.
+// A thread: eight channels of the keys and values of several heads at one slot, all loads in flight at once.
+constexpr int kReadHeads4 = 4;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 kv_read4_kernel(const Read4Params p) {
-    constexpr int PER = D / 8;
+    constexpr int PER = D / 8, HB = kReadHeads4;
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = i / PER;                       // slot number * hkv + head
-    const int octet = static_cast<int>(i - row * PER);
-    const int64_t at = row / p.hkv;
+    const int64_t job = i / PER;                       // slot number * groups of heads + group
+    const int octet = static_cast<int>(i - job * PER), groups = (p.hkv + HB - 1) / HB;
+    const int64_t at = job / groups;
     if (at >= p.n) return;
-    const int head = static_cast<int>(row - at * p.hkv);
+    const int h0 = static_cast<int>(job - at * groups) * HB;
     int64_t slot = __ldg(reinterpret_cast<const long long*>(p.slots) + at);
     if (slot >= p.num_slots) {
         attn_report(kAttnErrIndex);
         slot = -1;
     }
-    float k[8], v[8];
+    const int j = static_cast<int>(slot & 15), g = octet >> 2, u = 2 * (octet & 3);
+    unsigned kw[HB], vw[HB];
+    uint2 w[HB];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = v[e] = 0.0f;
-    if (slot >= 0) {
-        const unsigned char* tile = tile4_of(const_cast<unsigned char*>(p.cache), slot, head, p.hkv, p.page_shift, D);
-        const int j = static_cast<int>(slot & 15), g = octet >> 2, u = 2 * (octet & 3);
-        const unsigned kw = __ldg(reinterpret_cast<const unsigned*>(tile + key4_at(D, j, g, u)));
-        const unsigned vw = __ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u))) |
-                            static_cast<unsigned>(__ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u + 1)))) << 16;
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8));
-        const float ks = step4_of(w.x), kl = lo4_of(w.x), vs = step4_of(w.y), vl = lo4_of(w.y);
+    for (int h = 0; h < HB; ++h) {
+        kw[h] = vw[h] = 0;
+        w[h] = make_uint2(0, 0);
+        if (slot < 0 || h0 + h >= p.hkv) continue;
+        const unsigned char* tile = tile4_of(const_cast<unsigned char*>(p.cache), slot, h0 + h, p.hkv, p.page_shift, D);
+        kw[h] = __ldg(reinterpret_cast<const unsigned*>(tile + key4_at(D, j, g, u)));
+        vw[h] = __ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u))) |
+                static_cast<unsigned>(__ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u + 1)))) << 16;
+        w[h] = __ldg(reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8));
+    }
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+        if (h0 + h >= p.hkv) break;
+        const float ks = step4_of(w[h].x), kl = lo4_of(w[h].x), vs = step4_of(w[h].y), vl = lo4_of(w[h].y);
+        float k[8], v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            k[e] = __fadd_rn(kl, __fmul_rn(ks, static_cast<float>((kw >> (4 * e)) & 15u)));
-            v[e] = __fadd_rn(vl, __fmul_rn(vs, static_cast<float>((vw >> (4 * e)) & 15u)));
+            k[e] = __fadd_rn(kl, __fmul_rn(ks, code4_value(kw[h], e)));
+            v[e] = __fadd_rn(vl, __fmul_rn(vs, code4_value(vw[h], e)));
         }
+        const int64_t row = (at * p.hkv + h0 + h) * D + octet * 8;
+        store8(static_cast<T*>(p.k) + row, k);
+        store8(static_cast<T*>(p.v) + row, v);
     }
-    store8(static_cast<T*>(p.k) + row * D + octet * 8, k);
-    store8(static_cast<T*>(p.v) + row * D + octet * 8, v);
 }
 
 }  // namespace wht

@@ -29,10 +29,11 @@
 namespace wht {
 
 struct Attn4Params {
-    AttnParams a;            // queries, output, tables, lengths, sizes; part_ml, part_o: [2 * warps][rows of a unit]
+    AttnParams a;            // queries, output, tables, lengths, sizes; part_ml, part_o: [2 * warps][part_rows]
     const unsigned char* cache;
     int warps;               // runs
     int least;               // grains of a run, at least
+    int part_rows;           // rows of a part: those that a unit can have
     int grain;               // log2 of a grain's tiles: work is counted in grains, in 32 bits
     float* lse;              // [T * Hq] log2 of a row's softmax sum, or NULL
     const float* weights;    // [B x Hkv x table_width * page]: received so far
@@ -48,7 +49,7 @@ struct Attn4Geo {
     static constexpr int TERMS = F32 ? 2 : 1;                   // of queries and of weights
     static constexpr int TILE = tile4_bytes(D);
         static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
-    static constexpr int STAGES = U == 2 ? 3 : 4;               // steps of the ring
+    static constexpr int STAGES = U == 2 ? 2 : 4;               // steps of the ring
     static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
     static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;
     static constexpr int OFF_Q = STAGES * U * TILE;
@@ -596,12 +597,12 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                                              (o[n][2 * g + 1][e] * even + rr) * inv, (o[n][2 * g + 1][2 + e] * odd + rr) * inv);
                 const int ch = g * 32 + r4 * 4;
                 if (F32 || u.slot >= 0)
-                    *reinterpret_cast<float4*>(u.slot >= 0 ? a.part_o + (u.slot * Geo::ROWS + local) * D + ch : static_cast<float*>(a.out) + at * D + ch) = v;
+                    *reinterpret_cast<float4*>(u.slot >= 0 ? a.part_o + (u.slot * p.part_rows + local) * D + ch : static_cast<float*>(a.out) + at * D + ch) = v;
                 else
                     *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + ch) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
             }
             if (r4 != 0) continue;
-            if (u.slot >= 0) a.part_ml[u.slot * Geo::ROWS + local] = make_float2(m[n][e], ll);
+            if (u.slot >= 0) a.part_ml[u.slot * p.part_rows + local] = make_float2(m[n][e], ll);
             else if (p.lse) p.lse[at] = ll > 0.0f || ll != ll ? m[n][e] + log2f(ll) : INFINITY;
         }
 }
@@ -755,7 +756,7 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
     grid_dependency_wait();
     if (parts == 1) return;
     const int at = local - rt * unit_rows;
-    auto slot = [&](int i) { return ((2 * (w0 + i) + (i == 0 ? 1 : 0)) * unit_rows + at); };
+    auto slot = [&](int i) { return (2 * (w0 + i) + (i == 0 ? 1 : 0)) * p.part_rows + at; };
     float m = -INFINITY;
     for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[slot(i)].x);
 #pragma unroll

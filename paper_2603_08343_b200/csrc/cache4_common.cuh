@@ -52,13 +52,19 @@ struct Hold4 {
         inverse = step > 0.0f ? __fdiv_rn(1.0f, step) : 0.0f;
     }
     __device__ __forceinline__ unsigned code(float x) const {
-        const float y = __fmul_rn(__fsub_rn(x, lo), inverse);
-        // (a row that stands for NaN has inverse 0 and lo NaN: the conversion makes 0 of NaN)
-        return static_cast<unsigned>(max(0, min(15, __float2int_rn(y))));
+        // rounded to a whole number by the addition (2^23: the fraction has no bits left), which is cheaper than a conversion.  (A row that stands
+        // for NaN has inverse 0 and lo NaN: fmaxf makes 0 of NaN.)
+        const float y = fminf(fmaxf(__fmul_rn(__fsub_rn(x, lo), inverse), 0.0f), 15.0f);
+        return __float_as_uint(__fadd_rn(y, 8388608.0f)) & 15u;
     }
     // step in the lower half, lo in the upper
     __device__ __forceinline__ unsigned word() const { return (__float_as_uint(step) >> 16) | (__float_as_uint(lo) & 0xffff0000u); }
 };
+
+// the whole number that code e of a word stands for, without a conversion
+__device__ __forceinline__ float code4_value(unsigned word, int e) {
+    return __uint_as_float(((word >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.0f;
+}
 
 __device__ __forceinline__ float step4_of(unsigned word) { return __uint_as_float(word << 16); }
 __device__ __forceinline__ float lo4_of(unsigned word) { return __uint_as_float(word & 0xffff0000u); }

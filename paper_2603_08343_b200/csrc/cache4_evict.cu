@@ -9,7 +9,7 @@ using namespace wht;
 WHT_DEFINE_ATTN_ERROR_READER(take_attn_error_evict4)
 
 namespace {
-constexpr int kEvictThreads = 512;
+constexpr int kEvictThreads = 1024;
 
 template <int D>
 void move(const Evict4Params& p, unsigned blocks, cudaStream_t s) {

@@ -169,25 +169,14 @@ kv_evict4_choose_kernel(const Evict4Params p) {
     for (int64_t i = keep + tid; i < out_keys; i += THREADS) w_out[i] = 0.0f;
 }
 
-// A row of a tile in pieces that lie together: its codes of the key and of the value, then (step, lo).
+// Where 16-byte piece `piece` of row j lies in a tile: the codes of the key, then those of the value.
 template <int D>
-__device__ __forceinline__ void move_row4(const unsigned char* from, int j, unsigned char* to, int i, int piece) {
-    constexpr int KEY = D / 32;                        // 16-byte pieces of a key's codes
-    if (piece < KEY) {
-        *reinterpret_cast<uint4*>(to + i * (D / 2) + piece * 16) = __ldg(reinterpret_cast<const uint4*>(from + j * (D / 2) + piece * 16));
-    } else if constexpr (D == 128) {
-        const int u = piece - KEY;                     // eight pieces of 8 bytes, then (step, lo)
-        const int src = u < 8 ? 8 * D + value4_place(j) * 64 + ((u ^ (j & 4)) << 3) : tile4_rows(D) + j * 8;
-        const int dst = u < 8 ? 8 * D + value4_place(i) * 64 + ((u ^ (i & 4)) << 3) : tile4_rows(D) + i * 8;
-        *reinterpret_cast<uint2*>(to + dst) = __ldg(reinterpret_cast<const uint2*>(from + src));
-    } else if (piece < KEY + KEY) {                    // two pieces of 16 bytes, D = 96: one more from the section behind
-        const int u = piece - KEY;
-        const int src = u < 2 ? 8 * D + value4_place(j) * 32 + u * 16 : 8 * D + 512 + value4_place(j) * 16;
-        const int dst = u < 2 ? 8 * D + value4_place(i) * 32 + u * 16 : 8 * D + 512 + value4_place(i) * 16;
-        *reinterpret_cast<uint4*>(to + dst) = __ldg(reinterpret_cast<const uint4*>(from + src));
-    } else {
-        *reinterpret_cast<uint2*>(to + tile4_rows(D) + i * 8) = __ldg(reinterpret_cast<const uint2*>(from + tile4_rows(D) + j * 8));
-    }
+__device__ __forceinline__ int piece4_at(int j, int piece) {
+    constexpr int KEY = D / 32;                        // pieces of a key's codes, and of a value's
+    if (piece < KEY) return j * (D / 2) + piece * 16;
+    const int u = piece - KEY;
+    if constexpr (D == 128) return 8 * D + value4_place(j) * 64 + ((u * 16) ^ ((j & 4) << 3));
+    return u < 2 ? 8 * D + value4_place(j) * 32 + u * 16 : 8 * D + 512 + value4_place(j) * 16;
 }
 
 constexpr int kMove4Warps = 4;
@@ -195,7 +184,7 @@ constexpr int kMove4Warps = 4;
 template <int D>
 __global__ void __launch_bounds__(32 * kMove4Warps)
 kv_evict4_move_kernel(const Evict4Params p) {
-    constexpr int PIECES = D / 32 + (D == 128 ? 8 : D / 32) + 1;
+    constexpr int PIECES = D / 16, MINE = PIECES / 2;  // of a row, and of a lane: all of them in flight at once
     const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31;
     const int tiles = (p.budget + kTileKeys - 1) / kTileKeys;
@@ -229,13 +218,22 @@ kv_evict4_move_kernel(const Evict4Params p) {
         return;
     }
     unsigned char* to = p.cache + (((static_cast<int64_t>(out) * a.hkv + head) << shift) + (tile & in_page)) * tile4_bytes(D);
-#pragma unroll 4
-    for (int i = lane; i < (kTileKeys * PIECES + 31) / 32 * 32; i += 32) {
-        const int row = i / PIECES, piece = i - row * PIECES;
-        const int64_t src = __shfl_sync(kFullMask, from, row & 15);
-        if (row >= kTileKeys || src < 0) continue;
-        move_row4<D>(p.cache + (src >> 4) * tile4_bytes(D), static_cast<int>(src & 15), to, row, piece);
+    uint4 got[MINE];
+    uint2 row = make_uint2(0, 0);
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int n = i * 32 + lane, j = n / PIECES;
+        const int64_t src = __shfl_sync(kFullMask, from, j);
+        got[i] = make_uint4(0, 0, 0, 0);
+        if (src >= 0) got[i] = __ldg(reinterpret_cast<const uint4*>(p.cache + (src >> 4) * tile4_bytes(D) + piece4_at<D>(static_cast<int>(src & 15), n - j * PIECES)));
     }
+    if (from >= 0) row = __ldg(reinterpret_cast<const uint2*>(p.cache + (from >> 4) * tile4_bytes(D) + tile4_rows(D) + (from & 15) * 8));
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int n = i * 32 + lane, j = n / PIECES;
+        if (__shfl_sync(kFullMask, from, j) >= 0) *reinterpret_cast<uint4*>(to + piece4_at<D>(j, n - j * PIECES)) = got[i];
+    }
+    if (from >= 0) *reinterpret_cast<uint2*>(to + tile4_rows(D) + lane * 8) = row;
 }
 
 }  // namespace wht

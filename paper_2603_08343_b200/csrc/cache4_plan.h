@@ -14,7 +14,7 @@ constexpr int kLeastRun4 = 8;  // tiles of 16 keys: a shorter run would not pay 
 constexpr int kGrain4 = 1;     // log2 of the tiles in which work is counted: a step of the kernel takes two
 
 struct Attend4Plan {
-    int row_tiles, warps, grain, least;
+    int row_tiles, warps, grain, least, part_rows;
     size_t ml_bytes, o_bytes, lse_bytes, bytes;
 };
 
@@ -25,6 +25,7 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     const int group = Hq / Hkv;
     f.row_tiles = row_tiles4(static_cast<int64_t>(max_q_len) * group, dtype);
     const int rows = 8 * f.row_tiles;
+    f.part_rows = static_cast<int>(std::min<int64_t>(rows, static_cast<int64_t>(max_q_len) * group));
     // as many runs as fit the machine at once, unless the tables hold too few keys for that
     const double units = static_cast<double>(B) * Hkv * div_up(static_cast<int64_t>(max_q_len) * group, rows);
     const double tiles = units * static_cast<double>(std::max<int64_t>(1, static_cast<int64_t>(table_width) * page / 16));
@@ -35,8 +36,8 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     f.grain = kGrain4;
     while (units * static_cast<double>(div_up(static_cast<int64_t>(table_width) * page, 16ll << f.grain) + 1) > 2147483647.0 && f.grain < 26) ++f.grain;
     f.least = std::max(1, kLeastRun4 >> f.grain);
-    f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * rows * kPartStats);
-    f.o_bytes = static_cast<size_t>(2) * f.warps * rows * D * sizeof(float);
+    f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * f.part_rows * kPartStats);
+    f.o_bytes = static_cast<size_t>(2) * f.warps * f.part_rows * D * sizeof(float);
     f.lse_bytes = weigh ? static_cast<size_t>(T) * Hq * sizeof(float) : 0;
     f.bytes = f.ml_bytes + f.o_bytes + f.lse_bytes;
     return f;

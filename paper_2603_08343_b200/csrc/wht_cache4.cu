@@ -101,6 +101,7 @@ int wht_attn_paged4(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.warps = f.warps;
     p.least = f.least;
     p.grain = f.grain;
+    p.part_rows = f.part_rows;
     p.lse = weights_out ? reinterpret_cast<float*>(ws + f.ml_bytes + f.o_bytes) : nullptr;
     p.weights = weights;
     p.weights_out = weights_out;
