@@ -30,10 +30,10 @@ int launch_append4(Append4Params& p, int dtype, bool interleaved, int d, cudaStr
     const int hb = dtype == WHT_F32 ? kHeads4<float> : kHeads4<__nv_bfloat16>;
     p.a.q_blocks = static_cast<int>(ceil_div(p.a.hq, hb));
     p.a.kv_blocks = static_cast<int>(ceil_div(p.a.hkv, hb));
-    const long long q_grid = ceil_div(p.a.T * p.a.q_blocks * (d / 16), kAppend4Threads);
-    const long long blocks = q_grid + ceil_div(p.a.T * 2 * p.a.kv_blocks * (d == 64 ? 4 : 8), kAppend4Threads);
+    const long long kv_grid = ceil_div(p.a.T * 2 * p.a.kv_blocks * (d == 64 ? 4 : 8), kAppend4Threads);
+    const long long blocks = kv_grid + ceil_div(p.a.T * p.a.q_blocks * (d / 16), kAppend4Threads);
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
-    p.q_grid = static_cast<int>(q_grid);
+    p.kv_grid = static_cast<int>(kv_grid);
     const unsigned n = static_cast<unsigned>(blocks);
     if (dtype == WHT_F32) interleaved ? append<float, true>(p, d, n, s) : append<float, false>(p, d, n, s);
     else interleaved ? append<__nv_bfloat16, true>(p, d, n, s) : append<__nv_bfloat16, false>(p, d, n, s);

@@ -3,7 +3,7 @@
 //     q' = rotation(q)     row k' = rotation(k), row v: lo, step and codes (cache4_common.cuh)
 //
 // A pass over memory: each element is read once; queries are written as they came, keys and values in a quarter of the bytes or less.
-// Blocks take either queries or keys and values.  Four lanes (D = 64) or eight own a row of keys or values, 16 channels each as two groups of eight, so
+// Blocks take either queries or keys and values, whose arithmetic is several times as much.  Four lanes (D = 64) or eight own a row of keys or values, 16 channels each as two groups of eight, so
 // that a rotation's pairs never cross lanes, the row's extremes take two or three shuffles, and each group of eight channels is one word of
 // codes.  A thread takes the same channels of several heads, all loads in flight at once; they share the angles.
 #pragma once
@@ -15,7 +15,7 @@ namespace wht {
 struct Append4Params {
     AppendParams a;          // k_cache, v_cache, summary unused; q_blocks, kv_blocks: groups of heads that a thread takes
     unsigned char* cache;
-    int q_grid;              // thread blocks of the queries, which come first
+    int kv_grid;             // thread blocks of keys and values
 };
 
 // where the tile of a slot's row lies, and its place in the tile
@@ -80,11 +80,13 @@ kv_append4_kernel(const Append4Params p) {
     constexpr int HB = kHeads4<T>;
     constexpr int LANES = D == 64 ? 4 : 8;             // of a row
     const AppendParams& a = p.a;
-    if (static_cast<int>(blockIdx.x) < p.q_grid) {
-        append4_queries<T, INTERLEAVED, D>(a, static_cast<int64_t>(blockIdx.x) * kAppend4Threads + threadIdx.x);
+    // (blocks of rows compute where those of queries wait for memory: spread evenly among each other they share the SMs)
+    const int64_t before = static_cast<int64_t>(blockIdx.x) * p.kv_grid / gridDim.x, after = static_cast<int64_t>(blockIdx.x + 1ll) * p.kv_grid / gridDim.x;
+    if (after == before) {
+        append4_queries<T, INTERLEAVED, D>(a, (blockIdx.x - before) * kAppend4Threads + threadIdx.x);
         return;
     }
-    const int64_t job = (static_cast<int64_t>(blockIdx.x - p.q_grid) * kAppend4Threads + threadIdx.x) / LANES;
+    const int64_t job = (before * kAppend4Threads + threadIdx.x) / LANES;
     const int item = threadIdx.x % LANES;
     const int64_t t = job / (2 * a.kv_blocks);
     int group = static_cast<int>(job - t * 2 * a.kv_blocks);

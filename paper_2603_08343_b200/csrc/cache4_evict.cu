@@ -9,7 +9,7 @@ using namespace wht;
 WHT_DEFINE_ATTN_ERROR_READER(take_attn_error_evict4)
 
 namespace {
-constexpr int kEvictThreads = 1024;
+constexpr int kEvictThreads = 512;
 
 template <int D>
 void move(const Evict4Params& p, unsigned blocks, cudaStream_t s) {
@@ -17,23 +17,11 @@ void move(const Evict4Params& p, unsigned blocks, cudaStream_t s) {
 }
 }  // namespace
 
-int launch_evict4(Evict4Params& p, int d, cudaStream_t s) {
-    static int ready[kMaxDevices] = {};
-    int dev = 0, sms = 0;
-    const int rc = device_info(&dev, &sms);
-    if (rc != WHT_OK) return rc;
-    constexpr int kMost = 200 * 1024;
-    if (!ready[dev]) {
-        WHT_CUDA_TRY(cudaFuncSetAttribute(kv_evict4_choose_kernel<kEvictThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
-        ready[dev] = 1;
-    }
-    // the weights of one sequence and head stay in shared memory between the counts where they fit
-    const long long width = static_cast<long long>(p.a.table_width) << p.a.page_shift;
-    p.cached = static_cast<int>(width < kMost / 4 ? width : kMost / 4);
+int launch_evict4(const Evict4Params& p, int d, cudaStream_t s) {
     const long long rows = static_cast<long long>(p.a.B) * p.a.hkv;
     const long long blocks = ceil_div(rows * ceil_div(p.budget, kTileKeys), kMove4Warps);
     if (rows > 0x7fffffffll || blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
-    kv_evict4_choose_kernel<kEvictThreads><<<static_cast<unsigned>(rows), kEvictThreads, static_cast<size_t>(p.cached) * 4, s>>>(p);
+    kv_evict4_choose_kernel<kEvictThreads><<<static_cast<unsigned>(rows), kEvictThreads, 0, s>>>(p);
     WHT_CUDA_TRY(cudaGetLastError());
     const unsigned n = static_cast<unsigned>(blocks);
     d == 64 ? move<64>(p, n, s) : d == 96 ? move<96>(p, n, s) : move<128>(p, n, s);

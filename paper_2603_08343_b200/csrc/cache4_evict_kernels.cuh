@@ -2,7 +2,8 @@
 //
 // Two kernels.  The choice, a block per sequence and key head: the weights as ordered whole numbers; the spare-th largest found by
 // three counts of 11, 11 and 10 bits; then one walk in the order of the keys that lists what stays (above the threshold, or at it while there is
-// room: the lowest first).  Its bytes are 4 a key; what it costs is the chain of counts and scans.
+// room: the lowest first).  Its bytes are 4 a key; what it costs is the chain of counts and scans, so that the weights are asked for all at once
+// and the first 16384 stay in registers from there to the walk.
 // The move, a warp per 16 kept keys: a tile is gathered from wherever its rows lie and written as one piece, 2 (D + 8) bytes a row
 // moved, which memory bounds.
 #pragma once
@@ -19,7 +20,6 @@ struct Evict4Params {
     float* weights_out;      // [B x Hkv x out_width * page]
     int32_t *lens_out, *kept;  // [B], [B x Hkv x budget]
     int budget, first, last;
-    int cached;              // weights that the block's shared memory holds
 };
 
 constexpr int kEvictBins = 2048;
@@ -43,22 +43,29 @@ __device__ __forceinline__ unsigned block_scan4(unsigned x, unsigned* warp_sums,
     }
     if (lane == 31) warp_sums[warp] = upto;
     __syncthreads();
-    unsigned before = 0;
-    all = 0;
+    unsigned sums = lane < THREADS / 32 ? warp_sums[lane] : 0;       // (every warp adds them up: 32 at a time by shuffles)
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        const unsigned s = warp_sums[w];
-        before += w < warp ? s : 0;
-        all += s;
+    for (int i = 1; i < THREADS / 32; i <<= 1) {
+        const unsigned y = __shfl_up_sync(kFullMask, sums, i);
+        if (lane >= i) sums += y;
     }
+    all = __shfl_sync(kFullMask, sums, THREADS / 32 - 1);
+    unsigned before = __shfl_sync(kFullMask, sums, max(warp - 1, 0));
+    if (warp == 0) before = 0;
     __syncthreads();
     return before + upto - x;
 }
 
+// Four neighbouring weights from key i on; what lies behind the n-th is 0.
+__device__ __forceinline__ float4 weights4(const float* w, int i, int n) {
+    if (i + 3 < n) return __ldg(reinterpret_cast<const float4*>(w + i));
+    return make_float4(i < n ? __ldg(w + i) : 0.0f, i + 1 < n ? __ldg(w + i + 1) : 0.0f, i + 2 < n ? __ldg(w + i + 2) : 0.0f, 0.0f);
+}
+
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 2)
 kv_evict4_choose_kernel(const Evict4Params p) {
-    extern __shared__ __align__(16) unsigned evict_smem[];
+    constexpr int TILE = 4 * THREADS, HELD = 16384 / TILE;  // keys of a step, and steps whose weights stay in registers
     __shared__ unsigned bins[kEvictBins];
     __shared__ unsigned warp_sums[THREADS / 32];
     __shared__ unsigned found[2];                      // the bin that holds the threshold, and what is above it
@@ -76,9 +83,18 @@ kv_evict4_choose_kernel(const Evict4Params p) {
     float* w_out = p.weights_out + (static_cast<int64_t>(b) * a.hkv + head) * out_keys;
     int32_t* kept = p.kept + (static_cast<int64_t>(b) * a.hkv + head) * p.budget;
     if (head == 0 && tid == 0) p.lens_out[b] = keep;
+    float4 held[HELD];
+#pragma unroll
+    for (int r = 0; r < HELD; ++r) held[r] = weights4(w, r * TILE + 4 * tid, n);
+    // f(first key, four weights) for every step
+    auto walk = [&](auto f) {
+#pragma unroll
+        for (int r = 0; r < HELD; ++r)
+            if (r * TILE < n) f(r * TILE + 4 * tid, held[r]);
+        for (int base = HELD * TILE; base < n; base += TILE) f(base + 4 * tid, weights4(w, base + 4 * tid, n));
+    };
 
     const bool chosen = spare < to - from;             // (otherwise all stay)
-    const bool in_smem = chosen && n <= p.cached;
     unsigned threshold = 0, ties = 0;
     if (chosen && spare > 0) {
         unsigned known = 0, mask = 0, want = static_cast<unsigned>(spare);
@@ -87,19 +103,17 @@ kv_evict4_choose_kernel(const Evict4Params p) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, count = pass == 2 ? 1024 : 2048;
             for (int i = tid; i < count; i += THREADS) bins[i] = 0;
             __syncthreads();
-            for (int i = from + tid; i < to; i += THREADS) {
-                unsigned key;
-                if (pass == 0 || !in_smem) {
-                    key = ordered4(__ldg(w + i));
-                    if (in_smem) evict_smem[i] = key;
-                } else {
-                    key = evict_smem[i];
+            walk([&](int i, const float4& v) {
+                const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned key = ordered4(x[e]);
+                    if (i + e >= from && i + e < to && (key & mask) == known) atomicAdd(&bins[(key >> shift) & (count - 1)], 1u);
                 }
-                if ((key & mask) == known) atomicAdd(&bins[(key >> shift) & (count - 1)], 1u);
-            }
+            });
             __syncthreads();
-            // from the top: each thread four (two) bins, the highest first
-            const int per = count / THREADS, top = count - 1 - tid * per;
+            // from the top: each thread a few bins, the highest first
+            const int per = (count + THREADS - 1) / THREADS, top = count - 1 - tid * per;
             unsigned mine = 0;
             for (int i = 0; i < per; ++i) mine += bins[top - i];
             unsigned all;
@@ -124,19 +138,10 @@ kv_evict4_choose_kernel(const Evict4Params p) {
         ties = want;                                   // of the keys at the threshold, this many stay
     }
 
-    // the walk: four neighbouring keys a thread and step
     unsigned written = 0, tied = 0;
-    for (int base = 0; base < n; base += 4 * THREADS) {
-        const int i0 = base + 4 * tid;
-        float x[4];
+    walk([&](int i0, const float4& v) {
+        const float x[4] = {v.x, v.y, v.z, v.w};
         unsigned above = 0, at = 0;                    // bits: stays in any case; at the threshold
-        if (i0 + 3 < n) {
-            const float4 v = __ldg(reinterpret_cast<const float4*>(w + i0));
-            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = i0 + e < n ? __ldg(w + i0 + e) : 0.0f;
-        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = i0 + e;
@@ -164,7 +169,7 @@ kv_evict4_choose_kernel(const Evict4Params p) {
         }
         written += (all & 0xffffu) + (min(tied + (all >> 16), ties) - min(tied, ties));
         tied += all >> 16;
-    }
+    });
     for (int64_t i = keep + tid; i < p.budget; i += THREADS) kept[i] = -1;
     for (int64_t i = keep + tid; i < out_keys; i += THREADS) w_out[i] = 0.0f;
 }
