@@ -61,6 +61,16 @@ int weigh4(const Attn4Params& p, bool after, int dev, cudaStream_t s) {
     return WHT_OK;
 }
 
+int weigh4_scores(const Attn4Params& p, cudaStream_t s) {
+    const long long keys = static_cast<long long>(p.a.table_width) << p.a.page_shift;
+    const long long chunks = ceil_div(keys, 1024), blocks = chunks * p.a.hkv * p.a.B;
+    if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
+    if (blocks == 0) return WHT_OK;
+    launch_overlapped(attn4_weigh_scores_kernel, dim3(static_cast<unsigned>(blocks)), 256, 0, s, p, static_cast<int>(chunks));
+    WHT_CUDA_TRY(cudaGetLastError());
+    return WHT_OK;
+}
+
 template <typename T, int D>
 int weigh4_d(const Attn4Params& p, bool few_rows, bool after, int dev, cudaStream_t s) {
     if constexpr (std::is_same<T, float>::value) return weigh4<T, D, 1>(p, after, dev, s);  // (two terms: registers for one tile)
@@ -75,6 +85,7 @@ int launch_attend4(const Attn4Params& p, int row_tiles, int d, int dev, cudaStre
 }
 template <typename T>
 int launch_weigh4(const Attn4Params& p, bool few_rows, bool after, int d, int dev, cudaStream_t s) {
+    if (p.scores != nullptr) return weigh4_scores(p, s);
     return d == 64 ? weigh4_d<T, 64>(p, few_rows, after, dev, s)
                    : d == 96 ? weigh4_d<T, 96>(p, few_rows, after, dev, s) : weigh4_d<T, 128>(p, few_rows, after, dev, s);
 }

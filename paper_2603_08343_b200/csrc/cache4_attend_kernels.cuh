@@ -36,6 +36,7 @@ struct Attn4Params {
     int part_rows;           // rows of a part: those that a unit can have
     int grain;               // log2 of a grain's tiles: work is counted in grains, in 32 bits
     float* lse;              // [T * Hq] log2 of a row's softmax sum, or NULL
+    float* scores;           // [B * Hkv][tile][part_rows][16] log2 scores, or NULL: they are taken anew for the received weight
     const float* weights;    // [B x Hkv x table_width * page]: received so far
     float* weights_out;
 };
@@ -364,6 +365,7 @@ struct Segment4 {
     int head, row0;          // key head, first row of the unit: row r is token r / group, query head head * group + r % group
     int tile0, tile1;        // of the unit's tiles
     int64_t slot;            // where the part goes, or -1: the unit is finished here
+    float* scores;           // where the scores of the sequence and key head go, or NULL
 };
 
 // A warp's ring of tiles: how many have been asked for and taken since the start, over all its segments.
@@ -460,6 +462,17 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         for (int t = 0; t < U; ++t) {
             scores4<T, D, NR>(rw, tile + t * Geo::TILE, q_smem, s[t]);
             w[t].load(tile + t * Geo::TILE + tile4_rows(D));
+        }
+        if (NR == 1 && u.scores != nullptr) {
+#pragma unroll
+            for (int t = 0; t < U; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = i >> 1, e = i & 1, at = u.tile0 + j * U + t;
+                    if (2 * c4 + e < rows && j * U + t < tiles)
+                        u.scores[(static_cast<int64_t>(at) * p.part_rows + 2 * c4 + e) * kTileKeys + 8 * k + r4] =
+                            fmaf(step4_of(w[t].key(k)) * s[t][0][i], rw.factor[0][e], base4_of<T>(w[t].key(k)) * rw.sum[0][e]);
+                }
         }
         auto hidden = [&](int t, int n, int i) { return base + t * kTileKeys + 8 * (i >> 1) + r4 >= limit(n, i & 1); };
         // One score against the row's reference: its weight, and that times its value's step.
@@ -711,6 +724,7 @@ attn4_kernel(const Attn4Params p) {
             u.tile1 = static_cast<int>(g1 << p.grain);
             // a unit that began in an earlier run leaves its part in this one's first place, one that goes on in its second
             u.slot = g0 > 0 ? 2ll * blockIdx.x : g1 < s.grains ? 2ll * blockIdx.x + 1 : -1;
+            u.scores = p.scores == nullptr ? nullptr : p.scores + (static_cast<int64_t>(b) * a.hkv + u.head) * (static_cast<int64_t>(a.table_width) << a.page_shift) * p.part_rows;
             attn4_segment<T, D, NR>(p, u, ring, smem4);
             __syncwarp();
             f = start + g1;
@@ -799,6 +813,46 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
 }
 
 // ---- the weight that each key receives: weights_out = weights + sum over the sequence's tokens and the group's heads of exp(score - lse).
+// Sequences of up to eight rows a key head: the attention has left the scores, four bytes a row and key; to take them again from the
+// codes costs D / 2 + 8 bytes a key and the products (32 x 8192 keys, 4 rows: 48 us against 12).
+// Four keys a thread.
+__global__ static void __launch_bounds__(256)
+attn4_weigh_scores_kernel(const Attn4Params p, int chunks) {
+    const AttnParams& a = p.a;
+    const int chunk = static_cast<int>(blockIdx.x % chunks);
+    const int head = static_cast<int>((blockIdx.x / chunks) % a.hkv), b = static_cast<int>(blockIdx.x / chunks / a.hkv);
+    const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
+    const int64_t key0 = static_cast<int64_t>(chunk) * 1024 + 4 * threadIdx.x, at = (static_cast<int64_t>(b) * a.hkv + head) * width + key0;
+    int64_t token0;
+    int count;
+    attn_tokens(a, b, token0, count);
+    const int keys = attn_length(a, b), rows = count * a.group;
+    const bool there = key0 < keys;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (there && p.weights != nullptr) v = *reinterpret_cast<const float4*>(p.weights + at);
+    grid_dependency_wait();                                          // scores and sums come from the kernels before
+    if (key0 >= width) return;
+    if (there) {
+        const float* score = p.scores + (at - key0 % kTileKeys) * p.part_rows + key0 % kTileKeys;
+        float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int row = 0; row < rows; ++row) {
+            const int tok = row / a.group;
+            const float lse = __ldcg(p.lse + (token0 + tok) * a.hq + static_cast<int64_t>(head) * a.group + (row - tok * a.group));
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(score + row * kTileKeys));
+            const int64_t limit = static_cast<int64_t>(keys) - count + tok + 1 - key0;     // of these keys, those that the row sees
+            if (limit > 0) add.x += exp2_fast(x.x - lse);
+            if (limit > 1) add.y += exp2_fast(x.y - lse);
+            if (limit > 2) add.z += exp2_fast(x.z - lse);
+            if (limit > 3) add.w += exp2_fast(x.w - lse);
+        }
+        const int64_t here = keys - key0;
+        v = make_float4(v.x + add.x, here > 1 ? v.y + add.y : 0.0f, here > 2 ? v.z + add.z : 0.0f, here > 3 ? v.w + add.w : 0.0f);
+    }
+    *reinterpret_cast<float4*>(p.weights_out + at) = v;
+}
+
+// More rows, or more scores than there should be memory for:
 // A warp takes kWeightTiles tiles of one sequence and key head and goes through all rows that read them; one owner per key, so the sum has
 // one order.  Places from the sequence's length on become 0.
 constexpr int kWeightTiles = 32;

@@ -15,7 +15,7 @@ constexpr int kGrain4 = 1;     // log2 of the tiles in which work is counted: a 
 
 struct Attend4Plan {
     int row_tiles, warps, grain, least, part_rows;
-    size_t ml_bytes, o_bytes, lse_bytes, bytes;
+    size_t ml_bytes, o_bytes, lse_bytes, scores_bytes, bytes;
 };
 
 inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D,
@@ -38,8 +38,11 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     f.least = std::max(1, kLeastRun4 >> f.grain);
     f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * f.part_rows * kPartStats);
     f.o_bytes = static_cast<size_t>(2) * f.warps * f.part_rows * D * sizeof(float);
-    f.lse_bytes = weigh ? static_cast<size_t>(T) * Hq * sizeof(float) : 0;
-    f.bytes = f.ml_bytes + f.o_bytes + f.lse_bytes;
+    f.lse_bytes = weigh ? up256(static_cast<size_t>(T) * Hq * sizeof(float)) : 0;
+    // the scores of few rows are kept for the received weight, in a gigabyte at most
+    const double scores = 4.0 * f.part_rows * B * Hkv * static_cast<double>(table_width) * page;
+    f.scores_bytes = weigh && f.row_tiles == 1 && scores <= 1073741824.0 ? static_cast<size_t>(scores) : 0;
+    f.bytes = f.ml_bytes + up256(f.o_bytes) + f.lse_bytes + f.scores_bytes;
     return f;
 }
 

@@ -102,7 +102,8 @@ int wht_attn_paged4(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.least = f.least;
     p.grain = f.grain;
     p.part_rows = f.part_rows;
-    p.lse = weights_out ? reinterpret_cast<float*>(ws + f.ml_bytes + f.o_bytes) : nullptr;
+    p.lse = weights_out ? reinterpret_cast<float*>(ws + f.ml_bytes + up256(f.o_bytes)) : nullptr;
+    p.scores = f.scores_bytes ? reinterpret_cast<float*>(ws + f.ml_bytes + up256(f.o_bytes) + f.lse_bytes) : nullptr;
     p.weights = weights;
     p.weights_out = weights_out;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
