@@ -450,11 +450,11 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
 
     unsigned stage = ring.taken % STAGES, parity = (ring.taken / STAGES) & 1u;
     ring.taken += steps;
-    for (int j = 0; j < steps; ++j) {
+    auto step = [&](int j, auto masked) {
+        constexpr bool mask = masked.value;                          // rows may see less than all of these keys
         mbar_wait_bounded(ring.full + stage, parity);
         const unsigned char* tile = ring.base + stage * U * Geo::TILE;
         const int base = (u.tile0 + j * U) * kTileKeys;
-        const bool mask = base + U * kTileKeys > least_limit;
 
         float s[U][NR][4];
         Params4 w[U];
@@ -484,7 +484,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         // This lane's sums of a row: weights, weights times base values, products; and the products as operands, before their transposition.
         float sx[NR][2], sr[NR][2], sy[NR][2];
         uint32_t b[U][NR][TERMS][2];
-        auto add_up = [&](auto masked) {
+        auto add_up = [&] {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
                 sx[n][0] = sx[n][1] = sr[n][0] = sr[n][1] = sy[n][0] = sy[n][1] = 0.0f;
@@ -499,7 +499,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                             float x;
                             weigh(t, n, 2 * k + e, x, y[e]);
                             bool seen = true;
-                            if constexpr (masked.value) seen = !hidden(t, n, 2 * k + e);
+                            if constexpr (mask) seen = !hidden(t, n, 2 * k + e);
                             if (!seen) y[e] = x = 0.0f;
                             sx[n][e] += x;
                             sy[n][e] += y[e];
@@ -510,19 +510,15 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                     }
             }
         };
-        bool moved = false;                                          // (once a step: what is NaN stays NaN)
-        for (bool careful = mask;; careful = true) {
-            if (careful) add_up(std::true_type{});
-            else add_up(std::false_type{});
-            float all_x = 0.0f, all_y = 0.0f;
+        add_up();
+        float all_x = 0.0f, all_y = 0.0f;
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                all_x += sx[n][0] + sx[n][1];
-                all_y += sy[n][0] + sy[n][1];
-            }
-            // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
-            if (moved || __all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) break;
-            moved = true;
+        for (int n = 0; n < NR; ++n) {
+            all_x += sx[n][0] + sx[n][1];
+            all_y += sy[n][0] + sy[n][1];
+        }
+        // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
+        if (!__all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -557,6 +553,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                         o[n][d][2 + e] *= f;
                     }
                 }
+            add_up();
         }
 #pragma unroll
         for (int n = 0; n < NR; ++n)
@@ -591,7 +588,11 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
             stage = 0;
             parity ^= 1u;
         }
-    }
+    };
+    // steps whose keys all rows see, then the others
+    const int open = least_limit > u.tile0 * kTileKeys ? min(steps, (least_limit - u.tile0 * kTileKeys) / (U * kTileKeys)) : 0;
+    for (int j = 0; j < open; ++j) step(j, std::false_type{});
+    for (int j = open; j < steps; ++j) step(j, std::true_type{});
 
     // the results, four channels of a row at a time
 #pragma unroll
