@@ -167,7 +167,7 @@ struct Read4Params {
 };
 
 // A thread: eight channels of the keys and values of several heads at one slot, all loads in flight at once.
-constexpr int kReadHeads4 = 4;
+constexpr int kReadHeads4 = 2;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256)

@@ -37,10 +37,7 @@ int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
 
 template <typename T, int D>
 int attend4_d(const Attn4Params& p, int row_tiles, int dev, cudaStream_t s) {
-    if (row_tiles == 1) return attend4<T, D, 1>(p, dev, s);
-    if constexpr (!std::is_same<T, float>::value)
-        if (row_tiles == 4) return attend4<T, D, 4>(p, dev, s);
-    return attend4<T, D, 2>(p, dev, s);
+    return row_tiles == 1 ? attend4<T, D, 1>(p, dev, s) : attend4<T, D, 2>(p, dev, s);
 }
 
 template <typename T, int D, int NR>

@@ -5,8 +5,9 @@
 
 namespace wht_plan {
 
-// 8-row tiles of a unit (fp32 rows are two terms: half as many).
-inline int row_tiles4(int64_t rows, int dtype) { return rows <= 8 ? 1 : rows <= 16 || dtype == WHT_F32 ? 2 : 4; }
+// 8-row tiles of a unit.  (Four take a quarter of the instructions for the codes, but 255 registers, so that eight warps fit an SM: 8 x 64 questions over 5000
+// keys 62 us against 51, 100 tokens over 1000 25 us against 11; only 128 tokens over 30000 keys, 242 against 271, are better off.)
+inline int row_tiles4(int64_t rows) { return rows <= 8 ? 1 : 2; }
 // One-warp blocks that an SM holds at once.
 constexpr int resident4(int row_tiles, bool f32) { return row_tiles * (f32 ? 2 : 1) > 2 ? 8 : row_tiles * (f32 ? 2 : 1) > 1 ? 12 : 16; }
 
@@ -23,7 +24,7 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     Attend4Plan f{};
     if (T == 0) return f;
     const int group = Hq / Hkv;
-    f.row_tiles = row_tiles4(static_cast<int64_t>(max_q_len) * group, dtype);
+    f.row_tiles = row_tiles4(static_cast<int64_t>(max_q_len) * group);
     const int rows = 8 * f.row_tiles;
     f.part_rows = static_cast<int>(std::min<int64_t>(rows, static_cast<int64_t>(max_q_len) * group));
     // as many runs as fit the machine at once, unless the tables hold too few keys for that
