@@ -126,7 +126,7 @@ struct Query4 {
         }
         top = quad_max(top);
         total = quad_sum(total);
-        const int e = top > 0.0f ? max(exponent_of(top) - 13, -100) : 0;  // the largest becomes 2^13 and up to 2^14
+        const int e = top > 0.0f ? max(exponent_of(top) - 13, -113) : 0;  // the largest becomes 2^13 and up to 2^14
         const float shift = power_of_two(-e);
         factor = scale_log2 * power_of_two(e) * 16777216.0f;
         sum = scale_log2 * total;
@@ -766,6 +766,7 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
             const unsigned run = run4_grains(total, p.warps, p.least), start = before + (head * s.row_tiles + rt) * s.grains;
             w0 = start / run;
             parts = static_cast<int>((start + s.grains - 1) / run - w0) + 1;
+            if (w0 + parts > p.warps) parts = 1;       // (offsets that make no sense)
         }
     }
     grid_dependency_wait();

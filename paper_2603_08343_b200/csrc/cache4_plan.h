@@ -28,7 +28,10 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     const int rows = 8 * f.row_tiles;
     f.part_rows = static_cast<int>(std::min<int64_t>(rows, static_cast<int64_t>(max_q_len) * group));
     // as many runs as fit the machine at once, unless the tables hold too few keys for that
-    const double units = static_cast<double>(B) * Hkv * div_up(static_cast<int64_t>(max_q_len) * group, rows);
+    // (a sequence's last row tile may be a short one; offsets that let sequences overlap, which no call should have, may make for more units: the
+    // kernels then stay within their bounds)
+    const double units = static_cast<double>(Hkv) * std::min(static_cast<double>(B) * div_up(std::min<int64_t>(max_q_len, T) * group, rows),
+                                                             static_cast<double>(div_up(T * group, rows) + B));
     const double tiles = units * static_cast<double>(std::max<int64_t>(1, static_cast<int64_t>(table_width) * page / 16));
     const double runs = std::max(1.0, tiles / kLeastRun4 + 1.0);
     const int most = sms * resident4(f.row_tiles, dtype == WHT_F32);
