@@ -20,7 +20,8 @@ SOURCES = ["wht_affine.cu", "family_misc.cu", "family_bfly_fwd.cu", "family_bfly
            "family_mma.cu", "family_umma_fwd.cu", "family_umma_bwd.cu", "family_umma_tp.cu",
            "wht_attention.cu", "attn_append.cu", "attn_paged_bf16.cu", "attn_paged_f32.cu", "attn_select.cu",
            "attn_umma.cu", "attn_tma.cu",
-           "wht_cache4.cu", "cache4_append.cu", "cache4_attend_bf16.cu", "cache4_attend_f32.cu", "cache4_evict.cu"]
+           "wht_cache4.cu", "cache4_append.cu", "cache4_attend_bf16.cu", "cache4_attend_f32.cu", "cache4_umma.cu",
+           "cache4_evict.cu"]
 PYTHON_SOURCE = "attn_python.cpp"  # the Python entry of the serving attention: a CPython module beside the library
 PYTHON_PATH = os.path.join(HERE, "_attention.so")
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]

@@ -1,6 +1,8 @@
 // How a call of the attention over the 4-bit cache divides its work, and the workspace that follows from it.  Host arithmetic alone (no
 // CUDA), so that every shape can be checked without a device.
 #pragma once
+#include <cmath>
+
 #include "attn_plan.h"
 
 namespace wht_plan {
@@ -14,7 +16,22 @@ constexpr int resident4(int row_tiles, bool f32) { return row_tiles * (f32 ? 2 :
 constexpr int kLeastRun4 = 8;  // tiles of 16 keys: a shorter run would not pay for its start and its part of the join
 constexpr int kGrain4 = 1;     // log2 of the tiles in which work is counted: a step of the kernel takes two
 
+// Prompts of bf16 queries on tcgen05: rows of a unit, log2 of the tiles of a grain (a step takes 64 keys), blocks that an SM holds.
+constexpr int kUmma4Rows = 256, kUmma4Grain = 2, kUmma4Resident = 1;
+// Whether the tcgen05 kernel is the faster one, by a small model of both (lengths being on the device, as if the tables were full): a start of 30 us and
+// 1.9 us a step of 256 rows and 64 keys in a block, against 10 us and 0.085 us an SM (D = 128; 0.065 with D = 64) for 16 rows and
+// 16 keys in the kernel of few rows.
+// us, tcgen05 and the other: 128 tokens of 4 rows over 30000 keys, 8 key heads, 122 (269); 2048 over 4000 220 (515); 64 over 20000 74 (104); 100 over 10000
+// 87 (83); 16 x 128 over 2000 147 (134); 8 x 64 over 5000, 4 key heads, D = 96, 67 (51); 400 tokens of 32 heads over 800 50 (37); 256 over 300 45 (19).
+inline bool umma4_pays(int64_t keys, int64_t T, int32_t B, int group, int32_t Hkv, int32_t D, int sms) {
+    const double rows = static_cast<double>(T) * group, k = static_cast<double>(keys);
+    const double umma = 30.0 + 1.9 * std::ceil(Hkv * (rows / kUmma4Rows + 0.5 * B) * (k / 64) / sms);
+    const double other = 10.0 + (0.045 + D / 3200.0) * Hkv * (rows / 16 + 0.5 * B) * (k / 16) / sms;
+    return umma < other;
+}
+
 struct Attend4Plan {
+    bool umma;
     int row_tiles, warps, grain, least, part_rows;
     size_t ml_bytes, o_bytes, lse_bytes, scores_bytes, bytes;
 };
@@ -24,8 +41,9 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
     Attend4Plan f{};
     if (T == 0) return f;
     const int group = Hq / Hkv;
+    f.umma = dtype == WHT_BF16 && static_cast<int64_t>(max_q_len) * group > 16 && umma4_pays(static_cast<int64_t>(table_width) * page, T, B, group, Hkv, D, sms);
     f.row_tiles = row_tiles4(static_cast<int64_t>(max_q_len) * group);
-    const int rows = 8 * f.row_tiles;
+    const int rows = f.umma ? kUmma4Rows : 8 * f.row_tiles;
     f.part_rows = static_cast<int>(std::min<int64_t>(rows, static_cast<int64_t>(max_q_len) * group));
     // as many runs as fit the machine at once, unless the tables hold too few keys for that
     // (a sequence's last row tile may be a short one; offsets that let sequences overlap, which no call should have, may make for more units: the
@@ -34,10 +52,10 @@ inline Attend4Plan plan_attend4(int32_t table_width, int64_t T, int32_t B, int32
                                                              static_cast<double>(div_up(T * group, rows) + B));
     const double tiles = units * static_cast<double>(std::max<int64_t>(1, static_cast<int64_t>(table_width) * page / 16));
     const double runs = std::max(1.0, tiles / kLeastRun4 + 1.0);
-    const int most = sms * resident4(f.row_tiles, dtype == WHT_F32);
+    const int most = sms * (f.umma ? kUmma4Resident : resident4(f.row_tiles, dtype == WHT_F32));
     f.warps = runs < most ? static_cast<int>(runs) : most;
     // grains are counted in 32 bits, with room for a run's worth beyond the last (wide tables of many sequences take larger ones)
-    f.grain = kGrain4;
+    f.grain = f.umma ? kUmma4Grain : kGrain4;
     while (units * static_cast<double>(div_up(static_cast<int64_t>(table_width) * page, 16ll << f.grain) + 1) > 2147483647.0 && f.grain < 26) ++f.grain;
     f.least = std::max(1, kLeastRun4 >> f.grain);
     f.ml_bytes = up256(static_cast<size_t>(2) * f.warps * f.part_rows * kPartStats);

@@ -179,14 +179,15 @@ int wht_attn_device_status(void) {
     WHT_CUDA_TRY(cudaDeviceSynchronize());
     unsigned any = 0;
     for (auto take : {take_attn_error_append, take_attn_error_paged_bf16, take_attn_error_paged_f32, take_attn_error_select,
-                      take_attn_error_umma, take_attn_error_append4, take_attn_error_attend4_bf16, take_attn_error_attend4_f32, take_attn_error_evict4}) {
+                      take_attn_error_umma, take_attn_error_append4, take_attn_error_attend4_bf16, take_attn_error_attend4_f32,
+                      take_attn_error_umma4, take_attn_error_evict4}) {
         unsigned flag = 0;
         const int rc = take(&flag);
         if (rc != WHT_OK) return rc;
         any |= flag;
     }
     for (auto take : {take_device_error_attn_umma, take_device_error_attn_paged_bf16, take_device_error_attn_paged_f32,
-                      take_device_error_attend4_bf16, take_device_error_attend4_f32}) {
+                      take_device_error_attend4_bf16, take_device_error_attend4_f32, take_device_error_umma4}) {
         unsigned waits = 0;
         const int rc = take(&waits);
         if (rc != WHT_OK) return rc;

@@ -108,7 +108,8 @@ int wht_attn_paged4(const void* q, int64_t q_stride_t, int64_t q_stride_h, const
     p.weights_out = weights_out;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (T > 0) {
-        rc = dtype == WHT_F32 ? launch_attend4<float>(p, f.row_tiles, D, dev, s) : launch_attend4<__nv_bfloat16>(p, f.row_tiles, D, dev, s);
+        rc = f.umma ? launch_attend4_umma(p, D, dev, s)
+             : dtype == WHT_F32 ? launch_attend4<float>(p, f.row_tiles, D, dev, s) : launch_attend4<__nv_bfloat16>(p, f.row_tiles, D, dev, s);
         if (rc != WHT_OK) return rc;
     }
     if (!weights_out) return WHT_OK;

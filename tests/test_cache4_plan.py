@@ -28,12 +28,16 @@ def div_up(a, b):
     return -(-a // b)
 
 
+def unit_rows(f):
+    return 256 if f["umma"] else 8 * f["row_tiles"]
+
+
 def division(f, lens, counts, group, hkv):
     """Runs of the kernel: (total grains, grains of a run, grains of each unit)."""
     units = []
     for n, c in zip(lens, counts):
         grains = max(1, div_up(n, 16 << f["grain"]))
-        units += [grains] * (hkv * div_up(c * group, 8 * f["row_tiles"]))
+        units += [grains] * (hkv * div_up(c * group, unit_rows(f)))
     total = sum(units)
     return total, max(div_up(total, f["warps"]), f["least"]), units
 
@@ -63,7 +67,7 @@ def test_every_part_has_its_place(plan, seed):
                 assert slot not in used and slot < 2 * f["warps"]
                 used.add(slot)
         at += grains
-    assert f["part_rows"] >= min(8 * f["row_tiles"], max(counts) * group)
+    assert f["part_rows"] >= min(unit_rows(f), max(counts) * group)
     slots = 2 * f["warps"] * f["part_rows"]
     assert f["ml_bytes"] >= slots * 8 and f["o_bytes"] >= slots * D * 4
     assert f["lse_bytes"] >= sum(counts) * group * hkv * 4
@@ -78,10 +82,19 @@ def test_grains_fit_32_bits(plan, B, hkv, width, page, max_q, group):
     """At the widest tables, all full."""
     T = B if max_q == 1 else 1000
     f = plan(width, T, B, max_q, group * hkv, hkv, 128, page, BF16, 0)
-    units = hkv * min(B * div_up(min(max_q, T) * group, 8 * f["row_tiles"]), div_up(T * group, 8 * f["row_tiles"]) + B)
+    units = hkv * min(B * div_up(min(max_q, T) * group, unit_rows(f)), div_up(T * group, unit_rows(f)) + B)
     total = units * max(1, div_up(width * page, 16 << f["grain"]))
     run = max(div_up(total, f["warps"]), f["least"])
     assert total < 2 ** 31 + units and total < 2 ** 32 and run * f["warps"] < 2 ** 32
+
+
+def test_which_kernel(plan):
+    """Single tokens, short prompts and fp32 rows on the kernel of few rows, long prompts over long contexts on tcgen05."""
+    def umma(width, T, B, max_q, hq, hkv, dtype=BF16):
+        return plan(width, T, B, max_q, hq, hkv, 128, 64, dtype, 0)["umma"] == 1
+    assert umma(469, 128, 1, 128, 32, 8) and umma(63, 2048, 1, 2048, 32, 8)
+    assert not umma(469, 128, 1, 128, 32, 8, F32)
+    assert not umma(256, 64, 64, 1, 32, 8) and not umma(16, 300, 1, 300, 8, 8) and not umma(79, 260, 8, 64, 16, 4)
 
 
 def test_the_workspace_does_not_grow_with_the_table(plan):
