@@ -49,7 +49,7 @@ struct Attn4Geo {
     static constexpr int ROWS = 8 * NR;
     static constexpr int TERMS = F32 ? 2 : 1;                   // of queries and of weights
     static constexpr int TILE = tile4_bytes(D);
-        static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
+    static constexpr int U = NR == 1 ? 2 : 1;                   // tiles of a step
     static constexpr int STAGES = U == 2 ? 2 : 4;               // steps of the ring
     static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
     static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;

@@ -18,16 +18,18 @@ constexpr int kGrain4 = 1;     // log2 of the tiles in which work is counted: a 
 
 // Prompts of bf16 queries on tcgen05: rows of a unit, log2 of the tiles of a grain (a step takes 64 keys), blocks that an SM holds.
 constexpr int kUmma4Rows = 256, kUmma4Grain = 2, kUmma4Resident = 1;
-// Whether the tcgen05 kernel is the faster one, by a small model of both (lengths being on the device, as if the tables were full): a start of 30 us and
-// 1.9 us a step of 256 rows and 64 keys in a block, against 10 us and 0.085 us an SM (D = 128; 0.065 with D = 64) for 16 rows and
-// 16 keys in the kernel of few rows.
-// us, tcgen05 and the other: 128 tokens of 4 rows over 30000 keys, 8 key heads, 122 (269); 2048 over 4000 220 (515); 64 over 20000 74 (104); 100 over 10000
-// 87 (83); 16 x 128 over 2000 147 (134); 8 x 64 over 5000, 4 key heads, D = 96, 67 (51); 400 tokens of 32 heads over 800 50 (37); 256 over 300 45 (19).
+// Whether the tcgen05 kernel is the faster one, by a small model of both, in us (D = 128; less for fewer channels): a start of 28, 1.75 a step of 256 rows and
+// 64 keys in a block and 8 a further unit of it, against 10 and 0.085 an SM for 16 rows and 16 keys in the kernel of few rows.  Lengths are on the device: as
+// if the tokens were spread evenly and the tables full, with a quarter in hand, since lengths that are not favour the kernel of few rows.
+// us, tcgen05 and the other: 128 tokens of 4 rows over 30000 keys, 8 key heads, 120 (272); 2048 over 4000 218 (517); 64 over 20000 63 (105); 100 over 10000
+// 59 (83); 16 x 128 over up to 2000 97 (134); 8 x 64 over up to 5000, 4 key heads, D = 96, 51 (52); 400 tokens of 32 heads over 800 42 (37); 256 over 300 37 (19).
 inline bool umma4_pays(int64_t keys, int64_t T, int32_t B, int group, int32_t Hkv, int32_t D, int sms) {
-    const double rows = static_cast<double>(T) * group, k = static_cast<double>(keys);
-    const double umma = 30.0 + 1.9 * std::ceil(Hkv * (rows / kUmma4Rows + 0.5 * B) * (k / 64) / sms);
-    const double other = 10.0 + (0.045 + D / 3200.0) * Hkv * (rows / 16 + 0.5 * B) * (k / 16) / sms;
-    return umma < other;
+    const int64_t rows = (T + B - 1) / B * group;
+    const double heads = static_cast<double>(B) * Hkv, k = static_cast<double>(keys);
+    const double units = heads * static_cast<double>((rows + kUmma4Rows - 1) / kUmma4Rows), units_few = heads * static_cast<double>((rows + 15) / 16);
+    const double umma = 12.0 + D / 8.0 + (0.45 + 0.0102 * D) * std::ceil(units * (k / 64) / sms) + 8.0 * units / sms;
+    const double other = 10.0 + (0.045 + D / 3200.0) * units_few * (k / 16) / sms;
+    return 1.25 * umma < other;
 }
 
 struct Attend4Plan {

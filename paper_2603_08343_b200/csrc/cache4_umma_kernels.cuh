@@ -18,8 +18,8 @@
 // order in which their codes fall out of a word, and so do the queries'; the results' are put right when they are written.
 //
 // What bounds it: the softmax warps.  A step of both tiles takes 2800 clocks, 2100 of them the weights of 64 keys (64 exponentials, 7 packed operations a pair of
-// keys, two of a warp's reads of (step, lo)), 1000 the products.  128 tokens of 32 heads over 30000 keys of 8 key heads 122 us (0.5 PFLOP/s; 269 in the kernel of few rows),
-// 2048 tokens over 4000 220 us (515).  Slower: blocks of one tile, two an SM (96 registers a thread, 150 us), the issuing warp's loops not unrolled (a product
+// keys, two of a warp's reads of (step, lo)), 1000 the products.  128 tokens of 32 heads over 30000 keys of 8 key heads 120 us (0.5 PFLOP/s; 272 in the kernel of few rows),
+// 2048 tokens over 4000 218 us (517).  Slower: blocks of one tile, two an SM (96 registers a thread, 150 us), the issuing warp's loops not unrolled (a product
 // takes 100 clocks to issue, 133 us), (step, lo) unpacked by the softmax warps (147 us).
 //
 // Waits are bounded as in umma_kernels.cuh.
@@ -329,7 +329,8 @@ attn4_umma_kernel(const Attn4Params p) {
                 return true;
             }
             const int first_limit = u.keys - u.count + 1;
-            const int limit = row < rows ? min(end, first_limit + tok) : 0, least_limit = min(end, first_limit + (u.row0 + 128 * w) / a.group);
+            // (rows that are not there see zeros)
+            const int limit = row < rows ? min(end, first_limit + tok) : end, least_limit = min(end, first_limit + (u.row0 + 128 * w) / a.group);
             const int64_t at = (u.token0 + tok) * a.hq + static_cast<int64_t>(u.head) * a.group + (row - tok * a.group);
             float m = -INFINITY, l = 0.0f, r = 0.0f, qs = 0.0f;
             if (steps > 0) {
@@ -467,34 +468,60 @@ attn4_umma_kernel(const Attn4Params p) {
                 tc_fence_after();
             }
             const float inv = u.slot >= 0 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
-            auto put = [&](int ch, float x0, float x1, float x2, float x3) {             // four channels of the row
-                if (row >= rows) return;
-                const float4 v = make_float4((x0 + r) * inv, (x1 + r) * inv, (x2 + r) * inv, (x3 + r) * inv);
-                if (u.slot >= 0) *reinterpret_cast<float4*>(a.part_o + (u.slot * p.part_rows + local) * D + ch) = v;
-                else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at * D + ch) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-            };
+            // 32 channels at a time through this warp's rows of the queries' place, which no product reads any more: a row's four channels after the
+            // other go there, whole lines of 128 bytes (fp32) leave (a row a thread straight to memory: 16000 clocks a unit against 6000)
+            unsigned char* stage = smem + w * Geo::Q_TILE + (warp & 3) * 4096;
+            const int there = rows - u.row0 - warp * 32 - (lane >> 3);           // row 4 k of this lane is there if 4 k < there
+            const int groups = rows - u.row0 > warp * 32 ? D / 32 : 0;
+            const int64_t part0 = (u.slot * p.part_rows + warp * 32 + (lane >> 3)) * D + (lane & 7) * 4;
+            int line[8];                                                         // rows of the output, from the sequence's and head's first on
+            if (u.slot < 0) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int out_row = u.row0 + warp * 32 + (lane >> 3) + 4 * k, t = out_row / a.group;
+                    line[k] = t * a.hq + out_row - t * a.group;
+                }
+            }
+            __nv_bfloat16* out0 = static_cast<__nv_bfloat16*>(a.out) + (u.token0 * a.hq + static_cast<int64_t>(u.head) * a.group) * D + (lane & 7) * 4;
+            const unsigned char* from = stage + (lane >> 3) * 128;
+            const int piece0 = ((lane & 7) ^ (lane >> 3)) << 4;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-                float o[16];
-                if (steps > 0) {
-                    tmem_ld16(o_cols + c, o);
-                    tmem_wait_ld();
+            for (int g = 0; g < groups; ++g) {
+                // D = 128: column 16 u + 8 (g / 2) + 2 i + (g & 1) is channel 32 g + 4 u + i; else column 8 u + 2 i + g, and (D = 96) the last 32 as they are
+                const bool plain = D == 96 && g == 2;
+#pragma unroll
+                for (int v0 = 0; v0 < 8; v0 += 4) {
+                    float o[4][8] = {};
+                    if (steps > 0) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) tmem_ld8(o_cols + (D == 128 ? 16 * (v0 + v) + 8 * (g >> 1) : plain ? 64 + 4 * (v0 + v) : 8 * (v0 + v)), o[v]);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        float4 x = g & 1 ? make_float4(o[v][1], o[v][3] * 0.0625f, o[v][5], o[v][7] * 0.0625f)
+                                         : make_float4(o[v][0], o[v][2] * 0.0625f, o[v][4], o[v][6] * 0.0625f);
+                        if (plain) x = make_float4(o[v][0], o[v][1], o[v][2], o[v][3]);
+                        *reinterpret_cast<float4*>(stage + lane * 128 + (((v0 + v) ^ (lane & 7)) << 4)) =
+                            make_float4((x.x + r) * inv, (x.y + r) * inv, (x.z + r) * inv, (x.w + r) * inv);
+                    }
+                }
+                __syncwarp();
+                float4 x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const float4*>(from + k * 512 + (piece0 ^ ((k & 1) << 6)));
+                if (u.slot >= 0) {
+                    float* to = a.part_o + part0 + g * 32;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (4 * k < there) *reinterpret_cast<float4*>(to + k * 4 * D) = x[k];
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = 0.0f;
+                    for (int k = 0; k < 8; ++k)
+                        if (4 * k < there)
+                            *reinterpret_cast<uint2*>(out0 + static_cast<int64_t>(line[k]) * D + g * 32) = make_uint2(pack_bf16x2(x[k].x, x[k].y), pack_bf16x2(x[k].z, x[k].w));
                 }
-                if (D == 96 && c >= 64) {
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) put(c + e, o[e], o[e + 1], o[e + 2], o[e + 3]);
-                } else {
-                    // column 8 h + 2 i + s: D = 128 piece u = c / 16, channel 32 (2 h + s) + 4 u + i; else piece u = c / 8 + h, channel 32 s + 4 u + i
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int s = 0; s < 2; ++s)
-                            put(D == 128 ? 32 * (2 * h + s) + c / 4 : 32 * s + 4 * (c / 8 + h), o[8 * h + s], o[8 * h + 2 + s] * 0.0625f, o[8 * h + 4 + s],
-                                o[8 * h + 6 + s] * 0.0625f);
-                }
+                __syncwarp();
             }
             tc_fence_before();
             if (row < rows) {

@@ -105,3 +105,13 @@ def test_the_workspace_does_not_grow_with_the_table(plan):
     assert plan(100000, 64, 64, 1, 32, 8, 128, 64, BF16, 1)["scores_bytes"] == 0
     assert plan(10, 64, 64, 4, 32, 8, 128, 64, BF16, 1)["scores_bytes"] == 0
     assert plan(1000, 0, 64, 4, 32, 8, 128, 64, BF16, 1)["bytes"] == 0
+
+
+@pytest.mark.parametrize("d,hq,hkv,page,lens,counts", [
+    (128, 32, 8, 64, [5000], [600]), (128, 8, 2, 128, [16001, 9000, 700], [513, 1, 700]), (96, 12, 4, 32, [7000, 0, 40, 4000], [800, 3, 64, 1]),
+    (64, 16, 16, 16, [3000, 2999], [900, 411]), (64, 64, 1, 64, [12000], [77]), (128, 16, 4, 64, [6000], [500]), (96, 16, 4, 64, [5000], [500]),
+    (128, 8, 2, 64, [5000], [600]), (128, 32, 8, 64, [5000, 4000], [600, 500])])
+def test_the_sizes_of_the_prompt_tests(plan, d, hq, hkv, page, lens, counts):
+    """They are to reach the tcgen05 kernel (test_cache4_prompts_gpu.py)."""
+    width = max(1, max(div_up(n, page) for n in lens))
+    assert plan(width, sum(counts), len(lens), max(counts), hq, hkv, d, page, BF16, 0)["umma"] == 1
