@@ -22,9 +22,10 @@
  *     (csrc/cache4_common.cuh states it).  It has no storage type: queries and outputs of a call are WHT_F32 or WHT_BF16.
  *     Fresh memory may hold anything.
  *   - Scores, softmax statistics and sums are fp32.  Queries enter the product as fp16 numbers shifted by a power of two per row: bf16 ones
- *     keep all bits but those below 2^-35 of the row's largest, fp32 ones are two terms (22 bits).  The softmax weights, times the values' steps and a power
+ *     keep all bits but those below 2^-33 of the row's largest, fp32 ones are two terms (22 bits).  The softmax weights, times the values' steps and a power
  *     of two per row, enter the second product as one fp16 term (11 bits) where the output is bf16 and as two (22 bits) where it is fp32.
- *     Queries of 2^116 and more come out as NaN.
+ *     Queries of 2^116 and more (divided by the scale, where that is above 1) may come out as NaN.  Long prompts of bf16 queries over long contexts take a
+ *     tcgen05 kernel, by sizes that the host knows; there queries enter as they are, and the weights as one fp16 term.
  *   - The work is divided by the lengths themselves: a table wider than its sequences costs nothing but its memory.
  */
 #ifndef WHT_CACHE4_H_
@@ -36,7 +37,7 @@
 extern "C" {
 #endif
 
-/* Append: the arguments are those of wht_kv_append (strides, slots, positions, tables), without summaries. */
+/* Append: the arguments are those of wht_kv_append (strides, slots, positions, tables), without summaries.  No two tokens of a call share a slot. */
 int wht_kv_append4(const void* k, int64_t k_stride_t, int64_t k_stride_h,
                    const void* v, int64_t v_stride_t, int64_t v_stride_h,
                    const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out,
@@ -54,7 +55,10 @@ int wht_kv_read4(const void* cache, const int64_t* slots, void* k_out, void* v_o
  *   weights      [B x Hkv x table_width * page] float32 or NULL: what each key has received so far (NULL: nothing).
  *   weights_out  the same shape, or NULL: weights + the softmax weights of this call's tokens and the query heads of the key
  *                head, summed; 0 from kv_lens[b] on.  May be `weights` itself.  Sums have one order: results repeat bit for bit.
- *   workspace    at least wht_attn_paged4_workspace_bytes(...) bytes; weigh: whether weights_out is given.
+ *   workspace    at least wht_attn_paged4_workspace_bytes(...) bytes; weigh: whether weights_out is given (the scores of up to 8 rows a sequence and key head
+ *                are then kept for it, in 1 GiB at most; beyond that they are taken again).  It holds nothing between calls; calls that may run at the same time
+ *                need one each.
+ * Lengths, offsets and tables are read by several kernels of a call: they must not change before it has ended.
  */
 int wht_attn_paged4(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* cache,
                     const int32_t* page_table, int32_t table_width, const int32_t* kv_lens, const int32_t* q_start, void* out,

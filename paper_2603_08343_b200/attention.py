@@ -101,7 +101,7 @@ def cache4(num_pages: int, kv_heads: int, page: int, head_dim: int, device="cuda
 
 def kv_append4(k, v, cache, slots, positions=None, cos=None, sin=None, q=None, q_out=None, interleaved: bool = False, stream=None):
     """kv_append for a cache in 4 bits (`cache4`): rotates queries and keys, writes each key and value row of a head as 4-bit codes with a
-    least value and a step; returns the rotated queries, or None without q.  Arguments as for kv_append."""
+    least value and a step; returns the rotated queries, or None without q.  Arguments as for kv_append; no two tokens share a slot."""
     return _native.kv_append4(k, v, cache, slots, positions, cos, sin, q, q_out, interleaved, _raw(stream))
 
 
@@ -121,6 +121,7 @@ def paged_attention4(q, cache, page_table, kv_lens, q_start=None, max_q_len: int
     weights [batch, kv_heads, table pages * page] fp32: what each key has received so far.  With it (or with weights_out alone, starting from nothing)
     the call returns (out, weights_out): weights_out (allocated if None; may be weights itself) = weights + the softmax weights of
     this call's tokens, summed over them and the heads of each key head; 0 from a sequence's length on.
+    Long bf16 prompts over long contexts take a tcgen05 kernel, by the sizes of the call.
     """
     return _native.paged_attention4(q, cache, page_table, kv_lens, q_start, max_q_len, scale, out, weights, weights_out, _raw(stream))
 

@@ -8,15 +8,17 @@
 // number, c 2^-24 or 16 c 2^-24 (a subnormal one; the tensor core takes these as they are, but aligns a product by its operands'
 // exponents, so that sums keep about 20 bits), so that eight codes take four masks and one shift, exactly, and the powers of two go into the
 // queries and the result.  For fp32 results the values' codes become ordinary numbers, c - 8, by one exact subtraction a pair.
-// Queries enter as fp16 after a shift of each row by a power of two (bf16 ones keep all their bits but what lies below 2^-35 of the row's
+// Queries enter as fp16 after a shift of each row by a power of two (bf16 ones keep all their bits but what lies below 2^-33 of the row's
 // maximum; fp32 ones are two terms, 22 bits of it), and the weights p step' as fp16 times a power of two per row that keeps them in range: one
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
 //
-// What bounds it: memory, 2 (D / 2 + 4) bytes a key and key head.  At 23 B a clock and SM a tile of 16 keys of 128 channels has 378 clocks of an SM's
-// quarter; its 100 or so mask, select and shift instructions take two clocks each.  So instructions count, and products are taken
-// transposed, S^T = C Q^T and O^T = C'^T P^T: codes of 16 keys (channels) fill the 16-row operand and the rows sit on the 8-column one, so that 8 rows
-// waste nothing, a key's step and least value are wanted by the four lanes that hold its scores, and P^T changes from accumulator to operand layout by
-// one 8x8 transposition.  (With the rows on the 16-row operand, half of it empty: 364 instructions a tile, 242 us for 64 x 16384 keys of 8 key heads.)
+// What bounds it: memory, 2 (D / 2 + 4) bytes a key and key head, and instructions next to it.  At 23 B a clock and SM a tile of 16 keys of 128 channels has
+// 378 clocks of an SM's quarter; it takes 240 instructions for up to 8 rows, about 100 of which mask, select and shift, two clocks each.
+// So products are taken transposed, S^T = C Q^T and O^T = C'^T P^T: codes of 16 keys (channels) fill the 16-row operand and the rows sit on the 8-column one, so
+// that 8 rows waste nothing, a key's step and least value are wanted by the four lanes that hold its scores, and P^T changes from accumulator to operand
+// layout by one 8x8 transposition.  64 sequences of up to 16384 keys of 8 key heads of 128, 32 heads: 157-160 us, 5.4 TB/s (DRAM 70 % busy, issue slots 56 %, ALU
+// 56 %; with the rows on the 16-row operand, half of it empty, 364 instructions a tile and 242 us).  Two tiles a step, so that their latencies overlap (one:
+// 165-167).  200 x 1000 keys of 16 heads of 64: 56 us, 3.1 TB/s: a tile has half the bytes, but the softmax of as many scores.
 //
 // The division of work goes by the lengths themselves, which are on the device: the tiles of all units (sequence, key head, row tile)
 // are counted one after the other, and each warp (a block of its own) takes an equal run of them, whatever units it touches.  A unit that lies in one
@@ -816,7 +818,7 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
 
 // ---- the weight that each key receives: weights_out = weights + sum over the sequence's tokens and the group's heads of exp(score - lse).
 // Sequences of up to eight rows a key head: the attention has left the scores, four bytes a row and key; to take them again from the
-// codes costs D / 2 + 8 bytes a key and the products (32 x 8192 keys, 4 rows: 48 us against 12).
+// codes costs D / 2 + 8 bytes a key and the products (32 x up to 8192 keys of 8 key heads, 4 rows: 48 us against 12, and 4 more for the attention that writes them: 55 against 51).
 // Four keys a thread.
 __global__ static void __launch_bounds__(256)
 attn4_weigh_scores_kernel(const Attn4Params p, int chunks) {
