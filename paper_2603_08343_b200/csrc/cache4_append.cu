@@ -12,16 +12,16 @@ namespace {
 
 template <typename T, bool INTERLEAVED>
 void append(const Append4Params& p, int d, unsigned blocks, cudaStream_t s) {
-    if (d == 64) kv_append4_kernel<T, INTERLEAVED, 64><<<blocks, kAppend4Threads, 0, s>>>(p);
-    else if (d == 96) kv_append4_kernel<T, INTERLEAVED, 96><<<blocks, kAppend4Threads, 0, s>>>(p);
-    else kv_append4_kernel<T, INTERLEAVED, 128><<<blocks, kAppend4Threads, 0, s>>>(p);
+    if (d == 64) launch_overlapped(kv_append4_kernel<T, INTERLEAVED, 64>, dim3(blocks), kAppend4Threads, 0, s, p);
+    else if (d == 96) launch_overlapped(kv_append4_kernel<T, INTERLEAVED, 96>, dim3(blocks), kAppend4Threads, 0, s, p);
+    else launch_overlapped(kv_append4_kernel<T, INTERLEAVED, 128>, dim3(blocks), kAppend4Threads, 0, s, p);
 }
 
 template <typename T>
 void read(const Read4Params& p, int d, unsigned blocks, cudaStream_t s) {
-    if (d == 64) kv_read4_kernel<T, 64><<<blocks, 256, 0, s>>>(p);
-    else if (d == 96) kv_read4_kernel<T, 96><<<blocks, 256, 0, s>>>(p);
-    else kv_read4_kernel<T, 128><<<blocks, 256, 0, s>>>(p);
+    if (d == 64) launch_overlapped(kv_read4_kernel<T, 64>, dim3(blocks), 256, 0, s, p);
+    else if (d == 96) launch_overlapped(kv_read4_kernel<T, 96>, dim3(blocks), 256, 0, s, p);
+    else launch_overlapped(kv_read4_kernel<T, 128>, dim3(blocks), 256, 0, s, p);
 }
 
 }  // namespace

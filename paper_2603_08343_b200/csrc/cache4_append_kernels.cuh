@@ -81,6 +81,8 @@ kv_append4_kernel(const Append4Params p) {
     constexpr int HB = kHeads4<T>;
     constexpr int LANES = D == 64 ? 4 : 8;             // of a row
     const AppendParams& a = p.a;
+    grid_dependency_wait();
+    grid_launch_dependents();
     // (blocks of rows compute where those of queries wait for memory: spread evenly among each other they share the SMs)
     const int64_t before = static_cast<int64_t>(blockIdx.x) * p.kv_grid / gridDim.x, after = static_cast<int64_t>(blockIdx.x + 1ll) * p.kv_grid / gridDim.x;
     if (after == before) {
@@ -191,6 +193,8 @@ template <typename T, int D>
 __global__ void __launch_bounds__(256)
 kv_read4_kernel(const Read4Params p) {
     constexpr int PER = D / 8, HB = kReadHeads4;
+    grid_dependency_wait();                            // (slots and rows may come from the kernel before)
+    grid_launch_dependents();
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t job = i / PER;                       // slot number * groups of heads + group
     const int octet = static_cast<int>(i - job * PER), groups = (p.hkv + HB - 1) / HB;

@@ -27,7 +27,7 @@ int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
     static_assert(Geo::BLOCKS * (Geo::BYTES + 1024) <= 228 * 1024, "shared memory");
     int rc = prepare4(attn4_kernel<T, D, NR>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
-    attn4_kernel<T, D, NR><<<static_cast<unsigned>(p.warps), 32, Geo::BYTES, s>>>(p);
+    launch_overlapped(attn4_kernel<T, D, NR>, dim3(static_cast<unsigned>(p.warps)), 32, Geo::BYTES, s, p);
     WHT_CUDA_TRY(cudaGetLastError());
     const long long rows = static_cast<long long>(p.a.T) * p.a.hq;
     launch_overlapped(attn4_join_kernel<T, D>, dim3(static_cast<unsigned>(ceil_div(rows, 4))), 128, 0, s, p, static_cast<int>(Geo::ROWS));

@@ -703,6 +703,7 @@ attn4_kernel(const Attn4Params p) {
         fence_mbar_init();
     }
     __syncwarp();
+    grid_dependency_wait();
     grid_launch_dependents();
     if (a.q_start != nullptr)
         for (int head = blockIdx.x; head < a.hkv; head += gridDim.x) attn_uncovered<T, D>(a, head);

@@ -25,8 +25,8 @@ int launch_evict4(const Evict4Params& p, int d, cudaStream_t s) {
     int dev = 0, sms = 0;
     const int rc = device_info(&dev, &sms);
     if (rc != WHT_OK) return rc;
-    if (rows <= sms) kv_evict4_choose_kernel<1024><<<static_cast<unsigned>(rows), 1024, 0, s>>>(p);
-    else kv_evict4_choose_kernel<512><<<static_cast<unsigned>(rows), 512, 0, s>>>(p);
+    if (rows <= sms) launch_overlapped(kv_evict4_choose_kernel<1024>, dim3(static_cast<unsigned>(rows)), 1024, 0, s, p);
+    else launch_overlapped(kv_evict4_choose_kernel<512>, dim3(static_cast<unsigned>(rows)), 512, 0, s, p);
     WHT_CUDA_TRY(cudaGetLastError());
     const unsigned n = static_cast<unsigned>(blocks);
     d == 64 ? move<64>(p, n, s) : d == 96 ? move<96>(p, n, s) : move<128>(p, n, s);

@@ -73,6 +73,7 @@ kv_evict4_choose_kernel(const Evict4Params p) {
     const AttnParams& a = p.a;
     const int tid = threadIdx.x;
     const int b = blockIdx.x / a.hkv, head = blockIdx.x % a.hkv;
+    grid_dependency_wait();
     grid_launch_dependents();
     const int n = attn_length(a, b);
     const int keep = min(p.budget, n);

@@ -22,7 +22,7 @@ int launch(const Attn4Params& p, int dev, cudaStream_t s) {
         WHT_CUDA_TRY(cudaFuncSetAttribute(attn4_umma_kernel<D>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
         ready[dev] = 1;
     }
-    attn4_umma_kernel<D><<<static_cast<unsigned>(p.warps), kUmma4Threads, Geo::BYTES, s>>>(p);
+    launch_overlapped(attn4_umma_kernel<D>, dim3(static_cast<unsigned>(p.warps)), kUmma4Threads, Geo::BYTES, s, p);
     WHT_CUDA_TRY(cudaGetLastError());
     const long long rows = static_cast<long long>(p.a.T) * p.a.hq;
     launch_overlapped(attn4_join_kernel<__nv_bfloat16, D>, dim3(static_cast<unsigned>(ceil_div(rows, 4))), 128, 0, s, p, static_cast<int>(kUmma4Rows));

@@ -97,7 +97,8 @@ attn4_umma_kernel(const Attn4Params p) {
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + Geo::OFF_MISC + 4);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFullMask, tid >> 5, 0);
 
-    grid_launch_dependents();
+    // (tensor memory is taken after the kernel before, which may want it too, and before the one after may start)
+    grid_dependency_wait();
     if (warp == 12) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
@@ -124,6 +125,7 @@ attn4_umma_kernel(const Attn4Params p) {
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(kFullMask, *tmem_slot, 0);
+    grid_launch_dependents();
 
     unsigned run;
     const Place4 home = find_run4(p, kUmma4Rows, blockIdx.x, run);
