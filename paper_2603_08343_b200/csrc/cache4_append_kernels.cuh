@@ -215,10 +215,10 @@ kv_read4_kernel(const Read4Params p) {
         w[h] = make_uint2(0, 0);
         if (slot < 0 || h0 + h >= p.hkv) continue;
         const unsigned char* tile = tile4_of(const_cast<unsigned char*>(p.cache), slot, h0 + h, p.hkv, p.page_shift, D);
-        kw[h] = __ldg(reinterpret_cast<const unsigned*>(tile + key4_at(D, j, g, u)));
-        vw[h] = __ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u))) |
-                static_cast<unsigned>(__ldg(reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u + 1)))) << 16;
-        w[h] = __ldg(reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8));
+        kw[h] = *reinterpret_cast<const unsigned*>(tile + key4_at(D, j, g, u));
+        vw[h] = *reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u)) |
+                static_cast<unsigned>(*reinterpret_cast<const unsigned short*>(tile + value4_at(D, j, g, u + 1))) << 16;
+        w[h] = *reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8);
     }
 #pragma unroll
     for (int h = 0; h < HB; ++h) {

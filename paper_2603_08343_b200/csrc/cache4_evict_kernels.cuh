@@ -59,8 +59,8 @@ __device__ __forceinline__ unsigned block_scan4(unsigned x, unsigned* warp_sums,
 
 // Four neighbouring weights from key i on; what lies behind the n-th is 0.
 __device__ __forceinline__ float4 weights4(const float* w, int i, int n) {
-    if (i + 3 < n) return __ldg(reinterpret_cast<const float4*>(w + i));
-    return make_float4(i < n ? __ldg(w + i) : 0.0f, i + 1 < n ? __ldg(w + i + 1) : 0.0f, i + 2 < n ? __ldg(w + i + 2) : 0.0f, 0.0f);
+    if (i + 3 < n) return *reinterpret_cast<const float4*>(w + i);
+    return make_float4(i < n ? w[i] : 0.0f, i + 1 < n ? w[i + 1] : 0.0f, i + 2 < n ? w[i + 2] : 0.0f, 0.0f);
 }
 
 template <int THREADS>
@@ -232,9 +232,9 @@ kv_evict4_move_kernel(const Evict4Params p) {
         const int n = i * 32 + lane, j = n / PIECES;
         const int64_t src = __shfl_sync(kFullMask, from, j);
         got[i] = make_uint4(0, 0, 0, 0);
-        if (src >= 0) got[i] = __ldg(reinterpret_cast<const uint4*>(p.cache + (src >> 4) * tile4_bytes(D) + piece4_at<D>(static_cast<int>(src & 15), n - j * PIECES)));
+        if (src >= 0) got[i] = *reinterpret_cast<const uint4*>(p.cache + (src >> 4) * tile4_bytes(D) + piece4_at<D>(static_cast<int>(src & 15), n - j * PIECES));
     }
-    if (from >= 0) row = __ldg(reinterpret_cast<const uint2*>(p.cache + (from >> 4) * tile4_bytes(D) + tile4_rows(D) + (from & 15) * 8));
+    if (from >= 0) row = *reinterpret_cast<const uint2*>(p.cache + (from >> 4) * tile4_bytes(D) + tile4_rows(D) + (from & 15) * 8);
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
         const int n = i * 32 + lane, j = n / PIECES;

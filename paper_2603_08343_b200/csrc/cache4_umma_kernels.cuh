@@ -184,13 +184,13 @@ attn4_umma_kernel(const Attn4Params p) {
                 const unsigned char* tile = p.cache + (((static_cast<int64_t>(pg) * a.hkv + u.head) << shift) + (tile_of(i) & in_page)) * tile4_bytes(D);
                 if (!values) {
 #pragma unroll
-                    for (int n = 0; n < LOADS; ++n) next[n] = __ldg(reinterpret_cast<const uint4*>(tile + j * (D / 2)) + n);
+                    for (int n = 0; n < LOADS; ++n) next[n] = *(reinterpret_cast<const uint4*>(tile + j * (D / 2)) + n);
                 } else {
                     const int place = value4_place(j);
 #pragma unroll
                     for (int n = 0; n < LOADS; ++n)
-                        next[n] = __ldg(reinterpret_cast<const uint4*>(tile + 8 * D + (D == 128 ? place * 64 + n * 16 : n < 2 ? place * 32 + n * 16 : 512 + place * 16)));
-                    next_row = __ldg(reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8));
+                        next[n] = *reinterpret_cast<const uint4*>(tile + 8 * D + (D == 128 ? place * 64 + n * 16 : n < 2 ? place * 32 + n * 16 : 512 + place * 16));
+                    next_row = *reinterpret_cast<const uint2*>(tile + tile4_rows(D) + j * 8);
                 }
             };
             int page = look(0);
@@ -342,7 +342,7 @@ attn4_umma_kernel(const Attn4Params p) {
 #pragma unroll 8
                 for (int c = 0; c < D / 8; ++c) {
                     uint4 v = make_uint4(0, 0, 0, 0);
-                    if (row < rows) v = __ldg(reinterpret_cast<const uint4*>(src) + c);
+                    if (row < rows) v = *(reinterpret_cast<const uint4*>(src) + c);
                     qs += ((bf16lo_to_f32(v.x) + bf16hi_to_f32(v.x)) + (bf16lo_to_f32(v.y) + bf16hi_to_f32(v.y))) +
                           ((bf16lo_to_f32(v.z) + bf16hi_to_f32(v.z)) + (bf16lo_to_f32(v.w) + bf16hi_to_f32(v.w)));
                     *reinterpret_cast<uint4*>(smem + w * Geo::Q_TILE + piece_of(Geo::Q_BOX, local & 127, c)) =

@@ -405,3 +405,51 @@ def test_queries_of_any_size(A):
         got = A.paged_attention4(q.cuda(), cache, table.cuda(), ints(n), scale=2.0 ** -103)
         assert (got.cpu().double() - want).abs().max().item() <= C.tolerance(q, 8.0, 6.0, 2.0 ** -103)
     assert not math.isnan(A.paged_attention4(torch.zeros(1, 4, 64, device="cuda"), cache, table.cuda(), ints(n)).sum().item())
+
+
+@pytest.mark.parametrize("tokens", [1, 700])
+def test_calls_one_right_behind_the_other_see_what_came_before(A, tokens):
+    """Kernels start while the one before them drains: over and over the same slots are overwritten, attended to (few rows, and a prompt on
+    tcgen05), evicted from and read back, with and without waiting for each call; both give the same."""
+    n, hkv, group, d, page, budget = 5000, 4, 4, 128, 64, 1000
+    width, out_width = -(-n // page), -(-budget // page)
+    g = gen(tokens)
+    k, v = (torch.randn(3, n, hkv, d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(tokens, hkv * group, d, generator=g).bfloat16().cuda()
+    slots = torch.arange(n).cuda()
+    table = torch.arange(width).int().cuda()[None]
+    out_table = torch.arange(width, width + out_width).int().cuda()[None]
+    start = None if tokens == 1 else ints(0, tokens)
+
+    def rounds(wait):
+        cache = A.cache4(width + out_width, hkv, page, d)
+        weights = torch.zeros(1, hkv, width * page, device="cuda")
+        lens, seen = ints(n), []
+        torch.cuda.synchronize()
+        for i in range(12):
+            if i > 0:
+                A.kv_append4(k[i % 3], v[(i + 1) % 3], cache, slots)
+                wait()
+                out, _ = A.paged_attention4(q, cache, table, lens, q_start=start, max_q_len=tokens, weights=weights, weights_out=weights)
+                wait()
+                plain = A.paged_attention4(q, cache, table, lens, q_start=start, max_q_len=tokens)
+                wait()
+            else:
+                A.kv_append4(k[0], v[0], cache, slots)
+                out = plain = None
+                wait()
+            left, kept, moved = A.kv_evict4(cache, table, lens, weights, out_table, budget, 3, 20)
+            wait()
+            keys, values = A.kv_read4(cache, (out_table.long() * page)[0, :, None].add(torch.arange(page).cuda()).flatten()[:budget], torch.bfloat16)
+            wait()
+            after = A.paged_attention4(q[:1], cache, out_table, left)
+            wait()
+            seen += [t for t in (out, plain, left, kept, moved, keys, values, after, weights.clone()) if t is not None]
+        torch.cuda.synchronize()
+        return seen
+
+    patient = rounds(torch.cuda.synchronize)
+    for _ in range(4):
+        for a, b in zip(rounds(lambda: None), patient):
+            assert torch.equal(a, b)
+    A.device_status()
