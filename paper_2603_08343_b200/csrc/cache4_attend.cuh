@@ -19,15 +19,15 @@ int prepare4(Kernel kernel, int smem, int dev, int* cache) {
     return WHT_OK;
 }
 
-template <typename T, int D, int NR>
+template <typename T, int D, int NR, int E>
 int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
     static int ready[kMaxDevices] = {};
     using Geo = Attn4Geo<T, D, NR>;
     static_assert(Geo::BLOCKS == wht_plan::resident4(NR, Geo::F32), "the plan's blocks per SM");
     static_assert(Geo::BLOCKS * (Geo::BYTES + 1024) <= 228 * 1024, "shared memory");
-    int rc = prepare4(attn4_kernel<T, D, NR>, Geo::BYTES, dev, ready);
+    int rc = prepare4(attn4_kernel<T, D, NR, E>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
-    launch_overlapped(attn4_kernel<T, D, NR>, dim3(static_cast<unsigned>(p.warps)), 32, Geo::BYTES, s, p);
+    launch_overlapped(attn4_kernel<T, D, NR, E>, dim3(static_cast<unsigned>(p.warps)), 32, Geo::BYTES, s, p);
     WHT_CUDA_TRY(cudaGetLastError());
     const long long rows = static_cast<long long>(p.a.T) * p.a.hq;
     launch_overlapped(attn4_join_kernel<T, D>, dim3(static_cast<unsigned>(ceil_div(rows, 4))), 128, 0, s, p, static_cast<int>(Geo::ROWS));
@@ -37,7 +37,9 @@ int attend4(const Attn4Params& p, int dev, cudaStream_t s) {
 
 template <typename T, int D>
 int attend4_d(const Attn4Params& p, int row_tiles, int dev, cudaStream_t s) {
-    return row_tiles == 1 ? attend4<T, D, 1>(p, dev, s) : attend4<T, D, 2>(p, dev, s);
+    // (up to four rows a sequence and key head: see Rows4)
+    if (row_tiles == 1) return p.part_rows <= 4 ? attend4<T, D, 1, 1>(p, dev, s) : attend4<T, D, 1, 2>(p, dev, s);
+    return attend4<T, D, 2, 2>(p, dev, s);
 }
 
 template <typename T, int D, int NR>

@@ -16,9 +16,10 @@
 // 378 clocks of an SM's quarter; it takes 240 instructions for up to 8 rows, about 100 of which mask, select and shift, two clocks each.
 // So products are taken transposed, S^T = C Q^T and O^T = C'^T P^T: codes of 16 keys (channels) fill the 16-row operand and the rows sit on the 8-column one, so
 // that 8 rows waste nothing, a key's step and least value are wanted by the four lanes that hold its scores, and P^T changes from accumulator to operand
-// layout by one 8x8 transposition.  64 sequences of up to 16384 keys of 8 key heads of 128, 32 heads: 157-160 us, 5.4 TB/s (DRAM 70 % busy, issue slots 56 %, ALU
+// layout by one 8x8 transposition.  Up to four rows take every other column, half of the softmax's instructions (200 x 1000 keys 56 -> 51 us, 1 x 4096 8.7 ->
+// 8.2).  64 sequences of up to 16384 keys of 8 key heads of 128, 32 heads: 157-160 us, 5.4 TB/s (DRAM 70 % busy, issue slots 56 %, ALU
 // 56 %; with the rows on the 16-row operand, half of it empty, 364 instructions a tile and 242 us).  Two tiles a step, so that their latencies overlap (one:
-// 165-167).  200 x 1000 keys of 16 heads of 64: 56 us, 3.1 TB/s: a tile has half the bytes, but the softmax of as many scores.
+// 165-167).  200 x 1000 keys of 16 heads of 64: 51 us, 3.4 TB/s: a tile has half the bytes, but the softmax of as many scores.
 //
 // The division of work goes by the lengths themselves, which are on the device: the tiles of all units (sequence, key head, row tile)
 // are counted one after the other, and each warp (a block of its own) takes an equal run of them, whatever units it touches.  A unit that lies in one
@@ -158,25 +159,26 @@ struct Query4 {
     }
 };
 
-// The rows of a unit as the products take them (row 8 n + r4 as operand), and what belongs to rows 8 n + 2 c4 + e, whose accumulators a lane holds.
-template <typename T, int D, int NR>
+// The rows of a unit as the products take them: in column r4 of tile n row 8 n + r4, and what belongs to the rows of columns 2 c4 + e, e < E, whose accumulators a lane
+// holds.  E = 1: up to four rows, in the even columns alone, so that a lane has the softmax of one row for each key, not of two.
+template <typename T, int D, int NR, int E>
 struct Rows4 {
     using Geo = Attn4Geo<T, D, NR>;
     static constexpr int TERMS = Geo::TERMS;
     uint32_t q[Geo::Q_SHARED ? 1 : NR][TERMS][Geo::NG][2][2];
-    float factor[NR][2], sum[NR][2];
-    float first[NR][TERMS][2];                                       // (fp32) what the products of each term begin with
+    float factor[NR][E], sum[NR][E];
+    float first[NR][TERMS][E];                                       // (fp32) what the products of each term begin with
     __device__ __forceinline__ void load(const AttnParams& p, int64_t token0, int head, int row0, int rows, unsigned char* smem) {
         const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            const int row = row0 + n * 8 + r4, tok = row / p.group;
+            const int row = row0 + (E == 1 ? r4 >> 1 : n * 8 + r4), tok = row / p.group;
             const T* src = static_cast<const T*>(p.q) + (token0 + tok) * p.q_st +
                            (static_cast<int64_t>(head) * p.group + (row - tok * p.group)) * p.q_sh;
             Query4<T, Geo::NG> x;
-            x.load(src, row < rows, p.scale_log2);
+            x.load(src, row < rows && (E == 2 || !(r4 & 1)), p.scale_log2);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < E; ++e) {
                 const int from = (2 * c4 + e) * 4;
                 factor[n][e] = __shfl_sync(kFullMask, x.factor, from);
                 sum[n][e] = __shfl_sync(kFullMask, x.sum, from);
@@ -237,10 +239,10 @@ __device__ __forceinline__ float base4_of(unsigned word) {
 // S^T = C Q^T of a tile: s[n][2 k + e] = key r4 + 8 k, row 8 n + 2 c4 + e.
 // fp32 rows: the tensor core's accumulation truncates to about 24 bits of the largest product.  The first term of a query is therefore a
 // whole number of eighths of 2^-10 of the row's range: products with codes and sums of 128 of them take 22 bits, so nothing is lost.
-template <typename T, int D, int NR>
-__device__ __forceinline__ void scores4(const Rows4<T, D, NR>& rows, const unsigned char* tile, const unsigned char* q_smem,
+template <typename T, int D, int NR, int E>
+__device__ __forceinline__ void scores4(const Rows4<T, D, NR, E>& rows, const unsigned char* tile, const unsigned char* q_smem,
                                         float (&s)[NR][4]) {
-    constexpr int NG = D / 32, TERMS = Rows4<T, D, NR>::TERMS;
+    constexpr int NG = D / 32, TERMS = Rows4<T, D, NR, E>::TERMS;
     const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
     uint32_t w[2][NG];
 #pragma unroll
@@ -263,7 +265,7 @@ __device__ __forceinline__ void scores4(const Rows4<T, D, NR>& rows, const unsig
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][n][i] = TERMS == 2 ? rows.first[n][t][i & 1] : 0.0f;
+            for (int i = 0; i < 4; ++i) acc[t][n][i] = TERMS == 2 && (i & 1) < E ? rows.first[n][t][E == 2 ? i & 1 : 0] : 0.0f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         uint32_t a[2][4];
@@ -392,7 +394,7 @@ __device__ __forceinline__ int tiles4_of(const AttnParams& p, const int32_t* tab
 // How far a weight times a value's step, and a weight itself, may go before the row's reference moves.
 constexpr float kMostProduct4 = 16384.0f, kMostWeight4 = 0x1p100f;
 
-template <typename T, int D, int NR>
+template <typename T, int D, int NR, int E>
 __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segment4& u, Ring4& ring, unsigned char* smem) {
     using Geo = Attn4Geo<T, D, NR>;
     constexpr bool F32 = Geo::F32;
@@ -426,27 +428,29 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         if (lane == 0 && j < steps) ask((ring.taken + j) % STAGES, j, tile);
     }
     unsigned char* q_smem = smem + Geo::OFF_Q;
-    Rows4<T, D, NR> rw;
+    Rows4<T, D, NR, E> rw;
     rw.load(a, u.token0, u.head, u.row0, rows, q_smem);
     if constexpr (Geo::Q_SHARED) __syncwarp();
 
     // m: the reference of a row's weights exp2(score - m), which it shares with its products (weight times step): the largest product so far is 2^6 or
     // a little more, at most 2^14, so that products are fp16 numbers of full precision, whatever the values' size.
-    float m[NR][2], l[NR][2], r[NR][2];
+    float m[NR][E], l[NR][E], r[NR][E];
     float o[NR][D / 16][4];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < E; ++e) {
             m[n][e] = -INFINITY;
             l[n][e] = r[n][e] = 0.0f;
         }
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
     }
-    // keys that row 8 n + 2 c4 + e sees of these (rows that are not there see zeros); a step's second tile may lie behind the end
+    // the row of this lane's column 2 c4 + e
+    auto column_row = [&](int n, int e) { return E == 1 ? c4 : n * 8 + 2 * c4 + e; };
+    // keys that it sees of these (rows that are not there see zeros); a step's second tile may lie behind the end
     auto limit = [&](int n, int e) {
-        const int row = u.row0 + n * 8 + 2 * c4 + e;
+        const int row = u.row0 + column_row(n, e);
         return row < rows ? min(end, first_limit + row / a.group) : end;
     };
 
@@ -462,18 +466,18 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         Params4 w[U];
 #pragma unroll
         for (int t = 0; t < U; ++t) {
-            scores4<T, D, NR>(rw, tile + t * Geo::TILE, q_smem, s[t]);
+            scores4<T, D, NR, E>(rw, tile + t * Geo::TILE, q_smem, s[t]);
             w[t].load(tile + t * Geo::TILE + tile4_rows(D));
         }
         if (NR == 1 && u.scores != nullptr) {
 #pragma unroll
             for (int t = 0; t < U; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = i >> 1, e = i & 1, at = u.tile0 + j * U + t;
-                    if (2 * c4 + e < rows && j * U + t < tiles)
-                        u.scores[(static_cast<int64_t>(at) * p.part_rows + 2 * c4 + e) * kTileKeys + 8 * k + r4] =
-                            fmaf(step4_of(w[t].key(k)) * s[t][0][i], rw.factor[0][e], base4_of<T>(w[t].key(k)) * rw.sum[0][e]);
+                for (int i = 0; i < 2 * E; ++i) {
+                    const int k = i / E, e = i % E, at = u.tile0 + j * U + t, row = column_row(0, e);
+                    if (row < rows && j * U + t < tiles)
+                        u.scores[(static_cast<int64_t>(at) * p.part_rows + row) * kTileKeys + 8 * k + r4] =
+                            fmaf(step4_of(w[t].key(k)) * s[t][0][2 * k + e], rw.factor[0][e], base4_of<T>(w[t].key(k)) * rw.sum[0][e]);
                 }
         }
         auto hidden = [&](int t, int n, int i) { return base + t * kTileKeys + 8 * (i >> 1) + r4 >= limit(n, i & 1); };
@@ -484,20 +488,21 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
             y = x * step4_of(w[t].value(k));
         };
         // This lane's sums of a row: weights, weights times base values, products; and the products as operands, before their transposition.
-        float sx[NR][2], sr[NR][2], sy[NR][2];
+        float sx[NR][E], sr[NR][E], sy[NR][E];
         uint32_t b[U][NR][TERMS][2];
         auto add_up = [&] {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                sx[n][0] = sx[n][1] = sr[n][0] = sr[n][1] = sy[n][0] = sy[n][1] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) sx[n][e] = sr[n][e] = sy[n][e] = 0.0f;
 #pragma unroll
                 for (int t = 0; t < U; ++t)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const float base_value = base4_of<T>(w[t].value(k));
-                        float y[2];
+                        float y[2] = {0.0f, 0.0f};
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
+                        for (int e = 0; e < E; ++e) {
                             float x;
                             weigh(t, n, 2 * k + e, x, y[e]);
                             bool seen = true;
@@ -516,15 +521,18 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         float all_x = 0.0f, all_y = 0.0f;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            all_x += sx[n][0] + sx[n][1];
-            all_y += sy[n][0] + sy[n][1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                all_x += sx[n][e];
+                all_y += sy[n][e];
+            }
         }
         // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
         if (!__all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < E; ++e) {
                     // (a row moves its reference by its own scores alone: its result does not depend on the rows beside it)
                     int moves = !(sx[n][e] <= kMostWeight4 && sy[n][e] <= kMostProduct4);
 #pragma unroll
@@ -560,7 +568,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < E; ++e) {
                 l[n][e] += sx[n][e];
                 r[n][e] += sr[n][e];
             }
@@ -600,8 +608,8 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int local = n * 8 + 2 * c4 + e, row = u.row0 + local, tok = row / a.group;
+        for (int e = 0; e < E; ++e) {
+            const int local = column_row(n, e), row = u.row0 + local, tok = row / a.group;
             const float ll = column_sum(l[n][e]), rr = column_sum(r[n][e]);
             if (row >= rows) continue;
             const int64_t at = (u.token0 + tok) * a.hq + static_cast<int64_t>(u.head) * a.group + (row - tok * a.group);
@@ -690,7 +698,7 @@ __device__ __forceinline__ Place4 find_run4(const Attn4Params& p, int unit_rows,
     }
 }
 
-template <typename T, int D, int NR>
+template <typename T, int D, int NR, int E>
 __global__ void __launch_bounds__(32, (Attn4Geo<T, D, NR>::BLOCKS))
 attn4_kernel(const Attn4Params p) {
     using Geo = Attn4Geo<T, D, NR>;
@@ -729,7 +737,7 @@ attn4_kernel(const Attn4Params p) {
             // a unit that began in an earlier run leaves its part in this one's first place, one that goes on in its second
             u.slot = g0 > 0 ? 2ll * blockIdx.x : g1 < s.grains ? 2ll * blockIdx.x + 1 : -1;
             u.scores = p.scores == nullptr ? nullptr : p.scores + (static_cast<int64_t>(b) * a.hkv + u.head) * (static_cast<int64_t>(a.table_width) << a.page_shift) * p.part_rows;
-            attn4_segment<T, D, NR>(p, u, ring, smem4);
+            attn4_segment<T, D, NR, E>(p, u, ring, smem4);
             __syncwarp();
             f = start + g1;
         }
@@ -819,7 +827,7 @@ attn4_join_kernel(const Attn4Params p, int unit_rows) {
 
 // ---- the weight that each key receives: weights_out = weights + sum over the sequence's tokens and the group's heads of exp(score - lse).
 // Sequences of up to eight rows a key head: the attention has left the scores, four bytes a row and key; to take them again from the
-// codes costs D / 2 + 8 bytes a key and the products (32 x up to 8192 keys of 8 key heads, 4 rows: 48 us against 12, and 4 more for the attention that writes them: 55 against 51).
+// codes costs D / 2 + 8 bytes a key and the products (32 x up to 8192 keys of 8 key heads, 4 rows: 48 us against 12).
 // Four keys a thread.
 __global__ static void __launch_bounds__(256)
 attn4_weigh_scores_kernel(const Attn4Params p, int chunks) {
@@ -919,7 +927,7 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
             const int tile = __shfl_sync(kFullMask, tile_no, j);
             if (lane == 0 && j < n) ask((taken + j) % STAGES, tile);
         }
-        Rows4<T, D, NR> rw;
+        Rows4<T, D, NR, 2> rw;
         rw.load(a, token0, head, row0, rows, nullptr);
         int limit[NR][2];
         float lse[NR][2];
@@ -936,7 +944,7 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
             mbar_wait_bounded(full + stage, (taken / STAGES) & 1u);
             const unsigned char* tile = smem4 + stage * Geo::STAGE;
             float s[NR][4];
-            scores4<T, D, NR>(rw, tile, nullptr, s);
+            scores4<T, D, NR, 2>(rw, tile, nullptr, s);
             Params4 w;
             w.load(tile + 8 * D);
 #pragma unroll

@@ -453,3 +453,27 @@ def test_calls_one_right_behind_the_other_see_what_came_before(A, tokens):
         for a, b in zip(rounds(lambda: None), patient):
             assert torch.equal(a, b)
     A.device_status()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group,counts,d", [(1, (4, 0, 1, 3), 64), (2, (2, 1, 0, 2), 96), (3, (1, 1, 1, 1), 128), (4, (0, 1, 1, 0), 64), (5, (1, 1, 0, 1), 128)])
+def test_up_to_four_rows_and_a_few_more(A, dtype, group, counts, d):
+    """Four rows a sequence and key head sit in other columns of the products than five; told of more tokens than there are, the same call takes
+    the columns of eight."""
+    page, hkv, lens = 32, 2, (700, 40, 1, 333)
+    width = 22
+    cache, keys, values = filled(A, len(lens) * width, hkv, page, d, seed=group)
+    table = torch.randperm(len(lens) * width, generator=gen(9)).int().reshape(len(lens), width)
+    start = [0]
+    for c in counts:
+        start.append(start[-1] + c)
+    q = torch.randn(start[-1], hkv * group, d, generator=gen(group + 50)).to(dtype)
+    want, received = expected(q, keys, values, table, lens, page, start)
+    for most in (max(counts), 8):
+        out, weights = A.paged_attention4(q.cuda(), cache, table.cuda(), ints(*lens), q_start=ints(*start), max_q_len=most,
+                                          weights_out=torch.empty(len(lens), hkv, width * page, device="cuda"))
+        assert close(out, want, q)
+        for b, n in enumerate(lens):
+            assert ((weights[b, :, :n].cpu().double() - received[b]).abs() <= 1e-4 * received[b] + 1e-30).all()
+            assert (weights[b, :, n:] == 0).all()
+    A.device_status()
