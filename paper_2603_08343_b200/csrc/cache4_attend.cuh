@@ -49,13 +49,19 @@ int weigh4(const Attn4Params& p, bool after, int dev, cudaStream_t s) {
     int rc = prepare4(attn4_weigh_kernel<T, D, NR>, Geo::BYTES, dev, ready);
     if (rc != WHT_OK) return rc;
     const long long keys = static_cast<long long>(p.a.table_width) << p.a.page_shift;
-    const long long chunks = ceil_div(keys, kWeightTiles * kTileKeys), blocks = chunks * p.a.hkv * p.a.B;
+    int device = 0, sms = 0, tiles = kWeightTiles;
+    rc = device_info(&device, &sms);
+    if (rc != WHT_OK) return rc;
+    // (shorter chunks read the rows more often, but fill the machine.  us, chunks of 32 tiles alone and by this rule: 64 tokens of 4 rows over 4000 keys, 8 key
+    // heads, 225 and 56; 8 sequences of up to 8 tokens of 16 rows over 16652, 2 key heads, 174 and 78; 512 tokens of 16 heads over 2000 431 and 95)
+    while (tiles > 1 && ceil_div(keys, tiles * kTileKeys) * p.a.hkv * p.a.B < 12 * sms) tiles /= 2;
+    const long long chunks = ceil_div(keys, tiles * kTileKeys), blocks = chunks * p.a.hkv * p.a.B;
     if (blocks > 0x7fffffffll) return WHT_ERR_BAD_T;
     if (blocks == 0) return WHT_OK;
     if (after)
-        launch_overlapped(attn4_weigh_kernel<T, D, NR>, dim3(static_cast<unsigned>(blocks)), 32, Geo::BYTES, s, p, static_cast<int>(chunks));
+        launch_overlapped(attn4_weigh_kernel<T, D, NR>, dim3(static_cast<unsigned>(blocks)), 32, Geo::BYTES, s, p, tiles, static_cast<int>(chunks));
     else
-        attn4_weigh_kernel<T, D, NR><<<static_cast<unsigned>(blocks), 32, Geo::BYTES, s>>>(p, static_cast<int>(chunks));
+        attn4_weigh_kernel<T, D, NR><<<static_cast<unsigned>(blocks), 32, Geo::BYTES, s>>>(p, tiles, static_cast<int>(chunks));
     WHT_CUDA_TRY(cudaGetLastError());
     return WHT_OK;
 }

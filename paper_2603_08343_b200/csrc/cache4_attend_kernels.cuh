@@ -866,7 +866,7 @@ attn4_weigh_scores_kernel(const Attn4Params p, int chunks) {
 }
 
 // More rows, or more scores than there should be memory for:
-// A warp takes kWeightTiles tiles of one sequence and key head and goes through all rows that read them; one owner per key, so the sum has
+// A warp takes chunk_tiles (kWeightTiles at most) tiles of one sequence and key head and goes through all rows that read them; one owner per key, so the sum has
 // one order.  Places from the sequence's length on become 0.
 constexpr int kWeightTiles = 32;
 
@@ -881,7 +881,7 @@ struct Weigh4Geo {
 
 template <typename T, int D, int NR>
 __global__ void __launch_bounds__(32, 16)
-attn4_weigh_kernel(const Attn4Params p, int chunks) {
+attn4_weigh_kernel(const Attn4Params p, int chunk_tiles, int chunks) {
     using Geo = Weigh4Geo<T, D, NR>;
     constexpr int STAGES = Geo::STAGES;
     extern __shared__ __align__(128) unsigned char smem4[];
@@ -896,9 +896,9 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
     const int chunk = static_cast<int>(blockIdx.x % chunks);
     const int head = static_cast<int>((blockIdx.x / chunks) % a.hkv), b = static_cast<int>(blockIdx.x / chunks / a.hkv);
     const int width = a.table_width << a.page_shift;
-    const int key0 = chunk * kWeightTiles * kTileKeys;
+    const int chunk_keys = chunk_tiles * kTileKeys, key0 = chunk * chunk_keys;
     const int64_t at = (static_cast<int64_t>(b) * a.hkv + head) * width;
-    for (int i = lane; i < kWeightTiles * kTileKeys; i += 32) sums[i] = 0.0f;
+    for (int i = lane; i < chunk_keys; i += 32) sums[i] = 0.0f;
     __syncwarp();
     grid_dependency_wait();                                          // the rows' sums come from the kernels before
     int64_t token0;
@@ -907,7 +907,7 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
     const int keys = attn_length(a, b), first_limit = keys - count + 1;
     const int32_t* table = a.page_table + static_cast<int64_t>(b) * a.table_width;
     const int rows = count * a.group;
-    const int here = max(0, min(keys, key0 + kWeightTiles * kTileKeys) - key0);      // keys of this chunk
+    const int here = max(0, min(keys, key0 + chunk_keys) - key0);      // keys of this chunk
     const int tiles = (here + kTileKeys - 1) / kTileKeys;
     const int tile_no = tiles4_of(a, table, head, key0 / kTileKeys, key0 / kTileKeys + tiles);
     unsigned taken = 0;
@@ -967,7 +967,7 @@ attn4_weigh_kernel(const Attn4Params p, int chunks) {
         }
     }
     __syncwarp();
-    const int stop = min(width - key0, kWeightTiles * kTileKeys);
+    const int stop = min(width - key0, chunk_keys);
     for (int i = lane * 4; i < stop; i += 128) {                     // (a page holds whole tiles: widths are multiples of 16)
         float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
         if (p.weights && i < here) old = *reinterpret_cast<const float4*>(p.weights + at + key0 + i);
