@@ -2,12 +2,18 @@
 //
 //     k_j = lo_j + step_j c_j,   v_j = lo'_j + step'_j c'_j      (codes c, c' whole numbers 0 .. 15)
 //     score_j = scale (step_j (q . c_j) + lo_j sum(q))
-//     o = sum_j p_j v_j / sum_j p_j = (sum_j (p_j step'_j) c'_j + sum_j p_j lo'_j) / sum_j p_j,   p_j = exp(score_j - m)
+//     o = sum_j p_j v_j / sum_j p_j = (sum_j (p_j step'_j) (c'_j - z_j) + sum_j p_j (lo'_j + z_j step'_j)) / sum_j p_j,   p_j = exp(score_j - m)
 //
-// in one pass over the keys.  The codes are never turned into values: a half word of codes masked with 0x000f or 0x00f0 IS an fp16
+// in one pass over the keys.  The codes are never turned into values.  A half word of a key's codes masked with 0x000f or 0x00f0 IS an fp16
 // number, c 2^-24 or 16 c 2^-24 (a subnormal one; the tensor core takes these as they are, but aligns a product by its operands'
 // exponents, so that sums keep about 20 bits), so that eight codes take four masks and one shift, exactly, and the powers of two go into the
-// queries and the result.  For fp32 results the values' codes become ordinary numbers, c - 8, by one exact subtraction a pair.
+// queries and the result.  z_j keeps the two sums small: with z = 0 for all keys they are large, of opposite signs, and the result is their small
+// difference.  For bf16 results z is 0 for the keys of even places and 15 for the others, whose codes are turned over as they are loaded (15 - c) and whose
+// steps change sign, which costs next to nothing; for fp32 ones, whose values' codes become ordinary numbers by one exact subtraction a pair, z
+// is 8 and 7 (64 x 16384 in bf16 would then take 192 us instead of 164).
+// The tensor core's accumulation truncates towards zero, by up to 2^-23 of a sum in each addition, so that the loss grows with their
+// number: after kFold4 steps the accumulators are added to sums in shared memory, with rounding, and begin anew.  (With z = 0 and one accumulation a
+// run, 131072 keys of even weight were off by 0.38 of the result's norm and 1048576 by 13 times the norm; now by 0.0004 and 0.0007 beside the rounding to bf16.)
 // Queries enter as fp16 after a shift of each row by a power of two (bf16 ones keep all their bits but what lies below 2^-33 of the row's
 // maximum; fp32 ones are two terms, 22 bits of it), and the weights p step' as fp16 times a power of two per row that keeps them in range: one
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
@@ -57,7 +63,9 @@ struct Attn4Geo {
     static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
     static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;
     static constexpr int OFF_Q = STAGES * U * TILE;
-    static constexpr int OFF_BARS = OFF_Q + Q_BYTES;
+    static constexpr int OFF_FOLD = OFF_Q + Q_BYTES;            // a lane's sums of the steps before: [accumulator, then r and m of each row][lane]
+    static constexpr int FOLD_O = NR * (D / 4), FOLD = FOLD_O + 4 * NR;
+    static constexpr int OFF_BARS = OFF_FOLD + FOLD * 128;
     static constexpr int BYTES = OFF_BARS + STAGES * 8;
     static constexpr int BLOCKS = NR * TERMS > 2 ? 8 : NR * TERMS > 1 ? 12 : 16;  // on an SM
 };
@@ -229,12 +237,17 @@ struct Params4 {
     __device__ __forceinline__ uint32_t value(int k) const { return k ? upper.y : lower.y; }
 };
 
-// A row's base: its least value; for fp32 what code 8 stands for, since lo and the sum of codes, all positive, are several times what they weigh
+// A key's base: its least value; for fp32 what code 8 stands for, since lo and the sum of codes, all positive, are several times what they weigh
 // together in the end.
 template <typename T>
 __device__ __forceinline__ float base4_of(unsigned word) {
     return std::is_same<T, float>::value ? fmaf(8.0f, step4_of(word), lo4_of(word)) : lo4_of(word);
 }
+
+// What the code z of a value stands for.
+__device__ __forceinline__ float value4_of(unsigned word, float z) { return fmaf(z, step4_of(word), lo4_of(word)); }
+// A step with the sign that `turn` (0 or the sign's bit) gives it: one multiply-add.
+__device__ __forceinline__ float turned_step4_of(unsigned word, unsigned turn) { return __uint_as_float(word * 65536u + turn); }
 
 // S^T = C Q^T of a tile: s[n][2 k + e] = key r4 + 8 k, row 8 n + 2 c4 + e.
 // fp32 rows: the tensor core's accumulation truncates to about 24 bits of the largest product.  The first term of a query is therefore a
@@ -293,20 +306,23 @@ __device__ __forceinline__ void scores4(const Rows4<T, D, NR, E>& rows, const un
         for (int i = 0; i < 4; ++i) s[n][i] = TERMS == 2 ? acc[0][n][i] + acc[TERMS - 1][n][i] : acc[0][n][i];
 }
 
-// O^T += C'^T P^T of a tile; b[n][t]: the weights times the values' steps as operands (row r4; keys 2 c4, + 1 and 8 + 2 c4, + 1).
-// o[n][2 g + i][2 j + e]: channel 32 g + 4 r4 + 2 i + j, row 8 n + 2 c4 + e.
+// O^T += (C' - z)^T P^T of a tile; b[n][t]: the weights times the values' steps as operands (row r4; keys 2 c4, + 1 and 8 + 2 c4, + 1; bf16: those of odd
+// keys with the other sign).  o[n][2 g + i][2 j + e]: channel 32 g + 4 r4 + 2 i + j, row 8 n + 2 c4 + e.
 template <typename T, int D, int NR>
 __device__ __forceinline__ void add_values4(const unsigned char* tile, const uint32_t (&b)[NR][Attn4Geo<T, D, NR>::TERMS][2], float (&o)[NR][D / 16][4]) {
     constexpr int NG = D / 32;
     constexpr bool F32 = std::is_same<T, float>::value;
     const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
-    // this lane's codes of the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4, halves u = r4; two neighbouring keys side by side
+    // this lane's codes of the keys 2 c4, 2 c4 + 1, 8 + 2 c4, 9 + 2 c4, halves u = r4; two neighbouring keys side by side.  bf16: those of odd keys turned over
     const unsigned char* vt = tile + 8 * D;
     uint32_t pair[NG][2];
     if constexpr (NG == 4) {
         uint2 v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2*>(vt + (c4 + 4 * i) * 64 + ((r4 ^ ((c4 & 2) << 1)) << 3));
+        for (int i = 0; i < 4; ++i) {
+            v[i] = *reinterpret_cast<const uint2*>(vt + (c4 + 4 * i) * 64 + ((r4 ^ ((c4 & 2) << 1)) << 3));
+            if (!F32 && (i & 1)) v[i] = make_uint2(~v[i].x, ~v[i].y);
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             pair[0][i] = __byte_perm(v[2 * i].x, v[2 * i + 1].x, 0x5410);
@@ -317,7 +333,10 @@ __device__ __forceinline__ void add_values4(const unsigned char* tile, const uin
     } else {
         uint32_t v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(vt + (c4 + 4 * i) * 32 + r4 * 4);
+        for (int i = 0; i < 4; ++i) {
+            v[i] = *reinterpret_cast<const uint32_t*>(vt + (c4 + 4 * i) * 32 + r4 * 4);
+            if (!F32 && (i & 1)) v[i] = ~v[i];
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             pair[0][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
@@ -325,7 +344,10 @@ __device__ __forceinline__ void add_values4(const unsigned char* tile, const uin
         }
         if constexpr (NG == 3) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const unsigned short*>(vt + 512 + (c4 + 4 * i) * 16 + r4 * 2);
+            for (int i = 0; i < 4; ++i) {
+                v[i] = *reinterpret_cast<const unsigned short*>(vt + 512 + (c4 + 4 * i) * 16 + r4 * 2);
+                if (!F32 && (i & 1)) v[i] = ~v[i];
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) pair[2][i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
         }
@@ -338,11 +360,12 @@ __device__ __forceinline__ void add_values4(const unsigned char* tile, const uin
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t x = st ? pair[g][k] >> 8 : pair[g][k];
-                a[2 * k] = x & 0x000f000fu;
-                a[2 * k + 1] = x & 0x00f000f0u;
-                if (F32) {                                           // code - 8, exactly, as ordinary numbers
-                    a[2 * k] = minus_half2(a[2 * k] | 0x64006400u, 0x64086408u);
-                    a[2 * k + 1] = minus_half2(a[2 * k + 1] | 0x64006400u, 0x64806480u);
+                if constexpr (F32) {                                 // 1024 + c less 1024 + z; the lower half is the even key's
+                    a[2 * k] = minus_half2((x & 0x000f000fu) | 0x64006400u, 0x64076408u);
+                    a[2 * k + 1] = minus_half2((x & 0x00f000f0u) | 0x64006400u, 0x64706480u);
+                } else {
+                    a[2 * k] = x & 0x000f000fu;
+                    a[2 * k + 1] = x & 0x00f000f0u;
                 }
             }
 #pragma unroll
@@ -393,6 +416,8 @@ __device__ __forceinline__ int tiles4_of(const AttnParams& p, const int32_t* tab
 
 // How far a weight times a value's step, and a weight itself, may go before the row's reference moves.
 constexpr float kMostProduct4 = 16384.0f, kMostWeight4 = 0x1p100f;
+// Steps of which the tensor core holds the sum: 1024 keys (512 in units of 16 rows).
+constexpr int kFold4 = 32;
 
 template <typename T, int D, int NR, int E>
 __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segment4& u, Ring4& ring, unsigned char* smem) {
@@ -401,6 +426,9 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
     constexpr int NG = Geo::NG, STAGES = Geo::STAGES, U = Geo::U, TERMS = Geo::TERMS;
     const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31, r4 = lane >> 2, c4 = lane & 3;
+    // z of this lane's keys (with the sign of their steps); bf16: odd ones take their steps, and with them the products, with the other sign
+    const float zero_code = F32 ? (r4 & 1 ? 7.0f : 8.0f) : r4 & 1 ? -15.0f : 0.0f;
+    const unsigned turn = !F32 && (r4 & 1) ? 0x80000000u : 0u;
     const int rows = u.count * a.group;
     // the unit's last row sees the most keys, its first row the fewest
     const int last_row = min(rows, u.row0 + Geo::ROWS) - 1;
@@ -485,7 +513,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         auto weigh = [&](int t, int n, int i, float& x, float& y) {
             const int k = i >> 1, e = i & 1;
             x = exp2_fast(fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -m[n][e])));
-            y = x * step4_of(w[t].value(k));
+            y = x * turned_step4_of(w[t].value(k), turn);
         };
         // This lane's sums of a row: weights, weights times base values, products; and the products as operands, before their transposition.
         float sx[NR][E], sr[NR][E], sy[NR][E];
@@ -499,7 +527,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                 for (int t = 0; t < U; ++t)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float base_value = base4_of<T>(w[t].value(k));
+                        const float base_value = fmaf(zero_code, turned_step4_of(w[t].value(k), turn), lo4_of(w[t].value(k)));
                         float y[2] = {0.0f, 0.0f};
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
@@ -527,14 +555,14 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                 all_y += sy[n][e];
             }
         }
-        // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does)
-        if (!__all_sync(kFullMask, all_x <= kMostWeight4 && all_y <= kMostProduct4)) {
+        // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does; a lane's products have one sign)
+        if (!__all_sync(kFullMask, all_x <= kMostWeight4 && fabsf(all_y) <= kMostProduct4)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     // (a row moves its reference by its own scores alone: its result does not depend on the rows beside it)
-                    int moves = !(sx[n][e] <= kMostWeight4 && sy[n][e] <= kMostProduct4);
+                    int moves = !(sx[n][e] <= kMostWeight4 && fabsf(sy[n][e]) <= kMostProduct4);
 #pragma unroll
                     for (int i = 4; i < 32; i <<= 1) moves |= __shfl_xor_sync(kFullMask, moves, i);
                     if (!__any_sync(kFullMask, moves)) continue;
@@ -601,8 +629,44 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
     };
     // steps whose keys all rows see, then the others
     const int open = least_limit > u.tile0 * kTileKeys ? min(steps, (least_limit - u.tile0 * kTileKeys) / (U * kTileKeys)) : 0;
-    for (int j = 0; j < open; ++j) step(j, std::false_type{});
-    for (int j = open; j < steps; ++j) step(j, std::true_type{});
+    float* fold = reinterpret_cast<float*>(smem + Geo::OFF_FOLD) + lane;
+    for (int j = 0;;) {
+        const int stop = min(steps, j + kFold4), begin = j;
+        for (; j < min(stop, open); ++j) step(j, std::false_type{});
+        for (; j < stop; ++j) step(j, std::true_type{});
+        // the sums of the steps before, in the present reference
+        if (begin > 0) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float* before = fold + (Geo::FOLD_O + 4 * n + 2 * e) * 32;
+                    const float was = before[32], f = m[n][e] > was ? exp2_fast(was - m[n][e]) : 1.0f;
+                    r[n][e] = fmaf(before[0], f, r[n][e]);
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                        for (int i = e; i < 4; i += 2) o[n][d][i] = fmaf(fold[((n * (D / 16) + d) * 4 + i) * 32], f, o[n][d][i]);
+                }
+        }
+        if (j >= steps) break;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float* to = fold + (Geo::FOLD_O + 4 * n + 2 * e) * 32;
+                to[0] = r[n][e];
+                to[32] = m[n][e];
+                r[n][e] = 0.0f;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                    for (int i = e; i < 4; i += 2) {
+                        fold[((n * (D / 16) + d) * 4 + i) * 32] = o[n][d][i];
+                        o[n][d][i] = 0.0f;
+                    }
+            }
+    }
 
     // the results, four channels of a row at a time
 #pragma unroll

@@ -2,9 +2,11 @@
 //
 // The formulas are those of cache4_attend_kernels.cuh.  A unit is 256 rows (token, query head) of one sequence and key head, two tiles of 128, so that
 // with the queries as one operand and the codes of 64 keys as the other both products are dense:
-//     S = Q C^T (bf16: codes 0 .. 15 are exact)    P = exp2(score - m) step' as fp16, over S in tensor memory    O += P C' (fp16)
+//     S = Q C^T (bf16: codes 0 .. 15 are exact)    P = exp2(score - m) step' as fp16, over S in tensor memory    O += P (C' - z) (fp16)
 // with O in tensor memory too.  Codes become numbers on their way from the cache to shared memory, once per 256 rows: a half word masked and
-// joined with the exponent of 128 (bf16) or 1024 (fp16), less that number; values' odd codes stay 16 times too large until the end.
+// joined with the exponent of 128 (bf16) or 1024 (fp16), less that number (and, of a value, less z); values' odd codes stay 16 times too large until the end.
+// The tensor core truncates as it adds: every kFoldUmma4 steps a row's O moves to a sum in the workspace, where it is added with rounding (512 tokens over
+// 100000 keys 1115 us with it, 1091 without; every 32 steps 1161).
 //
 // A block of 13 warps has an SM to itself:
 //   warps 0 .. 3, 4 .. 7  softmax of the two tiles, a row a thread; the queries, and the results
@@ -32,6 +34,7 @@ namespace wht {
 constexpr int kUmma4Threads = 416;
 constexpr int kUmma4Rows = 256, kUmma4Keys = 64;
 constexpr float kMostUmma4 = 32768.0f;  // of the products of a row and 64 keys together
+constexpr int kFoldUmma4 = 64;          // steps of which the tensor core holds the sum: 4096 keys
 
 template <int D>
 struct Umma4Geo {
@@ -59,15 +62,15 @@ __device__ __forceinline__ uint32_t minus_bf162(uint32_t a, uint32_t b) {
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// Eight codes of a word as bf16 pairs (code i, code 4 + i), and as fp16 pairs, the odd ones times 16.
+// Eight codes of a word as bf16 pairs (code i, code 4 + i), and less `even` as fp16 pairs, the odd ones times 16 (less `odd`).
 __device__ __forceinline__ uint4 codes_bf16(uint32_t w) {
     auto two = [](uint32_t x) { return minus_bf162((x & 0x000f000fu) | 0x43004300u, 0x43004300u); };
     return make_uint4(two(w), two(w >> 4), two(w >> 8), two(w >> 12));
 }
-__device__ __forceinline__ uint4 codes_f16(uint32_t w) {
-    auto even = [](uint32_t x) { return minus_half2((x & 0x000f000fu) | 0x64006400u, 0x64006400u); };
-    auto odd = [](uint32_t x) { return minus_half2((x & 0x00f000f0u) | 0x64006400u, 0x64006400u); };
-    return make_uint4(even(w), odd(w), even(w >> 8), odd(w >> 8));
+__device__ __forceinline__ uint4 codes_f16(uint32_t w, uint32_t even, uint32_t odd) {
+    auto low = [&](uint32_t x) { return minus_half2((x & 0x000f000fu) | 0x64006400u, even); };
+    auto high = [&](uint32_t x) { return minus_half2((x & 0x00f000f0u) | 0x64006400u, odd); };
+    return make_uint4(low(w), high(w), low(w >> 8), high(w >> 8));
 }
 // Piece c of row r of an operand in the 128-byte swizzle, `box` bytes between blocks of 64 channels.
 __device__ __forceinline__ int piece_of(int box, int r, int c) { return (c >> 3) * box + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
@@ -166,6 +169,8 @@ attn4_umma_kernel(const Attn4Params p) {
         // codes of one key (value) a thread and step
         const bool values = warp >= 10;
         const int kk = tid & 63, j = kk & 15;
+        const float zero_code = j & 1 ? 7.0f : 8.0f;                 // z of this key; 1024 + z and 1024 + 16 z, twice
+        const uint32_t even = j & 1 ? 0x64076407u : 0x64086408u, odd = j & 1 ? 0x64706470u : 0x64806480u;
         constexpr int LOADS = D / 32;                                // 16 bytes each
         uint64_t *full = values ? v_full : k_full, *free_bar = values ? v_free : k_free;
         walk([&](const Segment4& u, int end, int steps, unsigned first) {
@@ -220,12 +225,12 @@ attn4_umma_kernel(const Attn4Params p) {
                         const uint32_t w = n % 4 == 0 ? raw[n / 4].x : n % 4 == 1 ? raw[n / 4].y : n % 4 == 2 ? raw[n / 4].z : raw[n / 4].w;
                         if constexpr (D == 128) {
                             const int at = 2 * ((n >> 1) ^ (j & 4)) + (n & 1);
-                            *reinterpret_cast<uint4*>(to + piece_of(Geo::BOX, kk, at)) = codes_f16(w);
+                            *reinterpret_cast<uint4*>(to + piece_of(Geo::BOX, kk, at)) = codes_f16(w, even, odd);
                         } else if (n < 8) {
-                            *reinterpret_cast<uint4*>(to + piece_of(Geo::BOX, kk, n)) = codes_f16(w);
+                            *reinterpret_cast<uint4*>(to + piece_of(Geo::BOX, kk, n)) = codes_f16(w, even, odd);
                         } else {
                             const uint32_t lo = (w & 0xffffu) | (w << 12), hi = (w >> 16) | ((w >> 4) & 0x0ffff000u);   // codes 0 and 1 (2 and 3) side by side
-                            auto two = [](uint32_t x) { return minus_half2((x & 0x000f000fu) | 0x64006400u, 0x64006400u); };
+                            auto two = [&](uint32_t x) { return minus_half2((x & 0x000f000fu) | 0x64006400u, even); };
                             *reinterpret_cast<uint4*>(to + piece_of(Geo::BOX, kk, n)) = make_uint4(two(lo), two(lo >> 8), two(hi), two(hi >> 8));
                         }
                     }
@@ -233,7 +238,7 @@ attn4_umma_kernel(const Attn4Params p) {
                     rows[0] = step4_of(row.x);
                     rows[2] = lo4_of(row.x);
                     rows[4] = step4_of(row.y);
-                    rows[6] = lo4_of(row.y);
+                    rows[6] = value4_of(row.y, zero_code);
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -353,121 +358,166 @@ attn4_umma_kernel(const Attn4Params p) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + w);
             }
-            for (int i = 0; i < steps; ++i) {
-                const unsigned step = first + i, buf = step & 1, phase = (step >> 1) & 1;
-                const int base = u.tile0 * kTileKeys + i * kUmma4Keys;
-                const bool mask = base + kUmma4Keys > least_limit;
-                if (!warp_poll_both(v_full + buf, s_full + buf, phase, abort_flag)) return false;
-                tc_fence_after();
-                const uint32_t s_cols = tmem + buf * 64 + lanes;
-                const float4* par = reinterpret_cast<const float4*>(smem + Geo::OFF_ROWS + buf * 1024);   // two keys, then their values
-                uint32_t y[32];
-                float sx, sy, sr;
-                auto weigh = [&](auto masked) {
-                    const uint64_t sl2 = pair(sl, sl), qs2 = pair(qs, qs), m2 = pair(-m, -m);
-                    uint64_t sx2 = 0, sy2 = 0, sr2 = 0;
-#pragma unroll
-                    for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
-                        float s[16];
-                        tmem_ld16(s_cols + c0, s);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const float4 key = par[c0 + e], val = par[c0 + e + 1];
-                            float x0, x1, y0, y1;
-                            unpair(fma2(mul2(pair(key.x, key.y), pair(s[e], s[e + 1])), sl2, fma2(pair(key.z, key.w), qs2, m2)), x0, x1);
-                            x0 = exp2_fast(x0);
-                            x1 = exp2_fast(x1);
-                            uint64_t x2 = pair(x0, x1), lo2 = pair(val.z, val.w), y2 = mul2(x2, pair(val.x, val.y));
-                            if constexpr (masked.value) {
-                                const bool see0 = base + c0 + e < limit, see1 = base + c0 + e + 1 < limit;
-                                unpair(y2, y0, y1);
-                                x2 = pair(see0 ? x0 : 0.0f, see1 ? x1 : 0.0f);
-                                lo2 = pair(see0 ? val.z : 0.0f, see1 ? val.w : 0.0f);
-                                y2 = pair(see0 ? y0 : 0.0f, see1 ? y1 : 0.0f);
-                            }
-                            sx2 = add2(sx2, x2);
-                            sy2 = add2(sy2, y2);
-                            sr2 = fma2(x2, lo2, sr2);
-                            unpair(y2, y0, y1);
-                            y[(c0 + e) / 2] = pack_half2(y0, y1);
-                        }
-                    }
-                    float p0, p1;
-                    unpair(sx2, p0, p1);
-                    sx = p0 + p1;
-                    unpair(sy2, p0, p1);
-                    sy = p0 + p1;
-                    unpair(sr2, p0, p1);
-                    sr = p0 + p1;
-                };
-                // A segment's first step, and later the rare case that some row's weights or products have grown too far: the row's reference moves so
-                // that its largest product becomes 2^6.  O and the sums follow.  (Once a step: what is NaN stays NaN.)
-                bool moved = false;
-                for (;;) {
-                    if (i > 0 || moved) {
-                        if (mask) weigh(std::true_type{});
-                        else weigh(std::false_type{});
-                        if (moved || __all_sync(kFullMask, sx <= kMostWeight4 && sy <= kMostUmma4)) break;
-                    } else {
-                        sx = INFINITY;
-                    }
-                    const bool moves = !(sx <= kMostWeight4 && sy <= kMostUmma4);
-                    float top = -INFINITY, heavy = -INFINITY;
+            // Sums of O from the steps before the last fold, in the reference of that time: [four channels][row] for a warp, in the part that the unit leaves (one that
+            // leaves none uses the place of the part that goes on, which is written after it).
+            const int part_lanes = min(32, p.part_rows - warp * 32);
+            float* kept = a.part_o + ((u.slot >= 0 ? u.slot : 2ll * blockIdx.x + 1) * p.part_rows + warp * 32) * D + lane * 4;
+            float kept_m = 0.0f;
+            // last: O becomes the whole sum; else the sum takes O, which begins anew
+            auto fold = [&](bool begun, bool last) {
+                const float f = m > kept_m ? exp2_fast(kept_m - m) : 1.0f;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
-                        float s[16];
-                        tmem_ld16(s_cols + c0, s);
-                        tmem_wait_ld();
+                for (int c = 0; c < D; c += 16) {
+                    float o[16];
+                    float* to = kept + c * part_lanes;
+                    tmem_ld16(o_cols + c, o);
+                    float4 x[4] = {};
+                    if (begun && row < rows)
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const float4 key = par[c0 + e], val = par[c0 + e + 1];
-                            const float z0 = fmaf(key.x * s[e], sl, key.z * qs), z1 = fmaf(key.y * s[e + 1], sl, key.w * qs);
-                            if (base + c0 + e < limit) {
-                                top = fmaxf(top, z0);
-                                heavy = fmaxf(heavy, z0 + __log2f(val.x));
-                            }
-                            if (base + c0 + e + 1 < limit) {
-                                top = fmaxf(top, z1);
-                                heavy = fmaxf(heavy, z1 + __log2f(val.y));
-                            }
-                        }
-                    }
-                    float to = heavy > -INFINITY ? fmaxf(heavy - 6.0f, top - 90.0f) : top;
-                    to = moves ? fmaxf(to, m) : m;
-                    const float f = to > m ? exp2_fast(m - to) : 1.0f;
-                    m = to;
-                    l *= f;
-                    r *= f;
-                    if (i > 0) {
-                        if (!warp_poll_or_abort(v_free + ((step - 1) & 1), ((step - 1) >> 1) & 1u, abort_flag)) return false;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < Geo::O_COLS; c += 16) {
-                            float o[16];
-                            tmem_ld16(o_cols + c, o);
-                            tmem_wait_ld();
-                            uint32_t z[16];
+                        for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(to + e * 4 * part_lanes);
+                    tmem_wait_ld();
+                    uint32_t z[16];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * f);
-                            tmem_st16(o_cols + c, z);
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = make_float4(fmaf(x[e].x, f, o[4 * e]), fmaf(x[e].y, f, o[4 * e + 1]), fmaf(x[e].z, f, o[4 * e + 2]), fmaf(x[e].w, f, o[4 * e + 3]));
+                        if (!last && row < rows) *reinterpret_cast<float4*>(to + e * 4 * part_lanes) = x[e];
+                        z[4 * e] = last ? __float_as_uint(x[e].x) : 0;
+                        z[4 * e + 1] = last ? __float_as_uint(x[e].y) : 0;
+                        z[4 * e + 2] = last ? __float_as_uint(x[e].z) : 0;
+                        z[4 * e + 3] = last ? __float_as_uint(x[e].w) : 0;
                     }
-                    moved = true;
+                    tmem_st16(o_cols + c, z);
                 }
-                l += sx;
-                r += sr;
-                tmem_st16(s_cols, y);
-                tmem_st16(s_cols + 16, y + 16);
                 tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready + buf);
+                kept_m = m;
+            };
+            for (int i = 0; i < steps;) {
+                if (i > 0) {
+                    const unsigned before = first + i - 1;
+                    if (!warp_poll_or_abort(v_free + (before & 1), (before >> 1) & 1u, abort_flag)) return false;
+                    tc_fence_after();
+                    fold(i > kFoldUmma4, false);
+                }
+                const int stop = min(steps, i + kFoldUmma4);
+#pragma unroll 1
+                for (; i < stop; ++i) {
+                    const unsigned step = first + i, buf = step & 1, phase = (step >> 1) & 1;
+                    const int base = u.tile0 * kTileKeys + i * kUmma4Keys;
+                    const bool mask = base + kUmma4Keys > least_limit;
+                    if (!warp_poll_both(v_full + buf, s_full + buf, phase, abort_flag)) return false;
+                    tc_fence_after();
+                    const uint32_t s_cols = tmem + buf * 64 + lanes;
+                    const float4* par = reinterpret_cast<const float4*>(smem + Geo::OFF_ROWS + buf * 1024);   // two keys, then their values
+                    uint32_t y[32];
+                    float sx, sy, sr;
+                    auto weigh = [&](auto masked) {
+                        const uint64_t sl2 = pair(sl, sl), qs2 = pair(qs, qs), m2 = pair(-m, -m);
+                        uint64_t sx2 = 0, sy2 = 0, sr2 = 0;
+    #pragma unroll
+                        for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
+                            float s[16];
+                            tmem_ld16(s_cols + c0, s);
+                            tmem_wait_ld();
+    #pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                const float4 key = par[c0 + e], val = par[c0 + e + 1];
+                                float x0, x1, y0, y1;
+                                unpair(fma2(mul2(pair(key.x, key.y), pair(s[e], s[e + 1])), sl2, fma2(pair(key.z, key.w), qs2, m2)), x0, x1);
+                                x0 = exp2_fast(x0);
+                                x1 = exp2_fast(x1);
+                                uint64_t x2 = pair(x0, x1), lo2 = pair(val.z, val.w), y2 = mul2(x2, pair(val.x, val.y));
+                                if constexpr (masked.value) {
+                                    const bool see0 = base + c0 + e < limit, see1 = base + c0 + e + 1 < limit;
+                                    unpair(y2, y0, y1);
+                                    x2 = pair(see0 ? x0 : 0.0f, see1 ? x1 : 0.0f);
+                                    lo2 = pair(see0 ? val.z : 0.0f, see1 ? val.w : 0.0f);
+                                    y2 = pair(see0 ? y0 : 0.0f, see1 ? y1 : 0.0f);
+                                }
+                                sx2 = add2(sx2, x2);
+                                sy2 = add2(sy2, y2);
+                                sr2 = fma2(x2, lo2, sr2);
+                                unpair(y2, y0, y1);
+                                y[(c0 + e) / 2] = pack_half2(y0, y1);
+                            }
+                        }
+                        float p0, p1;
+                        unpair(sx2, p0, p1);
+                        sx = p0 + p1;
+                        unpair(sy2, p0, p1);
+                        sy = p0 + p1;
+                        unpair(sr2, p0, p1);
+                        sr = p0 + p1;
+                    };
+                    // A segment's first step, and later the rare case that some row's weights or products have grown too far: the row's reference moves so
+                    // that its largest product becomes 2^6.  O and the sums follow.  (Once a step: what is NaN stays NaN.)
+                    bool moved = false;
+                    for (;;) {
+                        if (i > 0 || moved) {
+                            if (mask) weigh(std::true_type{});
+                            else weigh(std::false_type{});
+                            if (moved || __all_sync(kFullMask, sx <= kMostWeight4 && sy <= kMostUmma4)) break;
+                        } else {
+                            sx = INFINITY;
+                        }
+                        const bool moves = !(sx <= kMostWeight4 && sy <= kMostUmma4);
+                        float top = -INFINITY, heavy = -INFINITY;
+    #pragma unroll 1
+                        for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
+                            float s[16];
+                            tmem_ld16(s_cols + c0, s);
+                            tmem_wait_ld();
+    #pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                const float4 key = par[c0 + e], val = par[c0 + e + 1];
+                                const float z0 = fmaf(key.x * s[e], sl, key.z * qs), z1 = fmaf(key.y * s[e + 1], sl, key.w * qs);
+                                if (base + c0 + e < limit) {
+                                    top = fmaxf(top, z0);
+                                    heavy = fmaxf(heavy, z0 + __log2f(val.x));
+                                }
+                                if (base + c0 + e + 1 < limit) {
+                                    top = fmaxf(top, z1);
+                                    heavy = fmaxf(heavy, z1 + __log2f(val.y));
+                                }
+                            }
+                        }
+                        float to = heavy > -INFINITY ? fmaxf(heavy - 6.0f, top - 90.0f) : top;
+                        to = moves ? fmaxf(to, m) : m;
+                        const float f = to > m ? exp2_fast(m - to) : 1.0f;
+                        m = to;
+                        l *= f;
+                        r *= f;
+                        if (i > 0) {
+                            if (!warp_poll_or_abort(v_free + ((step - 1) & 1), ((step - 1) >> 1) & 1u, abort_flag)) return false;
+                            tc_fence_after();
+    #pragma unroll 1
+                            for (int c = 0; c < Geo::O_COLS; c += 16) {
+                                float o[16];
+                                tmem_ld16(o_cols + c, o);
+                                tmem_wait_ld();
+                                uint32_t z[16];
+    #pragma unroll
+                                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * f);
+                                tmem_st16(o_cols + c, z);
+                            }
+                        }
+                        moved = true;
+                    }
+                    l += sx;
+                    r += sr;
+                    tmem_st16(s_cols, y);
+                    tmem_st16(s_cols + 16, y + 16);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_ready + buf);
+                }
             }
             if (steps > 0) {
                 const unsigned step = first + steps - 1;
                 if (!warp_poll_or_abort(v_free + (step & 1), (step >> 1) & 1u, abort_flag)) return false;
                 tc_fence_after();
+                if (steps > kFoldUmma4) fold(true, true);
+                __syncwarp();                                            // (others write this row's part)
             }
             const float inv = u.slot >= 0 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
             // 32 channels at a time through this warp's rows of the queries' place, which no product reads any more: a row's four channels after the
