@@ -971,7 +971,7 @@ attn4_weigh_kernel(const Attn4Params p, int chunk_tiles, int chunks) {
     const int keys = attn_length(a, b), first_limit = keys - count + 1;
     const int32_t* table = a.page_table + static_cast<int64_t>(b) * a.table_width;
     const int rows = count * a.group;
-    const int here = max(0, min(keys, key0 + chunk_keys) - key0);      // keys of this chunk
+    const int here = max(0, min(keys - key0, chunk_keys));             // keys of this chunk (its end may pass 31 bits)
     const int tiles = (here + kTileKeys - 1) / kTileKeys;
     const int tile_no = tiles4_of(a, table, head, key0 / kTileKeys, key0 / kTileKeys + tiles);
     unsigned taken = 0;
