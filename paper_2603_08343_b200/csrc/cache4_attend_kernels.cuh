@@ -414,8 +414,10 @@ __device__ __forceinline__ int tiles4_of(const AttnParams& p, const int32_t* tab
     return ((pg * p.hkv + head) << shift) + (t & ((1 << shift) - 1));
 }
 
-// How far a weight times a value's step, and a weight itself, may go before the row's reference moves.
+// How far a weight times a value's step may go before the row's reference moves, and a weight and that times what the value's z stands for.
 constexpr float kMostProduct4 = 16384.0f, kMostWeight4 = 0x1p100f;
+// What z stands for counts in a reference only where it is larger than this (and then costs two logarithms a key).
+constexpr float kLargeBase4 = 256.0f;
 // Steps of which the tensor core holds the sum: 1024 keys (512 in units of 16 rows).
 constexpr int kFold4 = 32;
 
@@ -515,6 +517,8 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
             x = exp2_fast(fmaf(step4_of(w[t].key(k)) * s[t][n][i], rw.factor[n][e], fmaf(base4_of<T>(w[t].key(k)), rw.sum[n][e], -m[n][e])));
             y = x * turned_step4_of(w[t].value(k), turn);
         };
+        // What z stands for in a value of this lane.
+        auto value_base = [&](int t, int k) { return fmaf(zero_code, turned_step4_of(w[t].value(k), turn), lo4_of(w[t].value(k))); };
         // This lane's sums of a row: weights, weights times base values, products; and the products as operands, before their transposition.
         float sx[NR][E], sr[NR][E], sy[NR][E];
         uint32_t b[U][NR][TERMS][2];
@@ -527,7 +531,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                 for (int t = 0; t < U; ++t)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float base_value = fmaf(zero_code, turned_step4_of(w[t].value(k), turn), lo4_of(w[t].value(k)));
+                        const float base_value = value_base(t, k);
                         float y[2] = {0.0f, 0.0f};
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
@@ -551,18 +555,24 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
         for (int n = 0; n < NR; ++n) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                all_x += sx[n][e];
+                all_x += sx[n][e] + fabsf(sr[n][e]);
                 all_y += sy[n][e];
             }
         }
         // (NaN fails; the sum over a lane's rows passes whenever one of its rows' does; a lane's products have one sign)
         if (!__all_sync(kFullMask, all_x <= kMostWeight4 && fabsf(all_y) <= kMostProduct4)) {
+            bool far = false;
+#pragma unroll
+            for (int t = 0; t < U; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) far |= fabsf(value_base(t, k)) > kLargeBase4;
+            far = __any_sync(kFullMask, far);
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     // (a row moves its reference by its own scores alone: its result does not depend on the rows beside it)
-                    int moves = !(sx[n][e] <= kMostWeight4 && fabsf(sy[n][e]) <= kMostProduct4);
+                    int moves = !(sx[n][e] + fabsf(sr[n][e]) <= kMostWeight4 && fabsf(sy[n][e]) <= kMostProduct4);
 #pragma unroll
                     for (int i = 4; i < 32; i <<= 1) moves |= __shfl_xor_sync(kFullMask, moves, i);
                     if (!__any_sync(kFullMask, moves)) continue;
@@ -578,8 +588,20 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                         }
                     top = column_max(top);
                     heavy = column_max(heavy);
+                    float wide = top;                                // and score plus log2 of what z stands for, if that is large anywhere
+                    if (far) {
+#pragma unroll
+                        for (int t = 0; t < U; ++t)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                if (mask && hidden(t, n, 2 * k + e)) continue;
+                                const float score = fmaf(step4_of(w[t].key(k)) * s[t][n][2 * k + e], rw.factor[n][e], base4_of<T>(w[t].key(k)) * rw.sum[n][e]);
+                                wide = fmaxf(wide, score + __log2f(fabsf(value_base(t, k))));
+                            }
+                        wide = column_max(wide);
+                    }
                     // (without a step above 0 there are no products)
-                    float to = heavy > -INFINITY ? fmaxf(heavy - 6.0f, top - 90.0f) : top;
+                    float to = fmaxf(heavy > -INFINITY ? heavy - 6.0f : top, wide - 90.0f);
                     to = moves ? fmaxf(to, m[n][e]) : m[n][e];
                     const float f = to > m[n][e] ? exp2_fast(m[n][e] - to) : 1.0f;
                     m[n][e] = to;

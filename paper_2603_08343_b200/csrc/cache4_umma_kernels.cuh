@@ -98,6 +98,7 @@ attn4_umma_kernel(const Attn4Params p) {
     uint64_t *s_full = bars + 8, *p_ready = bars + 12, *q_full = bars + 16, *all_done = bars + 18;    // [tile][buffer], q_full [tile]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + Geo::OFF_MISC);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + Geo::OFF_MISC + 4);
+    uint32_t* far = reinterpret_cast<uint32_t*>(smem + Geo::OFF_MISC + 8);      // [buffer] whether what z stands for is large for a value, a half word a warp
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(kFullMask, tid >> 5, 0);
 
     // (tensor memory is taken after the kernel before, which may want it too, and before the one after may start)
@@ -238,7 +239,10 @@ attn4_umma_kernel(const Attn4Params p) {
                     rows[0] = step4_of(row.x);
                     rows[2] = lo4_of(row.x);
                     rows[4] = step4_of(row.y);
-                    rows[6] = value4_of(row.y, zero_code);
+                    const float base_value = value4_of(row.y, zero_code);
+                    rows[6] = base_value;
+                    const bool large = __any_sync(kFullMask, fabsf(base_value) > kLargeBase4);
+                    if (lane == 0) reinterpret_cast<unsigned short*>(far + buf)[warp & 1] = large;
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -413,12 +417,12 @@ attn4_umma_kernel(const Attn4Params p) {
                     auto weigh = [&](auto masked) {
                         const uint64_t sl2 = pair(sl, sl), qs2 = pair(qs, qs), m2 = pair(-m, -m);
                         uint64_t sx2 = 0, sy2 = 0, sr2 = 0;
-    #pragma unroll
+#pragma unroll
                         for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
                             float s[16];
                             tmem_ld16(s_cols + c0, s);
                             tmem_wait_ld();
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 16; e += 2) {
                                 const float4 key = par[c0 + e], val = par[c0 + e + 1];
                                 float x0, x1, y0, y1;
@@ -455,18 +459,19 @@ attn4_umma_kernel(const Attn4Params p) {
                         if (i > 0 || moved) {
                             if (mask) weigh(std::true_type{});
                             else weigh(std::false_type{});
-                            if (moved || __all_sync(kFullMask, sx <= kMostWeight4 && sy <= kMostUmma4)) break;
+                            if (moved || __all_sync(kFullMask, sx + fabsf(sr) <= kMostWeight4 && sy <= kMostUmma4)) break;
                         } else {
                             sx = INFINITY;
+                            sr = sy = 0.0f;
                         }
-                        const bool moves = !(sx <= kMostWeight4 && sy <= kMostUmma4);
+                        const bool moves = !(sx + fabsf(sr) <= kMostWeight4 && sy <= kMostUmma4);
                         float top = -INFINITY, heavy = -INFINITY;
-    #pragma unroll 1
+#pragma unroll 1
                         for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
                             float s[16];
                             tmem_ld16(s_cols + c0, s);
                             tmem_wait_ld();
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 16; e += 2) {
                                 const float4 key = par[c0 + e], val = par[c0 + e + 1];
                                 const float z0 = fmaf(key.x * s[e], sl, key.z * qs), z1 = fmaf(key.y * s[e + 1], sl, key.w * qs);
@@ -480,7 +485,22 @@ attn4_umma_kernel(const Attn4Params p) {
                                 }
                             }
                         }
-                        float to = heavy > -INFINITY ? fmaxf(heavy - 6.0f, top - 90.0f) : top;
+                        float wide = top;
+                        if (far[buf] != 0) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < kUmma4Keys; c0 += 16) {
+                                float s[16];
+                                tmem_ld16(s_cols + c0, s);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; e += 2) {
+                                    const float4 key = par[c0 + e], val = par[c0 + e + 1];
+                                    if (base + c0 + e < limit) wide = fmaxf(wide, fmaf(key.x * s[e], sl, key.z * qs) + __log2f(fabsf(val.z)));
+                                    if (base + c0 + e + 1 < limit) wide = fmaxf(wide, fmaf(key.y * s[e + 1], sl, key.w * qs) + __log2f(fabsf(val.w)));
+                                }
+                            }
+                        }
+                        float to = fmaxf(heavy > -INFINITY ? heavy - 6.0f : top, wide - 90.0f);
                         to = moves ? fmaxf(to, m) : m;
                         const float f = to > m ? exp2_fast(m - to) : 1.0f;
                         m = to;
@@ -489,13 +509,13 @@ attn4_umma_kernel(const Attn4Params p) {
                         if (i > 0) {
                             if (!warp_poll_or_abort(v_free + ((step - 1) & 1), ((step - 1) >> 1) & 1u, abort_flag)) return false;
                             tc_fence_after();
-    #pragma unroll 1
+#pragma unroll 1
                             for (int c = 0; c < Geo::O_COLS; c += 16) {
                                 float o[16];
                                 tmem_ld16(o_cols + c, o);
                                 tmem_wait_ld();
                                 uint32_t z[16];
-    #pragma unroll
+#pragma unroll
                                 for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * f);
                                 tmem_st16(o_cols + c, z);
                             }

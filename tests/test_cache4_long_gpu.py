@@ -103,3 +103,27 @@ def test_scores_that_change_along_the_keys(A, batch, hkv, group, d, page, tokens
     table, lens = order[None].repeat(batch, 1), torch.full((batch,), n, dtype=torch.int32, device="cuda")
     q = (torch.randn(batch * tokens, hkv * group, d, device="cuda", generator=g) * 0.1 + towards * d ** 0.5).bfloat16()
     assert off(A, q, cache, table, lens, tokens, (0, batch // 2, batch - 1)) <= BOUND[BF16]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,d", [(1, 64), (1, 128), (5, 96), (100, 64), (100, 128)])
+@pytest.mark.parametrize("kind", ["equal channels", "tiny beside them", "both signs"])
+def test_large_values_without_a_step_behind_a_leap_of_the_scores(A, dtype, tokens, d, kind):
+    """Rows of equal channels have no step and bring no products that would move a row's reference; their weights, times values of 2^60, stay in range all
+    the same, however the scores rise."""
+    n, page, batch, hkv, group = 6000, 64, 2, 2, 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(tokens + d)
+    at = torch.arange(n, device="cuda")
+    towards = torch.ones(d, device="cuda") / d ** 0.5
+    k = ((at > 64).float() * 60.0)[:, None, None] * towards + 0.05 * torch.randn(n, hkv, d, device="cuda", generator=g)   # 86 in log2, behind the first step
+    v = (torch.rand(n, hkv, 1, device="cuda", generator=g) + 0.5).bfloat16().float().mul(2.0 ** 60).expand(n, hkv, d).contiguous()
+    if kind == "tiny beside them":
+        v[::2] = torch.randn(n // 2, hkv, d, device="cuda", generator=g) * 2.0 ** -80
+    elif kind == "both signs":
+        v[::3] *= -0.5
+    cache = A.cache4(-(-n // page), hkv, page, d)
+    A.kv_append4(k, v, cache, at)
+    table, lens = torch.arange(-(-n // page), dtype=torch.int32, device="cuda")[None].repeat(batch, 1), torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    q = (0.05 * torch.randn(batch * tokens, hkv * group, d, device="cuda", generator=g) + towards * d ** 0.5).to(dtype)
+    assert off(A, q, cache, table, lens, tokens, (0, batch - 1)) <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -13)
