@@ -503,10 +503,11 @@ __device__ __forceinline__ void attn_run(const AttnParams& p, const AttnUnit& u,
     }
 }
 
-// A length read on the device, held to what the tables can hold.
+// A length read on the device, held to what the tables can hold.  (Lengths and offsets are read by ordinary loads: some of the kernels are resident while the
+// kernel before may write them.)
 __device__ __forceinline__ int attn_length(const AttnParams& p, int b) {
     const int64_t most = static_cast<int64_t>(p.table_width) << p.page_shift;
-    const int n = __ldg(p.kv_lens + b);
+    const int n = p.kv_lens[b];
     if (n < 0 || n > most) {
         attn_report(kAttnErrIndex);
         return n < 0 ? 0 : static_cast<int>(most);
@@ -520,7 +521,7 @@ __device__ __forceinline__ void attn_tokens(const AttnParams& p, int b, int64_t&
         count = 1;
         return;
     }
-    int64_t a = __ldg(p.q_start + b), e = __ldg(p.q_start + b + 1);
+    int64_t a = p.q_start[b], e = p.q_start[b + 1];
     if (a < 0 || e < a || e > p.T || e - a > p.max_q_len) {
         attn_report(kAttnErrIndex);
         a = a < 0 ? 0 : (a > p.T ? p.T : a);
@@ -542,7 +543,7 @@ __device__ __forceinline__ int64_t attn_place(const AttnParams& p, int b, int64_
 
 // The tokens that the sequences cover are first .. last - 1; says whether that is all of them.  (q_start is not NULL.)
 __device__ __forceinline__ bool attn_covered(const AttnParams& p, int64_t& first, int64_t& last) {
-    const int64_t a = __ldg(p.q_start), e = __ldg(p.q_start + p.B);
+    const int64_t a = p.q_start[0], e = p.q_start[p.B];
     first = a < 0 ? 0 : (a > p.T ? p.T : a);
     last = e < first ? first : (e > p.T ? p.T : e);
     return first == 0 && last == p.T;
@@ -655,7 +656,7 @@ __device__ __forceinline__ int attn_sequence_of(const AttnParams& p, int64_t t) 
     while (n > 1) {
         const int step = (n + 31) / 32;
         const int at = lo + lane * step;
-        const bool ok = lane * step < n && __ldg(p.q_start + at) <= t;
+        const bool ok = lane * step < n && p.q_start[at] <= t;
         const unsigned hits = __ballot_sync(kFullMask, ok);
         const int last = hits ? 31 - __clz(hits) : 0;
         lo += last * step;

@@ -1,4 +1,5 @@
 // Append to the cache held in 4 bits: rotation, quantisation, write; and the rows that the cache holds, read back.
+// All inputs are read by ordinary loads, behind the wait for the kernel before, which may have written them.
 //
 //     q' = rotation(q)     row k' = rotation(k), row v: lo, step and codes (cache4_common.cuh)
 //
@@ -28,7 +29,7 @@ __device__ __forceinline__ unsigned char* tile4_of(unsigned char* cache, int64_t
 
 template <typename T>
 constexpr int kHeads4 = sizeof(T) == 4 ? 2 : 4;
-constexpr int kAppend4Threads = 256;
+constexpr int kAppend4Threads = 256, kAppend4Blocks = 3;  // on an SM (two, which the compiler's own choice of 84 registers leaves: 87 us for the prompts above)
 
 // Queries: rotated and written; D / 16 lanes a row.
 template <typename T, bool INTERLEAVED, int D>
@@ -44,8 +45,8 @@ __device__ __forceinline__ void append4_queries(const AppendParams& a, int64_t i
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
         if (h < heads) {
-            lo[h].load(src + h * a.q_sh + it.lo);
-            hi[h].load(src + h * a.q_sh + it.hi);
+            lo[h].load_written(src + h * a.q_sh + it.lo);
+            hi[h].load_written(src + h * a.q_sh + it.hi);
         }
     }
     if (it.angle < 0) {
@@ -58,10 +59,10 @@ __device__ __forceinline__ void append4_queries(const AppendParams& a, int64_t i
         }
         return;
     }
-    const int pos = checked_position(a, append_position(a, t));
+    const int pos = checked_position(a, append_position<true>(a, t));
     float c[8], s[8];
-    load8(a.cos_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, c);
-    load8(a.sin_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, s);
+    load8_written(a.cos_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, c);
+    load8_written(a.sin_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, s);
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
         if (h < heads) {
@@ -76,7 +77,7 @@ __device__ __forceinline__ void append4_queries(const AppendParams& a, int64_t i
 }
 
 template <typename T, bool INTERLEAVED, int D>
-__global__ void __launch_bounds__(kAppend4Threads)
+__global__ void __launch_bounds__(kAppend4Threads, kAppend4Blocks)
 kv_append4_kernel(const Append4Params p) {
     constexpr int HB = kHeads4<T>;
     constexpr int LANES = D == 64 ? 4 : 8;             // of a row
@@ -97,8 +98,8 @@ kv_append4_kernel(const Append4Params p) {
     if (!is_k) group -= a.kv_blocks;
     const bool there = t < a.T && item < D / 16;       // (no lane leaves: rows fold by shuffles)
     const RowItem<T, INTERLEAVED> it(item < D / 16 ? item : 0, a.rot);
-    const int64_t slot = there ? append_slot(a, t) : -1;
-    int pos = there && it.angle >= 0 ? append_position(a, t) : 0;
+    const int64_t slot = there ? append_slot<true>(a, t) : -1;
+    int pos = there && it.angle >= 0 ? append_position<true>(a, t) : 0;
     const int h0 = group * HB, heads = slot < 0 ? 0 : a.hkv - h0;
     const T* src = is_k ? row_of<T>(a.k, t * a.k_st + h0 * a.k_sh) : row_of<T>(a.v, t * a.v_st + h0 * a.v_sh);
     const int64_t step = is_k ? a.k_sh : a.v_sh;
@@ -106,16 +107,16 @@ kv_append4_kernel(const Append4Params p) {
 #pragma unroll
     for (int i = 0; i < HB; ++i) {
         if (i < heads) {
-            lo[i].load(src + i * step + it.lo);
-            hi[i].load(src + i * step + it.hi);
+            lo[i].load_written(src + i * step + it.lo);
+            hi[i].load_written(src + i * step + it.hi);
         }
     }
     const bool turns = is_k && slot >= 0 && it.angle >= 0;
     float c[8], s[8];
     if (turns) {
         pos = checked_position(a, pos);
-        load8(a.cos_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, c);
-        load8(a.sin_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, s);
+        load8_written(a.cos_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, c);
+        load8_written(a.sin_t + static_cast<int64_t>(pos) * (a.rot / 2) + it.angle, s);
     }
     const int place = static_cast<int>(slot & 15);
 #pragma unroll
@@ -201,7 +202,7 @@ kv_read4_kernel(const Read4Params p) {
     const int64_t at = job / groups;
     if (at >= p.n) return;
     const int h0 = static_cast<int>(job - at * groups) * HB;
-    int64_t slot = __ldg(reinterpret_cast<const long long*>(p.slots) + at);
+    int64_t slot = p.slots[at];
     if (slot >= p.num_slots) {
         attn_report(kAttnErrIndex);
         slot = -1;

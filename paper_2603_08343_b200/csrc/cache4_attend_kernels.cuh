@@ -4,7 +4,7 @@
 //     score_j = scale (step_j (q . c_j) + lo_j sum(q))
 //     o = sum_j p_j v_j / sum_j p_j = (sum_j (p_j step'_j) (c'_j - z_j) + sum_j p_j (lo'_j + z_j step'_j)) / sum_j p_j,   p_j = exp(score_j - m)
 //
-// in one pass over the keys.  The codes are never turned into values.  A half word of a key's codes masked with 0x000f or 0x00f0 IS an fp16
+// in one pass over the keys.  (Inputs are read by ordinary loads: the kernel before may have written them while this one was resident.)  The codes are never turned into values.  A half word of a key's codes masked with 0x000f or 0x00f0 IS an fp16
 // number, c 2^-24 or 16 c 2^-24 (a subnormal one; the tensor core takes these as they are, but aligns a product by its operands'
 // exponents, so that sums keep about 20 bits), so that eight codes take four masks and one shift, exactly, and the powers of two go into the
 // queries and the result.  z_j keeps the two sums small: with z = 0 for all keys they are large, of opposite signs, and the result is their small
@@ -124,7 +124,7 @@ struct Query4 {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             if (there) {
-                load8(src + g * 32 + c4 * 8, v[g]);
+                load8_written(src + g * 32 + c4 * 8, v[g]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[g][i] = 0.0f;
@@ -406,7 +406,7 @@ struct Ring4 {
 __device__ __forceinline__ int tiles4_of(const AttnParams& p, const int32_t* table, int head, int first, int end) {
     const int t = first + static_cast<int>(threadIdx.x & 31), shift = p.page_shift - 4;
     if (t >= end) return 0;
-    int pg = __ldg(table + (t >> shift));
+    int pg = table[t >> shift];
     if (pg < 0 || pg >= p.num_pages) {
         attn_report(kAttnErrIndex);
         pg = 0;

@@ -210,7 +210,7 @@ kv_evict4_move_kernel(const Evict4Params p) {
         const int key = __ldcg(p.kept + bh * p.budget + at);
         if (key >= 0) {
             const int t = key >> 4;
-            int pg = __ldg(a.page_table + static_cast<int64_t>(b) * a.table_width + (t >> shift));
+            int pg = a.page_table[static_cast<int64_t>(b) * a.table_width + (t >> shift)];
             if (pg < 0 || pg >= a.num_pages) {
                 attn_report(kAttnErrIndex);
                 pg = 0;
@@ -219,7 +219,7 @@ kv_evict4_move_kernel(const Evict4Params p) {
         }
     }
     if (!__any_sync(kFullMask, from >= 0)) return;
-    const int out = __ldg(p.out_table + static_cast<int64_t>(b) * p.out_width + (tile >> shift));
+    const int out = p.out_table[static_cast<int64_t>(b) * p.out_width + (tile >> shift)];
     if (out < 0 || out >= a.num_pages) {
         attn_report(kAttnErrIndex);
         return;

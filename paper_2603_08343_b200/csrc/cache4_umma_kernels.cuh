@@ -181,7 +181,7 @@ attn4_umma_kernel(const Attn4Params p) {
             uint4 raw[LOADS], next[LOADS];
             uint2 row = make_uint2(0, 0), next_row = make_uint2(0, 0);
             auto tile_of = [&](int i) { return min(u.tile0 + i * (kUmma4Keys / kTileKeys) + (kk >> 4), last_tile); };   // (behind the end: any key, nobody sees it)
-            auto look = [&](int i) { return i < steps ? __ldg(u.table + (tile_of(i) >> shift)) : 0; };
+            auto look = [&](int i) { return i < steps ? u.table[tile_of(i) >> shift] : 0; };
             auto fetch = [&](int i, int pg) {
                 if (pg < 0 || pg >= a.num_pages) {
                     attn_report(kAttnErrIndex);

@@ -81,7 +81,11 @@ struct RowItem {
     }
 };
 
-__device__ __forceinline__ int append_position(const AppendParams& p, int64_t t) { return p.rot == 0 ? 0 : __ldg(p.positions + t); }
+// WRITTEN: by ordinary loads, for kernels that may be resident while the kernel before writes what they read.
+template <bool WRITTEN = false>
+__device__ __forceinline__ int append_position(const AppendParams& p, int64_t t) {
+    return p.rot == 0 ? 0 : WRITTEN ? p.positions[t] : __ldg(p.positions + t);
+}
 // The position held to the table: for tokens that use theirs (a dropped token's may be anything).
 __device__ __forceinline__ int checked_position(const AppendParams& p, int pos) {
     if (p.rot != 0 && (pos < 0 || pos >= p.max_pos)) {
@@ -91,8 +95,9 @@ __device__ __forceinline__ int checked_position(const AppendParams& p, int pos) 
     return pos;
 }
 // The token's slot, or -1 for padding and for slots outside the cache (reported).
+template <bool WRITTEN = false>
 __device__ __forceinline__ int64_t append_slot(const AppendParams& p, int64_t t) {
-    const int64_t s = __ldg(reinterpret_cast<const long long*>(p.slots) + t);
+    const int64_t s = WRITTEN ? p.slots[t] : __ldg(reinterpret_cast<const long long*>(p.slots) + t);
     if (s >= p.num_slots) {
         attn_report(kAttnErrIndex);
         return -1;
@@ -111,6 +116,10 @@ struct Raw8 {
     __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
         for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void load_written(const T* p) {     // by ordinary loads
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
     }
     __device__ __forceinline__ void narrow(const float (&v)[8]) {  // rounded to the type
         if constexpr (sizeof(T) == 4) {

@@ -33,6 +33,20 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* __restrict__ p, float
     v[4] = bf16lo_to_f32(q.z); v[5] = bf16hi_to_f32(q.z);
     v[6] = bf16lo_to_f32(q.w); v[7] = bf16hi_to_f32(q.w);
 }
+// The same by ordinary loads: for kernels that may be resident while the kernel before writes what they read (an ordinary load stays behind the wait for
+// it; __ldg is for memory that nobody writes as long as the kernel lives).
+__device__ __forceinline__ void load8_written(const float* p, float (&v)[8]) {
+    const float4 q0 = *reinterpret_cast<const float4*>(p), q1 = *(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = q0.x; v[1] = q0.y; v[2] = q0.z; v[3] = q0.w;
+    v[4] = q1.x; v[5] = q1.y; v[6] = q1.z; v[7] = q1.w;
+}
+__device__ __forceinline__ void load8_written(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    v[0] = bf16lo_to_f32(q.x); v[1] = bf16hi_to_f32(q.x);
+    v[2] = bf16lo_to_f32(q.y); v[3] = bf16hi_to_f32(q.y);
+    v[4] = bf16lo_to_f32(q.z); v[5] = bf16hi_to_f32(q.z);
+    v[6] = bf16lo_to_f32(q.w); v[7] = bf16hi_to_f32(q.w);
+}
 __device__ __forceinline__ void store8(float* __restrict__ p, const float (&v)[8]) {
     reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
