@@ -46,7 +46,8 @@ int wht_kv_append4(const void* k, int64_t k_stride_t, int64_t k_stride_h,
                    void* cache, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t rot, int32_t interleaved, int64_t max_pos,
                    int64_t num_pages, int32_t page, int dtype, void* stream);
 
-/* k_out, v_out [n x Hkv x D] of `dtype`: lo + step * code of the rows at slots [n]; zeros where a slot is negative. */
+/* k_out, v_out [n x Hkv x D] of `dtype`: lo + step * code of the rows at slots [n] (fp32: product and sum rounded; bf16: rounded once); zeros where a slot is
+ * negative. */
 int wht_kv_read4(const void* cache, const int64_t* slots, void* k_out, void* v_out, int64_t n, int32_t Hkv, int32_t D,
                  int64_t num_pages, int32_t page, int dtype, void* stream);
 

@@ -106,8 +106,8 @@ def kv_append4(k, v, cache, slots, positions=None, cos=None, sin=None, q=None, q
 
 
 def kv_read4(cache, slots, dtype=torch.float32, stream=None):
-    """The keys and values that the cache holds at `slots` [n] int64: two tensors [n, kv_heads, head_dim] of `dtype` (fp32 or bf16);
-    zeros where a slot is negative."""
+    """The keys and values that the cache holds at `slots` [n] int64: two tensors [n, kv_heads, head_dim] of `dtype` (fp32, or bf16: rounded
+    once); zeros where a slot is negative."""
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
     return _native.kv_read4(cache, slots, dtype == torch.float32, _raw(stream))

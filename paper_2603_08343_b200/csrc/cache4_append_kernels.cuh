@@ -171,8 +171,8 @@ struct Read4Params {
 };
 
 // bf16(lo + step * code) of the eight codes of a word, two at a time.  A pair's codes go to the low bits of two bf16 numbers of 128 and above (the
-// odd one times 8, with an eighth of the step), less 128, and one fused multiply-add with one rounding.  The result is that of fp32
-// arithmetic rounded to bf16: lo has 8 bits and step * code 12, so either their fp32 sum is exact, or the product is below 2^-12 of lo and both give lo.
+// odd one times 8, with an eighth of the step), less 128, and one fused multiply-add with one rounding: the bf16 number next to lo + step * code.
+// (fp32 arithmetic rounded to bf16 would lose a lo below 2^-24 of the product, whose up to 12 bits may lie half way between two bf16 numbers.)
 __device__ __forceinline__ uint4 held4_bf16(unsigned word, unsigned row) {
     const unsigned turned = word >> 1, lo2 = __byte_perm(row, 0, 0x3232);
     const unsigned step2 = (row & 0xffffu) | (__float_as_uint(step4_of(row) * 0.125f) & 0xffff0000u);
