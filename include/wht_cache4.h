@@ -12,7 +12,8 @@
  * A row x of D channels (of one key head: a key after its rotation, or a value) is held as
  *     lo = bf16(min x),  step = bf16((max x - lo) * fl(1/15)),  code_i = clamp(rint((x_i - lo) * fl(1/step)), 0, 15)
  * and stands for lo + step * code_i; a step below 2^-100 counts as 0 and makes all codes 0.  Every operation is fp32,
- * rounded on its own, so that the cache is a function of the inputs alone.  A row that holds a NaN or an infinity, or whose spread
+ * rounded on its own, so that the cache is a function of the inputs alone.  A channel is held to half a step or to 2^-8 of |min x| (lo is a bf16 number), whichever
+ * is more: rows whose offset is far above their spread keep little of it.  A row that holds a NaN or an infinity, or whose spread
  * passes fp32, stands for NaN.
  *
  * Conventions are those of wht_attention.h (device pointers, 16-byte aligned; streams; status codes; D in {64, 96, 128}, pages of 16, 32, 64 or

@@ -3,8 +3,9 @@
 // A row x of D channels (a key after its rotation, or a value) is held as
 //     lo = bf16(min x),  step = bf16((max x - lo) / 15),  code_i = clamp(rint((x_i - lo) / step), 0, 15)
 // and stands for lo + step * code_i.  All in fp32, each operation rounded on its own; the divisions are products with the rounded
-// reciprocals.  lo and step are rounded before the codes are found, so they cost no accuracy beyond a clamp of a
-// fiftieth of a step.  A step below 2^-100 (a row of equal channels) counts as 0, all codes 0.  A row with a NaN or an infinity (or one
+// reciprocals.  lo and step are rounded before the codes are found: a channel is held to half a step (that the step may come out short, by up to 2^-8, moves the
+// row's top by 15 / 256 of a step, which is less), or where lo is rounded up to that, 2^-8 of the least value's size.  A row whose offset is far above its spread
+// loses its codes to the latter: one from 100.3 to 100.6 has lo = 100.5.  A step below 2^-100 (a row of equal channels) counts as 0, all codes 0.  A row with a NaN or an infinity (or one
 // whose spread passes fp32) stands for NaN.
 //
 // A page of a key head is cut into tiles of 16 keys, each one contiguous piece of 16 D + 128 bytes that one asynchronous copy fetches:

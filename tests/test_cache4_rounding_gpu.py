@@ -56,3 +56,30 @@ def test_bf16_reads_are_rounded_once(A, d):
     k, _ = A.kv_read4(cache, slots, F32)
     assert torch.equal(k[:, 0].cpu(), C.hold(x))
     assert (k[:, 0].cpu().bfloat16().double() != want).any()  # (so the rows do tell the two apart)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_channel_is_held_to_half_a_step_or_the_rounding_of_the_least_value(A, dtype, d):
+    """... and to the roundings of fp32 on the way: of the reciprocal, the difference and its product, 2^-22 of 15 steps, and of the held value,
+    two of 2^-24."""
+    g = torch.Generator()
+    g.manual_seed(d)
+    rows = [torch.rand(d, generator=g) * 0.3 + 100.3]
+    for offset in (0.0, 1.0, -1.0, 37.0, -300.3, 1e4, -1e6):
+        for spread in (1.0, 0.01, 20.0):
+            rows += [torch.randn(d, generator=g) * spread + offset, torch.rand(d, generator=g) * spread + offset]
+    x = torch.stack(rows).to(dtype)
+    n = x.shape[0]
+    cache = A.cache4(n // 16 + 1, 1, 16, d)
+    slots = torch.arange(n, device="cuda")
+    A.kv_append4(x[:, None].cuda(), x[:, None].cuda(), cache, slots)
+    k, _ = A.kv_read4(cache, slots)
+    x, k = x.double(), k[:, 0].cpu().double()
+    lo = x.amin(-1).float().bfloat16().double()
+    step = ((x.amax(-1) - lo).clamp(min=0) / 15) * (1 + 2.0 ** -8)
+    least = (2.0 ** -8 * x.amin(-1).abs())
+    bound = torch.maximum(step * (0.5 + 15 * 2.0 ** -22), least) + 2.0 ** -23 * k.abs().amax(-1) + 15 * 2.0 ** -100
+    assert ((k - x).abs().amax(-1) <= bound).all()
+    if dtype == F32:                                        # the row from 100.3 to 100.6: below 100.5 nothing is told apart
+        assert (k[0][x[0] < 100.5] == 100.5).all()
