@@ -28,7 +28,10 @@
  *     of two per row, enter the second product as one fp16 term (11 bits) where the output is bf16 and as two (22 bits) where it is fp32.
  *     Queries of 2^116 and more (divided by the scale, where that is above 1) may come out as NaN.  Long prompts of bf16 queries over long contexts take a
  *     tcgen05 kernel, by sizes that the host knows; there queries enter as they are, and the weights as one fp16 term.
- *   - The work is divided by the lengths themselves: a table wider than its sequences costs nothing but its memory.
+ *   - The work is divided by the lengths themselves, so that a table wider than its sequences costs the attention of single tokens and short prompts nothing but its
+ *     memory.  The width counts in three places: the received weight is written (and zeros behind the lengths) over all of it, in pieces whose size follows it; the workspace for its
+ *     scores grows with it; and for bf16 prompts of more than 16 rows a sequence and key head the choice of kernel takes the tables as full, so that short contexts in
+ *     wide tables go to the tcgen05 kernel although the other one is faster, and the last bits of a result depend on the table's width.
  */
 #ifndef WHT_CACHE4_H_
 #define WHT_CACHE4_H_

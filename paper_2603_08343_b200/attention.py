@@ -117,11 +117,13 @@ def paged_attention4(q, cache, page_table, kv_lens, q_start=None, max_q_len: int
                      weights_out=None, stream=None):
     """Attention of each token to its sequence's keys up to itself, over a cache in 4 bits.  Returns [tokens, heads, head_dim].
 
-    page_table, kv_lens, q_start, max_q_len, scale as for shared_prefix_attention (a table wider than its sequences costs nothing here).
+    page_table, kv_lens, q_start, max_q_len, scale as for shared_prefix_attention (a table wider than its sequences costs single tokens and
+    short prompts nothing; with weights and for long bf16 prompts one about as wide as the longest sequence is fastest).
     weights [batch, kv_heads, table pages * page] fp32: what each key has received so far.  With it (or with weights_out alone, starting from nothing)
     the call returns (out, weights_out): weights_out (allocated if None; may be weights itself) = weights + the softmax weights of
-    this call's tokens, summed over them and the heads of each key head; 0 from a sequence's length on.
-    Long bf16 prompts over long contexts take a tcgen05 kernel, by the sizes of the call.
+    this call's tokens, summed over them and the heads of each key head; 0 from a sequence's length on.  Such a call takes a
+    workspace of up to 1 GiB, by its rows and the table's width.
+    Long bf16 prompts over long contexts take a tcgen05 kernel, by the sizes of the call, the table's width among them.
     """
     return _native.paged_attention4(q, cache, page_table, kv_lens, q_start, max_q_len, scale, out, weights, weights_out, _raw(stream))
 

@@ -798,7 +798,7 @@ attn4_kernel(const Attn4Params p) {
     }
     __syncwarp();
     grid_dependency_wait();
-    grid_launch_dependents();
+    grid_launch_dependents();                          // (never before the wait: see the join and the received weight)
     if (a.q_start != nullptr)
         for (int head = blockIdx.x; head < a.hkv; head += gridDim.x) attn_uncovered<T, D>(a, head);
     unsigned run;
@@ -836,6 +836,8 @@ attn4_kernel(const Attn4Params p) {
 template <typename T, int D>
 __global__ void __launch_bounds__(128)
 attn4_join_kernel(const Attn4Params p, int unit_rows) {
+    // This kernel starts once every block of the attention is past its wait, so whatever came before the attention has ended: the call's inputs (lengths,
+    // offsets) may be read before this one's wait, the parts may not.
     grid_launch_dependents();
     const AttnParams& a = p.a;
     const int lane = threadIdx.x & 31;
@@ -927,6 +929,8 @@ attn4_weigh_scores_kernel(const Attn4Params p, int chunks) {
     attn_tokens(a, b, token0, count);
     const int keys = attn_length(a, b), rows = count * a.group;
     const bool there = key0 < keys;
+    // (lengths, offsets and what has been received so far are read before the wait: this kernel starts after the attention's blocks are past theirs, hence after
+    // whatever wrote them has ended)
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (there && p.weights != nullptr) v = *reinterpret_cast<const float4*>(p.weights + at);
     grid_dependency_wait();                                          // scores and sums come from the kernels before

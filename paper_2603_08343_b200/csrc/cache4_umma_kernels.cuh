@@ -129,7 +129,7 @@ attn4_umma_kernel(const Attn4Params p) {
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(kFullMask, *tmem_slot, 0);
-    grid_launch_dependents();
+    grid_launch_dependents();                                        // (never before the wait: the join reads lengths and offsets ahead of its own)
 
     unsigned run;
     const Place4 home = find_run4(p, kUmma4Rows, blockIdx.x, run);
