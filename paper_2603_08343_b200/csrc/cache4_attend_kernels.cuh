@@ -19,13 +19,13 @@
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
 //
 // What bounds it: memory, 2 (D / 2 + 4) bytes a key and key head, and instructions next to it.  At 23 B a clock and SM a tile of 16 keys of 128 channels has
-// 378 clocks of an SM's quarter; it takes 240 instructions for up to 8 rows, about 100 of which mask, select and shift, two clocks each.
+// 378 clocks of an SM's quarter; it takes 239 instructions for up to 8 rows, about 100 of which mask, select and shift, two clocks each, and 208 for up to 4.
 // So products are taken transposed, S^T = C Q^T and O^T = C'^T P^T: codes of 16 keys (channels) fill the 16-row operand and the rows sit on the 8-column one, so
 // that 8 rows waste nothing, a key's step and least value are wanted by the four lanes that hold its scores, and P^T changes from accumulator to operand
 // layout by one 8x8 transposition.  Up to four rows take every other column, half of the softmax's instructions (200 x 1000 keys 56 -> 51 us, 1 x 4096 8.7 ->
-// 8.2).  64 sequences of up to 16384 keys of 8 key heads of 128, 32 heads: 157-160 us, 5.4 TB/s (DRAM 70 % busy, issue slots 56 %, ALU
-// 56 %; with the rows on the 16-row operand, half of it empty, 364 instructions a tile and 242 us).  Two tiles a step, so that their latencies overlap (one:
-// 165-167).  200 x 1000 keys of 16 heads of 64: 51 us, 3.4 TB/s: a tile has half the bytes, but the softmax of as many scores.
+// 8.2).  64 sequences of up to 16384 keys of 8 key heads of 128, 32 heads: 157-159 us, 5.4 TB/s (DRAM 65 % busy, issue slots 53 %, ALU
+// 58 %; with the rows on the 16-row operand, half of it empty, 364 instructions a tile and 242 us).  Two tiles a step, so that their latencies overlap (one:
+// 165-167).  200 x 1000 keys of 16 heads of 64: 52.6 us, 3.3 TB/s: a tile has half the bytes, but the softmax of as many scores.
 //
 // The division of work goes by the lengths themselves, which are on the device: the tiles of all units (sequence, key head, row tile)
 // are counted one after the other, and each warp (a block of its own) takes an equal run of them, whatever units it touches.  A unit that lies in one

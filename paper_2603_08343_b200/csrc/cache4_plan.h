@@ -21,8 +21,8 @@ constexpr int kUmma4Rows = 256, kUmma4Grain = 2, kUmma4Resident = 1;
 // Whether the tcgen05 kernel is the faster one, by a small model of both, in us (D = 128; less for fewer channels): a start of 28, 1.75 a step of 256 rows and
 // 64 keys in a block and 8 a further unit of it, against 10 and 0.085 an SM for 16 rows and 16 keys in the kernel of few rows.  Lengths are on the device: as
 // if the tokens were spread evenly and the tables full, with a quarter in hand, since lengths that are not favour the kernel of few rows.
-// us, tcgen05 and the other: 128 tokens of 4 rows over 30000 keys, 8 key heads, 120 (272); 2048 over 4000 218 (517); 64 over 20000 63 (105); 100 over 10000
-// 59 (83); 16 x 128 over up to 2000 97 (134); 8 x 64 over up to 5000, 4 key heads, D = 96, 51 (52); 400 tokens of 32 heads over 800 42 (37); 256 over 300 37 (19).
+// us, tcgen05 and the other: 128 tokens of 4 rows over 30000 keys, 8 key heads, 121 (275); 2048 over 4000 219 (528); 64 over 20000 66 (108); 100 over 10000
+// 61 (86); 16 x 128 over up to 2000 100 (138); 8 x 64 over up to 5000, 4 key heads, D = 96, 54 (54); 400 over 800 39 (41); 256 over 300 25 (25).
 inline bool umma4_pays(int64_t keys, int64_t T, int32_t B, int group, int32_t Hkv, int32_t D, int sms) {
     const int64_t rows = (T + B - 1) / B * group;
     const double heads = static_cast<double>(B) * Hkv, k = static_cast<double>(keys);

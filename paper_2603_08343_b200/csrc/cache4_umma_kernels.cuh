@@ -20,8 +20,8 @@
 // order in which their codes fall out of a word, and so do the queries'; the results' are put right when they are written.
 //
 // What bounds it: the softmax warps.  A step of both tiles takes 2800 clocks, 2100 of them the weights of 64 keys (64 exponentials, 7 packed operations a pair of
-// keys, two of a warp's reads of (step, lo)), 1000 the products.  128 tokens of 32 heads over 30000 keys of 8 key heads 120 us (0.5 PFLOP/s; 272 in the kernel of few rows),
-// 2048 tokens over 4000 218 us (517).  Slower: blocks of one tile, two an SM (96 registers a thread, 150 us), the issuing warp's loops not unrolled (a product
+// keys, two of a warp's reads of (step, lo)), 1000 the products.  128 tokens of 32 heads over 30000 keys of 8 key heads 121 us (0.5 PFLOP/s; 275 in the kernel of few rows),
+// 2048 tokens over 4000 219 us (528).  Slower: blocks of one tile, two an SM (96 registers a thread, 150 us), the issuing warp's loops not unrolled (a product
 // takes 100 clocks to issue, 133 us), (step, lo) unpacked by the softmax warps (147 us).
 //
 // Waits are bounded as in umma_kernels.cuh.
