@@ -64,7 +64,7 @@ def long_cache(A, n, hkv, d, page, seed, keys=None):
 
 # batch, key heads, heads of each, channels, page, tokens of a sequence.  The batch is large, so that a warp (a block) has a long run.
 SHAPES = [(128, 4, 4, 128, 64, 1), (256, 2, 8, 64, 128, 1), (128, 4, 2, 96, 16, 1), (32, 2, 4, 96, 64, 4), (32, 4, 3, 128, 32, 5), (32, 4, 8, 64, 64, 2),
-          (4, 2, 4, 128, 64, 150), (8, 2, 8, 64, 128, 70), (4, 2, 3, 96, 16, 200)]
+          (4, 2, 4, 128, 64, 150), (8, 2, 8, 64, 128, 70), (4, 2, 3, 96, 16, 200), (8, 2, 4, 128, 64, 27), (8, 2, 4, 64, 64, 26)]
 
 
 @pytest.mark.parametrize("size", [0.0, 0.5, 1.5])
