@@ -4,9 +4,10 @@
 //     score_j = scale (step_j (q . c_j) + lo_j sum(q))
 //     o = sum_j p_j v_j / sum_j p_j = (sum_j (p_j step'_j) (c'_j - z_j) + sum_j p_j (lo'_j + z_j step'_j)) / sum_j p_j,   p_j = exp(score_j - m)
 //
-// in one pass over the keys.  (Inputs are read by ordinary loads: the kernel before may have written them while this one was resident.)  The codes are never turned into values.  A half word of a key's codes masked with 0x000f or 0x00f0 IS an fp16
-// number, c 2^-24 or 16 c 2^-24 (a subnormal one; the tensor core takes these as they are, but aligns a product by its operands'
-// exponents, so that sums keep about 20 bits), so that eight codes take four masks and one shift, exactly, and the powers of two go into the
+// in one pass over the keys.  (Inputs are read by ordinary loads: the kernel before may have written them while this one was resident.)
+// The codes are never turned into values.  A half word of a key's codes masked with 0x000f or 0x00f0 IS an fp16 number, c 2^-24 or 16 c 2^-24
+// (a subnormal one; the tensor core takes these as they are, but aligns a product by its operands' exponents, so that sums keep about
+// 20 bits), so that eight codes take four masks and one shift, exactly, and the powers of two go into the
 // queries and the result.  z_j keeps the two sums small: with z = 0 for all keys they are large, of opposite signs, and the result is their small
 // difference.  For bf16 results z is 0 for the keys of even places and 15 for the others, whose codes are turned over as they are loaded (15 - c) and whose
 // steps change sign, which costs next to nothing; for fp32 ones, whose values' codes become ordinary numbers by one exact subtraction a pair, z

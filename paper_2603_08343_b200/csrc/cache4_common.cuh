@@ -5,8 +5,8 @@
 // and stands for lo + step * code_i.  All in fp32, each operation rounded on its own; the divisions are products with the rounded
 // reciprocals.  lo and step are rounded before the codes are found: a channel is held to half a step (that the step may come out short, by up to 2^-8, moves the
 // row's top by 15 / 256 of a step, which is less), or where lo is rounded up to that, 2^-8 of the least value's size.  A row whose offset is far above its spread
-// loses its codes to the latter: one from 100.3 to 100.6 has lo = 100.5.  A step below 2^-100 (a row of equal channels) counts as 0, all codes 0.  A row with a NaN or an infinity (or one
-// whose spread passes fp32) stands for NaN.
+// loses its codes to the latter: one from 100.3 to 100.6 has lo = 100.5.  A step below 2^-100 (a row of equal channels) counts as 0, all codes 0.  A row
+// with a NaN or an infinity (or one whose spread passes fp32) stands for NaN.
 //
 // A page of a key head is cut into tiles of 16 keys, each one contiguous piece of 16 D + 128 bytes that one asynchronous copy fetches:
 // the codes of the keys, those of the values, then (step, lo) of the key and of the value, 8 bytes a key.  Inside a
