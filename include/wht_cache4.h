@@ -22,7 +22,7 @@
  *     values, and for each key step and lo of the key, step and lo of the value (bf16).  The order of the codes is the library's own
  *     (csrc/cache4_common.cuh states it).  It has no storage type: queries and outputs of a call are WHT_F32 or WHT_BF16.
  *     Fresh memory may hold anything.
- *   - Scores, softmax statistics and the weights' sums are fp32.  Products are summed by the tensor core, which truncates as it adds: those of a score over its
+ *   - Scores, softmax statistics and the weights' sums are fp32, long sums in pieces.  Products are summed by the tensor core, which truncates as it adds: those of a score over its
  *     channels, to about 20 bits; those of the output over 1024 keys at most (4096 in the tcgen05 kernel), whose sums are then added in fp32 with rounding.  Queries enter the product as fp16 numbers shifted by a power of two per row: bf16 ones
  *     keep all bits but those below 2^-33 of the row's largest, fp32 ones are two terms (22 bits).  The softmax weights, times the values' steps and a power
  *     of two per row, enter the second product as one fp16 term (11 bits) where the output is bf16 and as two (22 bits) where it is fp32.

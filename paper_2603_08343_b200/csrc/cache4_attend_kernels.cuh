@@ -13,8 +13,8 @@
 // steps change sign, which costs next to nothing; for fp32 ones, whose values' codes become ordinary numbers by one exact subtraction a pair, z
 // is 8 and 7 (64 x 16384 in bf16 would then take 192 us instead of 164).
 // The tensor core's accumulation truncates towards zero, by up to 2^-23 of a sum in each addition, so that the loss grows with their
-// number: after kFold4 steps the accumulators are added to sums in shared memory, with rounding, and begin anew.  (With z = 0 and one accumulation a
-// run, 131072 keys of even weight were off by 0.38 of the result's norm and 1048576 by 13 times the norm; now by 0.0004 and 0.0007 beside the rounding to bf16.)
+// number (and equal weights that are added one by one round alike): after kFold4 steps all sums are added to others in shared memory, with rounding, and begin anew.  (With z = 0 and one accumulation a
+// run, 131072 keys of even weight were off by 0.38 of the result's norm and 1048576 by 15 times the norm; now by 0.0004 and 0.0007 beside the rounding to bf16.)
 // Queries enter as fp16 after a shift of each row by a power of two (bf16 ones keep all their bits but what lies below 2^-33 of the row's
 // maximum; fp32 ones are two terms, 22 bits of it), and the weights p step' as fp16 times a power of two per row that keeps them in range: one
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
@@ -64,9 +64,9 @@ struct Attn4Geo {
     static constexpr bool Q_SHARED = NR * TERMS > 2;            // query operands in shared memory
     static constexpr int Q_BYTES = Q_SHARED ? NR * TERMS * NG * 512 : 0;
     static constexpr int OFF_Q = STAGES * U * TILE;
-    static constexpr int OFF_FOLD = OFF_Q + Q_BYTES;            // a lane's sums of the steps before: [accumulator, then r and m of each row][lane]
+    static constexpr int OFF_FOLD = OFF_Q + Q_BYTES;            // a lane's sums of the steps before: [accumulator, then l and r of each row][lane]; then the rows' m
     static constexpr int FOLD_O = NR * (D / 4), FOLD = FOLD_O + 4 * NR;
-    static constexpr int OFF_BARS = OFF_FOLD + FOLD * 128;
+    static constexpr int OFF_BARS = OFF_FOLD + FOLD * 128 + ROWS * 4;
     static constexpr int BYTES = OFF_BARS + STAGES * 8;
     static constexpr int BLOCKS = NR * TERMS > 2 ? 8 : NR * TERMS > 1 ? 12 : 16;  // on an SM
 };
@@ -652,7 +652,7 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
     };
     // steps whose keys all rows see, then the others
     const int open = least_limit > u.tile0 * kTileKeys ? min(steps, (least_limit - u.tile0 * kTileKeys) / (U * kTileKeys)) : 0;
-    float* fold = reinterpret_cast<float*>(smem + Geo::OFF_FOLD) + lane;
+    float *fold = reinterpret_cast<float*>(smem + Geo::OFF_FOLD) + lane, *fold_m = reinterpret_cast<float*>(smem + Geo::OFF_FOLD) + Geo::FOLD * 32;
     for (int j = 0;;) {
         const int stop = min(steps, j + kFold4), begin = j;
         for (; j < min(stop, open); ++j) step(j, std::false_type{});
@@ -664,8 +664,9 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float* before = fold + (Geo::FOLD_O + 4 * n + 2 * e) * 32;
-                    const float was = before[32], f = m[n][e] > was ? exp2_fast(was - m[n][e]) : 1.0f;
-                    r[n][e] = fmaf(before[0], f, r[n][e]);
+                    const float was = fold_m[n * 8 + 2 * c4 + e], f = m[n][e] > was ? exp2_fast(was - m[n][e]) : 1.0f;
+                    l[n][e] = fmaf(before[0], f, l[n][e]);
+                    r[n][e] = fmaf(before[32], f, r[n][e]);
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
@@ -673,14 +674,16 @@ __device__ __forceinline__ void attn4_segment(const Attn4Params& p, const Segmen
                 }
         }
         if (j >= steps) break;
+        __syncwarp();                                                // (all have read the rows' references)
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 float* to = fold + (Geo::FOLD_O + 4 * n + 2 * e) * 32;
-                to[0] = r[n][e];
-                to[32] = m[n][e];
-                r[n][e] = 0.0f;
+                to[0] = l[n][e];
+                to[32] = r[n][e];
+                if (r4 == 0) fold_m[n * 8 + 2 * c4 + e] = m[n][e];
+                l[n][e] = r[n][e] = 0.0f;
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d)
 #pragma unroll

@@ -366,7 +366,7 @@ attn4_umma_kernel(const Attn4Params p) {
             // leaves none uses the place of the part that goes on, which is written after it).
             const int part_lanes = min(32, p.part_rows - warp * 32);
             float* kept = a.part_o + ((u.slot >= 0 ? u.slot : 2ll * blockIdx.x + 1) * p.part_rows + warp * 32) * D + lane * 4;
-            float kept_m = 0.0f;
+            float kept_m = 0.0f, kept_l = 0.0f, kept_r = 0.0f;           // (and those of l and r)
             // last: O becomes the whole sum; else the sum takes O, which begins anew
             auto fold = [&](bool begun, bool last) {
                 const float f = m > kept_m ? exp2_fast(kept_m - m) : 1.0f;
@@ -394,6 +394,10 @@ attn4_umma_kernel(const Attn4Params p) {
                 }
                 tmem_wait_st();
                 kept_m = m;
+                kept_l = fmaf(kept_l, f, l);
+                kept_r = fmaf(kept_r, f, r);
+                l = last ? kept_l : 0.0f;
+                r = last ? kept_r : 0.0f;
             };
             for (int i = 0; i < steps;) {
                 if (i > 0) {

@@ -87,6 +87,22 @@ def test_fp32_over_131071_keys(A, batch, hkv, group, d, page, tokens, size):
     assert off(A, q, cache, table, lens, tokens, (0, batch // 2, batch - 1)) <= BOUND[F32]
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_prompts_of_even_weights(A, d):
+    """600 tokens over 262143 keys of one weight: a warp adds up tens of thousands of equal numbers, whose roundings are alike; values about 3, so that
+    nothing but the sums' own errors shows."""
+    n, batch, hkv, group, page = (1 << 18) - 1, 4, 2, 8, 128
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    cache = A.cache4(-(-n // page), hkv, page, d)
+    for i in range(0, n, 1 << 16):
+        k, v = (torch.randn(min(n - i, 1 << 16), hkv, d, device="cuda", generator=g) for _ in range(2))
+        A.kv_append4(k, v + 3, cache, torch.arange(i, i + k.shape[0], device="cuda"))
+    table, lens = torch.arange(-(-n // page), dtype=torch.int32, device="cuda")[None].repeat(batch, 1), torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    q = torch.zeros(batch * 600, hkv * group, d, device="cuda")
+    assert off(A, q, cache, table, lens, 600, (0, batch - 1)) <= BOUND[F32]
+
+
 @pytest.mark.parametrize("batch,hkv,group,d,page,tokens", [(64, 8, 4, 128, 64, 1), (64, 8, 8, 64, 64, 1), (64, 4, 2, 96, 32, 6), (8, 4, 4, 128, 64, 100), (8, 4, 4, 64, 64, 100)])
 @pytest.mark.parametrize("course", ["rising", "falling", "a leap"])
 def test_scores_that_change_along_the_keys(A, batch, hkv, group, d, page, tokens, course):
