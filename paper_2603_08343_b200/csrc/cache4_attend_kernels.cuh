@@ -12,9 +12,10 @@
 // difference.  For bf16 results z is 0 for the keys of even places and 15 for the others, whose codes are turned over as they are loaded (15 - c) and whose
 // steps change sign, which costs next to nothing; for fp32 ones, whose values' codes become ordinary numbers by one exact subtraction a pair, z
 // is 8 and 7 (64 x 16384 in bf16 would then take 192 us instead of 164).
-// The tensor core's accumulation truncates towards zero, by up to 2^-23 of a sum in each addition, so that the loss grows with their
-// number (and equal weights that are added one by one round alike): after kFold4 steps all sums are added to others in shared memory, with rounding, and begin anew.  (With z = 0 and one accumulation a
-// run, 131072 keys of even weight were off by 0.38 of the result's norm and 1048576 by 15 times the norm; now by 0.0004 and 0.0007 beside the rounding to bf16.)
+// The tensor core's accumulation truncates towards zero, by up to 2^-23 of a sum in each addition, so that the loss grows with their number, and equal
+// weights that are added one by one round alike: after kFold4 steps all sums are added to others in shared memory, with rounding, and begin
+// anew.  (With z = 0 and one accumulation a run, 131072 keys of even weight were off by 0.38 of the result's norm and 1048576 by 15 times the norm; now by
+// 0.0004 and 0.0007 beside the rounding to bf16.)
 // Queries enter as fp16 after a shift of each row by a power of two (bf16 ones keep all their bits but what lies below 2^-33 of the row's
 // maximum; fp32 ones are two terms, 22 bits of it), and the weights p step' as fp16 times a power of two per row that keeps them in range: one
 // term of 11 bits where the output is rounded to 8, two where it is fp32.
