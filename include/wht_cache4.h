@@ -61,6 +61,7 @@ int wht_kv_read4(const void* cache, const int64_t* slots, void* k_out, void* v_o
  *   weights      [B x Hkv x table_width * page] float32 or NULL: what each key has received so far (NULL: nothing).
  *   weights_out  the same shape, or NULL: weights + the softmax weights of this call's tokens and the query heads of the key
  *                head, summed; 0 from kv_lens[b] on.  May be `weights` itself.  Sums have one order: results repeat bit for bit.
+ *                Queries may be read again for it, after `out` has been written: `out` does not overlap them.
  *   workspace    at least wht_attn_paged4_workspace_bytes(...) bytes; weigh: whether weights_out is given (the scores of up to 8 rows a sequence and key head
  *                are then kept for it, in 1 GiB at most; beyond that they are taken again).  It holds nothing between calls; calls that may run at the same time
  *                need one each.
